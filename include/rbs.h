@@ -22,6 +22,15 @@
  *                       prompts are separate causal sequences, never one
  *                       concatenated sequence)
  *
+ * and the calls around them in a serving step, over a paged key-value cache:
+ *
+ *   rbs_pages_extend,   pages, slots and positions of a batch's new tokens,
+ *   rbs_pages_release   and the pages of finished rows given back
+ *   rbs_qk_norm_rope    per-head norm and rotary position of queries and keys
+ *                       (the form the stages above take them in), keys and
+ *                       values put into the cache in the same pass
+ *   rbs_paged_decode    attention of one new token per row over the cache
+ *
  * Conventions shared by every call
  *   - Tensors live in device memory.  Q, K, V and O are indexed by (head,
  *     token, dimension) with the dimension contiguous and the head and token
@@ -367,6 +376,165 @@ int rbs_sparse_prefill_varlen(const rbs_shape* shape, const rbs_batch* batch, co
                               float softmax_scale, void* O, float* lse, void* workspace, void* stream);
 int rbs_dense_indices_varlen(const rbs_shape* shape, const rbs_batch* batch, int32_t* counts,
                              int32_t* indices, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Paged key-value cache: the tokens that follow a prompt.
+ *
+ * A cache holds n_pages pages of page_size tokens for every KV head.  A row (a
+ * request in the batch) owns the pages listed in its row of the page table:
+ * its token at position p lies in place p % page_size of page
+ * page_table[row][p / page_size].  A token's slot is page * page_size + place.
+ * Row lengths live on the GPU (seq_lens): 0 is an empty row, a negative length
+ * an unused one, which every call leaves as it is.
+ */
+enum { RBS_CACHE_BF16 = 0, RBS_CACHE_FP8 = 1 };
+
+#define RBS_MAX_ROWS 4096 /* rows of a page table */
+
+/*
+ * Keys and values (device memory, the same strides for both):
+ *   element (page, g, place, j) at page stride_page + g stride_head + place stride_tok + j
+ * Zero strides mean the dense [n_pages][H_kv][page_size][d]; any strides that
+ * are multiples of 16 elements, with stride_tok and stride_head at least d, will
+ * do ([n_pages][page_size][H_kv][d], both in one buffer), as long as distinct
+ * places do not overlap, which is the caller's to see to.
+ *   RBS_CACHE_BF16  bf16
+ *   RBS_CACHE_FP8   E4M3 codes, scaled per KV head as in the FP8 calls:
+ *                   code = E4M3(x * (448 / amax)), values past amax saturating;
+ *                   amax fp32 [2 H_kv], K heads then V heads (the tail of
+ *                   rbs_fp8_amax's array, kept while the cache is in use; 0: scale 1)
+ */
+typedef struct {
+  int32_t n_pages;     /* n_pages * page_size < 2^31 */
+  int32_t page_size;   /* 16, 32, 64, 128 or 256 */
+  int32_t n_kv_heads;
+  int32_t head_dim;    /* 128 */
+  int32_t format;      /* RBS_CACHE_* */
+  int64_t stride_page;
+  int64_t stride_head;
+  int64_t stride_tok;
+  void* K;
+  void* V;
+  const float* amax;   /* RBS_CACHE_FP8 only */
+} rbs_cache;
+
+/*
+ * The bookkeeping of a cache's pages (device memory):
+ *   page_table  int32 [n_rows][max_pages]
+ *   free_pages  int32 [n_pages], a stack: the free ones are free_pages[0 .. n_free)
+ */
+typedef struct {
+  int32_t n_rows;     /* 1 .. RBS_MAX_ROWS */
+  int32_t max_pages;  /* max_pages * page_size < 2^31 */
+  int32_t n_pages;
+  int32_t page_size;
+  int32_t* page_table;
+  int32_t* free_pages;
+} rbs_pages;
+
+#define RBS_MAX_NEW_TOKENS (1 << 24) /* of one rbs_pages_extend or rbs_qk_norm_rope call */
+
+/* Bits of the status word that the page calls write (0: done). */
+enum {
+  RBS_PAGES_FEW = 1,    /* fewer free pages than the new tokens need */
+  RBS_PAGES_ROW = 2,    /* a row longer than its row of the page table */
+  RBS_PAGES_TOKENS = 4, /* more new tokens than max_tokens */
+  RBS_PAGES_STACK = 8   /* n_free outside 0 .. n_pages, or past it with the released pages */
+};
+
+/*
+ * Room for new tokens.  Row s with length len_s >= 0 gets new_tokens[s] tokens
+ * more (fewer than 0: none; new_tokens NULL: one), its missing pages taken from
+ * the top of the stack, for row 0 first and in the order of their positions.
+ * Outputs, with a_s the tokens added to row s:
+ *   page_table  the new pages' entries; the others keep their values
+ *   seq_lens_out [n_rows] len_s + a_s;  n_free_out [1];  cu_tokens [n_rows + 1]
+ *               exclusive sums of a_s (the batch's tokens packed row after row)
+ *   positions, slots [max_tokens]: of token t; -1 from cu_tokens[n_rows] on
+ *   status [1]  0, or RBS_PAGES_* bits: then no page is taken, the lengths and
+ *               n_free are passed on unchanged, cu_tokens is 0 and positions
+ *               and slots are -1
+ * seq_lens_out may be seq_lens and n_free_out may be n_free (one extra launch
+ * then, where max_tokens is large); no other two buffers may overlap.
+ * All int32, device memory.  free_pages is only read.
+ * Errors: RBS_ERR_NULL, RBS_ERR_SHAPE (counts and sizes), RBS_ERR_UNSUPPORTED
+ * (page size), RBS_ERR_ALIGN.
+ */
+int rbs_pages_extend(const rbs_pages* pages, const int32_t* seq_lens, const int32_t* new_tokens,
+                     const int32_t* n_free, int32_t max_tokens, int32_t* seq_lens_out, int32_t* n_free_out,
+                     int32_t* cu_tokens, int32_t* positions, int32_t* slots, int32_t* status, void* stream);
+
+/*
+ * The pages of every row s with released[s] != 0 and a length >= 0 go back on
+ * the stack (row after row, in the order of their positions), and its length
+ * becomes -1.  seq_lens and n_free are updated in place; status as above, and
+ * where it is not 0 nothing else has changed.  int32, device memory.
+ */
+int rbs_pages_release(const rbs_pages* pages, const int32_t* released, int32_t* seq_lens, int32_t* n_free,
+                      int32_t* status, void* stream);
+
+/*
+ * Norm and rotation of rbs_qk_norm_rope (device pointers):
+ *   norm      x / sqrt(mean(x^2) + eps) * weight, per head; a NULL weight
+ *             leaves that tensor unnormed
+ *   rotation  of the pairs (j, j + rot_dim / 2), or (2 j, 2 j + 1) with
+ *             interleaved, j < rot_dim / 2, by the angle position * inv_freq[j]
+ *             (formed in 64 bits), the result multiplied by factor (1 except for
+ *             frequencies scaled for long contexts); elements from rot_dim on
+ *             are only normed
+ */
+typedef struct {
+  const void* q_weight;   /* bf16 [d] or NULL */
+  const void* k_weight;   /* bf16 [d] or NULL */
+  const float* inv_freq;  /* fp32 [rot_dim / 2]; may be NULL with rot_dim 0 */
+  int32_t rot_dim;        /* 0 .. d, a multiple of 8 */
+  int32_t interleaved;
+  float eps;              /* >= 0 */
+  float factor;           /* finite */
+} rbs_rope;
+
+/*
+ * Queries and keys ready for attention, and keys and values into the cache.
+ * in: sizes (n_tokens up to RBS_MAX_NEW_TOKENS, H_q up to 512, any block_size) and
+ * the strides of Q and of K and V.
+ * out: NULL, or a shape with the strides of Q_out (q_*) and K_out (kv_*); NULL
+ * means those of Q and K.  positions int32 [n_tokens].
+ *   Q_out = rotate(norm(Q)), K_out = rotate(norm(K)), fp32 inside, rounded once
+ *   to bf16.  Q_out may be Q and K_out may be K with the same strides;
+ *   otherwise outputs and inputs do not overlap.  K_out may be NULL.
+ *   cache NULL: no cache.  Otherwise the key (rounded to the cache's type from
+ *   fp32) and V's row go to slots[t] (int32 [n_tokens]); a slot outside the
+ *   cache (-1) writes none.  Tokens with a slot of their own each.
+ * Tokens with a negative position are left out: nothing of theirs is written.
+ * V and slots are read only with a cache.
+ */
+int rbs_qk_norm_rope(const rbs_shape* in, const rbs_shape* out, const rbs_rope* rope, const void* Q, const void* K,
+                     const void* V, const int32_t* positions, void* Q_out, void* K_out, const rbs_cache* cache,
+                     const int32_t* slots, void* stream);
+
+/* Workspace of rbs_paged_decode, 16-byte aligned; contents on entry are ignored.
+ * Calls that share one must be ordered, like those that share an output: a
+ * captured graph that may run beside another call needs one of its own. */
+size_t rbs_decode_workspace_bytes(void);
+
+/*
+ * Attention of one new token per row over the row's cached tokens (the new
+ * token's own key and value among them, put there by rbs_qk_norm_rope).
+ * shape: n_tokens rows (up to RBS_MAX_ROWS), H_q (up to 512) and H_kv heads, strides of Q and O (any
+ * block_size; kv strides are not used).  For query head h of row s
+ *   O = sum_j softmax_j(q . k_j * scale) v_j over the first seq_lens[s] tokens
+ * with fp32 sums, rounded to bf16; Q, O bf16 (head, row, dimension) with the
+ * strides of Q.  softmax_scale <= 0 selects 1/sqrt(d).  lse: NULL or fp32
+ * [H_q][n_tokens], natural log.  A row of length 0: O = 0, lse = -inf; an
+ * unused row (negative length): its O and lse are left as they were.
+ * page_table int32 [n_tokens][max_pages], seq_lens int32 [n_tokens].  Both are trusted
+ * like the prefill's lists: page numbers are clamped to the cache and lengths
+ * to the table, so that no access leaves the buffers.  Places past a row's
+ * length may hold anything.
+ */
+int rbs_paged_decode(const rbs_shape* shape, const rbs_cache* cache, const void* Q, const int32_t* page_table,
+                     int32_t max_pages, const int32_t* seq_lens, float softmax_scale, void* O, float* lse,
+                     void* workspace, void* stream);
 
 /* Static description of a status code. */
 const char* rbs_status_str(int status);

@@ -9,6 +9,14 @@
     batch = Batch([n0, n1, ...]); shape = varlen_shape(batch, H_q, H_kv, B)   # independent sequences, packed
     stats = rbs_block_stats_varlen(shape, batch, K); ...; rbs_sparse_prefill_varlen(shape, batch, Q, K, V, ...)
     f8 = rbs_fp8_prepare(shape, Q, K, V); O = rbs_sparse_prefill_fp8(shape, f8, counts, indices)  # FP8 inputs
+
+and around a paged key-value cache (the tokens that follow a prompt):
+
+    pages = Pages.allocate(n_rows, max_pages, n_pages, page_size); cache = PagedCache.allocate(n_pages, page_size, H_kv)
+    step = rbs_pages_extend(pages, new_tokens, max_tokens)             # pages, positions, slots of new tokens
+    Q, K = rbs_qk_norm_rope(shape, rope, Q, K, step.positions, V=V, cache=cache, slots=step.slots)
+    O = rbs_paged_decode(shape, Q, cache, pages.page_table, step.seq_lens)   # one new token per row
+    rbs_pages_release(pages, released)                                 # finished rows
 """
 
 from ._lib import (  # noqa: F401
@@ -60,4 +68,27 @@ from ._lib import (  # noqa: F401
     rbs_summary_bytes,
     LIB_PATH,
     RBS_ERR_RANGE,
+)
+from ._paged import (  # noqa: F401
+    RBS_CACHE_BF16,
+    RBS_CACHE_FP8,
+    RBS_MAX_ROWS,
+    RBS_PAGES_FEW,
+    RBS_PAGES_ROW,
+    RBS_PAGES_STACK,
+    RBS_PAGES_TOKENS,
+    PagedCache,
+    Pages,
+    PageStep,
+    Rope,
+    decode_workspace,
+    rbs_cache,
+    rbs_decode_workspace_bytes,
+    rbs_paged_decode,
+    rbs_pages,
+    rbs_pages_extend,
+    rbs_pages_release,
+    rbs_qk_norm_rope,
+    rbs_rope,
+    rope_frequencies,
 )

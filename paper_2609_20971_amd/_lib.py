@@ -134,6 +134,8 @@ def load() -> ctypes.CDLL:
     lib.rbs_sparse_prefill_varlen.restype = ctypes.c_int
     lib.rbs_dense_indices_varlen.argtypes = [SP, BP, P, P, P]
     lib.rbs_dense_indices_varlen.restype = ctypes.c_int
+    from . import _paged
+    _paged.declare(lib)
     lib.rbs_status_str.argtypes = [ctypes.c_int]
     lib.rbs_status_str.restype = ctypes.c_char_p
     lib.rbs_set_debug.argtypes = [ctypes.c_int]

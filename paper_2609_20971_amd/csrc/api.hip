@@ -14,6 +14,7 @@
 namespace {
 
 constexpr int kMaxTokens = 262144;
+constexpr int kMaxHeads = 512;  // query heads of the calls around the paged cache
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -159,6 +160,65 @@ int check_batch(const rbs_shape* s, const rbs_batch* b, rbs::SeqTable* t) {
   if ((int64_t)s->n_q_heads * blk > INT32_MAX / 2) return RBS_ERR_SHAPE;
   rbs::Strides st;
   return strides_of(s, &st);
+}
+
+// ---- Paged cache.
+
+// log2 of a page size, or -1 if it is not one of 16 .. 256.
+int page_shift_of(int32_t page_size) {
+  for (int s = 4; s <= 8; ++s)
+    if (page_size == 1 << s) return s;
+  return -1;
+}
+
+int check_cache(const rbs_cache* c, rbs::CacheView* out) {
+  if (c == nullptr) return RBS_ERR_NULL;
+  const int shift = page_shift_of(c->page_size);
+  if (c->head_dim != 128 || shift < 0) return RBS_ERR_UNSUPPORTED;
+  if (c->format != RBS_CACHE_BF16 && c->format != RBS_CACHE_FP8) return RBS_ERR_ARG;
+  if (c->n_kv_heads < 1 || c->n_pages < 1 || c->n_pages > (INT32_MAX >> shift)) return RBS_ERR_SHAPE;
+  rbs::CacheView v{};
+  v.tok = c->stride_tok == 0 ? 128 : c->stride_tok;
+  v.head = c->stride_head == 0 ? (int64_t)c->page_size * 128 : c->stride_head;
+  v.page = c->stride_page == 0 ? (int64_t)c->n_kv_heads * c->page_size * 128 : c->stride_page;
+  if (v.tok < 128 || v.head < 128 || v.page < 128 || v.tok % 16 != 0 || v.head % 16 != 0 || v.page % 16 != 0)
+    return RBS_ERR_SHAPE;
+  // The largest offset (in bytes) has to fit 63 bits, and a place's inside its page the kernels' 31.
+  if (v.tok > INT32_MAX / 1024 || v.head > (int64_t(1) << 40) || v.page > (int64_t(1) << 60) / c->n_pages)
+    return RBS_ERR_SHAPE;
+  if (c->K == nullptr || c->V == nullptr || (c->format == RBS_CACHE_FP8 && c->amax == nullptr)) return RBS_ERR_NULL;
+  if (!aligned16(c->K) || !aligned16(c->V) || (c->format == RBS_CACHE_FP8 && !aligned16(c->amax)))
+    return RBS_ERR_ALIGN;
+  v.K = c->K;
+  v.V = c->V;
+  v.amax = c->format == RBS_CACHE_FP8 ? c->amax : nullptr;
+  v.n_pages = c->n_pages;
+  v.page_shift = shift;
+  *out = v;
+  return RBS_OK;
+}
+
+int check_pages(const rbs_pages* p, int* shift) {
+  if (p == nullptr) return RBS_ERR_NULL;
+  *shift = page_shift_of(p->page_size);
+  if (*shift < 0) return RBS_ERR_UNSUPPORTED;
+  if (p->n_rows < 1 || p->n_rows > RBS_MAX_ROWS || p->max_pages < 1 || p->max_pages > (INT32_MAX >> *shift) ||
+      p->n_pages < 1 || p->n_pages > (INT32_MAX >> *shift))
+    return RBS_ERR_SHAPE;
+  if (p->page_table == nullptr || p->free_pages == nullptr) return RBS_ERR_NULL;
+  if (!aligned16(p->page_table) || !aligned16(p->free_pages)) return RBS_ERR_ALIGN;
+  return RBS_OK;
+}
+
+// Sizes and strides of the calls around the cache: as check_shape, without its
+// rules on blocks and with its own limit on tokens.
+int check_heads(const rbs_shape* s, int max_tokens) {
+  if (s == nullptr) return RBS_ERR_NULL;
+  if (s->head_dim != 128) return RBS_ERR_UNSUPPORTED;
+  if (s->n_tokens < 1 || s->n_tokens > max_tokens || s->n_q_heads < 1 || s->n_kv_heads < 1 ||
+      s->n_q_heads > kMaxHeads || s->n_q_heads % s->n_kv_heads != 0)
+    return RBS_ERR_SHAPE;
+  return RBS_OK;
 }
 
 // Byte offset of the half-widths in the box summary (centres first, 256-aligned).
@@ -695,6 +755,141 @@ int rbs_sparse_prefill_fp8(const rbs_shape* shape, const void* Q8, const void* K
       shape->n_tokens, shape->n_q_heads, shape->n_kv_heads, shape->block_size, M, counts, indices,
       rbs_index_capacity(M), scale, static_cast<uint16_t*>(O), st.q_head, st.q_tok, lse,
       static_cast<int*>(workspace), static_cast<hipStream_t>(stream)), stream);
+}
+
+int rbs_pages_extend(const rbs_pages* pages, const int32_t* seq_lens, const int32_t* new_tokens,
+                     const int32_t* n_free, int32_t max_tokens, int32_t* seq_lens_out, int32_t* n_free_out,
+                     int32_t* cu_tokens, int32_t* positions, int32_t* slots, int32_t* status, void* stream) {
+  int shift;
+  int rc = check_pages(pages, &shift);
+  if (rc != RBS_OK) return rc;
+  if (max_tokens < 1 || max_tokens > RBS_MAX_NEW_TOKENS) return RBS_ERR_SHAPE;
+  if (seq_lens == nullptr || n_free == nullptr || seq_lens_out == nullptr || n_free_out == nullptr ||
+      cu_tokens == nullptr || positions == nullptr || slots == nullptr || status == nullptr)
+    return RBS_ERR_NULL;
+  if (!aligned16(seq_lens) || (new_tokens != nullptr && !aligned16(new_tokens)) || !aligned16(n_free) ||
+      !aligned16(seq_lens_out) || !aligned16(n_free_out) || !aligned16(cu_tokens) || !aligned16(positions) ||
+      !aligned16(slots) || !aligned16(status))
+    return RBS_ERR_ALIGN;
+  rbs::PagesArgs a;
+  a.n_rows = pages->n_rows;
+  a.max_pages = pages->max_pages;
+  a.n_pages = pages->n_pages;
+  a.page_shift = shift;
+  a.page_table = pages->page_table;
+  a.free_pages = pages->free_pages;
+  a.seq_lens = seq_lens;
+  a.new_tokens = new_tokens;
+  a.n_free = n_free;
+  a.max_tokens = max_tokens;
+  a.seq_lens_out = seq_lens_out;
+  a.n_free_out = n_free_out;
+  a.cu_tokens = cu_tokens;
+  a.positions = positions;
+  a.slots = slots;
+  a.status = status;
+  return finish(rbs::launch_pages_extend(a, static_cast<hipStream_t>(stream)), stream);
+}
+
+int rbs_pages_release(const rbs_pages* pages, const int32_t* released, int32_t* seq_lens, int32_t* n_free,
+                      int32_t* status, void* stream) {
+  int shift;
+  int rc = check_pages(pages, &shift);
+  if (rc != RBS_OK) return rc;
+  if (released == nullptr || seq_lens == nullptr || n_free == nullptr || status == nullptr) return RBS_ERR_NULL;
+  if (!aligned16(released) || !aligned16(seq_lens) || !aligned16(n_free) || !aligned16(status)) return RBS_ERR_ALIGN;
+  return finish(rbs::launch_pages_release(pages->n_rows, pages->max_pages, pages->n_pages, shift, pages->page_table,
+                                          pages->free_pages, released, seq_lens, n_free, status,
+                                          static_cast<hipStream_t>(stream)), stream);
+}
+
+int rbs_qk_norm_rope(const rbs_shape* in, const rbs_shape* out, const rbs_rope* rope, const void* Q, const void* K,
+                     const void* V, const int32_t* positions, void* Q_out, void* K_out, const rbs_cache* cache,
+                     const int32_t* slots, void* stream) {
+  int rc = check_heads(in, RBS_MAX_NEW_TOKENS);
+  if (rc != RBS_OK) return rc;
+  rbs::RopeArgs a{};
+  if ((rc = strides_of(in, &a.in)) != RBS_OK) return rc;
+  a.out = a.in;
+  if (out != nullptr) {
+    if (out->n_tokens != in->n_tokens || out->n_q_heads != in->n_q_heads || out->n_kv_heads != in->n_kv_heads ||
+        out->head_dim != in->head_dim)
+      return RBS_ERR_SHAPE;
+    if ((rc = strides_of(out, &a.out)) != RBS_OK) return rc;
+  }
+  if (rope == nullptr || Q == nullptr || K == nullptr || positions == nullptr || Q_out == nullptr)
+    return RBS_ERR_NULL;
+  if (rope->rot_dim < 0 || rope->rot_dim > 128 || rope->rot_dim % 8 != 0) return RBS_ERR_UNSUPPORTED;
+  if (!(rope->eps >= 0.f) || isinf(rope->eps) || !(rope->factor == rope->factor) || isinf(rope->factor))
+    return RBS_ERR_ARG;
+  if (rope->rot_dim > 0 && rope->inv_freq == nullptr) return RBS_ERR_NULL;
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(positions) || !aligned16(Q_out) || !aligned16(K_out) ||
+      !aligned16(rope->q_weight) || !aligned16(rope->k_weight) || !aligned16(rope->inv_freq))
+    return RBS_ERR_ALIGN;
+  // In place only row by row: the same pointer needs the same strides.
+  if ((Q_out == Q && (a.out.q_head != a.in.q_head || a.out.q_tok != a.in.q_tok)) ||
+      (K_out == K && (a.out.kv_head != a.in.kv_head || a.out.kv_tok != a.in.kv_tok)))
+    return RBS_ERR_SHAPE;
+  if (cache != nullptr) {
+    if ((rc = check_cache(cache, &a.cache)) != RBS_OK) return rc;
+    if (cache->n_kv_heads != in->n_kv_heads) return RBS_ERR_SHAPE;
+    if (V == nullptr || slots == nullptr) return RBS_ERR_NULL;
+    if (!aligned16(V) || !aligned16(slots)) return RBS_ERR_ALIGN;
+    a.cached = true;
+  }
+  a.Q = static_cast<const uint16_t*>(Q);
+  a.K = static_cast<const uint16_t*>(K);
+  a.V = static_cast<const uint16_t*>(V);
+  a.n_tokens = in->n_tokens;
+  a.n_q_heads = in->n_q_heads;
+  a.n_kv_heads = in->n_kv_heads;
+  a.q_weight = static_cast<const uint16_t*>(rope->q_weight);
+  a.k_weight = static_cast<const uint16_t*>(rope->k_weight);
+  a.inv_freq = rope->inv_freq;
+  a.rot_dim = rope->rot_dim;
+  a.interleaved = rope->interleaved != 0;
+  a.eps = rope->eps;
+  a.factor = rope->factor;
+  a.positions = positions;
+  a.slots = slots;
+  a.Q_out = static_cast<uint16_t*>(Q_out);
+  a.K_out = static_cast<uint16_t*>(K_out);
+  return finish(rbs::launch_qk_norm_rope(a, static_cast<hipStream_t>(stream)), stream);
+}
+
+size_t rbs_decode_workspace_bytes(void) { return rbs::decode_workspace_bytes(); }
+
+int rbs_paged_decode(const rbs_shape* shape, const rbs_cache* cache, const void* Q, const int32_t* page_table,
+                     int32_t max_pages, const int32_t* seq_lens, float softmax_scale, void* O, float* lse,
+                     void* workspace, void* stream) {
+  int rc = check_heads(shape, RBS_MAX_ROWS);
+  if (rc != RBS_OK) return rc;
+  static_assert(RBS_MAX_ROWS == rbs::kMaxRows, "rows of a page table");
+  rbs::DecodeArgs a{};
+  if ((rc = resolve_strides(shape->q_stride_head, shape->q_stride_tok, shape->n_q_heads, shape->n_tokens, &a.q_head,
+                            &a.q_tok)) != RBS_OK)
+    return rc;
+  if ((rc = check_cache(cache, &a.cache)) != RBS_OK) return rc;
+  if (cache->n_kv_heads != shape->n_kv_heads || max_pages < 1 || max_pages > (INT32_MAX >> a.cache.page_shift))
+    return RBS_ERR_SHAPE;
+  if (Q == nullptr || page_table == nullptr || seq_lens == nullptr || O == nullptr || workspace == nullptr)
+    return RBS_ERR_NULL;
+  if (!(softmax_scale == softmax_scale) || isinf(softmax_scale)) return RBS_ERR_ARG;
+  if (!aligned16(Q) || !aligned16(page_table) || !aligned16(seq_lens) || !aligned16(O) || !aligned16(lse) ||
+      !aligned16(workspace))
+    return RBS_ERR_ALIGN;
+  a.Q = static_cast<const uint16_t*>(Q);
+  a.n_rows = shape->n_tokens;
+  a.n_q_heads = shape->n_q_heads;
+  a.n_kv_heads = shape->n_kv_heads;
+  a.page_table = page_table;
+  a.max_pages = max_pages;
+  a.seq_lens = seq_lens;
+  a.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)shape->head_dim);
+  a.O = static_cast<uint16_t*>(O);
+  a.lse = lse;
+  a.workspace = static_cast<float*>(workspace);
+  return finish(rbs::launch_paged_decode(a, static_cast<hipStream_t>(stream)), stream);
 }
 
 const char* rbs_status_str(int status) {

@@ -48,8 +48,8 @@ def run_abi_tests() -> int:
     env = dict(os.environ)
     env.update(LD_PRELOAD=asan_runtime(), ASAN_OPTIONS="detect_leaks=0:abort_on_error=1",
                UBSAN_OPTIONS="halt_on_error=1:print_stacktrace=1", RBS_LIB_PATH=SAN_LIB)
-    tests = os.path.join(_build.ROOT, "tests", "test_abi.py")
-    return subprocess.run([sys.executable, "-m", "pytest", tests, "-x", "-q", "-p", "no:cacheprovider"],
+    tests = [os.path.join(_build.ROOT, "tests", f) for f in ("test_abi.py", "test_abi_paged.py")]
+    return subprocess.run([sys.executable, "-m", "pytest", *tests, "-x", "-q", "-p", "no:cacheprovider"],
                           cwd=_build.ROOT, env=env).returncode
 
 

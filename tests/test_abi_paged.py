@@ -1,0 +1,271 @@
+"""Refusals of the calls over a paged cache, on the CPU: the C ABI's (nothing here
+reaches a launch: each call fails validation first) and the binding's."""
+
+from __future__ import annotations
+
+import ctypes
+import math
+
+import pytest
+import torch
+
+import paper_2609_20971_amd as rbs
+
+FAKE, MIS = 0x10000, 0x10008  # never dereferenced: validation fails before use
+OK_PAST = 1                   # RBS_ERR_NULL of an argument checked after those in question
+
+
+def _lib():
+    return rbs.load()
+
+
+def _pages(**over):
+    v = dict(n_rows=4, max_pages=8, n_pages=20, page_size=16, page_table=FAKE, free_pages=FAKE)
+    v.update(over)
+    return rbs.rbs_pages(**v)
+
+
+def _cache(**over):
+    v = dict(n_pages=20, page_size=16, n_kv_heads=2, head_dim=128, format=0, stride_page=0, stride_head=0, stride_tok=0,
+             K=FAKE, V=FAKE, amax=None)
+    v.update(over)
+    return rbs.rbs_cache(**v)
+
+
+EXTEND = dict(seq_lens=FAKE, new_tokens=FAKE, n_free=FAKE, max_tokens=4, seq_lens_out=FAKE, n_free_out=FAKE,
+              cu_tokens=FAKE, positions=FAKE, slots=FAKE, status=FAKE)
+
+
+def _extend(pages, **over):
+    a = dict(EXTEND, **over)
+    return _lib().rbs_pages_extend(pages, *a.values(), None)
+
+
+def _release(pages, **over):
+    a = dict(dict(released=FAKE, seq_lens=FAKE, n_free=FAKE, status=FAKE), **over)
+    return _lib().rbs_pages_release(pages, *a.values(), None)
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(page_size=15), 3), (dict(page_size=8), 3), (dict(page_size=512), 3), (dict(page_size=48), 3),
+    (dict(page_size=0), 3), (dict(page_size=-16), 3),
+    (dict(n_rows=0), 2), (dict(n_rows=4097), 2), (dict(max_pages=0), 2), (dict(n_pages=0), 2), (dict(n_pages=-1), 2),
+    (dict(max_pages=2**27, page_size=16), 2), (dict(n_pages=2**23, page_size=256), 2),
+    (dict(page_table=None), 1), (dict(free_pages=None), 1), (dict(page_table=MIS), 5), (dict(free_pages=MIS), 5),
+])
+def test_pages_validation(over, code):
+    assert _extend(_pages(**over)) == code
+    assert _release(_pages(**over)) == code
+
+
+def test_extend_and_release_arguments():
+    assert _lib().rbs_pages_extend(None, *EXTEND.values(), None) == 1
+    for name in EXTEND:
+        if name == "max_tokens":
+            continue
+        if name != "new_tokens":
+            assert _extend(_pages(), **{name: None}) == 1, name
+        assert _extend(_pages(), **{name: MIS}) == 5, name
+    for bad in (0, -1, (1 << 24) + 1):
+        assert _extend(_pages(), max_tokens=bad) == 2
+    for name in ("released", "seq_lens", "n_free", "status"):
+        assert _release(_pages(), **{name: None}) == 1
+        assert _release(_pages(), **{name: MIS}) == 5
+    assert _release(None) == 1
+
+
+CACHE_BAD = [
+    (dict(page_size=8), 3), (dict(page_size=100), 3), (dict(head_dim=64), 3), (dict(format=2), 4), (dict(format=-1), 4),
+    (dict(n_pages=0), 2), (dict(n_pages=2**23, page_size=256), 2), (dict(n_kv_heads=3), 2), (dict(n_kv_heads=0), 2),
+    (dict(stride_tok=64), 2), (dict(stride_tok=136), 2), (dict(stride_head=-128), 2), (dict(stride_page=8), 2),
+    (dict(stride_tok=2**22), 2), (dict(stride_page=2**60), 2),
+    (dict(K=None), 1), (dict(V=None), 1), (dict(K=MIS), 5), (dict(V=MIS), 5),
+    (dict(format=1), 1), (dict(format=1, amax=MIS), 5),
+]
+
+
+def _rope_c(**over):
+    v = dict(q_weight=FAKE, k_weight=FAKE, inv_freq=FAKE, rot_dim=128, interleaved=0, eps=1e-6, factor=1.0)
+    v.update(over)
+    return rbs.rbs_rope(**v)
+
+
+def _rope(shape=None, out=None, rope=None, cache=None, **over):
+    shape = rbs.make_shape(10, 4, 2, 64) if shape is None else shape
+    a = dict(Q=FAKE, K=FAKE, V=FAKE, positions=FAKE, Q_out=FAKE, K_out=FAKE)
+    a.update({k: v for k, v in over.items() if k in a})
+    return _lib().rbs_qk_norm_rope(shape, out, _rope_c() if rope is None else rope, *a.values(), cache,
+                                   over.get("slots", FAKE), None)
+
+
+def _decode(shape=None, cache=None, **over):
+    shape = rbs.make_shape(10, 4, 2, 64) if shape is None else shape
+    a = dict(Q=FAKE, page_table=FAKE, max_pages=4, seq_lens=FAKE, scale=0.0, O=FAKE, lse=FAKE, workspace=FAKE)
+    a.update(over)
+    return _lib().rbs_paged_decode(shape, _cache() if cache is None else cache, *a.values(), None)
+
+
+@pytest.mark.parametrize("over,code", CACHE_BAD)
+def test_cache_validation(over, code):
+    assert _decode(cache=_cache(**over)) == code
+    assert _rope(cache=_cache(**over)) == code
+
+
+@pytest.mark.parametrize("field,value,code", [
+    ("head_dim", 64, 3), ("n_tokens", 0, 2), ("n_q_heads", 3, 2), ("n_q_heads", 514, 2), ("n_kv_heads", 0, 2),
+    ("q_stride_tok", 64, 2), ("q_stride_head", 4, 2),
+])
+def test_shapes(field, value, code):
+    s = rbs.make_shape(10, 4, 2, 64)
+    setattr(s, field, value)
+    assert _decode(shape=s) == code
+    assert _rope(shape=s) == code
+
+
+def test_limits():
+    assert _decode(shape=rbs.make_shape(4097, 4, 2, 64)) == 2
+    assert _decode(shape=rbs.make_shape(4096, 4, 2, 64), Q=None) == OK_PAST
+    assert _rope(shape=rbs.make_shape((1 << 24) + 1, 4, 2, 64)) == 2
+    assert _rope(shape=rbs.make_shape(1 << 24, 4, 2, 64), Q=None) == OK_PAST
+    assert _decode(max_pages=0) == 2 and _decode(max_pages=2**27) == 2
+    # Any block size, unlike the prefill's calls.
+    assert _decode(shape=rbs.make_shape(10, 4, 2, 7), Q=None) == OK_PAST
+
+
+def test_decode_arguments():
+    assert _lib().rbs_paged_decode(rbs.make_shape(10, 4, 2, 64), None, FAKE, FAKE, 4, FAKE, 0.0, FAKE, None, FAKE, None) == 1
+    for name in ("Q", "page_table", "seq_lens", "O", "workspace"):
+        assert _decode(**{name: None}) == 1
+    for name in ("Q", "page_table", "seq_lens", "O", "workspace", "lse"):
+        assert _decode(**{name: MIS}) == 5
+    for bad in (math.nan, math.inf):
+        assert _decode(scale=bad) == 4
+    assert rbs.rbs_decode_workspace_bytes() % 4 == 0
+
+
+def test_rope_arguments():
+    for name in ("Q", "K", "positions", "Q_out"):
+        assert _rope(**{name: None}) == 1
+    for name in ("Q", "K", "positions", "Q_out", "K_out"):
+        assert _rope(**{name: MIS}) == 5
+    for name in ("V", "slots"):
+        assert _rope(cache=_cache(), **{name: None}) == 1
+        assert _rope(cache=_cache(), **{name: MIS}) == 5
+    for over, code in ((dict(rot_dim=-8), 3), (dict(rot_dim=136), 3), (dict(rot_dim=60), 3), (dict(eps=-1.0), 4),
+                       (dict(eps=math.nan), 4), (dict(factor=math.inf), 4), (dict(inv_freq=None), 1),
+                       (dict(inv_freq=MIS), 5), (dict(q_weight=MIS), 5), (dict(k_weight=MIS), 5)):
+        assert _rope(rope=_rope_c(**over)) == code, over
+    s, out = rbs.make_shape(10, 4, 2, 64), rbs.make_shape(10, 4, 2, 64)
+    out.q_stride_head, out.q_stride_tok = 128, 4 * 128
+    assert _rope(shape=s, out=out) == 2            # in place with other strides
+    out = rbs.make_shape(11, 4, 2, 64)
+    assert _rope(shape=s, out=out) == 2
+    out = rbs.make_shape(10, 4, 2, 64)
+    out.kv_stride_tok = 8
+    assert _rope(shape=s, out=out) == 2
+
+
+# ------------------------------------------------------------------ the binding
+
+def _i32(*shape):
+    return torch.zeros(*shape, dtype=torch.int32)
+
+
+def _bf(*shape):
+    return torch.zeros(*shape, dtype=torch.bfloat16)
+
+
+@pytest.mark.parametrize("args,message", [
+    ((_bf(4, 2, 16, 128), _bf(4, 2, 16, 128)), "must be on a GPU"),
+    ((_bf(4, 2, 16, 128), _bf(4, 2, 16, 64)), "V must have shape"),
+    ((_bf(4, 2, 16), _bf(4, 2, 16)), r"\[n_pages\]"),
+    ((_bf(4, 2, 16, 128).float(), _bf(4, 2, 16, 128)), "must be torch.bfloat16"),
+    ((_bf(4, 2, 16, 128), _bf(4, 2, 16, 128), torch.zeros(4)), "must be torch.uint8"),
+    ((_bf(4, 2, 16, 128).byte(), _bf(4, 2, 16, 128).byte(), torch.zeros(3)), "amax must have shape"),
+    ((_bf(4, 2, 16, 128), _bf(4, 16, 2, 128).transpose(1, 2)), "differ from K strides"),
+    ((_bf(1, 2, 16, 128).expand(4, 2, 16, 128), _bf(1, 2, 16, 128).expand(4, 2, 16, 128)), "overlap"),
+    ((_bf(0, 2, 16, 128), _bf(0, 2, 16, 128)), "overlap|holds none"),
+])
+def test_paged_cache_checks(args, message):
+    with pytest.raises(ValueError, match=message):
+        rbs.PagedCache(*args)
+
+
+@pytest.mark.parametrize("over,message", [
+    (dict(), "must be on a GPU"),
+    (dict(page_table=_i32(4)), r"\[n_rows\]"),
+    (dict(page_table=_i32(4, 5).long()), "must be torch.int32"),
+    (dict(free_pages=_i32(4, 5)), "must have shape"),
+    (dict(n_free=_i32(2)), "must have shape"),
+    (dict(seq_lens=_i32(5)), "must have shape"),
+    (dict(page_table=_i32(5, 4).t()), "must be contiguous"),
+])
+def test_pages_checks(over, message):
+    a = dict(page_table=_i32(4, 5), free_pages=_i32(20), n_free=_i32(1), seq_lens=_i32(4))
+    a.update(over)
+    with pytest.raises(ValueError, match=message):
+        rbs.Pages(*a.values(), 16)
+
+
+def test_step_and_rope_checks():
+    with pytest.raises(ValueError, match="cu_tokens must have shape"):
+        rbs.PageStep(_i32(4), _i32(1), _i32(4), _i32(9), _i32(9), _i32(1))
+    with pytest.raises(ValueError, match="slots must have shape"):
+        rbs.PageStep(_i32(4), _i32(1), _i32(5), _i32(9), _i32(8), _i32(1))
+    with pytest.raises(ValueError, match="must be on a GPU"):
+        rbs.PageStep(_i32(4), _i32(1), _i32(5), _i32(9), _i32(9), _i32(1))
+    with pytest.raises(ValueError, match="inv_freq must be torch.float32"):
+        rbs.Rope(torch.zeros(64, dtype=torch.float64))
+    with pytest.raises(ValueError, match="k_weight must have shape"):
+        rbs.Rope(None, None, _bf(64))
+    with pytest.raises(ValueError, match="must be on a GPU"):
+        rbs.Rope(torch.zeros(64))
+    for call in (lambda: rbs.rbs_pages_extend(object()), lambda: rbs.rbs_pages_release(object(), _i32(4))):
+        with pytest.raises(ValueError, match="must be a Pages"):
+            call()
+
+
+def test_call_checks():
+    shape = rbs.make_shape(10, 4, 2, 64)
+    Q, K = _bf(4, 10, 128), _bf(2, 10, 128)
+    rope = rbs.Rope(None)
+    pos = _i32(10)
+    for args, more, message in [
+        ((Q, K, pos.long()), {}, "positions must be torch.int32"),
+        ((Q, K, pos[:9]), {}, "positions must have shape"),
+        ((Q[:3], K, pos), {}, "Q must have shape"),
+        ((Q, K.float(), pos), {}, "K must be torch.bfloat16"),
+        ((Q, K, pos), dict(Q_out=Q[:, :5]), "Q_out must have shape"),
+        ((Q, K, pos), dict(K_out=K.float()), "K_out must be torch.bfloat16"),
+        ((Q, K, pos), dict(cache=object()), "must be a PagedCache"),
+        ((Q, K, pos), {}, "must be on a GPU"),
+    ]:
+        with pytest.raises(ValueError, match=message):
+            rbs.rbs_qk_norm_rope(shape, rope, *args, **more)
+    with pytest.raises(ValueError, match="must be a Rope"):
+        rbs.rbs_qk_norm_rope(shape, object(), Q, K, pos)
+    with pytest.raises(ValueError, match="must be a PagedCache"):
+        rbs.rbs_paged_decode(shape, Q, object(), _i32(10, 3), pos)
+    with pytest.raises(ValueError, match="Q must have shape"):
+        rbs.rbs_paged_decode(shape, Q[:, :9], object(), _i32(10, 3), pos)
+
+
+def test_rope_frequencies():
+    f, factor = rbs.rope_frequencies(8, base=10000.0, device="cpu")
+    assert factor == 1.0 and f.dtype == torch.float32
+    assert torch.allclose(f.double(), torch.tensor([1.0, 0.1, 0.01, 0.001], dtype=torch.float64), rtol=1e-7)
+    g, factor = rbs.rope_frequencies(8, base=10000.0, scaling="linear", scale=4.0, device="cpu")
+    assert factor == 1.0 and torch.allclose(g, f / 4, rtol=1e-7)
+    g, factor = rbs.rope_frequencies(128, scaling="parts", scale=4.0, device="cpu")
+    full, _ = rbs.rope_frequencies(128, device="cpu")
+    turns = 32768 * full.double() / (2 * math.pi)
+    assert factor == pytest.approx(0.1 * math.log(4.0) + 1)
+    # Whole turns decide; the interpolation runs over whole indices, so that pairs next to its ends are left out.
+    assert torch.equal(g[turns > 45], full[turns > 45])
+    assert torch.allclose(g[turns < 0.8], full[turns < 0.8] / 4, rtol=1e-6)
+    ratio = (g / full).double()
+    assert bool((ratio.diff() <= 1e-7).all()) and bool((ratio >= 0.25 - 1e-7).all())
+    for bad in (dict(rot_dim=3), dict(base=1.0), dict(scale=0.5), dict(scaling="other"),
+                dict(scaling="parts", fast=1.0, slow=2.0)):
+        with pytest.raises(ValueError):
+            rbs.rope_frequencies(**bad, device="cpu")
