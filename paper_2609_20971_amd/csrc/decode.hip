@@ -1,95 +1,476 @@
 // Attention of one new token per row over a paged key-value cache.
+//
+// Bound by the read of K and V: each is read once, for all query heads of its KV
+// head (4 H_q d flops for 4 H_kv d bytes a key: 8 flops a byte at a group of 8,
+// where the card has 300).  So everything is arranged for loads in flight:
+//
+// - K and V go from memory to registers as matrix operands, with no LDS and no
+//   barrier in the loop; a wave streams 32 keys at a time and asks for the next
+//   ones as soon as an operand has been used.
+// - S^T = K Q^T and O^T = V^T P^T in 16x16x32 products with the (up to 16) query
+//   heads of a KV head as columns.  Lane l holds column l % 16 of S, keys
+//   4 (l / 16) + r of each 16, which is what the second product takes as its
+//   right operand if V's rows come in the same order: P never leaves its lane.
+//   V's operand needs eight keys of one element; a lane reads eight elements of
+//   eight keys (16 lanes: whole rows) and regroups them with byte permutes.
+// - The keys of all rows together are dealt out evenly: a tile is 128 keys of
+//   one row, and worker w of a KV head takes tiles [T w / W, T (w + 1) / W) of
+//   the T tiles of all rows.  Lengths are on the GPU, so that every workgroup
+//   sums them up for itself.  A row that several workers share is left in parts
+//   (maximum, sum, weighted values in fp32) that a second launch joins, in the
+//   order of the workers: the result depends on the lengths alone.
+//
+// The exponentials' sum and the products are in fp32.  The weights go to the
+// matrix core as two bf16 parts (the value and what its rounding left), off by
+// 2^-16 together: in one part they would be off by half as much as the result's
+// own rounding, and the second product costs nothing here.
 #include "rbs_device.hpp"
 #include "rbs_launch.hpp"
 
 namespace rbs {
 
-size_t decode_workspace_bytes() { return 16; }
+namespace {
 
-// E4M3 code -> fp32, through the hardware conversion of one byte of a word.
-template <int kByte>
-__device__ __forceinline__ float e4m3(uint32_t w) {
-  return __builtin_amdgcn_cvt_f32_fp8((int)w, kByte);
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr int kWaveKeys = 32;
+constexpr int kTile = kWaves * kWaveKeys;  // keys of one row that a workgroup takes at a time
+constexpr int kCols = 16;                  // query heads of a unit
+constexpr int kWorkers = 512;              // workgroups of a launch: two on each of 256 compute units
+constexpr int kPartFloats = kCols * kHeadDim + 2 * kCols;  // weighted values, maxima, sums
+constexpr int kPad = kHeadDim + 4;                         // floats between LDS rows (banks)
+
+struct Work {
+  int units, tiles_of_cols, workers;  // KV heads x column tiles; workers of a unit
+};
+
+__host__ __device__ inline Work work_of_heads(int n_q_heads, int n_kv_heads) {
+  const int group = n_q_heads / n_kv_heads;
+  Work w;
+  w.tiles_of_cols = (group + kCols - 1) / kCols;
+  w.units = n_kv_heads * w.tiles_of_cols;
+  w.workers = kWorkers / w.units > 1 ? kWorkers / w.units : 1;
+  return w;
 }
 
-// One workgroup per (row, query head).  16 lanes hold a key's 128 elements,
-// eight each; a wave takes four keys at a time and the workgroup 16, each group
-// of 16 lanes with a softmax state (running maximum, sum, weighted values) of its
-// own, joined at the end.
-template <bool kFp8>
-__global__ __launch_bounds__(256) void paged_decode_kernel(DecodeArgs a) {
-  const int row = blockIdx.x, h = blockIdx.y, g = h / (a.n_q_heads / a.n_kv_heads);
-  const int lane = threadIdx.x & 63, i = lane & 15, group = threadIdx.x >> 4;
-  const int shift = a.cache.page_shift;
-  int len = a.seq_lens[row];
-  if (len < 0) return;
-  len = min((int64_t)len, (int64_t)a.max_pages << shift);
-  const int32_t* table = a.page_table + (int64_t)row * a.max_pages;
-  float q[8];
-  unpack8(*reinterpret_cast<const uint4*>(a.Q + h * a.q_head + row * a.q_tok + 8 * i), q);
-  const float k_scale = kFp8 && a.cache.amax[g] > 0.f ? a.cache.amax[g] / 448.f : 1.f;
-  const float v_scale = kFp8 && a.cache.amax[a.n_kv_heads + g] > 0.f ? a.cache.amax[a.n_kv_heads + g] / 448.f : 1.f;
-  auto load = [&](const void* base, int64_t at, float* out) __attribute__((always_inline)) {
-    if (kFp8) {
-      const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(base) + at);
-      out[0] = e4m3<0>(w.x); out[1] = e4m3<1>(w.x); out[2] = e4m3<2>(w.x); out[3] = e4m3<3>(w.x);
-      out[4] = e4m3<0>(w.y); out[5] = e4m3<1>(w.y); out[6] = e4m3<2>(w.y); out[7] = e4m3<3>(w.y);
-    } else {
-      unpack8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + at), out);
-    }
-  };
-  float m = -INFINITY, l = 0.f, o[8] = {};
-  for (int j = group; j < len; j += 16) {
-    const int page = min(max(table[j >> shift], 0), a.cache.n_pages - 1);
-    const int64_t at = page * a.cache.page + g * a.cache.head + (int64_t)(j & ((1 << shift) - 1)) * a.cache.tok + 8 * i;
-    float k[8], v[8], x = 0.f;
-    load(a.cache.K, at, k);
-    load(a.cache.V, at, v);
+__device__ __forceinline__ int clamped_length(const DecodeArgs& a, int row) {
+  const int64_t cap = (int64_t)a.max_pages << a.cache.page_shift;
+  const int len = a.seq_lens[row];
+  return (int)(len < cap ? len : cap);
+}
+
+// first[row]: tiles of the rows before it, first[n_rows]: of all.  Each thread
+// sums n_rows / 256 rows, then a scan over the threads.
+__device__ __forceinline__ void tile_offsets(const DecodeArgs& a, int* first, int* sums) {
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int per = (a.n_rows + kThreads - 1) / kThreads, row0 = t * per;
+  int mine = 0;
+  for (int i = 0; i < per && row0 + i < a.n_rows; ++i)
+    mine += (max(clamped_length(a, row0 + i), 0) + kTile - 1) / kTile;
+  int x = mine;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x = fmaf(q[e], k[e], x);
-    x += dpp_f<0xb1>(x);
-    x += dpp_f<0x4e>(x);
-    x += dpp_f<0x124>(x);
-    x += dpp_f<0x128>(x);
-    x *= k_scale * a.scale;
-    const float top = fmaxf(m, x), keep = m == top ? 1.f : expf(m - top), p = x == top ? 1.f : expf(x - top);
-    m = top;
-    l = l * keep + p;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = o[e] * keep + p * v[e];
+  for (int d = 1; d < 64; d <<= 1) {
+    const int u = __shfl_up(x, d);
+    if (lane >= d) x += u;
   }
-  __shared__ float ms[16], ls[16], os[16][kHeadDim];
-  if (i == 0) {
-    ms[group] = m;
-    ls[group] = l;
-  }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) os[group][8 * i + e] = o[e];
+  if (lane == 63) sums[wave] = x;
   __syncthreads();
-  if (threadIdx.x >= kHeadDim) return;
-  const int e = threadIdx.x;
-  float top = -INFINITY, sum = 0.f, out = 0.f;
-  for (int w = 0; w < 16; ++w)
-    if (ls[w] > 0.f) top = fmaxf(top, ms[w]);
-  for (int w = 0; w < 16; ++w) {
-    if (ls[w] == 0.f) continue;  // no key here
-    const float f = ms[w] == top ? 1.f : expf(ms[w] - top);
-    sum += ls[w] * f;
-    out += os[w][e] * f;
+  int before = x - mine;
+  for (int w = 0; w < wave; ++w) before += sums[w];
+  for (int i = 0; i < per && row0 + i < a.n_rows; ++i) {
+    first[row0 + i] = before;
+    before += (max(clamped_length(a, row0 + i), 0) + kTile - 1) / kTile;
   }
-  out = len > 0 ? out * v_scale / sum : 0.f;
-  const __bf16 b = (__bf16)out;
-  a.O[h * a.q_head + row * a.q_tok + e] = __builtin_bit_cast(uint16_t, b);
-  if (e == 0 && a.lse != nullptr) a.lse[(int64_t)h * a.n_rows + row] = len > 0 ? top + logf(sum) : -INFINITY;
+  if (t == kThreads - 1) first[a.n_rows] = before;
+  __syncthreads();
 }
+
+// Worker w of W starts at tile T w / W; the worker that tile t belongs to.
+__device__ __forceinline__ int start_of(int T, int w, int W) { return (int)((int64_t)T * w / W); }
+__device__ __forceinline__ int worker_of(int T, int t, int W) { return (int)(((int64_t)(t + 1) * W - 1) / T); }
+
+__device__ __forceinline__ f32x4 mfma16(const uint4& a, const uint4& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                 0, 0);
+}
+
+// x combined over lanes l, l ^ 16, l ^ 32, l ^ 48.
+template <typename Op>
+__device__ __forceinline__ float over_rows(float x, Op op) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return op(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+
+// bf16 of eight E4M3 codes (exact).
+__device__ __forceinline__ uint4 widen(uint32_t lo, uint32_t hi) {
+  auto pair = [](uint32_t w, bool top) __attribute__((always_inline)) {
+    return top ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.f, true))
+               : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.f, false));
+  };
+  return make_uint4(pair(lo, false), pair(lo, true), pair(hi, false), pair(hi, true));
+}
+
+__device__ __forceinline__ uint32_t word_of(const uint4& v, int i) {
+  return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
+}
+
+// One wave's softmax state over the keys it has seen, for 16 query heads: o[i][r]
+// is element 8 (4 (l / 16) + r) + i of column l % 16, in units of 2^m.
+struct State {
+  float m, l;
+  f32x4 o[8];
+};
+
+template <bool kFp8>
+struct Tile {
+  uint4 k[2][kFp8 ? 2 : 4];   // 16 keys each: lane l % 16's key
+  uint4 v[kFp8 ? 4 : 8];      // keys 16 t + 4 (l / 16) + r of the 32, elements 8 (l % 16) ..
+};
+
+template <bool kFp8>
+struct Stream {
+  const char* K;  // this KV head's
+  const char* V;
+  int64_t page_bytes;
+  int tok_bytes, n_pages, shift, last_page;
+  const int32_t* table;  // this row's
+  uint32_t k_off, v_off;  // this lane's, within 16 keys
+
+  // Byte offset of key j0 (a multiple of 16: within one page).
+  __device__ __forceinline__ int64_t at(int j0) const {
+    const int page = min(max(table[min(j0 >> shift, last_page)], 0), n_pages - 1);
+    return page * page_bytes + (int64_t)(j0 & ((1 << shift) - 1)) * tok_bytes;
+  }
+  __device__ __forceinline__ void load_k(Tile<kFp8>& t, const int64_t* base) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int s = 0; s < (kFp8 ? 2 : 4); ++s)
+        t.k[h][s] = *reinterpret_cast<const uint4*>(K + base[h] + k_off + 64 * s);
+  }
+  __device__ __forceinline__ void load_v(Tile<kFp8>& t, const int64_t* base) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const char* p = V + base[h] + v_off + r * tok_bytes;
+        if (kFp8) {
+          const uint2 w = *reinterpret_cast<const uint2*>(p);
+          uint4& d = t.v[2 * h + (r >> 1)];
+          if (r & 1) {
+            d.z = w.x;
+            d.w = w.y;
+          } else {
+            d.x = w.x;
+            d.y = w.y;
+          }
+        } else {
+          t.v[4 * h + r] = *reinterpret_cast<const uint4*>(p);
+        }
+      }
+  }
+};
+
+// The tiles [begin, end) of a row for this wave: keys kTile t + 32 wave ..
+template <bool kFp8>
+__device__ __forceinline__ void attend_tiles(const Stream<kFp8>& st, const uint4* q, float scale_log2, int len,
+                                             int begin, int end, int wave, State& s) {
+  const int c = (threadIdx.x & 63) >> 4;
+  s.m = -INFINITY;
+  s.l = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto keys_of = [&](int t) __attribute__((always_inline)) { return t * kTile + wave * kWaveKeys; };
+  while (end > begin && keys_of(end - 1) >= len) --end;  // (the row's last tile may have no key for this wave)
+  if (begin >= end) return;
+
+  Tile<kFp8> tile;
+  int64_t base[2], next[2];
+  int j0 = keys_of(begin);
+  base[0] = st.at(j0);
+  base[1] = st.at(j0 + 16);
+  st.load_k(tile, base);
+  st.load_v(tile, base);
+  for (int t = begin; t < end; ++t) {
+    const int j = keys_of(t), jn = keys_of(min(t + 1, end - 1));
+    next[0] = st.at(jn);
+    next[1] = st.at(jn + 16);
+    f32x4 sc[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      sc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (kFp8) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          sc[h] = mfma16(widen(tile.k[h][x].x, tile.k[h][x].y), q[2 * x], sc[h]);
+          sc[h] = mfma16(widen(tile.k[h][x].z, tile.k[h][x].w), q[2 * x + 1], sc[h]);
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) sc[h] = mfma16(tile.k[h][x], q[x], sc[h]);
+      }
+    }
+    if (t + 1 < end) st.load_k(tile, next);
+
+    const bool partial = j + kWaveKeys > len;
+    float x[8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float y = sc[h][r] * scale_log2;
+        x[4 * h + r] = partial && j + 16 * h + 4 * c + r >= len ? -INFINITY : y;
+      }
+    float top = x[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
+    top = over_rows(top, [](float a, float b) { return fmaxf(a, b); });
+    if (__any(top > s.m)) {
+      const float m = fmaxf(s.m, top);
+      const float keep = fast_exp2(s.m - (m == -INFINITY ? 0.f : m));
+      s.m = m;
+      s.l *= keep;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s.o[i] *= keep;
+    }
+    // (Logits of -inf alone, from infinite inputs, weigh nothing.)
+    const float ref = s.m == -INFINITY ? 0.f : s.m;
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const float p0 = fast_exp2(x[e] - ref), p1 = fast_exp2(x[e + 1] - ref);
+      s.l += p0 + p1;
+      typedef __bf16 bf16x2 __attribute__((__vector_size__(2 * sizeof(__bf16))));
+      const bf16x2 h = {(__bf16)p0, (__bf16)p1};
+      hi[e / 2] = __builtin_bit_cast(uint32_t, h);
+      const bf16x2 rest = {(__bf16)(p0 - bf16_lo(hi[e / 2])), (__bf16)(p1 - bf16_hi(hi[e / 2]))};
+      lo[e / 2] = __builtin_bit_cast(uint32_t, rest);
+    }
+    const uint4 p_hi = make_uint4(hi[0], hi[1], hi[2], hi[3]), p_lo = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+
+    uint4 v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (kFp8)
+        v[e] = (e & 1) ? widen(tile.v[e / 2].z, tile.v[e / 2].w) : widen(tile.v[e / 2].x, tile.v[e / 2].y);
+      else
+        v[e] = tile.v[e];
+      if (partial) {  // places past the row's length may hold anything, NaN too
+        const bool in = j + 16 * (e >> 2) + 4 * c + (e & 3) < len;
+        v[e].x = in ? v[e].x : 0u;
+        v[e].y = in ? v[e].y : 0u;
+        v[e].z = in ? v[e].z : 0u;
+        v[e].w = in ? v[e].w : 0u;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t sel = (i & 1) ? 0x07060302u : 0x05040100u;
+      uint32_t w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        w[k] = __builtin_amdgcn_perm(word_of(v[2 * k + 1], i >> 1), word_of(v[2 * k], i >> 1), sel);
+      const uint4 op = make_uint4(w[0], w[1], w[2], w[3]);
+      s.o[i] = mfma16(op, p_hi, s.o[i]);
+      s.o[i] = mfma16(op, p_lo, s.o[i]);
+    }
+    if (t + 1 < end) st.load_v(tile, next);
+  }
+  s.l = over_rows(s.l, [](float a, float b) { return a + b; });
+}
+
+__device__ __forceinline__ uint32_t two_bf16(float a, float b) {
+  typedef __bf16 bf16x2 __attribute__((__vector_size__(2 * sizeof(__bf16))));
+  const bf16x2 v = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// The result of one column of a row: o holds 8 elements from 8 part on of the
+// sum of weighted values, l the sum of weights in units of 2^m.
+__device__ __forceinline__ void write_row(const DecodeArgs& a, int row, int head, int part, const float* o, float m,
+                                          float l, float v_scale) {
+  const float f = v_scale / l;
+  const uint4 w = make_uint4(two_bf16(o[0] * f, o[1] * f), two_bf16(o[2] * f, o[3] * f),
+                             two_bf16(o[4] * f, o[5] * f), two_bf16(o[6] * f, o[7] * f));
+  *reinterpret_cast<uint4*>(a.O + head * a.q_head + row * a.q_tok + 8 * part) = w;
+  if (part == 0 && a.lse != nullptr) a.lse[(int64_t)head * a.n_rows + row] = (m + __log2f(l)) * 0.69314718055994531f;
+}
+
+template <bool kFp8>
+__device__ __forceinline__ float value_scale(const DecodeArgs& a, int g) {
+  if (!kFp8) return 1.f;
+  const float m = a.cache.amax[a.n_kv_heads + g];
+  return m > 0.f ? m / 448.f : 1.f;
+}
+
+template <bool kFp8>
+__global__ __launch_bounds__(kThreads) void paged_decode_kernel(DecodeArgs a) {
+  __shared__ int first[kMaxRows + 1], sums[kWaves];
+  __shared__ __align__(16) float acc[kWaves][kCols][kPad];
+  __shared__ float ms[kWaves][kCols], ls[kWaves][kCols];
+  const int lane = threadIdx.x & 63, c = lane >> 4, col = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Work wk = work_of_heads(a.n_q_heads, a.n_kv_heads);
+  const int unit = blockIdx.x % wk.units, worker = blockIdx.x / wk.units;
+  const int g = unit / wk.tiles_of_cols, group = a.n_q_heads / a.n_kv_heads;
+  const int head0 = g * group + (unit % wk.tiles_of_cols) * kCols;
+  const int cols = min(kCols, (g + 1) * group - head0);
+  tile_offsets(a, first, sums);
+  const int T = first[a.n_rows];
+  int t = start_of(T, worker, wk.workers);
+  const int t_end = start_of(T, worker + 1, wk.workers);
+
+  // Empty rows: zeros, and -inf.
+  for (int row = worker; row < a.n_rows; row += wk.workers) {
+    if (first[row + 1] != first[row] || a.seq_lens[row] != 0) continue;
+    for (int x = threadIdx.x; x < cols * (kHeadDim / 8); x += kThreads)
+      *reinterpret_cast<uint4*>(a.O + (head0 + x / 16) * a.q_head + row * a.q_tok + 8 * (x % 16)) =
+          make_uint4(0u, 0u, 0u, 0u);
+    if (a.lse != nullptr && (int)threadIdx.x < cols)
+      a.lse[(int64_t)(head0 + threadIdx.x) * a.n_rows + row] = -INFINITY;
+  }
+  if (t >= t_end) return;
+
+  constexpr int kBytes = kFp8 ? 1 : 2;
+  Stream<kFp8> st;
+  st.K = static_cast<const char*>(a.cache.K) + g * a.cache.head * kBytes;
+  st.V = static_cast<const char*>(a.cache.V) + g * a.cache.head * kBytes;
+  st.page_bytes = a.cache.page * kBytes;
+  st.tok_bytes = (int)a.cache.tok * kBytes;
+  st.n_pages = a.cache.n_pages;
+  st.shift = a.cache.page_shift;
+  st.k_off = col * st.tok_bytes + 16 * c;
+  st.v_off = 4 * c * st.tok_bytes + 8 * kBytes * col;
+  float scale_log2 = a.scale * kLog2e;
+  if (kFp8 && a.cache.amax[g] > 0.f) scale_log2 *= a.cache.amax[g] / 448.f;
+  const float v_scale = value_scale<kFp8>(a, g);
+
+  int row = seq_of(first, a.n_rows, t);
+  for (bool is_first = true; t < t_end; is_first = false) {
+    while (first[row + 1] <= t) ++row;
+    const int begin = __builtin_amdgcn_readfirstlane(t - first[row]);
+    const int stop = min(first[row + 1], t_end);
+    const int end = __builtin_amdgcn_readfirstlane(stop - first[row]);
+    const int r = __builtin_amdgcn_readfirstlane(row);
+    const int len = __builtin_amdgcn_readfirstlane(clamped_length(a, r));
+    const bool whole = begin == 0 && stop == first[row + 1];
+    st.table = a.page_table + (int64_t)r * a.max_pages;
+    st.last_page = (len - 1) >> st.shift;
+    uint4 q[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      // Elements that the K operand's lane holds: 32 x + 8 c, FP8 64 (x / 2) + 16 c + 8 (x % 2).
+      const int d = kFp8 ? 64 * (x >> 1) + 16 * c + 8 * (x & 1) : 32 * x + 8 * c;
+      q[x] = make_uint4(0u, 0u, 0u, 0u);
+      if (col < cols) q[x] = *reinterpret_cast<const uint4*>(a.Q + (head0 + col) * a.q_head + r * a.q_tok + d);
+    }
+    State s;
+    attend_tiles<kFp8>(st, q, scale_log2, len, begin, end, wave, s);
+
+    // The four waves' states joined.
+    if (c == 0) {
+      ms[wave][col] = s.m;
+      ls[wave][col] = s.l;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float* at = &acc[wave][col][8 * (4 * c + e)];
+      *reinterpret_cast<float4*>(at) = make_float4(s.o[0][e], s.o[1][e], s.o[2][e], s.o[3][e]);
+      *reinterpret_cast<float4*>(at + 4) = make_float4(s.o[4][e], s.o[5][e], s.o[6][e], s.o[7][e]);
+    }
+    __syncthreads();
+    const int hc = threadIdx.x >> 4, part = threadIdx.x & 15;
+    if (hc < cols) {
+      float m = ms[0][hc], l = 0.f, o[8] = {};
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) m = fmaxf(m, ms[w][hc]);
+      const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = fast_exp2(ms[w][hc] - ref);
+        l += ls[w][hc] * f;
+        const float4 x = *reinterpret_cast<const float4*>(&acc[w][hc][8 * part]);
+        const float4 y = *reinterpret_cast<const float4*>(&acc[w][hc][8 * part + 4]);
+        o[0] += x.x * f; o[1] += x.y * f; o[2] += x.z * f; o[3] += x.w * f;
+        o[4] += y.x * f; o[5] += y.y * f; o[6] += y.z * f; o[7] += y.w * f;
+      }
+      if (whole) {
+        write_row(a, r, head0 + hc, part, o, m, l, v_scale);
+      } else {
+        float* slot = a.workspace + (size_t)(2 * blockIdx.x + (is_first ? 0 : 1)) * kPartFloats;
+        *reinterpret_cast<float4*>(slot + hc * kHeadDim + 8 * part) = make_float4(o[0], o[1], o[2], o[3]);
+        *reinterpret_cast<float4*>(slot + hc * kHeadDim + 8 * part + 4) = make_float4(o[4], o[5], o[6], o[7]);
+        if (part == 0) {
+          slot[kCols * kHeadDim + hc] = m;
+          slot[kCols * kHeadDim + kCols + hc] = l;
+        }
+      }
+    }
+    __syncthreads();
+    t = stop;
+  }
+}
+
+// Joins the parts of a row that several workers share: one workgroup per row and
+// unit, 16 threads to a column.
+template <bool kFp8>
+__global__ __launch_bounds__(kThreads) void paged_decode_join_kernel(DecodeArgs a) {
+  __shared__ int first[kMaxRows + 1], sums[kWaves];
+  const Work wk = work_of_heads(a.n_q_heads, a.n_kv_heads);
+  const int row = blockIdx.x, unit = blockIdx.y;
+  const int g = unit / wk.tiles_of_cols, group = a.n_q_heads / a.n_kv_heads;
+  const int head0 = g * group + (unit % wk.tiles_of_cols) * kCols;
+  const int cols = min(kCols, (g + 1) * group - head0);
+  tile_offsets(a, first, sums);
+  const int T = first[a.n_rows], begin = first[row], end = first[row + 1];
+  if (begin == end) return;
+  const int wa = worker_of(T, begin, wk.workers), wb = worker_of(T, end - 1, wk.workers);
+  if (wa == wb) return;
+  const int hc = threadIdx.x >> 4, part = threadIdx.x & 15;
+  if (hc >= cols) return;
+  auto slot_of = [&](int w) __attribute__((always_inline)) -> const float* {
+    const int second = w == wa && start_of(T, w, wk.workers) < begin ? 1 : 0;
+    return a.workspace + (size_t)(2 * (w * wk.units + unit) + second) * kPartFloats;
+  };
+  auto idle = [&](int w) __attribute__((always_inline)) {
+    return start_of(T, w, wk.workers) == start_of(T, w + 1, wk.workers);
+  };
+  float m = -INFINITY;
+  for (int w = wa; w <= wb; ++w)
+    if (!idle(w)) m = fmaxf(m, slot_of(w)[kCols * kHeadDim + hc]);
+  const float ref = m == -INFINITY ? 0.f : m;
+  float l = 0.f, o[8] = {};
+  for (int w = wa; w <= wb; ++w) {
+    if (idle(w)) continue;
+    const float* slot = slot_of(w);
+    const float f = fast_exp2(slot[kCols * kHeadDim + hc] - ref);
+    l += slot[kCols * kHeadDim + kCols + hc] * f;
+    const float4 x = *reinterpret_cast<const float4*>(slot + hc * kHeadDim + 8 * part);
+    const float4 y = *reinterpret_cast<const float4*>(slot + hc * kHeadDim + 8 * part + 4);
+    o[0] += x.x * f; o[1] += x.y * f; o[2] += x.z * f; o[3] += x.w * f;
+    o[4] += y.x * f; o[5] += y.y * f; o[6] += y.z * f; o[7] += y.w * f;
+  }
+  write_row(a, row, head0 + hc, part, o, m, l, value_scale<kFp8>(a, g));
+}
+
+template <bool kFp8>
+hipError_t launch(const DecodeArgs& a, hipStream_t s) {
+  const Work wk = work_of_heads(a.n_q_heads, a.n_kv_heads);
+  hipLaunchKernelGGL(paged_decode_kernel<kFp8>, dim3(wk.units * wk.workers), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL(paged_decode_join_kernel<kFp8>, dim3(a.n_rows, wk.units), dim3(kThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// Two parts for each worker; the workers of all units are kWorkers at most, or
+// one for each unit (units <= query heads).
+size_t decode_workspace_bytes() { return sizeof(float) * 2 * kWorkers * kPartFloats; }
 
 hipError_t launch_paged_decode(const DecodeArgs& a, hipStream_t s) {
-  const dim3 grid(a.n_rows, a.n_q_heads);
-  if (a.cache.amax != nullptr)
-    hipLaunchKernelGGL(paged_decode_kernel<true>, grid, dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL(paged_decode_kernel<false>, grid, dim3(256), 0, s, a);
-  return hipGetLastError();
+  return a.cache.amax != nullptr ? launch<true>(a, s) : launch<false>(a, s);
 }
 
 }  // namespace rbs
