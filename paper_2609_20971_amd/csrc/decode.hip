@@ -39,6 +39,16 @@ constexpr int kCols = 16;                  // query heads of a unit
 constexpr int kWorkers = 512;              // workgroups of a launch: two on each of 256 compute units
 constexpr int kPartFloats = kCols * kHeadDim + 2 * kCols;  // weighted values, maxima, sums
 constexpr int kPad = kHeadDim + 4;                         // floats between LDS rows (banks)
+constexpr int kJoinThreads = 512;
+
+// What a worker leaves for the join, at the workspace's end: where the row whose
+// first tile but not whose last is its own goes on.
+struct Shared {
+  int row;   // -1: no such row
+  int last;  // the row's last worker
+  int slot;  // this worker's part of it, 0 or 1 (the others': 0)
+  int unused;
+};
 
 struct Work {
   int units, tiles_of_cols, workers;  // KV heads x column tiles; workers of a unit
@@ -85,7 +95,8 @@ __device__ __forceinline__ void tile_offsets(const DecodeArgs& a, int* first, in
   __syncthreads();
 }
 
-// Worker w of W starts at tile T w / W; the worker that tile t belongs to.
+// Worker w of W (at most T, so that each has one) starts at tile T w / W; the
+// worker that tile t belongs to.
 __device__ __forceinline__ int start_of(int T, int w, int W) { return (int)((int64_t)T * w / W); }
 __device__ __forceinline__ int worker_of(int T, int t, int W) { return (int)(((int64_t)(t + 1) * W - 1) / T); }
 
@@ -318,9 +329,10 @@ __global__ __launch_bounds__(kThreads) void paged_decode_kernel(DecodeArgs a) {
   const int head0 = g * group + (unit % wk.tiles_of_cols) * kCols;
   const int cols = min(kCols, (g + 1) * group - head0);
   tile_offsets(a, first, sums);
-  const int T = first[a.n_rows];
-  int t = start_of(T, worker, wk.workers);
-  const int t_end = start_of(T, worker + 1, wk.workers);
+  const int T = first[a.n_rows], W = min(wk.workers, T);
+  int t = worker < W ? start_of(T, worker, W) : T;
+  const int t_end = worker < W ? start_of(T, worker + 1, W) : T;
+  Shared shared{-1, 0, 0, 0};
 
   // Empty rows: zeros, and -inf.
   for (int row = worker; row < a.n_rows; row += wk.workers) {
@@ -331,7 +343,6 @@ __global__ __launch_bounds__(kThreads) void paged_decode_kernel(DecodeArgs a) {
     if (a.lse != nullptr && (int)threadIdx.x < cols)
       a.lse[(int64_t)(head0 + threadIdx.x) * a.n_rows + row] = -INFINITY;
   }
-  if (t >= t_end) return;
 
   constexpr int kBytes = kFp8 ? 1 : 2;
   Stream<kFp8> st;
@@ -347,7 +358,7 @@ __global__ __launch_bounds__(kThreads) void paged_decode_kernel(DecodeArgs a) {
   if (kFp8 && a.cache.amax[g] > 0.f) scale_log2 *= a.cache.amax[g] / 448.f;
   const float v_scale = value_scale<kFp8>(a, g);
 
-  int row = seq_of(first, a.n_rows, t);
+  int row = t < t_end ? seq_of(first, a.n_rows, t) : 0;
   for (bool is_first = true; t < t_end; is_first = false) {
     while (first[row + 1] <= t) ++row;
     const int begin = __builtin_amdgcn_readfirstlane(t - first[row]);
@@ -409,57 +420,91 @@ __global__ __launch_bounds__(kThreads) void paged_decode_kernel(DecodeArgs a) {
       }
     }
     __syncthreads();
+    if (begin == 0 && !whole) shared = Shared{r, worker_of(T, first[row + 1] - 1, W), is_first ? 0 : 1, 0};
     t = stop;
   }
+  if (threadIdx.x == 0)
+    reinterpret_cast<Shared*>(a.workspace + (size_t)2 * kWorkers * kPartFloats)[blockIdx.x] = shared;
 }
 
-// Joins the parts of a row that several workers share: one workgroup per row and
-// unit, 16 threads to a column.
+// Joins the parts of the row that starts in worker blockIdx.x and ends in
+// another.  16 threads take a column's 128 elements, and as many sets of 16 as
+// there are threads for take every so many-th part; eight parts' loads are in
+// flight at a time (a row of 128K keys has 128 parts).
 template <bool kFp8>
-__global__ __launch_bounds__(kThreads) void paged_decode_join_kernel(DecodeArgs a) {
-  __shared__ int first[kMaxRows + 1], sums[kWaves];
+__global__ __launch_bounds__(kJoinThreads) void paged_decode_join_kernel(DecodeArgs a) {
+  constexpr int kSets = kJoinThreads / 16, kBatch = 8;
+  __shared__ __align__(16) float acc[kSets][kPad];
+  __shared__ float ms[kSets], ls[kSets];
+  const Shared shared = reinterpret_cast<const Shared*>(a.workspace + (size_t)2 * kWorkers * kPartFloats)[blockIdx.x];
+  if (shared.row < 0) return;
   const Work wk = work_of_heads(a.n_q_heads, a.n_kv_heads);
-  const int row = blockIdx.x, unit = blockIdx.y;
+  const int unit = blockIdx.x % wk.units, wa = blockIdx.x / wk.units;
   const int g = unit / wk.tiles_of_cols, group = a.n_q_heads / a.n_kv_heads;
   const int head0 = g * group + (unit % wk.tiles_of_cols) * kCols;
   const int cols = min(kCols, (g + 1) * group - head0);
-  tile_offsets(a, first, sums);
-  const int T = first[a.n_rows], begin = first[row], end = first[row + 1];
-  if (begin == end) return;
-  const int wa = worker_of(T, begin, wk.workers), wb = worker_of(T, end - 1, wk.workers);
-  if (wa == wb) return;
-  const int hc = threadIdx.x >> 4, part = threadIdx.x & 15;
-  if (hc >= cols) return;
-  auto slot_of = [&](int w) __attribute__((always_inline)) -> const float* {
-    const int second = w == wa && start_of(T, w, wk.workers) < begin ? 1 : 0;
-    return a.workspace + (size_t)(2 * (w * wk.units + unit) + second) * kPartFloats;
-  };
-  auto idle = [&](int w) __attribute__((always_inline)) {
-    return start_of(T, w, wk.workers) == start_of(T, w + 1, wk.workers);
-  };
-  float m = -INFINITY;
-  for (int w = wa; w <= wb; ++w)
-    if (!idle(w)) m = fmaxf(m, slot_of(w)[kCols * kHeadDim + hc]);
-  const float ref = m == -INFINITY ? 0.f : m;
-  float l = 0.f, o[8] = {};
-  for (int w = wa; w <= wb; ++w) {
-    if (idle(w)) continue;
-    const float* slot = slot_of(w);
-    const float f = fast_exp2(slot[kCols * kHeadDim + hc] - ref);
-    l += slot[kCols * kHeadDim + kCols + hc] * f;
-    const float4 x = *reinterpret_cast<const float4*>(slot + hc * kHeadDim + 8 * part);
-    const float4 y = *reinterpret_cast<const float4*>(slot + hc * kHeadDim + 8 * part + 4);
-    o[0] += x.x * f; o[1] += x.y * f; o[2] += x.z * f; o[3] += x.w * f;
-    o[4] += y.x * f; o[5] += y.y * f; o[6] += y.z * f; o[7] += y.w * f;
+  const int set = threadIdx.x >> 4, part = threadIdx.x & 15;
+  const int sets_each = kSets / cols, hc = set % cols, mine = set / cols;  // (sets past cols * sets_each are idle)
+  const int parts = shared.last - wa + 1;
+  const float* base = a.workspace + (size_t)2 * blockIdx.x * kPartFloats;
+  float m = -INFINITY, l = 0.f, o[8] = {};
+  if (mine < sets_each) {
+    for (int p0 = mine; p0 < parts; p0 += kBatch * sets_each) {
+      float pm[kBatch], pl[kBatch];
+      float4 x[kBatch], y[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const int p = min(p0 + i * sets_each, parts - 1);
+        const float* slot = base + (size_t)(2 * p * wk.units + (p == 0 ? shared.slot : 0)) * kPartFloats;
+        pm[i] = slot[kCols * kHeadDim + hc];
+        pl[i] = slot[kCols * kHeadDim + kCols + hc];
+        x[i] = *reinterpret_cast<const float4*>(slot + hc * kHeadDim + 8 * part);
+        y[i] = *reinterpret_cast<const float4*>(slot + hc * kHeadDim + 8 * part + 4);
+      }
+      float top = m;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) top = fmaxf(top, pm[i]);
+      const float ref = top == -INFINITY ? 0.f : top, keep = fast_exp2(m - ref);
+      m = top;
+      l *= keep;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] *= keep;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        if (p0 + i * sets_each >= parts) break;
+        const float f = fast_exp2(pm[i] - ref);
+        l += pl[i] * f;
+        o[0] += x[i].x * f; o[1] += x[i].y * f; o[2] += x[i].z * f; o[3] += x[i].w * f;
+        o[4] += y[i].x * f; o[5] += y[i].y * f; o[6] += y[i].z * f; o[7] += y[i].w * f;
+      }
+    }
   }
-  write_row(a, row, head0 + hc, part, o, m, l, value_scale<kFp8>(a, g));
+  if (part == 0) {
+    ms[set] = m;
+    ls[set] = l;
+  }
+  *reinterpret_cast<float4*>(&acc[set][8 * part]) = make_float4(o[0], o[1], o[2], o[3]);
+  *reinterpret_cast<float4*>(&acc[set][8 * part + 4]) = make_float4(o[4], o[5], o[6], o[7]);
+  __syncthreads();
+  if (mine > 0) return;
+  float top = m;
+  for (int i = 1; i < sets_each; ++i) top = fmaxf(top, ms[hc + i * cols]);
+  const float ref = top == -INFINITY ? 0.f : top;
+  float sum = 0.f, out[8] = {};
+  for (int i = 0; i < sets_each; ++i) {
+    const float f = fast_exp2(ms[hc + i * cols] - ref);
+    sum += ls[hc + i * cols] * f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) out[e] += acc[hc + i * cols][8 * part + e] * f;
+  }
+  write_row(a, shared.row, head0 + hc, part, out, top, sum, value_scale<kFp8>(a, g));
 }
 
 template <bool kFp8>
 hipError_t launch(const DecodeArgs& a, hipStream_t s) {
   const Work wk = work_of_heads(a.n_q_heads, a.n_kv_heads);
   hipLaunchKernelGGL(paged_decode_kernel<kFp8>, dim3(wk.units * wk.workers), dim3(kThreads), 0, s, a);
-  hipLaunchKernelGGL(paged_decode_join_kernel<kFp8>, dim3(a.n_rows, wk.units), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL(paged_decode_join_kernel<kFp8>, dim3(wk.units * wk.workers), dim3(kJoinThreads), 0, s, a);
   return hipGetLastError();
 }
 
@@ -467,7 +512,7 @@ hipError_t launch(const DecodeArgs& a, hipStream_t s) {
 
 // Two parts for each worker; the workers of all units are kWorkers at most, or
 // one for each unit (units <= query heads).
-size_t decode_workspace_bytes() { return sizeof(float) * 2 * kWorkers * kPartFloats; }
+size_t decode_workspace_bytes() { return sizeof(float) * 2 * kWorkers * kPartFloats + kWorkers * sizeof(Shared); }
 
 hipError_t launch_paged_decode(const DecodeArgs& a, hipStream_t s) {
   return a.cache.amax != nullptr ? launch<true>(a, s) : launch<false>(a, s);
