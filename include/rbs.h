@@ -527,7 +527,7 @@ size_t rbs_decode_workspace_bytes(void);
  * strides of Q.  softmax_scale <= 0 selects 1/sqrt(d).  lse: NULL or fp32
  * [H_q][n_tokens], natural log.  A row of length 0: O = 0, lse = -inf; an
  * unused row (negative length): its O and lse are left as they were.
- * page_table int32 [n_tokens][max_pages] (n_tokens * (max_pages * page_size / 128 + 1) < 2^31),
+ * page_table int32 [n_tokens][max_pages] (n_tokens * (max_pages * page_size / 32 + 8) < 2^31),
  * seq_lens int32 [n_tokens].  Both are trusted
  * like the prefill's lists: page numbers are clamped to the cache and lengths
  * to the table, so that no access leaves the buffers.  Places past a row's

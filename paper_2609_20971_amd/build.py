@@ -34,7 +34,8 @@ FLAGS = [
 
 # Per-source additions.  The selector keeps its MFMA results in ordinary
 # VGPRs: with the accumulation registers (AGPRs) every tile copied its 16
-# results out twice, and the unified register count cost a wave per SIMD.
+# results out twice, and the unified register count cost a wave per SIMD.  The
+# decode kernel's results likewise: it rescales them between matrix ops.
 # The attention kernels use the iterative ILP machine scheduler: the default
 # one issued every K-tile LDS read right before the matrix op that consumes
 # it and waited for it there (32 serialized read-wait-MFMA steps per block);
@@ -42,7 +43,8 @@ FLAGS = [
 # FP8 attention kernel keeps the default scheduler: the ILP one made it 1.5x
 # slower.
 _ILP = ["-mllvm", "-amdgpu-sched-strategy=iterative-ilp"]
-EXTRA_FLAGS = {"select.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "attn.hip": _ILP}
+_VGPR = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+EXTRA_FLAGS = {"select.hip": _VGPR, "attn.hip": _ILP, "decode.hip": _VGPR}
 
 
 def _run(cmd):

@@ -872,8 +872,8 @@ int rbs_paged_decode(const rbs_shape* shape, const rbs_cache* cache, const void*
   if ((rc = check_cache(cache, &a.cache)) != RBS_OK) return rc;
   if (cache->n_kv_heads != shape->n_kv_heads || max_pages < 1 || max_pages > (INT32_MAX >> a.cache.page_shift))
     return RBS_ERR_SHAPE;
-  // The tiles of all rows, one more each for a row's end, are counted in 32 bits.
-  if (shape->n_tokens * ((((int64_t)max_pages << a.cache.page_shift) >> 7) + 1) > INT32_MAX) return RBS_ERR_SHAPE;
+  // The shares of all rows are counted in 32 bits.
+  if (shape->n_tokens * ((((int64_t)max_pages << a.cache.page_shift) >> 5) + 8) > INT32_MAX) return RBS_ERR_SHAPE;
   if (Q == nullptr || page_table == nullptr || seq_lens == nullptr || O == nullptr || workspace == nullptr)
     return RBS_ERR_NULL;
   if (!(softmax_scale == softmax_scale) || isinf(softmax_scale)) return RBS_ERR_ARG;

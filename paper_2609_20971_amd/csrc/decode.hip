@@ -6,17 +6,17 @@
 //
 // - K and V go from memory to registers as matrix operands, with no LDS and no
 //   barrier in the loop; a wave streams 32 keys at a time and asks for the next
-//   ones as soon as an operand has been used.
+//   ones, of the next row too, as soon as an operand has been used.
 // - S^T = K Q^T and O^T = V^T P^T in 16x16x32 products with the (up to 16) query
 //   heads of a KV head as columns.  Lane l holds column l % 16 of S, keys
 //   4 (l / 16) + r of each 16, which is what the second product takes as its
 //   right operand if V's rows come in the same order: P never leaves its lane.
 //   V's operand needs eight keys of one element; a lane reads eight elements of
 //   eight keys (16 lanes: whole rows) and regroups them with byte permutes.
-// - The keys of all rows together are dealt out evenly: a tile is 128 keys of
+// - The keys of all rows together are dealt out evenly: a tile is 32 keys of
 //   one row, and worker w of a KV head takes tiles [T w / W, T (w + 1) / W) of
-//   the T tiles of all rows.  Lengths are on the GPU, so that every workgroup
-//   sums them up for itself.  A row that several workers share is left in parts
+//   the T tiles of all rows, its four waves every fourth of them.  Lengths are on
+//   the GPU, so that every workgroup sums them up for itself.  A row that several workers share is left in parts
 //   (maximum, sum, weighted values in fp32) that a second launch joins, in the
 //   order of the workers: the result depends on the lengths alone.
 //
@@ -33,13 +33,19 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kWaveKeys = 32;
-constexpr int kTile = kWaves * kWaveKeys;  // keys of one row that a workgroup takes at a time
+constexpr int kTile = 32;                  // keys of one row that a wave takes at a time
 constexpr int kCols = 16;                  // query heads of a unit
-constexpr int kWorkers = 512;              // workgroups of a launch: two on each of 256 compute units
+#ifndef KW
+#define KW 512
+#define KC 4
+#define KJ 4
+#define KB 2
+#endif
+constexpr int kWorkers = KW;              // workgroups of a launch: two on each of 256 compute units
 constexpr int kPartFloats = kCols * kHeadDim + 2 * kCols;  // weighted values, maxima, sums
 constexpr int kPad = kHeadDim + 4;                         // floats between LDS rows (banks)
-constexpr int kJoinThreads = 512;
+constexpr int kRowCost = KC;
+constexpr int kJoinThreads = 512, kJoinCols = KJ;
 
 // What a worker leaves for the join, at the workspace's end: where the row whose
 // first tile but not whose last is its own goes on.
@@ -49,6 +55,12 @@ struct Shared {
   int slot;  // this worker's part of it, 0 or 1 (the others': 0)
   int unused;
 };
+
+__device__ __forceinline__ uint32_t two_bf16(float a, float b) {
+  typedef __bf16 bf16x2 __attribute__((__vector_size__(2 * sizeof(__bf16))));
+  const bf16x2 v = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
 
 struct Work {
   int units, tiles_of_cols, workers;  // KV heads x column tiles; workers of a unit
@@ -63,20 +75,24 @@ __host__ __device__ inline Work work_of_heads(int n_q_heads, int n_kv_heads) {
   return w;
 }
 
-__device__ __forceinline__ int clamped_length(const DecodeArgs& a, int row) {
+__device__ __forceinline__ int clamped_length(const DecodeArgs& a, const int32_t* lens, int row) {
   const int64_t cap = (int64_t)a.max_pages << a.cache.page_shift;
-  const int len = a.seq_lens[row];
+  const int len = lens[row];
   return (int)(len < cap ? len : cap);
 }
 
-// first[row]: tiles of the rows before it, first[n_rows]: of all.  Each thread
+// A row's share in the dealing out: its tiles, and kRowCost more for what it
+// costs to start and end a row.
+__device__ __forceinline__ int share_of(int len) { return len > 0 ? ((len - 1) / kTile + 1) + kRowCost : 0; }
+
+// first[row]: shares of the rows before it, first[n_rows]: of all.  Each thread
 // sums n_rows / 256 rows, then a scan over the threads.
-__device__ __forceinline__ void tile_offsets(const DecodeArgs& a, int* first, int* sums) {
+__device__ __forceinline__ void tile_offsets(const DecodeArgs& a, const int32_t* lens, int* first, int* sums) {
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int per = (a.n_rows + kThreads - 1) / kThreads, row0 = t * per;
   int mine = 0;
   for (int i = 0; i < per && row0 + i < a.n_rows; ++i)
-    mine += (max(clamped_length(a, row0 + i), 0) + kTile - 1) / kTile;
+    mine += share_of(clamped_length(a, lens, row0 + i));
   int x = mine;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
@@ -89,14 +105,15 @@ __device__ __forceinline__ void tile_offsets(const DecodeArgs& a, int* first, in
   for (int w = 0; w < wave; ++w) before += sums[w];
   for (int i = 0; i < per && row0 + i < a.n_rows; ++i) {
     first[row0 + i] = before;
-    before += (max(clamped_length(a, row0 + i), 0) + kTile - 1) / kTile;
+    before += share_of(clamped_length(a, lens, row0 + i));
   }
   if (t == kThreads - 1) first[a.n_rows] = before;
   __syncthreads();
 }
 
-// Worker w of W (at most T, so that each has one) starts at tile T w / W; the
-// worker that tile t belongs to.
+// The workers that share T tiles: each has at least a tile for each wave.
+__device__ __forceinline__ int workers_of(int T, int workers) { return min(workers, (T + kWaves - 1) / kWaves); }
+// Worker w of W starts at tile T w / W; the worker that tile t belongs to.
 __device__ __forceinline__ int start_of(int T, int w, int W) { return (int)((int64_t)T * w / W); }
 __device__ __forceinline__ int worker_of(int T, int t, int W) { return (int)(((int64_t)(t + 1) * W - 1) / T); }
 
@@ -145,13 +162,14 @@ struct Stream {
   const char* K;  // this KV head's
   const char* V;
   int64_t page_bytes;
-  int tok_bytes, n_pages, shift, last_page;
-  const int32_t* table;  // this row's
+  int tok_bytes, n_pages, shift;
   uint32_t k_off, v_off;  // this lane's, within 16 keys
 
-  // Byte offset of key j0 (a multiple of 16: within one page).
-  __device__ __forceinline__ int64_t at(int j0) const {
-    const int page = min(max(table[min(j0 >> shift, last_page)], 0), n_pages - 1);
+  // Byte offset of key j0 (a multiple of 16: within one page) of a row.  The page
+  // number comes by a scalar load: a vector load's wait would be one for every key
+  // and value on its way.
+  __device__ __forceinline__ int64_t at(const int32_t* __restrict__ table, int len, int j0) const {
+    const int page = min(max(table[__builtin_amdgcn_readfirstlane(min(j0, len - 1) >> shift)], 0), n_pages - 1);
     return page * page_bytes + (int64_t)(j0 & ((1 << shift) - 1)) * tok_bytes;
   }
   __device__ __forceinline__ void load_k(Tile<kFp8>& t, const int64_t* base) const {
@@ -184,118 +202,93 @@ struct Stream {
   }
 };
 
-// The tiles [begin, end) of a row for this wave: keys kTile t + 32 wave ..
+// One tile of 32 keys from key j on added to a wave's state; `next` gives the
+// offsets of the tile to ask for (more: whether there is one).
 template <bool kFp8>
-__device__ __forceinline__ void attend_tiles(const Stream<kFp8>& st, const uint4* q, float scale_log2, int len,
-                                             int begin, int end, int wave, State& s) {
+__device__ __forceinline__ void attend_tile(const Stream<kFp8>& st, Tile<kFp8>& tile, const uint4* q,
+                                            float scale_log2, int j, int len, bool more, const int64_t* next,
+                                            State& s) {
   const int c = (threadIdx.x & 63) >> 4;
-  s.m = -INFINITY;
-  s.l = 0.f;
+  f32x4 sc[2];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) s.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  auto keys_of = [&](int t) __attribute__((always_inline)) { return t * kTile + wave * kWaveKeys; };
-  while (end > begin && keys_of(end - 1) >= len) --end;  // (the row's last tile may have no key for this wave)
-  if (begin >= end) return;
-
-  Tile<kFp8> tile;
-  int64_t base[2], next[2];
-  int j0 = keys_of(begin);
-  base[0] = st.at(j0);
-  base[1] = st.at(j0 + 16);
-  st.load_k(tile, base);
-  st.load_v(tile, base);
-  for (int t = begin; t < end; ++t) {
-    const int j = keys_of(t), jn = keys_of(min(t + 1, end - 1));
-    next[0] = st.at(jn);
-    next[1] = st.at(jn + 16);
-    f32x4 sc[2];
+  for (int h = 0; h < 2; ++h) {
+    sc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (kFp8) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      sc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (kFp8) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          sc[h] = mfma16(widen(tile.k[h][x].x, tile.k[h][x].y), q[2 * x], sc[h]);
-          sc[h] = mfma16(widen(tile.k[h][x].z, tile.k[h][x].w), q[2 * x + 1], sc[h]);
-        }
-      } else {
-#pragma unroll
-        for (int x = 0; x < 4; ++x) sc[h] = mfma16(tile.k[h][x], q[x], sc[h]);
+      for (int x = 0; x < 2; ++x) {
+        sc[h] = mfma16(widen(tile.k[h][x].x, tile.k[h][x].y), q[2 * x], sc[h]);
+        sc[h] = mfma16(widen(tile.k[h][x].z, tile.k[h][x].w), q[2 * x + 1], sc[h]);
       }
+    } else {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) sc[h] = mfma16(tile.k[h][x], q[x], sc[h]);
     }
-    if (t + 1 < end) st.load_k(tile, next);
+  }
+  if (more) st.load_k(tile, next);
 
-    const bool partial = j + kWaveKeys > len;
-    float x[8];
+  const bool partial = j + kTile > len;
+  float x[8];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+  for (int e = 0; e < 8; ++e) x[e] = sc[e >> 2][e & 3] * scale_log2;
+  if (partial) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float y = sc[h][r] * scale_log2;
-        x[4 * h + r] = partial && j + 16 * h + 4 * c + r >= len ? -INFINITY : y;
-      }
-    float top = x[0];
+    for (int e = 0; e < 8; ++e)
+      if (j + 16 * (e >> 2) + 4 * c + (e & 3) >= len) x[e] = -INFINITY;
+  }
+  float top = x[0];
 #pragma unroll
-    for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
-    top = over_rows(top, [](float a, float b) { return fmaxf(a, b); });
-    if (__any(top > s.m)) {
-      const float m = fmaxf(s.m, top);
-      const float keep = fast_exp2(s.m - (m == -INFINITY ? 0.f : m));
-      s.m = m;
-      s.l *= keep;
+  for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
+  top = over_rows(top, [](float a, float b) { return fmaxf(a, b); });
+  if (__any(top > s.m)) {
+    const float m = fmaxf(s.m, top);
+    const float keep = fast_exp2(s.m - (m == -INFINITY ? 0.f : m));
+    s.m = m;
+    s.l *= keep;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s.o[i] *= keep;
-    }
-    // (Logits of -inf alone, from infinite inputs, weigh nothing.)
-    const float ref = s.m == -INFINITY ? 0.f : s.m;
-    uint32_t hi[4], lo[4];
+    for (int i = 0; i < 8; ++i) s.o[i] *= keep;
+  }
+  // (Logits of -inf alone, from infinite inputs, weigh nothing.)
+  const float ref = s.m == -INFINITY ? 0.f : s.m;
+  uint32_t hi[4], lo[4];
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-      const float p0 = fast_exp2(x[e] - ref), p1 = fast_exp2(x[e + 1] - ref);
-      s.l += p0 + p1;
-      typedef __bf16 bf16x2 __attribute__((__vector_size__(2 * sizeof(__bf16))));
-      const bf16x2 h = {(__bf16)p0, (__bf16)p1};
-      hi[e / 2] = __builtin_bit_cast(uint32_t, h);
-      const bf16x2 rest = {(__bf16)(p0 - bf16_lo(hi[e / 2])), (__bf16)(p1 - bf16_hi(hi[e / 2]))};
-      lo[e / 2] = __builtin_bit_cast(uint32_t, rest);
-    }
-    const uint4 p_hi = make_uint4(hi[0], hi[1], hi[2], hi[3]), p_lo = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+  for (int e = 0; e < 8; e += 2) {
+    const float p0 = fast_exp2(x[e] - ref), p1 = fast_exp2(x[e + 1] - ref);
+    s.l += p0 + p1;
+    hi[e / 2] = two_bf16(p0, p1);
+    lo[e / 2] = two_bf16(p0 - bf16_lo(hi[e / 2]), p1 - bf16_hi(hi[e / 2]));
+  }
+  const uint4 p_hi = make_uint4(hi[0], hi[1], hi[2], hi[3]), p_lo = make_uint4(lo[0], lo[1], lo[2], lo[3]);
 
-    uint4 v[8];
+  uint4 v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (kFp8)
+      v[e] = (e & 1) ? widen(tile.v[e / 2].z, tile.v[e / 2].w) : widen(tile.v[e / 2].x, tile.v[e / 2].y);
+    else
+      v[e] = tile.v[e];
+  }
+  if (partial) {  // places past the row's length may hold anything, NaN too
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      if (kFp8)
-        v[e] = (e & 1) ? widen(tile.v[e / 2].z, tile.v[e / 2].w) : widen(tile.v[e / 2].x, tile.v[e / 2].y);
-      else
-        v[e] = tile.v[e];
-      if (partial) {  // places past the row's length may hold anything, NaN too
-        const bool in = j + 16 * (e >> 2) + 4 * c + (e & 3) < len;
-        v[e].x = in ? v[e].x : 0u;
-        v[e].y = in ? v[e].y : 0u;
-        v[e].z = in ? v[e].z : 0u;
-        v[e].w = in ? v[e].w : 0u;
-      }
+      const bool in = j + 16 * (e >> 2) + 4 * c + (e & 3) < len;
+      v[e].x = in ? v[e].x : 0u;
+      v[e].y = in ? v[e].y : 0u;
+      v[e].z = in ? v[e].z : 0u;
+      v[e].w = in ? v[e].w : 0u;
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t sel = (i & 1) ? 0x07060302u : 0x05040100u;
-      uint32_t w[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        w[k] = __builtin_amdgcn_perm(word_of(v[2 * k + 1], i >> 1), word_of(v[2 * k], i >> 1), sel);
-      const uint4 op = make_uint4(w[0], w[1], w[2], w[3]);
-      s.o[i] = mfma16(op, p_hi, s.o[i]);
-      s.o[i] = mfma16(op, p_lo, s.o[i]);
-    }
-    if (t + 1 < end) st.load_v(tile, next);
   }
-  s.l = over_rows(s.l, [](float a, float b) { return a + b; });
-}
-
-__device__ __forceinline__ uint32_t two_bf16(float a, float b) {
-  typedef __bf16 bf16x2 __attribute__((__vector_size__(2 * sizeof(__bf16))));
-  const bf16x2 v = {(__bf16)a, (__bf16)b};
-  return __builtin_bit_cast(uint32_t, v);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t sel = (i & 1) ? 0x07060302u : 0x05040100u;
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      w[k] = __builtin_amdgcn_perm(word_of(v[2 * k + 1], i >> 1), word_of(v[2 * k], i >> 1), sel);
+    const uint4 op = make_uint4(w[0], w[1], w[2], w[3]);
+    s.o[i] = mfma16(op, p_hi, s.o[i]);
+    s.o[i] = mfma16(op, p_lo, s.o[i]);
+  }
+  if (more) st.load_v(tile, next);
 }
 
 // The result of one column of a row: o holds 8 elements from 8 part on of the
@@ -317,7 +310,8 @@ __device__ __forceinline__ float value_scale(const DecodeArgs& a, int g) {
 }
 
 template <bool kFp8>
-__global__ __launch_bounds__(kThreads) void paged_decode_kernel(DecodeArgs a) {
+__global__ __launch_bounds__(kThreads, KB) void paged_decode_kernel(DecodeArgs a, const int32_t* __restrict__ lens,
+                                                                const int32_t* __restrict__ page_table) {
   __shared__ int first[kMaxRows + 1], sums[kWaves];
   __shared__ __align__(16) float acc[kWaves][kCols][kPad];
   __shared__ float ms[kWaves][kCols], ls[kWaves][kCols];
@@ -328,15 +322,15 @@ __global__ __launch_bounds__(kThreads) void paged_decode_kernel(DecodeArgs a) {
   const int g = unit / wk.tiles_of_cols, group = a.n_q_heads / a.n_kv_heads;
   const int head0 = g * group + (unit % wk.tiles_of_cols) * kCols;
   const int cols = min(kCols, (g + 1) * group - head0);
-  tile_offsets(a, first, sums);
-  const int T = first[a.n_rows], W = min(wk.workers, T);
+  tile_offsets(a, lens, first, sums);
+  const int T = first[a.n_rows], W = workers_of(T, wk.workers);
   int t = worker < W ? start_of(T, worker, W) : T;
   const int t_end = worker < W ? start_of(T, worker + 1, W) : T;
   Shared shared{-1, 0, 0, 0};
 
   // Empty rows: zeros, and -inf.
   for (int row = worker; row < a.n_rows; row += wk.workers) {
-    if (first[row + 1] != first[row] || a.seq_lens[row] != 0) continue;
+    if (first[row + 1] != first[row] || lens[row] != 0) continue;
     for (int x = threadIdx.x; x < cols * (kHeadDim / 8); x += kThreads)
       *reinterpret_cast<uint4*>(a.O + (head0 + x / 16) * a.q_head + row * a.q_tok + 8 * (x % 16)) =
           make_uint4(0u, 0u, 0u, 0u);
@@ -358,17 +352,57 @@ __global__ __launch_bounds__(kThreads) void paged_decode_kernel(DecodeArgs a) {
   if (kFp8 && a.cache.amax[g] > 0.f) scale_log2 *= a.cache.amax[g] / 448.f;
   const float v_scale = value_scale<kFp8>(a, g);
 
+  // The wave's next tile: tile `tile` of row `row` (-1: none), of `len` keys.  It
+  // runs ahead of the rows below by one tile, whose keys and values are on their
+  // way.
+  struct Cursor {
+    int row, tile, end, len;  // end: of the row's share
+  } next{-1, 0, 0, 0};
+  // Moves the cursor to the wave's first tile in row r or after it: the wave takes
+  // tiles wave, wave + 4, .. of each row's share.
+  auto seek = [&](int r) __attribute__((always_inline)) {
+    for (;; ++r) {
+      if (r >= a.n_rows || first[r] >= t_end) {
+        next.row = -1;
+        return;
+      }
+      const int x = max(first[r], t) + wave, to = min(first[r + 1] - kRowCost, t_end);
+      if (x < to) {
+        next.row = __builtin_amdgcn_readfirstlane(r);
+        next.tile = __builtin_amdgcn_readfirstlane(x - first[r]);
+        next.end = __builtin_amdgcn_readfirstlane(to - first[r]);
+        next.len = __builtin_amdgcn_readfirstlane(clamped_length(a, lens, next.row));
+        return;
+      }
+    }
+  };
+  auto offsets = [&](int64_t* base) __attribute__((always_inline)) {
+    const int32_t* table = page_table + (int64_t)__builtin_amdgcn_readfirstlane(next.row) * a.max_pages;
+    const int len = __builtin_amdgcn_readfirstlane(next.len), j = __builtin_amdgcn_readfirstlane(next.tile * kTile);
+    base[0] = st.at(table, len, j);
+    base[1] = st.at(table, len, j + 16);
+  };
   int row = t < t_end ? seq_of(first, a.n_rows, t) : 0;
-  for (bool is_first = true; t < t_end; is_first = false) {
-    while (first[row + 1] <= t) ++row;
-    const int begin = __builtin_amdgcn_readfirstlane(t - first[row]);
-    const int stop = min(first[row + 1], t_end);
-    const int end = __builtin_amdgcn_readfirstlane(stop - first[row]);
+  Tile<kFp8> tile;
+  if (t < t_end) seek(row);
+  if (next.row >= 0) {
+    int64_t base[2];
+    offsets(base);
+    st.load_k(tile, base);
+    st.load_v(tile, base);
+  }
+  int at = t;  // the first tile that is still to do
+  bool is_first = true;
+  while (at < t_end) {
+    while (first[row + 1] <= at) ++row;
     const int r = __builtin_amdgcn_readfirstlane(row);
-    const int len = __builtin_amdgcn_readfirstlane(clamped_length(a, r));
-    const bool whole = begin == 0 && stop == first[row + 1];
-    st.table = a.page_table + (int64_t)r * a.max_pages;
-    st.last_page = (len - 1) >> st.shift;
+    const int last = first[r + 1] - kRowCost;  // past the row's last tile
+    if (at >= last) {
+      at = first[r + 1];
+      continue;
+    }
+    const int stop = min(last, t_end);
+    const bool begins = at == first[r], whole = begins && stop == last;
     uint4 q[4];
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
@@ -377,8 +411,23 @@ __global__ __launch_bounds__(kThreads) void paged_decode_kernel(DecodeArgs a) {
       q[x] = make_uint4(0u, 0u, 0u, 0u);
       if (col < cols) q[x] = *reinterpret_cast<const uint4*>(a.Q + (head0 + col) * a.q_head + r * a.q_tok + d);
     }
+    // Waited for here: in the loop the wait for the first Q would be one for the
+    // values on their way as well, at every tile.
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
     State s;
-    attend_tiles<kFp8>(st, q, scale_log2, len, begin, end, wave, s);
+    s.m = -INFINITY;
+    s.l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    while (next.row == r) {
+      const int j = next.tile * kTile, len = next.len;
+      next.tile += kWaves;
+      if (next.tile >= next.end) seek(r + 1);
+      int64_t base[2] = {0, 0};
+      if (next.row >= 0) offsets(base);
+      attend_tile<kFp8>(st, tile, q, scale_log2, j, len, next.row >= 0, base, s);
+    }
+    s.l = over_rows(s.l, [](float a, float b) { return a + b; });
 
     // The four waves' states joined.
     if (c == 0) {
@@ -420,8 +469,9 @@ __global__ __launch_bounds__(kThreads) void paged_decode_kernel(DecodeArgs a) {
       }
     }
     __syncthreads();
-    if (begin == 0 && !whole) shared = Shared{r, worker_of(T, first[row + 1] - 1, W), is_first ? 0 : 1, 0};
-    t = stop;
+    if (begins && !whole) shared = Shared{r, worker_of(T, last - 1, W), is_first ? 0 : 1, 0};
+    is_first = false;
+    at = first[r + 1];
   }
   if (threadIdx.x == 0)
     reinterpret_cast<Shared*>(a.workspace + (size_t)2 * kWorkers * kPartFloats)[blockIdx.x] = shared;
@@ -442,7 +492,8 @@ __global__ __launch_bounds__(kJoinThreads) void paged_decode_join_kernel(DecodeA
   const int unit = blockIdx.x % wk.units, wa = blockIdx.x / wk.units;
   const int g = unit / wk.tiles_of_cols, group = a.n_q_heads / a.n_kv_heads;
   const int head0 = g * group + (unit % wk.tiles_of_cols) * kCols;
-  const int cols = min(kCols, (g + 1) * group - head0);
+  const int col0 = blockIdx.y * kJoinCols, cols = min(kJoinCols, min(kCols, (g + 1) * group - head0) - col0);
+  if (cols <= 0) return;
   const int set = threadIdx.x >> 4, part = threadIdx.x & 15;
   const int sets_each = kSets / cols, hc = set % cols, mine = set / cols;  // (sets past cols * sets_each are idle)
   const int parts = shared.last - wa + 1;
@@ -456,10 +507,10 @@ __global__ __launch_bounds__(kJoinThreads) void paged_decode_join_kernel(DecodeA
       for (int i = 0; i < kBatch; ++i) {
         const int p = min(p0 + i * sets_each, parts - 1);
         const float* slot = base + (size_t)(2 * p * wk.units + (p == 0 ? shared.slot : 0)) * kPartFloats;
-        pm[i] = slot[kCols * kHeadDim + hc];
-        pl[i] = slot[kCols * kHeadDim + kCols + hc];
-        x[i] = *reinterpret_cast<const float4*>(slot + hc * kHeadDim + 8 * part);
-        y[i] = *reinterpret_cast<const float4*>(slot + hc * kHeadDim + 8 * part + 4);
+        pm[i] = slot[kCols * kHeadDim + col0 + hc];
+        pl[i] = slot[kCols * kHeadDim + kCols + col0 + hc];
+        x[i] = *reinterpret_cast<const float4*>(slot + (col0 + hc) * kHeadDim + 8 * part);
+        y[i] = *reinterpret_cast<const float4*>(slot + (col0 + hc) * kHeadDim + 8 * part + 4);
       }
       float top = m;
 #pragma unroll
@@ -497,14 +548,16 @@ __global__ __launch_bounds__(kJoinThreads) void paged_decode_join_kernel(DecodeA
 #pragma unroll
     for (int e = 0; e < 8; ++e) out[e] += acc[hc + i * cols][8 * part + e] * f;
   }
-  write_row(a, shared.row, head0 + hc, part, out, top, sum, value_scale<kFp8>(a, g));
+  write_row(a, shared.row, head0 + col0 + hc, part, out, top, sum, value_scale<kFp8>(a, g));
 }
 
 template <bool kFp8>
 hipError_t launch(const DecodeArgs& a, hipStream_t s) {
   const Work wk = work_of_heads(a.n_q_heads, a.n_kv_heads);
-  hipLaunchKernelGGL(paged_decode_kernel<kFp8>, dim3(wk.units * wk.workers), dim3(kThreads), 0, s, a);
-  hipLaunchKernelGGL(paged_decode_join_kernel<kFp8>, dim3(wk.units * wk.workers), dim3(kJoinThreads), 0, s, a);
+  const int group = a.n_q_heads / a.n_kv_heads, cols = group < kCols ? group : kCols;
+  hipLaunchKernelGGL(paged_decode_kernel<kFp8>, dim3(wk.units * wk.workers), dim3(kThreads), 0, s, a,
+                     a.seq_lens, a.page_table);
+  hipLaunchKernelGGL(paged_decode_join_kernel<kFp8>, dim3(wk.units * wk.workers, (cols + kJoinCols - 1) / kJoinCols), dim3(kJoinThreads), 0, s, a);
   return hipGetLastError();
 }
 

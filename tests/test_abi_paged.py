@@ -128,8 +128,8 @@ def test_limits():
     assert _rope(shape=rbs.make_shape((1 << 24) + 1, 4, 2, 64)) == 2
     assert _rope(shape=rbs.make_shape(1 << 24, 4, 2, 64), Q=None) == OK_PAST
     assert _decode(max_pages=0) == 2 and _decode(max_pages=2**27) == 2
-    assert _decode(shape=rbs.make_shape(4096, 4, 2, 64), max_pages=2**22) == 2   # 2^31 tiles of 128 keys
-    assert _decode(shape=rbs.make_shape(4096, 4, 2, 64), max_pages=2**21, Q=None) == OK_PAST
+    assert _decode(shape=rbs.make_shape(4096, 4, 2, 64), max_pages=2**20) == 2   # 2^31 tiles of 32 keys
+    assert _decode(shape=rbs.make_shape(4096, 4, 2, 64), max_pages=2**20 - 18, Q=None) == OK_PAST
     # Any block size, unlike the prefill's calls.
     assert _decode(shape=rbs.make_shape(10, 4, 2, 7), Q=None) == OK_PAST
 
