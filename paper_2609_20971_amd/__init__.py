@@ -81,7 +81,6 @@ from ._paged import (  # noqa: F401
     Pages,
     PageStep,
     Rope,
-    decode_workspace,
     rbs_cache,
     rbs_decode_workspace_bytes,
     rbs_paged_decode,

@@ -77,13 +77,27 @@ def declare(lib):
     lib.rbs_paged_decode.restype = ctypes.c_int
 
 
-def _on(device: int, stream, call):
-    """call(stream handle) with `device` current: a launch goes to the current
-    device, and the default stream is that device's."""
-    if device == torch.cuda.current_device():
-        return call(L._stream(stream))
+def _handle(device: int, stream):
+    # (The stream object that torch.cuda.current_stream() makes costs 2.7 us, as much as a launch.)
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else L._stream(stream)
+
+
+def _on(device: int, stream, call, *args):
+    """call(*args, stream handle) with `device` current: a launch goes to the
+    current device, and the default stream is that device's."""
+    if device == torch._C._cuda_getDevice():
+        return call(*args, _handle(device, stream))
     with torch.cuda.device(device):
-        return call(L._stream(stream))
+        return call(*args, _handle(device, stream))
+
+
+def _same_gpu(t, *named) -> int:
+    """L._on_gpu of the named tensors, of which t is one, short where all is well."""
+    dev = t.get_device()
+    for _, x in named:
+        if x is not None and (x.get_device() != dev or dev < 0):
+            return L._on_gpu(*named)
+    return dev
 
 
 def _one_dimensional(name, t, dtype, n=None):
@@ -152,6 +166,7 @@ class Pages:
     page_size: int
     c: rbs_pages = field(init=False, repr=False, compare=False)
     device: int = field(init=False, repr=False, compare=False)
+    state: tuple = field(init=False, repr=False, compare=False)  # addresses of seq_lens and n_free
 
     def __post_init__(self):
         i32, table = torch.int32, self.page_table
@@ -166,6 +181,7 @@ class Pages:
         object.__setattr__(self, "c", rbs_pages(table.shape[0], table.shape[1], self.free_pages.numel(),
                                                 self.page_size, table.data_ptr(), self.free_pages.data_ptr()))
         object.__setattr__(self, "device", dev)
+        object.__setattr__(self, "state", (self.seq_lens.data_ptr(), self.n_free.data_ptr()))
 
     @classmethod
     def allocate(cls, n_rows: int, max_pages: int, n_pages: int, page_size: int, device="cuda") -> "Pages":
@@ -189,6 +205,8 @@ class PageStep:
     slots: torch.Tensor      # [max_tokens]
     status: torch.Tensor     # [1]
     device: int = field(init=False, repr=False, compare=False)
+    max_tokens: int = field(init=False, repr=False, compare=False)
+    out: tuple = field(init=False, repr=False, compare=False)  # the tensors' addresses
 
     def __post_init__(self):
         i32 = torch.int32
@@ -201,6 +219,9 @@ class PageStep:
         object.__setattr__(self, "device", L._on_gpu(
             ("step.seq_lens", self.seq_lens), ("step.n_free", self.n_free), ("step.cu_tokens", self.cu_tokens),
             ("step.positions", self.positions), ("step.slots", self.slots), ("step.status", self.status)))
+        object.__setattr__(self, "max_tokens", self.positions.numel())
+        object.__setattr__(self, "out", tuple(t.data_ptr() for t in (
+            self.seq_lens, self.n_free, self.cu_tokens, self.positions, self.slots, self.status)))
 
     @classmethod
     def allocate(cls, pages: Pages, max_tokens: int, in_place: bool = True) -> "PageStep":
@@ -233,13 +254,11 @@ def rbs_pages_extend(pages: Pages, new_tokens=None, max_tokens: int | None = Non
             raise ValueError(f"step is on cuda:{step.device}, pages on cuda:{pages.device}")
         if step.seq_lens.shape != pages.seq_lens.shape:
             raise ValueError(f"step is for {step.seq_lens.numel()} rows, pages has {pages.n_rows}")
-        if max_tokens is not None and max_tokens != step.positions.numel():
-            raise ValueError(f"max_tokens = {max_tokens} disagrees with the step's {step.positions.numel()}")
-    lib = L.load()
-    L._check("rbs_pages_extend", _on(pages.device, stream, lambda s: lib.rbs_pages_extend(
-        pages.c, pages.seq_lens.data_ptr(), L._ptr(new_tokens), pages.n_free.data_ptr(), step.positions.numel(),
-        step.seq_lens.data_ptr(), step.n_free.data_ptr(), step.cu_tokens.data_ptr(), step.positions.data_ptr(),
-        step.slots.data_ptr(), step.status.data_ptr(), s)))
+        if max_tokens is not None and max_tokens != step.max_tokens:
+            raise ValueError(f"max_tokens = {max_tokens} disagrees with the step's {step.max_tokens}")
+    lens, n_free = pages.state
+    L._check("rbs_pages_extend", _on(pages.device, stream, L.load().rbs_pages_extend, pages.c, lens,
+                                     L._ptr(new_tokens), n_free, step.max_tokens, *step.out))
     return step
 
 
@@ -254,9 +273,8 @@ def rbs_pages_release(pages: Pages, released, status=None, stream=None) -> torch
     L._on_gpu(("page_table", pages.page_table), ("released", released), ("status", status))
     if status is None:
         status = torch.empty(1, dtype=torch.int32, device=pages.page_table.device)
-    lib = L.load()
-    L._check("rbs_pages_release", _on(pages.device, stream, lambda s: lib.rbs_pages_release(
-        pages.c, released.data_ptr(), pages.seq_lens.data_ptr(), pages.n_free.data_ptr(), status.data_ptr(), s)))
+    L._check("rbs_pages_release", _on(pages.device, stream, L.load().rbs_pages_release, pages.c, released.data_ptr(),
+                                      *pages.state, status.data_ptr()))
     return status
 
 
@@ -333,7 +351,6 @@ def rbs_qk_norm_rope(shape: L.rbs_shape, rope: Rope, Q, K, positions, V=None, ca
     qs = L._heads_tokens("Q", Q, hq, n, d)
     ks = L._heads_tokens("K", K, hkv, n, d)
     L._check_tensor("positions", positions, torch.int32, (n,))
-    dev = Q.get_device()
     if cache is not None:
         if not isinstance(cache, PagedCache):
             raise ValueError("cache must be a PagedCache")
@@ -342,13 +359,13 @@ def rbs_qk_norm_rope(shape: L.rbs_shape, rope: Rope, Q, K, positions, V=None, ca
         if L._heads_tokens("V", V, hkv, n, d) != ks:
             raise ValueError(f"V strides {V.stride()[:2]} differ from K strides {ks}; the library takes one pair")
         L._check_tensor("slots", slots, torch.int32, (n,))
-        if cache.device != dev or V.get_device() != dev or slots.get_device() != dev:
-            L._on_gpu(("Q", Q), ("V", V), ("slots", slots), ("cache.K", cache.K))
     if Q_out is not None:
         L._heads_tokens("Q_out", Q_out, hq, n, d)
     if K_out is not None:
         L._heads_tokens("K_out", K_out, hkv, n, d)
-    L._on_gpu(("Q", Q), ("K", K), ("positions", positions), ("Q_out", Q_out), ("K_out", K_out))
+    dev = _same_gpu(Q, ("Q", Q), ("K", K), ("positions", positions), ("V", V if cache is not None else None),
+                    ("slots", slots if cache is not None else None), ("cache.K", None if cache is None else cache.K),
+                    ("Q_out", Q_out), ("K_out", K_out))
     if rope.device is not None and rope.device != dev:
         raise ValueError(f"rope is on cuda:{rope.device}, the other arguments on cuda:{dev}")
     if Q_out is None:
@@ -358,10 +375,9 @@ def rbs_qk_norm_rope(shape: L.rbs_shape, rope: Rope, Q, K, positions, V=None, ca
     sh = L._with_strides(shape, q=qs, kv=ks)
     out = L.rbs_shape(n, hq, hkv, d, shape.block_size, *Q_out.stride()[:2],
                       *(ks if K_out is None else K_out.stride()[:2]))
-    lib = L.load()
-    L._check("rbs_qk_norm_rope", _on(dev, stream, lambda s: lib.rbs_qk_norm_rope(
-        sh, out, rope.c, Q.data_ptr(), K.data_ptr(), L._ptr(V), positions.data_ptr(), Q_out.data_ptr(),
-        L._ptr(K_out), None if cache is None else cache.c, L._ptr(slots), s)))
+    L._check("rbs_qk_norm_rope", _on(dev, stream, L.load().rbs_qk_norm_rope, sh, out, rope.c, Q.data_ptr(),
+                                     K.data_ptr(), L._ptr(V), positions.data_ptr(), Q_out.data_ptr(), L._ptr(K_out),
+                                     None if cache is None else cache.c, L._ptr(slots)))
     return Q_out, K_out
 
 
@@ -372,19 +388,17 @@ def rbs_decode_workspace_bytes() -> int:
     return int(L.load().rbs_decode_workspace_bytes())
 
 
-def decode_workspace(device, stream=None) -> torch.Tensor:
-    """A workspace of rbs_paged_decode: one per (device, stream), whose calls are
-    ordered; a new one while the stream is being captured, which belongs to the
-    graph's memory (graphs captured on one stream may run side by side)."""
-    index = torch.device(device).index
-    index = torch.cuda.current_device() if index is None else index
-    key = (index, L._stream(stream))
-    ws = _decode_workspaces.get(key)
-    capturing = torch.cuda.is_current_stream_capturing()
-    if ws is None or capturing:
-        ws = torch.empty(rbs_decode_workspace_bytes() // 4, dtype=torch.float32, device=torch.device("cuda", index))
+def _auto_workspace(device: int, handle: int) -> torch.Tensor:
+    """The workspace of a (device, stream): calls on one stream are ordered, so
+    they may share it.  While the current stream is being captured, a new one,
+    which belongs to the graph's memory: graphs that were captured on one stream
+    may run side by side."""
+    ws = _decode_workspaces.get((device, handle))
+    if ws is None or torch.cuda.is_current_stream_capturing():
+        capturing = torch.cuda.is_current_stream_capturing()
+        ws = torch.empty(rbs_decode_workspace_bytes() // 4, dtype=torch.float32, device=torch.device("cuda", device))
         if not capturing:
-            _decode_workspaces[key] = ws
+            _decode_workspaces[device, handle] = ws
     return ws
 
 
@@ -404,27 +418,27 @@ def rbs_paged_decode(shape: L.rbs_shape, Q, cache: PagedCache, page_table, seq_l
         L._check_out(O, Q)
     if lse is not None:
         L._check_tensor("lse", lse, torch.float32, (hq, n))
-    dev = L._on_gpu(("cache.K", cache.K), ("Q", Q), ("page_table", page_table), ("seq_lens", seq_lens), ("O", O),
+    dev = _same_gpu(Q, ("cache.K", cache.K), ("Q", Q), ("page_table", page_table), ("seq_lens", seq_lens), ("O", O),
                     ("lse", lse))
     if O is None:
-        O = L._like_q(Q)
-    sh = L._with_strides(shape, q=qs)
-    lib = L.load()
-
-    def call(s):
-        if isinstance(workspace, str):
-            if workspace != L.AUTO:
-                raise ValueError(f"workspace must be AUTO or a tensor, not {workspace!r}")
-            ws = decode_workspace(Q.device, stream)
-        else:
-            ws = workspace
-            if not isinstance(ws, torch.Tensor) or ws.get_device() != dev or not ws.is_contiguous():
-                raise ValueError("workspace must be AUTO or a contiguous tensor on the inputs' GPU")
-            if ws.numel() * ws.element_size() < rbs_decode_workspace_bytes():
-                raise ValueError("workspace is smaller than rbs_decode_workspace_bytes()")
-        return lib.rbs_paged_decode(sh, cache.c, Q.data_ptr(), page_table.data_ptr(), page_table.shape[1],
-                                    seq_lens.data_ptr(), float(softmax_scale), O.data_ptr(), L._ptr(lse),
-                                    ws.data_ptr(), s)
-
-    L._check("rbs_paged_decode", _on(dev, stream, call))
+        O = torch.empty_like(Q)
+        if O.stride() != Q.stride():
+            O = L._like_q(Q)
+    if isinstance(workspace, str):
+        if workspace != L.AUTO:
+            raise ValueError(f"workspace must be AUTO or a tensor, not {workspace!r}")
+    elif not isinstance(workspace, torch.Tensor) or workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be AUTO or a contiguous tensor on the inputs' GPU")
+    elif workspace.numel() * workspace.element_size() < rbs_decode_workspace_bytes():
+        raise ValueError("workspace is smaller than rbs_decode_workspace_bytes()")
+    L._check("rbs_paged_decode", _on(dev, stream, _decode, L._with_strides(shape, q=qs), cache, Q, page_table, seq_lens,
+                                     softmax_scale, O, lse, workspace, dev))
     return O
+
+
+def _decode(shape, cache, Q, page_table, seq_lens, softmax_scale, O, lse, workspace, dev, s):
+    # (With the inputs' device current, which tells whether its stream is being captured.)
+    ws = _auto_workspace(dev, s) if isinstance(workspace, str) else workspace
+    return L.load().rbs_paged_decode(shape, cache.c, Q.data_ptr(), page_table.data_ptr(), page_table.shape[1],
+                                     seq_lens.data_ptr(), float(softmax_scale), O.data_ptr(), L._ptr(lse),
+                                     ws.data_ptr(), s)

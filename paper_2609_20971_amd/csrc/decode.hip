@@ -5,7 +5,7 @@
 // where the card has 300).  So everything is arranged for loads in flight:
 //
 // - K and V go from memory to registers as matrix operands, with no LDS and no
-//   barrier in the loop; a wave streams 32 keys at a time and asks for the next
+//   barrier in the loop; a wave streams 32 keys at a time (64 in FP8) and asks for the next
 //   ones, of the next row too, as soon as an operand has been used.
 // - S^T = K Q^T and O^T = V^T P^T in 16x16x32 products with the (up to 16) query
 //   heads of a KV head as columns.  Lane l holds column l % 16 of S, keys
@@ -13,7 +13,7 @@
 //   right operand if V's rows come in the same order: P never leaves its lane.
 //   V's operand needs eight keys of one element; a lane reads eight elements of
 //   eight keys (16 lanes: whole rows) and regroups them with byte permutes.
-// - The keys of all rows together are dealt out evenly: a tile is 32 keys of
+// - The keys of all rows together are dealt out evenly: a tile is 32 (64) keys of
 //   one row, and worker w of a KV head takes tiles [T w / W, T (w + 1) / W) of
 //   the T tiles of all rows, its four waves every fourth of them.  Lengths are on
 //   the GPU, so that every workgroup sums them up for itself.  A row that several workers share is left in parts
@@ -33,7 +33,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kTile = 32;                  // keys of one row that a wave takes at a time
+// Keys of one row that a wave takes at a time: 16 KB of K and V in either type.
+template <bool kFp8>
+constexpr int kTile = kFp8 ? 64 : 32;
 constexpr int kCols = 16;                  // query heads of a unit
 #ifndef KW
 #define KW 512
@@ -83,16 +85,20 @@ __device__ __forceinline__ int clamped_length(const DecodeArgs& a, const int32_t
 
 // A row's share in the dealing out: its tiles, and kRowCost more for what it
 // costs to start and end a row.
-__device__ __forceinline__ int share_of(int len) { return len > 0 ? ((len - 1) / kTile + 1) + kRowCost : 0; }
+template <bool kFp8>
+__device__ __forceinline__ int share_of(int len) {
+  return len > 0 ? (len - 1) / kTile<kFp8> + 1 + kRowCost : 0;
+}
 
 // first[row]: shares of the rows before it, first[n_rows]: of all.  Each thread
 // sums n_rows / 256 rows, then a scan over the threads.
+template <bool kFp8>
 __device__ __forceinline__ void tile_offsets(const DecodeArgs& a, const int32_t* lens, int* first, int* sums) {
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int per = (a.n_rows + kThreads - 1) / kThreads, row0 = t * per;
   int mine = 0;
   for (int i = 0; i < per && row0 + i < a.n_rows; ++i)
-    mine += share_of(clamped_length(a, lens, row0 + i));
+    mine += share_of<kFp8>(clamped_length(a, lens, row0 + i));
   int x = mine;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
@@ -105,7 +111,7 @@ __device__ __forceinline__ void tile_offsets(const DecodeArgs& a, const int32_t*
   for (int w = 0; w < wave; ++w) before += sums[w];
   for (int i = 0; i < per && row0 + i < a.n_rows; ++i) {
     first[row0 + i] = before;
-    before += share_of(clamped_length(a, lens, row0 + i));
+    before += share_of<kFp8>(clamped_length(a, lens, row0 + i));
   }
   if (t == kThreads - 1) first[a.n_rows] = before;
   __syncthreads();
@@ -153,8 +159,9 @@ struct State {
 
 template <bool kFp8>
 struct Tile {
-  uint4 k[2][kFp8 ? 2 : 4];   // 16 keys each: lane l % 16's key
-  uint4 v[kFp8 ? 4 : 8];      // keys 16 t + 4 (l / 16) + r of the 32, elements 8 (l % 16) ..
+  static constexpr int kSteps = kTile<kFp8> / 16;
+  uint4 k[kSteps][kFp8 ? 2 : 4];  // of 16 keys, lane l % 16's
+  uint4 v[kSteps][kFp8 ? 2 : 4];  // of 16 keys, 4 (l / 16) + r, elements 8 (l % 16) .. (FP8: two of them in 16 bytes)
 };
 
 template <bool kFp8>
@@ -174,20 +181,20 @@ struct Stream {
   }
   __device__ __forceinline__ void load_k(Tile<kFp8>& t, const int64_t* base) const {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < Tile<kFp8>::kSteps; ++h)
 #pragma unroll
       for (int s = 0; s < (kFp8 ? 2 : 4); ++s)
         t.k[h][s] = *reinterpret_cast<const uint4*>(K + base[h] + k_off + 64 * s);
   }
   __device__ __forceinline__ void load_v(Tile<kFp8>& t, const int64_t* base) const {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < Tile<kFp8>::kSteps; ++h)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const char* p = V + base[h] + v_off + r * tok_bytes;
         if (kFp8) {
           const uint2 w = *reinterpret_cast<const uint2*>(p);
-          uint4& d = t.v[2 * h + (r >> 1)];
+          uint4& d = t.v[h][r >> 1];
           if (r & 1) {
             d.z = w.x;
             d.w = w.y;
@@ -196,22 +203,23 @@ struct Stream {
             d.y = w.y;
           }
         } else {
-          t.v[4 * h + r] = *reinterpret_cast<const uint4*>(p);
+          t.v[h][r] = *reinterpret_cast<const uint4*>(p);
         }
       }
   }
 };
 
-// One tile of 32 keys from key j on added to a wave's state; `next` gives the
-// offsets of the tile to ask for (more: whether there is one).
+// One tile from key j on added to a wave's state; `next` gives the offsets of the
+// tile to ask for (more: whether there is one).
 template <bool kFp8>
 __device__ __forceinline__ void attend_tile(const Stream<kFp8>& st, Tile<kFp8>& tile, const uint4* q,
                                             float scale_log2, int j, int len, bool more, const int64_t* next,
                                             State& s) {
+  constexpr int kSteps = Tile<kFp8>::kSteps;
   const int c = (threadIdx.x & 63) >> 4;
-  f32x4 sc[2];
+  f32x4 sc[kSteps];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
+  for (int h = 0; h < kSteps; ++h) {
     sc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (kFp8) {
 #pragma unroll
@@ -226,18 +234,18 @@ __device__ __forceinline__ void attend_tile(const Stream<kFp8>& st, Tile<kFp8>& 
   }
   if (more) st.load_k(tile, next);
 
-  const bool partial = j + kTile > len;
-  float x[8];
+  const bool partial = j + kTile<kFp8> > len;
+  float x[4 * kSteps];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = sc[e >> 2][e & 3] * scale_log2;
+  for (int e = 0; e < 4 * kSteps; ++e) x[e] = sc[e >> 2][e & 3] * scale_log2;
   if (partial) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int e = 0; e < 4 * kSteps; ++e)
       if (j + 16 * (e >> 2) + 4 * c + (e & 3) >= len) x[e] = -INFINITY;
   }
   float top = x[0];
 #pragma unroll
-  for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
+  for (int e = 1; e < 4 * kSteps; ++e) top = fmaxf(top, x[e]);
   top = over_rows(top, [](float a, float b) { return fmaxf(a, b); });
   if (__any(top > s.m)) {
     const float m = fmaxf(s.m, top);
@@ -249,44 +257,48 @@ __device__ __forceinline__ void attend_tile(const Stream<kFp8>& st, Tile<kFp8>& 
   }
   // (Logits of -inf alone, from infinite inputs, weigh nothing.)
   const float ref = s.m == -INFINITY ? 0.f : s.m;
-  uint32_t hi[4], lo[4];
-#pragma unroll
-  for (int e = 0; e < 8; e += 2) {
-    const float p0 = fast_exp2(x[e] - ref), p1 = fast_exp2(x[e + 1] - ref);
-    s.l += p0 + p1;
-    hi[e / 2] = two_bf16(p0, p1);
-    lo[e / 2] = two_bf16(p0 - bf16_lo(hi[e / 2]), p1 - bf16_hi(hi[e / 2]));
-  }
-  const uint4 p_hi = make_uint4(hi[0], hi[1], hi[2], hi[3]), p_lo = make_uint4(lo[0], lo[1], lo[2], lo[3]);
 
-  uint4 v[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    if (kFp8)
-      v[e] = (e & 1) ? widen(tile.v[e / 2].z, tile.v[e / 2].w) : widen(tile.v[e / 2].x, tile.v[e / 2].y);
-    else
-      v[e] = tile.v[e];
-  }
-  if (partial) {  // places past the row's length may hold anything, NaN too
+  for (int b = 0; b < kSteps / 2; ++b) {  // 32 keys: the depth of a matrix product
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const float p0 = fast_exp2(x[8 * b + e] - ref), p1 = fast_exp2(x[8 * b + e + 1] - ref);
+      s.l += p0 + p1;
+      hi[e / 2] = two_bf16(p0, p1);
+      lo[e / 2] = two_bf16(p0 - bf16_lo(hi[e / 2]), p1 - bf16_hi(hi[e / 2]));
+    }
+    const uint4 p_hi = make_uint4(hi[0], hi[1], hi[2], hi[3]), p_lo = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    uint4 v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const bool in = j + 16 * (e >> 2) + 4 * c + (e & 3) < len;
-      v[e].x = in ? v[e].x : 0u;
-      v[e].y = in ? v[e].y : 0u;
-      v[e].z = in ? v[e].z : 0u;
-      v[e].w = in ? v[e].w : 0u;
+      const int h = 2 * b + (e >> 2), r = e & 3;
+      if (kFp8)
+        v[e] = (r & 1) ? widen(tile.v[h][r / 2].z, tile.v[h][r / 2].w) : widen(tile.v[h][r / 2].x, tile.v[h][r / 2].y);
+      else
+        v[e] = tile.v[h][r];
     }
-  }
+    if (partial) {  // places past the row's length may hold anything, NaN too
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t sel = (i & 1) ? 0x07060302u : 0x05040100u;
-    uint32_t w[4];
+      for (int e = 0; e < 8; ++e) {
+        const bool in = j + 32 * b + 16 * (e >> 2) + 4 * c + (e & 3) < len;
+        v[e].x = in ? v[e].x : 0u;
+        v[e].y = in ? v[e].y : 0u;
+        v[e].z = in ? v[e].z : 0u;
+        v[e].w = in ? v[e].w : 0u;
+      }
+    }
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      w[k] = __builtin_amdgcn_perm(word_of(v[2 * k + 1], i >> 1), word_of(v[2 * k], i >> 1), sel);
-    const uint4 op = make_uint4(w[0], w[1], w[2], w[3]);
-    s.o[i] = mfma16(op, p_hi, s.o[i]);
-    s.o[i] = mfma16(op, p_lo, s.o[i]);
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t sel = (i & 1) ? 0x07060302u : 0x05040100u;
+      uint32_t w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        w[k] = __builtin_amdgcn_perm(word_of(v[2 * k + 1], i >> 1), word_of(v[2 * k], i >> 1), sel);
+      const uint4 op = make_uint4(w[0], w[1], w[2], w[3]);
+      s.o[i] = mfma16(op, p_hi, s.o[i]);
+      s.o[i] = mfma16(op, p_lo, s.o[i]);
+    }
   }
   if (more) st.load_v(tile, next);
 }
@@ -309,7 +321,19 @@ __device__ __forceinline__ float value_scale(const DecodeArgs& a, int g) {
   return m > 0.f ? m / 448.f : 1.f;
 }
 
-template <bool kFp8>
+// The first row whose share starts at x or after it (n_rows: none).
+__device__ __forceinline__ int row_from(const int* first, int n_rows, int x) {
+  int lo = 0, hi = n_rows;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (first[mid] >= x) hi = mid;
+    else lo = mid + 1;
+  }
+  return lo;
+}
+
+// kWhole: a row is one worker's, so that there is nothing to join.
+template <bool kFp8, bool kWhole>
 __global__ __launch_bounds__(kThreads, KB) void paged_decode_kernel(DecodeArgs a, const int32_t* __restrict__ lens,
                                                                 const int32_t* __restrict__ page_table) {
   __shared__ int first[kMaxRows + 1], sums[kWaves];
@@ -322,10 +346,13 @@ __global__ __launch_bounds__(kThreads, KB) void paged_decode_kernel(DecodeArgs a
   const int g = unit / wk.tiles_of_cols, group = a.n_q_heads / a.n_kv_heads;
   const int head0 = g * group + (unit % wk.tiles_of_cols) * kCols;
   const int cols = min(kCols, (g + 1) * group - head0);
-  tile_offsets(a, lens, first, sums);
+  tile_offsets<kFp8>(a, lens, first, sums);
   const int T = first[a.n_rows], W = workers_of(T, wk.workers);
-  int t = worker < W ? start_of(T, worker, W) : T;
-  const int t_end = worker < W ? start_of(T, worker + 1, W) : T;
+  int t = worker < W ? start_of(T, worker, W) : T, t_end = worker < W ? start_of(T, worker + 1, W) : T;
+  if (kWhole) {
+    t = first[row_from(first, a.n_rows, t)];
+    t_end = first[row_from(first, a.n_rows, t_end)];
+  }
   Shared shared{-1, 0, 0, 0};
 
   // Empty rows: zeros, and -inf.
@@ -338,7 +365,7 @@ __global__ __launch_bounds__(kThreads, KB) void paged_decode_kernel(DecodeArgs a
       a.lse[(int64_t)(head0 + threadIdx.x) * a.n_rows + row] = -INFINITY;
   }
 
-  constexpr int kBytes = kFp8 ? 1 : 2;
+  constexpr int kBytes = kFp8 ? 1 : 2, kSteps = Tile<kFp8>::kSteps;
   Stream<kFp8> st;
   st.K = static_cast<const char*>(a.cache.K) + g * a.cache.head * kBytes;
   st.V = static_cast<const char*>(a.cache.V) + g * a.cache.head * kBytes;
@@ -378,15 +405,15 @@ __global__ __launch_bounds__(kThreads, KB) void paged_decode_kernel(DecodeArgs a
   };
   auto offsets = [&](int64_t* base) __attribute__((always_inline)) {
     const int32_t* table = page_table + (int64_t)__builtin_amdgcn_readfirstlane(next.row) * a.max_pages;
-    const int len = __builtin_amdgcn_readfirstlane(next.len), j = __builtin_amdgcn_readfirstlane(next.tile * kTile);
-    base[0] = st.at(table, len, j);
-    base[1] = st.at(table, len, j + 16);
+    const int len = __builtin_amdgcn_readfirstlane(next.len), j = __builtin_amdgcn_readfirstlane(next.tile * kTile<kFp8>);
+#pragma unroll
+    for (int h = 0; h < kSteps; ++h) base[h] = st.at(table, len, j + 16 * h);
   };
   int row = t < t_end ? seq_of(first, a.n_rows, t) : 0;
   Tile<kFp8> tile;
   if (t < t_end) seek(row);
   if (next.row >= 0) {
-    int64_t base[2];
+    int64_t base[kSteps];
     offsets(base);
     st.load_k(tile, base);
     st.load_v(tile, base);
@@ -420,10 +447,10 @@ __global__ __launch_bounds__(kThreads, KB) void paged_decode_kernel(DecodeArgs a
 #pragma unroll
     for (int i = 0; i < 8; ++i) s.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     while (next.row == r) {
-      const int j = next.tile * kTile, len = next.len;
+      const int j = next.tile * kTile<kFp8>, len = next.len;
       next.tile += kWaves;
       if (next.tile >= next.end) seek(r + 1);
-      int64_t base[2] = {0, 0};
+      int64_t base[kSteps] = {};
       if (next.row >= 0) offsets(base);
       attend_tile<kFp8>(st, tile, q, scale_log2, j, len, next.row >= 0, base, s);
     }
@@ -456,7 +483,7 @@ __global__ __launch_bounds__(kThreads, KB) void paged_decode_kernel(DecodeArgs a
         o[0] += x.x * f; o[1] += x.y * f; o[2] += x.z * f; o[3] += x.w * f;
         o[4] += y.x * f; o[5] += y.y * f; o[6] += y.z * f; o[7] += y.w * f;
       }
-      if (whole) {
+      if (kWhole || whole) {
         write_row(a, r, head0 + hc, part, o, m, l, v_scale);
       } else {
         float* slot = a.workspace + (size_t)(2 * blockIdx.x + (is_first ? 0 : 1)) * kPartFloats;
@@ -469,11 +496,11 @@ __global__ __launch_bounds__(kThreads, KB) void paged_decode_kernel(DecodeArgs a
       }
     }
     __syncthreads();
-    if (begins && !whole) shared = Shared{r, worker_of(T, last - 1, W), is_first ? 0 : 1, 0};
+    if (!kWhole && begins && !whole) shared = Shared{r, worker_of(T, last - 1, W), is_first ? 0 : 1, 0};
     is_first = false;
     at = first[r + 1];
   }
-  if (threadIdx.x == 0)
+  if (!kWhole && threadIdx.x == 0)
     reinterpret_cast<Shared*>(a.workspace + (size_t)2 * kWorkers * kPartFloats)[blockIdx.x] = shared;
 }
 
@@ -551,13 +578,21 @@ __global__ __launch_bounds__(kJoinThreads) void paged_decode_join_kernel(DecodeA
   write_row(a, shared.row, head0 + col0 + hc, part, out, top, sum, value_scale<kFp8>(a, g));
 }
 
+#ifndef KWHOLE
+#define KWHOLE 768
+#endif
 template <bool kFp8>
 hipError_t launch(const DecodeArgs& a, hipStream_t s) {
   const Work wk = work_of_heads(a.n_q_heads, a.n_kv_heads);
   const int group = a.n_q_heads / a.n_kv_heads, cols = group < kCols ? group : kCols;
-  hipLaunchKernelGGL(paged_decode_kernel<kFp8>, dim3(wk.units * wk.workers), dim3(kThreads), 0, s, a,
-                     a.seq_lens, a.page_table);
-  hipLaunchKernelGGL(paged_decode_join_kernel<kFp8>, dim3(wk.units * wk.workers, (cols + kJoinCols - 1) / kJoinCols), dim3(kJoinThreads), 0, s, a);
+  const dim3 grid(wk.units * wk.workers);
+  if (((int64_t)a.max_pages << a.cache.page_shift) <= KWHOLE) {
+    hipLaunchKernelGGL((paged_decode_kernel<kFp8, true>), grid, dim3(kThreads), 0, s, a, a.seq_lens, a.page_table);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((paged_decode_kernel<kFp8, false>), grid, dim3(kThreads), 0, s, a, a.seq_lens, a.page_table);
+  hipLaunchKernelGGL(paged_decode_join_kernel<kFp8>, dim3(wk.units * wk.workers, (cols + kJoinCols - 1) / kJoinCols),
+                     dim3(kJoinThreads), 0, s, a);
   return hipGetLastError();
 }
 
