@@ -40,22 +40,25 @@ constexpr int kCols = 16;                  // query heads of a unit
 #ifndef KW
 #define KW 512
 #define KC 4
-#define KJ 4
 #define KB 2
 #endif
 constexpr int kWorkers = KW;              // workgroups of a launch: two on each of 256 compute units
 constexpr int kPartFloats = kCols * kHeadDim + 2 * kCols;  // weighted values, maxima, sums
 constexpr int kPad = kHeadDim + 4;                         // floats between LDS rows (banks)
 constexpr int kRowCost = KC;
-constexpr int kJoinThreads = 512, kJoinCols = KJ;
+#ifndef KF
+#define KF 512
+#endif
+constexpr int kJoinThreads = 512, kFewJoins = KF;
 
-// What a worker leaves for the join, at the workspace's end: where the row whose
-// first tile but not whose last is its own goes on.
+// What the worker that has a row's first tile leaves for the join, at the
+// workspace's end: one for each row and unit, or where there are more rows than
+// workers, one for each worker (the row that goes on after it).
 struct Shared {
-  int row;   // -1: no such row
-  int last;  // the row's last worker
-  int slot;  // this worker's part of it, 0 or 1 (the others': 0)
-  int unused;
+  int row;    // -1: no row in parts
+  int first;  // its first worker
+  int last;   // and its last
+  int slot;   // the first one's part, 0 or 1 (the others': 0)
 };
 
 __device__ __forceinline__ uint32_t two_bf16(float a, float b) {
@@ -321,6 +324,10 @@ __device__ __forceinline__ float value_scale(const DecodeArgs& a, int g) {
   return m > 0.f ? m / 448.f : 1.f;
 }
 
+__device__ __forceinline__ Shared* shared_rows(const DecodeArgs& a) {
+  return reinterpret_cast<Shared*>(a.workspace + (size_t)2 * kWorkers * kPartFloats);
+}
+
 // The first row whose share starts at x or after it (n_rows: none).
 __device__ __forceinline__ int row_from(const int* first, int n_rows, int x) {
   int lo = 0, hi = n_rows;
@@ -353,6 +360,7 @@ __global__ __launch_bounds__(kThreads, KB) void paged_decode_kernel(DecodeArgs a
     t = first[row_from(first, a.n_rows, t)];
     t_end = first[row_from(first, a.n_rows, t_end)];
   }
+  const bool by_row = a.n_rows <= wk.workers;
   Shared shared{-1, 0, 0, 0};
 
   // Empty rows: zeros, and -inf.
@@ -496,27 +504,33 @@ __global__ __launch_bounds__(kThreads, KB) void paged_decode_kernel(DecodeArgs a
       }
     }
     __syncthreads();
-    if (!kWhole && begins && !whole) shared = Shared{r, worker_of(T, last - 1, W), is_first ? 0 : 1, 0};
+    if (!kWhole && begins) {
+      shared = Shared{whole ? -1 : r, worker, worker_of(T, last - 1, W), is_first ? 0 : 1};
+      if (by_row && threadIdx.x == 0) shared_rows(a)[r * wk.units + unit] = shared;
+    }
     is_first = false;
     at = first[r + 1];
   }
-  if (!kWhole && threadIdx.x == 0)
-    reinterpret_cast<Shared*>(a.workspace + (size_t)2 * kWorkers * kPartFloats)[blockIdx.x] = shared;
+  if (!kWhole && !by_row && threadIdx.x == 0) shared_rows(a)[blockIdx.x] = shared;
 }
 
-// Joins the parts of the row that starts in worker blockIdx.x and ends in
-// another.  16 threads take a column's 128 elements, and as many sets of 16 as
-// there are threads for take every so many-th part; eight parts' loads are in
-// flight at a time (a row of 128K keys has 128 parts).
-template <bool kFp8>
+// Joins the parts of a row.  16 threads take a column's 128 elements, and as many
+// sets of 16 as there are threads for take every so many-th part; eight parts'
+// loads are in flight at a time (a row of 128K keys has 128 parts).  One column to
+// a workgroup where that makes few of them, otherwise four: most workgroups of a
+// large batch find nothing to join.
+template <bool kFp8, int kJoinCols>
 __global__ __launch_bounds__(kJoinThreads) void paged_decode_join_kernel(DecodeArgs a) {
-  constexpr int kSets = kJoinThreads / 16, kBatch = 8;
+  constexpr int kSets = kJoinThreads / 16, kBatch = kJoinCols == 1 ? 4 : 8;
   __shared__ __align__(16) float acc[kSets][kPad];
   __shared__ float ms[kSets], ls[kSets];
-  const Shared shared = reinterpret_cast<const Shared*>(a.workspace + (size_t)2 * kWorkers * kPartFloats)[blockIdx.x];
-  if (shared.row < 0) return;
   const Work wk = work_of_heads(a.n_q_heads, a.n_kv_heads);
-  const int unit = blockIdx.x % wk.units, wa = blockIdx.x / wk.units;
+  const bool by_row = a.n_rows <= wk.workers;
+  const int unit = blockIdx.x % wk.units;
+  if (by_row && a.seq_lens[blockIdx.x / wk.units] <= 0) return;  // (no worker has it)
+  const Shared shared = shared_rows(a)[blockIdx.x];
+  if (shared.row < 0) return;
+  const int wa = shared.first;
   const int g = unit / wk.tiles_of_cols, group = a.n_q_heads / a.n_kv_heads;
   const int head0 = g * group + (unit % wk.tiles_of_cols) * kCols;
   const int col0 = blockIdx.y * kJoinCols, cols = min(kJoinCols, min(kCols, (g + 1) * group - head0) - col0);
@@ -524,7 +538,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_decode_join_kernel(DecodeA
   const int set = threadIdx.x >> 4, part = threadIdx.x & 15;
   const int sets_each = kSets / cols, hc = set % cols, mine = set / cols;  // (sets past cols * sets_each are idle)
   const int parts = shared.last - wa + 1;
-  const float* base = a.workspace + (size_t)2 * blockIdx.x * kPartFloats;
+  const float* base = a.workspace + (size_t)2 * (wa * wk.units + unit) * kPartFloats;
   float m = -INFINITY, l = 0.f, o[8] = {};
   if (mine < sets_each) {
     for (int p0 = mine; p0 < parts; p0 += kBatch * sets_each) {
@@ -591,8 +605,11 @@ hipError_t launch(const DecodeArgs& a, hipStream_t s) {
     return hipGetLastError();
   }
   hipLaunchKernelGGL((paged_decode_kernel<kFp8, false>), grid, dim3(kThreads), 0, s, a, a.seq_lens, a.page_table);
-  hipLaunchKernelGGL(paged_decode_join_kernel<kFp8>, dim3(wk.units * wk.workers, (cols + kJoinCols - 1) / kJoinCols),
-                     dim3(kJoinThreads), 0, s, a);
+  const int joins = wk.units * (a.n_rows < wk.workers ? a.n_rows : wk.workers);
+  if (joins * cols <= kFewJoins)
+    hipLaunchKernelGGL((paged_decode_join_kernel<kFp8, 1>), dim3(joins, cols), dim3(kJoinThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((paged_decode_join_kernel<kFp8, 4>), dim3(joins, (cols + 3) / 4), dim3(kJoinThreads), 0, s, a);
   return hipGetLastError();
 }
 
