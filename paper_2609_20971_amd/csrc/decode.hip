@@ -45,6 +45,16 @@ constexpr int kCols = 16;                  // query heads of a unit
 constexpr int kWorkers = KW;              // workgroups of a launch: two on each of 256 compute units
 constexpr int kPartFloats = kCols * kHeadDim + 2 * kCols;  // weighted values, maxima, sums
 constexpr int kPad = kHeadDim + 4;                         // floats between LDS rows (banks)
+// A launch that reads more than this of K and V reads them past the caches: what
+// it would leave there is gone before the next step reads it, and making room
+// costs, most where the caches hold what others wrote.  Cached / past them, after a
+// copy of 2 GB: 24 rows of up to 9000 keys (69 MB) 24.4 / 18.0 us, one of 20000
+// (41 MB) 16.9 / 13.4, one of 131000 (268 MB) 76 / 46, 3000 (6 MB) 8.1 / 8.2; step
+// after step, over more than the Infinity Cache, 32 rows of 9000 to 16000 keys
+// (1.6 GB) 291 / 261, within it, 24 rows 20.6 / 22.0, 3000 11.0 / 12.0.  Not with
+// more than 16 query heads to a KV head, whose units read the same keys (128
+// heads: 190 / 223).
+constexpr int64_t kCachedBytes = int64_t(16) << 20;
 constexpr int kRowCost = KC;
 #ifndef KF
 #define KF 512
@@ -167,6 +177,22 @@ struct Tile {
   uint4 v[kSteps][kFp8 ? 2 : 4];  // of 16 keys, 4 (l / 16) + r, elements 8 (l % 16) .. (FP8: two of them in 16 bytes)
 };
 
+// 16 (8) bytes of K or V; kOnce: without a place in the caches.
+template <bool kOnce>
+__device__ __forceinline__ uint4 load16(const char* p) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  if (!kOnce) return *reinterpret_cast<const uint4*>(p);
+  const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+template <bool kOnce>
+__device__ __forceinline__ uint2 load8(const char* p) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  if (!kOnce) return *reinterpret_cast<const uint2*>(p);
+  const u32x2 v = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
+  return make_uint2(v.x, v.y);
+}
+
 template <bool kFp8>
 struct Stream {
   const char* K;  // this KV head's
@@ -174,6 +200,7 @@ struct Stream {
   int64_t page_bytes;
   int tok_bytes, n_pages, shift;
   uint32_t k_off, v_off;  // this lane's, within 16 keys
+  bool once;              // see kCachedBytes
 
   // Byte offset of key j0 (a multiple of 16: within one page) of a row.  The page
   // number comes by a scalar load: a vector load's wait would be one for every key
@@ -183,20 +210,29 @@ struct Stream {
     return page * page_bytes + (int64_t)(j0 & ((1 << shift) - 1)) * tok_bytes;
   }
   __device__ __forceinline__ void load_k(Tile<kFp8>& t, const int64_t* base) const {
+    if (once) load_k_as<true>(t, base);
+    else load_k_as<false>(t, base);
+  }
+  __device__ __forceinline__ void load_v(Tile<kFp8>& t, const int64_t* base) const {
+    if (once) load_v_as<true>(t, base);
+    else load_v_as<false>(t, base);
+  }
+  template <bool kOnce>
+  __device__ __forceinline__ void load_k_as(Tile<kFp8>& t, const int64_t* base) const {
 #pragma unroll
     for (int h = 0; h < Tile<kFp8>::kSteps; ++h)
 #pragma unroll
-      for (int s = 0; s < (kFp8 ? 2 : 4); ++s)
-        t.k[h][s] = *reinterpret_cast<const uint4*>(K + base[h] + k_off + 64 * s);
+      for (int s = 0; s < (kFp8 ? 2 : 4); ++s) t.k[h][s] = load16<kOnce>(K + base[h] + k_off + 64 * s);
   }
-  __device__ __forceinline__ void load_v(Tile<kFp8>& t, const int64_t* base) const {
+  template <bool kOnce>
+  __device__ __forceinline__ void load_v_as(Tile<kFp8>& t, const int64_t* base) const {
 #pragma unroll
     for (int h = 0; h < Tile<kFp8>::kSteps; ++h)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const char* p = V + base[h] + v_off + r * tok_bytes;
         if (kFp8) {
-          const uint2 w = *reinterpret_cast<const uint2*>(p);
+          const uint2 w = load8<kOnce>(p);
           uint4& d = t.v[h][r >> 1];
           if (r & 1) {
             d.z = w.x;
@@ -206,7 +242,7 @@ struct Stream {
             d.y = w.y;
           }
         } else {
-          t.v[h][r] = *reinterpret_cast<const uint4*>(p);
+          t.v[h][r] = load16<kOnce>(p);
         }
       }
   }
@@ -381,6 +417,7 @@ __global__ __launch_bounds__(kThreads, KB) void paged_decode_kernel(DecodeArgs a
   st.tok_bytes = (int)a.cache.tok * kBytes;
   st.n_pages = a.cache.n_pages;
   st.shift = a.cache.page_shift;
+  st.once = wk.tiles_of_cols == 1 && (int64_t)T * wk.units * (kTile<kFp8> * 2 * kHeadDim * kBytes) >= kCachedBytes;
   st.k_off = col * st.tok_bytes + 16 * c;
   st.v_off = 4 * c * st.tok_bytes + 8 * kBytes * col;
   float scale_log2 = a.scale * kLog2e;
