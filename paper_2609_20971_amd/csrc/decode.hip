@@ -37,13 +37,14 @@ constexpr int kWaves = kThreads / 64;
 template <bool kFp8>
 constexpr int kTile = kFp8 ? 64 : 32;
 constexpr int kCols = 16;                  // query heads of a unit
-#ifndef KW
-#define KW 512
-#define KC 4
-#define KB 2
-#endif
-constexpr int kWorkers = KW;              // workgroups of a launch: two on each of 256 compute units
+constexpr int kWorkers = 512;             // workgroups of a launch: two on each of 256 compute units
 constexpr int kPartFloats = kCols * kHeadDim + 2 * kCols;  // weighted values, maxima, sums
+// Rows that the table holds up to so many keys of are a worker's alone, and there
+// is no second launch (4 us, and 3.7 us of the calling thread).  In parts / whole,
+// the GPU's time alone: one row of 500 keys 9.9 / 9.2, 700 9.8 / 11.0, 1000 10.3 /
+// 13.5; 64 rows of 200 to 500 18.9 / 16.5, to 1000 20.8 / 22.6; called one by one
+// 700 12.4 / 11.1.
+constexpr int kWholeKeys = 768;
 constexpr int kPad = kHeadDim + 4;                         // floats between LDS rows (banks)
 // A launch that reads more than this of K and V reads them past the caches: what
 // it would leave there is gone before the next step reads it, and making room
@@ -55,11 +56,13 @@ constexpr int kPad = kHeadDim + 4;                         // floats between LDS
 // more than 16 query heads to a KV head, whose units read the same keys (128
 // heads: 190 / 223).
 constexpr int64_t kCachedBytes = int64_t(16) << 20;
-constexpr int kRowCost = KC;
-#ifndef KF
-#define KF 512
-#endif
-constexpr int kJoinThreads = 512, kFewJoins = KF;
+// Tiles that a row's start and end cost: with none of them a worker of many short
+// rows comes late (24 rows of 1 to 9000 keys 28.4 us, 1: 23.4, 2 to 8: 21.3; 300
+// rows of 10 to 600 keys 1: 33.7, 4: 30.3, 8: 32.8).
+constexpr int kRowCost = 4;
+// A join by single columns takes at most so many workgroups: one row of 20000 keys
+// 18.2 us and not 20.8, of 131000 57 and not 60; but 64 rows 72 and not 65.
+constexpr int kJoinThreads = 512, kFewJoins = 512;
 
 // What the worker that has a row's first tile leaves for the join, at the
 // workspace's end: one for each row and unit, or where there are more rows than
@@ -377,7 +380,7 @@ __device__ __forceinline__ int row_from(const int* first, int n_rows, int x) {
 
 // kWhole: a row is one worker's, so that there is nothing to join.
 template <bool kFp8, bool kWhole>
-__global__ __launch_bounds__(kThreads, KB) void paged_decode_kernel(DecodeArgs a, const int32_t* __restrict__ lens,
+__global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(DecodeArgs a, const int32_t* __restrict__ lens,
                                                                 const int32_t* __restrict__ page_table) {
   __shared__ int first[kMaxRows + 1], sums[kWaves];
   __shared__ __align__(16) float acc[kWaves][kCols][kPad];
@@ -629,15 +632,12 @@ __global__ __launch_bounds__(kJoinThreads) void paged_decode_join_kernel(DecodeA
   write_row(a, shared.row, head0 + col0 + hc, part, out, top, sum, value_scale<kFp8>(a, g));
 }
 
-#ifndef KWHOLE
-#define KWHOLE 768
-#endif
 template <bool kFp8>
 hipError_t launch(const DecodeArgs& a, hipStream_t s) {
   const Work wk = work_of_heads(a.n_q_heads, a.n_kv_heads);
   const int group = a.n_q_heads / a.n_kv_heads, cols = group < kCols ? group : kCols;
   const dim3 grid(wk.units * wk.workers);
-  if (((int64_t)a.max_pages << a.cache.page_shift) <= KWHOLE) {
+  if (((int64_t)a.max_pages << a.cache.page_shift) <= kWholeKeys) {
     hipLaunchKernelGGL((paged_decode_kernel<kFp8, true>), grid, dim3(kThreads), 0, s, a, a.seq_lens, a.page_table);
     return hipGetLastError();
   }

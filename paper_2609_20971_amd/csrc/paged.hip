@@ -8,11 +8,25 @@ namespace rbs {
 
 // ------------------------------------------------------------------ pages
 
-constexpr int kPageThreads = 1024;
+constexpr int kPageThreads = 256;
+constexpr int kRowsPerThread = kMaxRows / kPageThreads;
 constexpr int kFillTokens = 4 * kPageThreads;  // tokens (and new pages) of one workgroup
 constexpr int kMost = 1 << 29;                 // sums stop here, past every limit that they are compared with
 
 __device__ __forceinline__ int capped_add(int a, int b) { return min(a + b, kMost); }  // a, b in 0 .. kMost
+
+// x of the lanes before this one and its own, summed: within each row of 16 lanes,
+// then the last lane of row 0 (2) onto row 1 (3), then that of the first two rows
+// onto the others.  A lane or row with no source takes 0.
+__device__ __forceinline__ int wave_scan(int x) {
+  x = capped_add(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));  // row_shr 1
+  x = capped_add(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));  // row_shr 2
+  x = capped_add(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));  // row_shr 4
+  x = capped_add(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));  // row_shr 8
+  x = capped_add(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));  // row_bcast 15
+  x = capped_add(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));  // row_bcast 31
+  return x;
+}
 
 // Sums of two counts over the threads before this one, and over all of them.
 // Capped addition of nonnegative numbers is associative, so that the order of
@@ -20,24 +34,15 @@ __device__ __forceinline__ int capped_add(int a, int b) { return min(a + b, kMos
 __device__ __forceinline__ void scan_pair(int a, int b, int* sums, int& a_before, int& b_before, int& a_all,
                                           int& b_all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int x = a, y = b;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int u = __shfl_up(x, d), v = __shfl_up(y, d);
-    if (lane >= d) {
-      x = capped_add(x, u);
-      y = capped_add(y, v);
-    }
-  }
+  const int x = wave_scan(a), y = wave_scan(b);
   constexpr int kWaves = kPageThreads / 64;
   if (lane == 63) {
     sums[wave] = x;
     sums[kWaves + wave] = y;
   }
-  const int px = __shfl_up(x, 1), py = __shfl_up(y, 1);
   __syncthreads();
-  a_before = lane == 0 ? 0 : px;
-  b_before = lane == 0 ? 0 : py;
+  a_before = __builtin_amdgcn_update_dpp(0, x, 0x138, 0xf, 0xf, false);  // wave_shr 1
+  b_before = __builtin_amdgcn_update_dpp(0, y, 0x138, 0xf, 0xf, false);
   a_all = b_all = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
@@ -55,25 +60,32 @@ __device__ __forceinline__ void scan_pair(int a, int b, int* sums, int& a_before
 // table of sums between two.  The state (lengths, n_free, offsets, status) is
 // workgroup 0's, where `state` is set.  Bound by latency: three dependent loads
 // and a scan.
+//
+// kOne: a token each (a decode step).  A row's thread then writes the row's token
+// itself, and asks for its last page before the sums (48 rows 6.3 -> 2.8 us).
+template <bool kOne>
 __global__ __launch_bounds__(kPageThreads) void pages_extend_kernel(PagesArgs a, bool fill, bool state) {
   __shared__ int sums[2 * kPageThreads / 64];
   __shared__ int first_token[kMaxRows + 1], first_page[kMaxRows + 1], length[kMaxRows];
   const int t = threadIdx.x, shift = a.page_shift, places = (1 << shift) - 1;
-  const int per = (a.n_rows + kPageThreads - 1) / kPageThreads;  // rows per thread, 1 .. 4
+  const int per = (a.n_rows + kPageThreads - 1) / kPageThreads;  // rows per thread
   const int row0 = t * per;
   const int n_free = *a.n_free;
-  int add[kMaxRows / kPageThreads], need[kMaxRows / kPageThreads];
+  int add[kRowsPerThread], need[kRowsPerThread], page_of[kOne ? kRowsPerThread : 1];
   int tokens = 0, pages = 0;
   bool too_long = false;
 #pragma unroll
-  for (int i = 0; i < kMaxRows / kPageThreads; ++i) {
-    add[i] = need[i] = 0;
+  for (int i = 0; i < kRowsPerThread; ++i) add[i] = need[i] = 0;
+#pragma unroll
+  for (int i = 0; i < kRowsPerThread; ++i) {
     const int row = row0 + i;
-    if (i < per && row < a.n_rows) {
+    if (i >= per) break;
+    if (row < a.n_rows) {
       const int len = a.seq_lens[row];
       length[row] = len;
       if (len >= 0) {
-        const int more = a.new_tokens != nullptr ? max(a.new_tokens[row], 0) : 1;
+        const int more = kOne ? 1 : max(a.new_tokens[row], 0);
+        if (kOne) page_of[i] = a.page_table[(int64_t)row * a.max_pages + min(len >> shift, a.max_pages - 1)];
         const int64_t held = ((int64_t)len + places) >> shift;
         const int64_t after = ((int64_t)len + more + places) >> shift;
         too_long |= after > a.max_pages;
@@ -87,9 +99,10 @@ __global__ __launch_bounds__(kPageThreads) void pages_extend_kernel(PagesArgs a,
   int token, page, all_tokens, all_pages;
   scan_pair(tokens, pages, sums, token, page, all_tokens, all_pages);
 #pragma unroll
-  for (int i = 0; i < kMaxRows / kPageThreads; ++i) {
+  for (int i = 0; i < kRowsPerThread; ++i) {
     const int row = row0 + i;
-    if (i < per && row < a.n_rows) {
+    if (i >= per) break;
+    if (row < a.n_rows) {
       first_token[row] = token;
       first_page[row] = page;
       token = capped_add(token, add[i]);
@@ -107,36 +120,57 @@ __global__ __launch_bounds__(kPageThreads) void pages_extend_kernel(PagesArgs a,
 
   if (fill) {
     const int begin = blockIdx.x * kFillTokens;
-    if (ok) {
-      for (int k = begin + t; k < min(begin + kFillTokens, all_pages); k += kPageThreads) {
-        const int row = seq_of(first_page, a.n_rows, k);
-        const int at = ((length[row] + places) >> shift) + k - first_page[row];
-        a.page_table[(int64_t)row * a.max_pages + at] = a.free_pages[n_free - 1 - k];
-      }
-    }
-    const int tok = begin + 4 * t;
-    if (tok < a.max_tokens) {
-      int pos[4], slot[4];
-      int row = ok ? seq_of(first_token, a.n_rows, min(tok, max(all_tokens - 1, 0))) : 0;
+    if (kOne) {
+      if (blockIdx.x == 0 && ok) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        pos[i] = slot[i] = -1;
-        if (ok && tok + i < all_tokens) {
-          while (first_token[row + 1] <= tok + i) ++row;
-          pos[i] = length[row] + tok + i - first_token[row];
-          const int at = pos[i] >> shift, held = (length[row] + places) >> shift;
-          const int p = at < held ? a.page_table[(int64_t)row * a.max_pages + at]
-                                  : a.free_pages[n_free - 1 - (first_page[row] + at - held)];
-          slot[i] = (p << shift) + (pos[i] & places);
+        for (int i = 0; i < kRowsPerThread; ++i) {
+          const int row = row0 + i;
+          if (i >= per) break;
+          if (row >= a.n_rows || add[i] == 0) continue;
+          const int len = length[row], tok = first_token[row];
+          if (need[i] != 0) {  // (its length is a whole number of pages)
+            page_of[i] = a.free_pages[n_free - 1 - first_page[row]];
+            a.page_table[(int64_t)row * a.max_pages + (len >> shift)] = page_of[i];
+          }
+          a.positions[tok] = len;
+          a.slots[tok] = (page_of[i] << shift) + (len & places);
         }
       }
-      if (tok + 4 <= a.max_tokens) {
-        *reinterpret_cast<int4*>(a.positions + tok) = make_int4(pos[0], pos[1], pos[2], pos[3]);
-        *reinterpret_cast<int4*>(a.slots + tok) = make_int4(slot[0], slot[1], slot[2], slot[3]);
-      } else {
-        for (int i = 0; i < 4 && tok + i < a.max_tokens; ++i) {
-          a.positions[tok + i] = pos[i];
-          a.slots[tok + i] = slot[i];
+      for (int tok = max(begin, ok ? all_tokens : 0) + t; tok < min(begin + kFillTokens, a.max_tokens);
+           tok += kPageThreads)
+        a.positions[tok] = a.slots[tok] = -1;
+    } else {
+      if (ok) {
+        for (int k = begin + t; k < min(begin + kFillTokens, all_pages); k += kPageThreads) {
+          const int row = seq_of(first_page, a.n_rows, k);
+          const int at = ((length[row] + places) >> shift) + k - first_page[row];
+          a.page_table[(int64_t)row * a.max_pages + at] = a.free_pages[n_free - 1 - k];
+        }
+      }
+      const int tok = begin + 4 * t;
+      if (tok < a.max_tokens) {
+        int pos[4], slot[4];
+        int row = ok ? seq_of(first_token, a.n_rows, min(tok, max(all_tokens - 1, 0))) : 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          pos[i] = slot[i] = -1;
+          if (ok && tok + i < all_tokens) {
+            while (first_token[row + 1] <= tok + i) ++row;
+            pos[i] = length[row] + tok + i - first_token[row];
+            const int at = pos[i] >> shift, held = (length[row] + places) >> shift;
+            const int p = at < held ? a.page_table[(int64_t)row * a.max_pages + at]
+                                    : a.free_pages[n_free - 1 - (first_page[row] + at - held)];
+            slot[i] = (p << shift) + (pos[i] & places);
+          }
+        }
+        if (tok + 4 <= a.max_tokens) {
+          *reinterpret_cast<int4*>(a.positions + tok) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+          *reinterpret_cast<int4*>(a.slots + tok) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+        } else {
+          for (int i = 0; i < 4 && tok + i < a.max_tokens; ++i) {
+            a.positions[tok + i] = pos[i];
+            a.slots[tok + i] = slot[i];
+          }
         }
       }
     }
@@ -145,9 +179,10 @@ __global__ __launch_bounds__(kPageThreads) void pages_extend_kernel(PagesArgs a,
   // outputs may be the inputs.
   if (state && blockIdx.x == 0) {
 #pragma unroll
-    for (int i = 0; i < kMaxRows / kPageThreads; ++i) {
+    for (int i = 0; i < kRowsPerThread; ++i) {
       const int row = row0 + i;
-      if (i < per && row < a.n_rows) {
+      if (i >= per) break;
+      if (row < a.n_rows) {
         a.seq_lens_out[row] = length[row] + (ok ? add[i] : 0);
         a.cu_tokens[row] = ok ? first_token[row] : 0;
       }
@@ -166,8 +201,9 @@ hipError_t launch_pages_extend(const PagesArgs& a, hipStream_t s) {
   // over the inputs by a launch of its own.
   const bool in_place = a.seq_lens_out == a.seq_lens || a.n_free_out == a.n_free;
   const bool split = groups > 1 && in_place;
-  hipLaunchKernelGGL(pages_extend_kernel, dim3(groups), dim3(kPageThreads), 0, s, a, true, !split);
-  if (split) hipLaunchKernelGGL(pages_extend_kernel, dim3(1), dim3(kPageThreads), 0, s, a, false, true);
+  const auto kernel = a.new_tokens == nullptr ? pages_extend_kernel<true> : pages_extend_kernel<false>;
+  hipLaunchKernelGGL(kernel, dim3(groups), dim3(kPageThreads), 0, s, a, true, !split);
+  if (split) hipLaunchKernelGGL(kernel, dim3(1), dim3(kPageThreads), 0, s, a, false, true);
   return hipGetLastError();
 }
 
@@ -187,16 +223,20 @@ __global__ __launch_bounds__(kPageThreads) void pages_release_kernel(int n_rows,
   const int per = (n_rows + kPageThreads - 1) / kPageThreads;
   const int row0 = t * per;
   const int n_free = *n_free_io;
-  int held[kMaxRows / kPageThreads];
-  bool drop[kMaxRows / kPageThreads];
+  int held[kRowsPerThread];
+  bool drop[kRowsPerThread];
   int pages = 0;
   bool too_long = false;
 #pragma unroll
-  for (int i = 0; i < kMaxRows / kPageThreads; ++i) {
+  for (int i = 0; i < kRowsPerThread; ++i) {
     held[i] = 0;
     drop[i] = false;
+  }
+#pragma unroll
+  for (int i = 0; i < kRowsPerThread; ++i) {
     const int row = row0 + i;
-    if (i < per && row < n_rows) {
+    if (i >= per) break;
+    if (row < n_rows) {
       const int len = seq_lens[row];
       if (len >= 0 && released[row] != 0) {
         drop[i] = true;
@@ -209,9 +249,10 @@ __global__ __launch_bounds__(kPageThreads) void pages_release_kernel(int n_rows,
   int page, all_pages, none, none_all;
   scan_pair(pages, 0, sums, page, none, all_pages, none_all);
 #pragma unroll
-  for (int i = 0; i < kMaxRows / kPageThreads; ++i) {
+  for (int i = 0; i < kRowsPerThread; ++i) {
     const int row = row0 + i;
-    if (i < per && row < n_rows) {
+    if (i >= per) break;
+    if (row < n_rows) {
       first_page[row] = page;
       page = capped_add(page, held[i]);
     }
@@ -225,7 +266,7 @@ __global__ __launch_bounds__(kPageThreads) void pages_release_kernel(int n_rows,
     free_pages[n_free + k] = page_table[(int64_t)row * max_pages + k - first_page[row]];
   }
 #pragma unroll
-  for (int i = 0; i < kMaxRows / kPageThreads; ++i)
+  for (int i = 0; i < kRowsPerThread; ++i)
     if (drop[i]) seq_lens[row0 + i] = -1;
   if (t == 0) *n_free_io = n_free + all_pages;
 }
@@ -240,12 +281,13 @@ hipError_t launch_pages_release(int n_rows, int max_pages, int n_pages, int page
 
 // ------------------------------------------------------------------ norm, rotation, cache
 
-// One wave works on one token's head rows, four at a time: 16 lanes to a row of
-// 128, eight elements to a lane.  Lane i of a row holds pairs 4 i .. 4 i + 3, so
-// that a rotation needs no other lane: elements 8 i .. 8 i + 7 where neighbours
-// pair up, and 4 i .. 4 i + 3 with 4 i + rot_dim / 2 .. + 3 where halves do (past
-// the rotated part, two runs of four of the rest).  The row's mean square takes
-// four steps over its 16 lanes.
+// A wave works on one token's head rows, 64 / kLanes of them at a time: kLanes lanes
+// to a row of 128, two runs of kRun = 64 / kLanes elements to a lane.  Lane i of a
+// row holds pairs kRun i .. + kRun - 1, so that a rotation needs no other lane: runs
+// 2 i and 2 i + 1 where neighbours pair up, and run i and the one rot_dim / 2 after
+// it where halves do (past the rotated part, two runs of the rest).  Runs of eight
+// elements, 16 bytes, move a row with half as many loads as runs of four, and need
+// pairs in multiples of eight.
 //
 // Angles: position * inv_freq / (2 pi) in 64 bits, of which the fraction of a
 // turn goes to 32-bit sine and cosine: in 32 bits alone the product would be off
@@ -257,12 +299,25 @@ hipError_t launch_pages_release(int n_rows, int max_pages, int n_pages, int page
 // latency for a few tokens.
 constexpr int kRopeThreads = 256;
 constexpr int kRopeWaves = kRopeThreads / 64;
+// From this many bytes of rows on a call reads and writes past the caches, and in
+// runs of eight: 128K tokens of 32 / 4 heads (1.3 GB) cached, in runs of four 534 us,
+// past the caches 490, in runs of eight as well 478; 8000 tokens (82 MB) 34.2 and
+// 33.4.  Below, the next call finds the rows in the Infinity Cache, and what runs
+// of eight save is less than their fewer waves cost: 3001 tokens of 28 / 4 heads (28
+// MB) 12.4 cached in runs of four, 14.9 in runs of eight, 17.0 past the caches as
+// well; 96 of 64 / 8 3.9 and 4.3.
+constexpr int64_t kRopeCachedBytes = int64_t(64) << 20;
+// Waves that a call of few tokens is spread over, a token's rows in several parts:
+// 512 tokens of 32 / 4 heads 2048 5.2 us, 4096 4.6, 8192 4.6; 3001 of 28 / 4 2048
+// 13.0, 4096 14.9, 8192 15.8 (runs of eight).
+constexpr int kRopeSpread = 4096;
 
-__device__ __forceinline__ float row_sum16(float x) {
-  x += dpp_f<0xb1>(x);   // quad_perm [1, 0, 3, 2]
-  x += dpp_f<0x4e>(x);   // quad_perm [2, 3, 0, 1]
-  x += dpp_f<0x124>(x);  // row_ror 4
-  x += dpp_f<0x128>(x);  // row_ror 8
+template <int kLanes>
+__device__ __forceinline__ float row_sum(float x) {
+  x += dpp_f<0xb1>(x);                      // quad_perm [1, 0, 3, 2]
+  x += dpp_f<0x4e>(x);                      // quad_perm [2, 3, 0, 1]
+  x += dpp_f<0x141>(x);                     // row_half_mirror: the other quad of eight lanes
+  if (kLanes == 16) x += dpp_f<0x128>(x);   // row_ror 8
   return x;
 }
 
@@ -285,9 +340,28 @@ __device__ __forceinline__ uint32_t pack_e4m3(const float* x, float scale) {
   return __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
 }
 
-template <bool kInterleaved>
+// kWords words between memory and registers; kOnce: with no place in the caches.
+template <int kWords, bool kOnce>
+__device__ __forceinline__ void load_words(const void* p, uint32_t* w) {
+  typedef uint32_t Vec __attribute__((ext_vector_type(kWords)));
+  const Vec v = kOnce ? __builtin_nontemporal_load(static_cast<const Vec*>(p)) : *static_cast<const Vec*>(p);
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) w[i] = v[i];
+}
+template <int kWords, bool kOnce>
+__device__ __forceinline__ void store_words(void* p, const uint32_t* w) {
+  typedef uint32_t Vec __attribute__((ext_vector_type(kWords)));
+  Vec v;
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) v[i] = w[i];
+  if (kOnce) __builtin_nontemporal_store(v, static_cast<Vec*>(p));
+  else *static_cast<Vec*>(p) = v;
+}
+
+template <int kLanes, bool kInterleaved, bool kOnce>
 __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a, int parts, int rows_per_part) {
-  __shared__ float2 turn[kRopeWaves][64];
+  constexpr int kRun = 64 / kLanes, kRows = 64 / kLanes, kUnroll = 2;
+  __shared__ __align__(16) float cosines[kRopeWaves][64], sines[kRopeWaves][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t item = (int64_t)blockIdx.x * kRopeWaves + wave;
   const int64_t tok = item / parts;
@@ -298,34 +372,35 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a, 
     const float part_turn = (float)(turns - rint(turns));
     float sn, cs;
     sincospif(2.f * part_turn, &sn, &cs);
-    turn[wave][lane] = make_float2(cs * a.factor, sn * a.factor);
+    cosines[wave][lane] = cs * a.factor;
+    sines[wave][lane] = sn * a.factor;
   }
   __syncthreads();
   if (position < 0) return;
 
-  const int sub = lane >> 4, i = lane & 15;
+  const int sub = lane / kLanes, i = lane % kLanes;
   const int half = a.rot_dim >> 1;
-  const bool rotated = 4 * i < half;
-  // The lane's two runs of four elements.
-  const int lo = kInterleaved ? 8 * i : rotated ? 4 * i : half + 4 * i;
-  const int hi = kInterleaved ? 8 * i + 4 : rotated ? 4 * i + half : 64 + 4 * i;
-  float cs[4], sn[4];
+  const bool rotated = kRun * i < half;
+  // The lane's two runs.
+  const int lo = kInterleaved ? 2 * kRun * i : rotated ? kRun * i : half + kRun * i;
+  const int hi = kInterleaved ? lo + kRun : rotated ? lo + half : 64 + kRun * i;
+  float cs[kRun], sn[kRun];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float2 v = rotated ? turn[wave][4 * i + e] : make_float2(1.f, 0.f);
-    cs[e] = v.x;
-    sn[e] = v.y;
+  for (int e = 0; e < kRun; ++e) {
+    cs[e] = rotated ? cosines[wave][kRun * i + e] : 1.f;
+    sn[e] = rotated ? sines[wave][kRun * i + e] : 0.f;
   }
-  float wq[8], wk[8];
-  {
-    auto weights = [&](const uint16_t* w, float* out) __attribute__((always_inline)) {
-      const uint2 u = w == nullptr ? make_uint2(0x3f803f80u, 0x3f803f80u) : *reinterpret_cast<const uint2*>(w + lo);
-      const uint2 v = w == nullptr ? make_uint2(0x3f803f80u, 0x3f803f80u) : *reinterpret_cast<const uint2*>(w + hi);
-      unpack8(make_uint4(u.x, u.y, v.x, v.y), out);
-    };
-    weights(a.q_weight, wq);
-    weights(a.k_weight, wk);
-  }
+  // (Weights of the two tensors in turn, kept as bf16 pairs.)
+  uint32_t wq[kRun], wk[kRun];
+  auto weights = [&](const uint16_t* w, uint32_t* out) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < kRun; ++e) out[e] = 0x3f803f80u;
+    if (w == nullptr) return;
+    load_words<kRun / 2, false>(w + lo, out);
+    load_words<kRun / 2, false>(w + hi, out + kRun / 2);
+  };
+  weights(a.q_weight, wq);
+  weights(a.k_weight, wk);
   const int64_t slots = (int64_t)a.cache.n_pages << a.cache.page_shift;
   const int slot = a.cached ? a.slots[tok] : -1;
   const bool cached = slot >= 0 && slot < slots;
@@ -334,56 +409,84 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a, 
                                : 0;
   const int rows = a.n_q_heads + a.n_kv_heads * (a.cached ? 2 : 1);
   const int end = min(rows, (part + 1) * rows_per_part);
-  for (int row = part * rows_per_part + sub; row < end; row += 4) {
-    const bool is_q = row < a.n_q_heads;
-    const bool is_v = row >= a.n_q_heads + a.n_kv_heads;
-    const int head = is_q ? row : is_v ? row - a.n_q_heads - a.n_kv_heads : row - a.n_q_heads;
-    const uint16_t* src = is_q ? a.Q + head * a.in.q_head + tok * a.in.q_tok
-                               : (is_v ? a.V : a.K) + head * a.in.kv_head + tok * a.in.kv_tok;
-    const uint2 u = *reinterpret_cast<const uint2*>(src + lo);
-    const uint2 v = *reinterpret_cast<const uint2*>(src + hi);
-    float x[8];
-    unpack8(make_uint4(u.x, u.y, v.x, v.y), x);
-    if (!is_v) {
-      float sq = 0.f;
+
+  for (int row0 = part * rows_per_part + sub; row0 < end; row0 += kRows * kUnroll) {
+    uint32_t w[kUnroll][kRun];  // lo's elements in the first half of the words, then hi's
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sq = fmaf(x[e], x[e], sq);
-      sq = row_sum16(sq);  // (16 lanes of one row: all of them are here)
-      const bool normed = (is_q ? a.q_weight : a.k_weight) != nullptr;
-      const float inv = normed ? 1.f / sqrtf(sq * (1.f / kHeadDim) + a.eps) : 1.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] *= inv * (is_q ? wq[e] : wk[e]);
-      float y[8];
-      if (rotated) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int p = kInterleaved ? 2 * e : e, q = kInterleaved ? 2 * e + 1 : e + 4;
-          y[p] = x[p] * cs[e] - x[q] * sn[e];
-          y[q] = x[q] * cs[e] + x[p] * sn[e];
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = y[e];
+    for (int u = 0; u < kUnroll; ++u) {
+      const int row = row0 + u * kRows;
+      if (row < end) {
+        const bool is_q = row < a.n_q_heads, is_v = row >= a.n_q_heads + a.n_kv_heads;
+        const int head = is_q ? row : is_v ? row - a.n_q_heads - a.n_kv_heads : row - a.n_q_heads;
+        const uint16_t* src = is_q ? a.Q + head * a.in.q_head + tok * a.in.q_tok
+                                   : (is_v ? a.V : a.K) + head * a.in.kv_head + tok * a.in.kv_tok;
+        load_words<kRun / 2, kOnce>(src + lo, w[u]);
+        load_words<kRun / 2, kOnce>(src + hi, w[u] + kRun / 2);
       }
     }
-    const uint2 b_lo = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
-    const uint2 b_hi = make_uint2(pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-    uint16_t* dst = is_q ? a.Q_out + head * a.out.q_head + tok * a.out.q_tok
-                         : is_v || a.K_out == nullptr ? nullptr : a.K_out + head * a.out.kv_head + tok * a.out.kv_tok;
-    if (dst != nullptr) {
-      *reinterpret_cast<uint2*>(dst + lo) = b_lo;
-      *reinterpret_cast<uint2*>(dst + hi) = b_hi;
-    }
-    if (!is_q && cached) {
-      const int64_t at = place + head * a.cache.head;
-      void* base = is_v ? a.cache.V : a.cache.K;
-      if (a.cache.amax == nullptr) {
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(base) + at + lo) = b_lo;
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(base) + at + hi) = b_hi;
-      } else {
-        const float m = a.cache.amax[is_v ? a.n_kv_heads + head : head];
-        const float scale = m > 0.f ? 448.f / m : 1.f;
-        *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(base) + at + lo) = pack_e4m3(x, scale);
-        *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(base) + at + hi) = pack_e4m3(x + 4, scale);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int row = row0 + u * kRows;
+      if (row >= end) break;
+      const bool is_q = row < a.n_q_heads, is_v = row >= a.n_q_heads + a.n_kv_heads;
+      const int head = is_q ? row : is_v ? row - a.n_q_heads - a.n_kv_heads : row - a.n_q_heads;
+      float x[2 * kRun];
+#pragma unroll
+      for (int e = 0; e < kRun; ++e) {
+        x[2 * e] = bf16_lo(w[u][e]);
+        x[2 * e + 1] = bf16_hi(w[u][e]);
+      }
+      if (!is_v) {
+        float sq = 0.f;
+#pragma unroll
+        for (int e = 0; e < 2 * kRun; ++e) sq = fmaf(x[e], x[e], sq);
+        sq = row_sum<kLanes>(sq);  // (the row's lanes are all here)
+        const bool normed = (is_q ? a.q_weight : a.k_weight) != nullptr;
+        const float inv = normed ? 1.f / sqrtf(sq * (1.f / kHeadDim) + a.eps) : 1.f;
+#pragma unroll
+        for (int e = 0; e < kRun; ++e) {
+          const uint32_t g = is_q ? wq[e] : wk[e];
+          x[2 * e] *= inv * bf16_lo(g);
+          x[2 * e + 1] *= inv * bf16_hi(g);
+        }
+        if (rotated) {
+#pragma unroll
+          for (int e = 0; e < kRun; ++e) {
+            const int p = kInterleaved ? 2 * e : e, q = kInterleaved ? 2 * e + 1 : e + kRun;
+            const float xp = x[p], xq = x[q];
+            x[p] = xp * cs[e] - xq * sn[e];
+            x[q] = xq * cs[e] + xp * sn[e];
+          }
+        }
+      }
+      uint32_t b[kRun];
+#pragma unroll
+      for (int e = 0; e < kRun; ++e) b[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
+      if (is_v) {  // (as it came: a NaN keeps its bits)
+#pragma unroll
+        for (int e = 0; e < kRun; ++e) b[e] = w[u][e];
+      }
+      uint16_t* dst = is_q ? a.Q_out + head * a.out.q_head + tok * a.out.q_tok
+                           : is_v || a.K_out == nullptr ? nullptr : a.K_out + head * a.out.kv_head + tok * a.out.kv_tok;
+      if (dst != nullptr) {
+        store_words<kRun / 2, kOnce>(dst + lo, b);
+        store_words<kRun / 2, kOnce>(dst + hi, b + kRun / 2);
+      }
+      if (!is_q && cached) {
+        const int64_t at = place + head * a.cache.head;
+        void* base = is_v ? a.cache.V : a.cache.K;
+        if (a.cache.amax == nullptr) {
+          store_words<kRun / 2, kOnce>(static_cast<uint16_t*>(base) + at + lo, b);
+          store_words<kRun / 2, kOnce>(static_cast<uint16_t*>(base) + at + hi, b + kRun / 2);
+        } else {
+          const float m = a.cache.amax[is_v ? a.n_kv_heads + head : head];
+          const float scale = m > 0.f ? 448.f / m : 1.f;
+          uint32_t code[kRun / 2];
+#pragma unroll
+          for (int e = 0; e < kRun / 2; ++e) code[e] = pack_e4m3(x + 4 * e, scale);
+          store_words<kRun / 4, kOnce>(static_cast<uint8_t*>(base) + at + lo, code);
+          store_words<kRun / 4, kOnce>(static_cast<uint8_t*>(base) + at + hi, code + kRun / 4);
+        }
       }
     }
   }
@@ -391,15 +494,21 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a, 
 
 hipError_t launch_qk_norm_rope(const RopeArgs& a, hipStream_t s) {
   const int rows = a.n_q_heads + a.n_kv_heads * (a.cached ? 2 : 1);
+  const bool once = (int64_t)a.n_tokens * rows * (2 * kHeadDim) >= kRopeCachedBytes;
+  const bool wide = once && a.rot_dim % 16 == 0;
+  const int at_once = wide ? 8 : 4;
   int parts = 1;
-  while (parts * 4 < rows && (int64_t)a.n_tokens * parts < 4096) parts *= 2;
-  const int rows_per_part = ((rows + parts - 1) / parts + 3) / 4 * 4;
+  while (parts * at_once < rows && (int64_t)a.n_tokens * parts < kRopeSpread) parts *= 2;
+  const int rows_per_part = ((rows + parts - 1) / parts + at_once - 1) / at_once * at_once;
+  parts = (rows + rows_per_part - 1) / rows_per_part;
   const int64_t waves = (int64_t)a.n_tokens * parts;
   const dim3 grid((unsigned)((waves + kRopeWaves - 1) / kRopeWaves));
-  if (a.interleaved)
-    hipLaunchKernelGGL(qk_norm_rope_kernel<true>, grid, dim3(kRopeThreads), 0, s, a, parts, rows_per_part);
-  else
-    hipLaunchKernelGGL(qk_norm_rope_kernel<false>, grid, dim3(kRopeThreads), 0, s, a, parts, rows_per_part);
+  using Kernel = void (*)(RopeArgs, int, int);
+  static constexpr Kernel kernels[3][2] = {
+      {qk_norm_rope_kernel<16, false, false>, qk_norm_rope_kernel<16, true, false>},
+      {qk_norm_rope_kernel<16, false, true>, qk_norm_rope_kernel<16, true, true>},
+      {qk_norm_rope_kernel<8, false, true>, qk_norm_rope_kernel<8, true, true>}};
+  hipLaunchKernelGGL(kernels[wide ? 2 : once][a.interleaved], grid, dim3(kRopeThreads), 0, s, a, parts, rows_per_part);
   return hipGetLastError();
 }
 

@@ -209,6 +209,9 @@ ROPE = [
     (41, 12, 2, 120, False, False, True, 16, "qkv", "tokens", "new"),
     (4500, 9, 3, 96, False, True, False, 16, "qkv", "heads", "new"),
     (6, 512, 1, 128, False, True, False, 16, "tokens", "heads", "new"),
+    (4111, 64, 8, 128, False, True, False, 16, "qkv", "heads", "in place"),   # 84 MB of rows: past the caches
+    (4111, 64, 8, 96, True, True, True, 128, "qkv", "tokens", "new"),
+    (4111, 64, 8, 72, False, True, False, 64, "tokens", "heads", "new"),       # (in runs of four)
 ]
 
 
