@@ -93,12 +93,6 @@ __host__ __device__ inline Work work_of_heads(int n_q_heads, int n_kv_heads) {
   return w;
 }
 
-__device__ __forceinline__ int clamped_length(const DecodeArgs& a, const int32_t* lens, int row) {
-  const int64_t cap = (int64_t)a.max_pages << a.cache.page_shift;
-  const int len = lens[row];
-  return (int)(len < cap ? len : cap);
-}
-
 // A row's share in the dealing out: its tiles, and kRowCost more for what it
 // costs to start and end a row.
 template <bool kFp8>
@@ -106,28 +100,39 @@ __device__ __forceinline__ int share_of(int len) {
   return len > 0 ? (len - 1) / kTile<kFp8> + 1 + kRowCost : 0;
 }
 
-// first[row]: shares of the rows before it, first[n_rows]: of all.  Each thread
-// sums n_rows / 256 rows, then a scan over the threads.
+// first[row]: shares of the rows before it, first[n_rows]: of all; length[row].
+// Each thread sums n_rows / 256 rows, then a scan over the threads.
 template <bool kFp8>
-__device__ __forceinline__ void tile_offsets(const DecodeArgs& a, const int32_t* lens, int* first, int* sums) {
+__device__ __forceinline__ void tile_offsets(const DecodeArgs& a, const int32_t* lens, int* first, int* length,
+                                             int* sums) {
+  constexpr int kPer = kMaxRows / kThreads;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int per = (a.n_rows + kThreads - 1) / kThreads, row0 = t * per;
-  int mine = 0;
-  for (int i = 0; i < per && row0 + i < a.n_rows; ++i)
-    mine += share_of<kFp8>(clamped_length(a, lens, row0 + i));
-  int x = mine;
+  const int64_t cap = (int64_t)a.max_pages << a.cache.page_shift;
+  int share[kPer], mine = 0;
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int u = __shfl_up(x, d);
-    if (lane >= d) x += u;
+  for (int i = 0; i < kPer; ++i) share[i] = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    if (i >= per) break;
+    if (row0 + i < a.n_rows) {
+      const int len = lens[row0 + i], clamped = (int)(len < cap ? len : cap);
+      length[row0 + i] = clamped;
+      share[i] = share_of<kFp8>(clamped);
+    }
+    mine += share[i];
   }
+  const int x = wave_scan(mine, [](int u, int v) { return u + v; });
   if (lane == 63) sums[wave] = x;
   __syncthreads();
   int before = x - mine;
-  for (int w = 0; w < wave; ++w) before += sums[w];
-  for (int i = 0; i < per && row0 + i < a.n_rows; ++i) {
-    first[row0 + i] = before;
-    before += share_of<kFp8>(clamped_length(a, lens, row0 + i));
+#pragma unroll
+  for (int w = 0; w < kWaves - 1; ++w) before += w < wave ? sums[w] : 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    if (i >= per) break;
+    if (row0 + i < a.n_rows) first[row0 + i] = before;
+    before += share[i];
   }
   if (t == kThreads - 1) first[a.n_rows] = before;
   __syncthreads();
@@ -382,7 +387,7 @@ __device__ __forceinline__ int row_from(const int* first, int n_rows, int x) {
 template <bool kFp8, bool kWhole>
 __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(DecodeArgs a, const int32_t* __restrict__ lens,
                                                                 const int32_t* __restrict__ page_table) {
-  __shared__ int first[kMaxRows + 1], sums[kWaves];
+  __shared__ int first[kMaxRows + 1], length[kMaxRows], sums[kWaves];
   __shared__ __align__(16) float acc[kWaves][kCols][kPad];
   __shared__ float ms[kWaves][kCols], ls[kWaves][kCols];
   const int lane = threadIdx.x & 63, c = lane >> 4, col = lane & 15;
@@ -392,7 +397,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(DecodeArgs a,
   const int g = unit / wk.tiles_of_cols, group = a.n_q_heads / a.n_kv_heads;
   const int head0 = g * group + (unit % wk.tiles_of_cols) * kCols;
   const int cols = min(kCols, (g + 1) * group - head0);
-  tile_offsets<kFp8>(a, lens, first, sums);
+  tile_offsets<kFp8>(a, lens, first, length, sums);
   const int T = first[a.n_rows], W = workers_of(T, wk.workers);
   int t = worker < W ? start_of(T, worker, W) : T, t_end = worker < W ? start_of(T, worker + 1, W) : T;
   if (kWhole) {
@@ -404,7 +409,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(DecodeArgs a,
 
   // Empty rows: zeros, and -inf.
   for (int row = worker; row < a.n_rows; row += wk.workers) {
-    if (first[row + 1] != first[row] || lens[row] != 0) continue;
+    if (length[row] != 0) continue;
     for (int x = threadIdx.x; x < cols * (kHeadDim / 8); x += kThreads)
       *reinterpret_cast<uint4*>(a.O + (head0 + x / 16) * a.q_head + row * a.q_tok + 8 * (x % 16)) =
           make_uint4(0u, 0u, 0u, 0u);
@@ -446,7 +451,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(DecodeArgs a,
         next.row = __builtin_amdgcn_readfirstlane(r);
         next.tile = __builtin_amdgcn_readfirstlane(x - first[r]);
         next.end = __builtin_amdgcn_readfirstlane(to - first[r]);
-        next.len = __builtin_amdgcn_readfirstlane(clamped_length(a, lens, next.row));
+        next.len = __builtin_amdgcn_readfirstlane(length[next.row]);
         return;
       }
     }
@@ -567,9 +572,9 @@ __global__ __launch_bounds__(kJoinThreads) void paged_decode_join_kernel(DecodeA
   const Work wk = work_of_heads(a.n_q_heads, a.n_kv_heads);
   const bool by_row = a.n_rows <= wk.workers;
   const int unit = blockIdx.x % wk.units;
-  if (by_row && a.seq_lens[blockIdx.x / wk.units] <= 0) return;  // (no worker has it)
   const Shared shared = shared_rows(a)[blockIdx.x];
-  if (shared.row < 0) return;
+  const int len = by_row ? a.seq_lens[blockIdx.x / wk.units] : 1;
+  if (len <= 0 || shared.row < 0) return;  // (a row of no length is no worker's)
   const int wa = shared.first;
   const int g = unit / wk.tiles_of_cols, group = a.n_q_heads / a.n_kv_heads;
   const int head0 = g * group + (unit % wk.tiles_of_cols) * kCols;

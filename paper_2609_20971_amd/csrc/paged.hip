@@ -15,26 +15,13 @@ constexpr int kMost = 1 << 29;                 // sums stop here, past every lim
 
 __device__ __forceinline__ int capped_add(int a, int b) { return min(a + b, kMost); }  // a, b in 0 .. kMost
 
-// x of the lanes before this one and its own, summed: within each row of 16 lanes,
-// then the last lane of row 0 (2) onto row 1 (3), then that of the first two rows
-// onto the others.  A lane or row with no source takes 0.
-__device__ __forceinline__ int wave_scan(int x) {
-  x = capped_add(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));  // row_shr 1
-  x = capped_add(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));  // row_shr 2
-  x = capped_add(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));  // row_shr 4
-  x = capped_add(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));  // row_shr 8
-  x = capped_add(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));  // row_bcast 15
-  x = capped_add(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));  // row_bcast 31
-  return x;
-}
-
 // Sums of two counts over the threads before this one, and over all of them.
 // Capped addition of nonnegative numbers is associative, so that the order of
 // the partial sums does not matter.
 __device__ __forceinline__ void scan_pair(int a, int b, int* sums, int& a_before, int& b_before, int& a_all,
                                           int& b_all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int x = wave_scan(a), y = wave_scan(b);
+  const int x = wave_scan(a, capped_add), y = wave_scan(b, capped_add);
   constexpr int kWaves = kPageThreads / 64;
   if (lane == 63) {
     sums[wave] = x;
