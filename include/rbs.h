@@ -520,18 +520,18 @@ size_t rbs_decode_workspace_bytes(void);
 /*
  * Attention of one new token per row over the row's cached tokens (the new
  * token's own key and value among them, put there by rbs_qk_norm_rope).
- * shape: n_tokens rows (up to RBS_MAX_ROWS), H_q (up to 512) and H_kv heads, strides of Q and O (any
- * block_size; kv strides are not used).  For query head h of row s
+ * shape: n_tokens rows (up to RBS_MAX_ROWS), H_q (up to 512) and H_kv heads,
+ * strides of Q and O (any block_size; kv strides are not used).  For query head h
+ * of row s
  *   O = sum_j softmax_j(q . k_j * scale) v_j over the first seq_lens[s] tokens
  * with fp32 sums, rounded to bf16; Q, O bf16 (head, row, dimension) with the
  * strides of Q.  softmax_scale <= 0 selects 1/sqrt(d).  lse: NULL or fp32
  * [H_q][n_tokens], natural log.  A row of length 0: O = 0, lse = -inf; an
  * unused row (negative length): its O and lse are left as they were.
- * page_table int32 [n_tokens][max_pages] (n_tokens * (max_pages * page_size / 32 + 8) < 2^31),
- * seq_lens int32 [n_tokens].  Both are trusted
- * like the prefill's lists: page numbers are clamped to the cache and lengths
- * to the table, so that no access leaves the buffers.  Places past a row's
- * length may hold anything.
+ * page_table int32 [n_tokens][max_pages], seq_lens int32 [n_tokens], with
+ * n_tokens * (max_pages * page_size / 32 + 8) < 2^31.  Both are trusted like the
+ * prefill's lists: page numbers are clamped to the cache and lengths to the table, so that no access leaves the buffers.  Places past a row's
+ * length may hold anything; an infinity in a value that is attended may give NaN.
  */
 int rbs_paged_decode(const rbs_shape* shape, const rbs_cache* cache, const void* Q, const int32_t* page_table,
                      int32_t max_pages, const int32_t* seq_lens, float softmax_scale, void* O, float* lse,

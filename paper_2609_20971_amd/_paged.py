@@ -106,7 +106,7 @@ def _one_dimensional(name, t, dtype, n=None):
     L._check_tensor(name, t, dtype, (n,) if n is not None else (-1,))
 
 
-@dataclass(frozen=True)
+@dataclass(frozen=True, eq=False)
 class PagedCache:
     """Keys and values of a paged cache: K and V [n_pages][H_kv][page_size][d]
     views of any strides the library takes (for [n_pages][page_size][H_kv][d]
@@ -115,8 +115,8 @@ class PagedCache:
     K: torch.Tensor
     V: torch.Tensor
     amax: torch.Tensor | None = None
-    c: rbs_cache = field(init=False, repr=False, compare=False)
-    device: int = field(init=False, repr=False, compare=False)
+    c: rbs_cache = field(init=False, repr=False)
+    device: int = field(init=False, repr=False)
 
     def __post_init__(self):
         K, V = self.K, self.V
@@ -153,7 +153,7 @@ class PagedCache:
         return self.K.shape[2]
 
 
-@dataclass(frozen=True)
+@dataclass(frozen=True, eq=False)
 class Pages:
     """The bookkeeping of a cache's pages (int32 device tensors): the page table
     [n_rows][max_pages], the stack of free pages [n_pages] and how many it
@@ -164,9 +164,9 @@ class Pages:
     n_free: torch.Tensor
     seq_lens: torch.Tensor
     page_size: int
-    c: rbs_pages = field(init=False, repr=False, compare=False)
-    device: int = field(init=False, repr=False, compare=False)
-    state: tuple = field(init=False, repr=False, compare=False)  # addresses of seq_lens and n_free
+    c: rbs_pages = field(init=False, repr=False)
+    device: int = field(init=False, repr=False)
+    state: tuple = field(init=False, repr=False)  # addresses of seq_lens and n_free
 
     def __post_init__(self):
         i32, table = torch.int32, self.page_table
@@ -195,7 +195,7 @@ class Pages:
         return self.page_table.shape[0]
 
 
-@dataclass(frozen=True)
+@dataclass(frozen=True, eq=False)
 class PageStep:
     """Outputs of rbs_pages_extend (int32 device tensors)."""
     seq_lens: torch.Tensor   # [n_rows]
@@ -204,9 +204,9 @@ class PageStep:
     positions: torch.Tensor  # [max_tokens]
     slots: torch.Tensor      # [max_tokens]
     status: torch.Tensor     # [1]
-    device: int = field(init=False, repr=False, compare=False)
-    max_tokens: int = field(init=False, repr=False, compare=False)
-    out: tuple = field(init=False, repr=False, compare=False)  # the tensors' addresses
+    device: int = field(init=False, repr=False)
+    max_tokens: int = field(init=False, repr=False)
+    out: tuple = field(init=False, repr=False)  # the tensors' addresses
 
     def __post_init__(self):
         i32 = torch.int32
@@ -278,7 +278,7 @@ def rbs_pages_release(pages: Pages, released, status=None, stream=None) -> torch
     return status
 
 
-@dataclass(frozen=True)
+@dataclass(frozen=True, eq=False)
 class Rope:
     """Norm and rotation of rbs_qk_norm_rope: inv_freq fp32 [rot_dim / 2] (None:
     no rotation), norm weights bf16 [d] (None: that tensor is not normed)."""
@@ -289,8 +289,8 @@ class Rope:
     interleaved: bool = False
     factor: float = 1.0
     head_dim: int = 128
-    c: rbs_rope = field(init=False, repr=False, compare=False)
-    device: int | None = field(init=False, repr=False, compare=False)
+    c: rbs_rope = field(init=False, repr=False)
+    device: int | None = field(init=False, repr=False)
 
     def __post_init__(self):
         if self.inv_freq is not None:
@@ -390,12 +390,16 @@ def rbs_decode_workspace_bytes() -> int:
 
 def _auto_workspace(device: int, handle: int) -> torch.Tensor:
     """The workspace of a (device, stream): calls on one stream are ordered, so
-    they may share it.  While the current stream is being captured, a new one,
-    which belongs to the graph's memory: graphs that were captured on one stream
-    may run side by side."""
-    ws = _decode_workspaces.get((device, handle))
-    if ws is None or torch.cuda.is_current_stream_capturing():
-        capturing = torch.cuda.is_current_stream_capturing()
+    they may share it.  While the stream is being captured, a new one, which
+    belongs to the graph's memory: graphs that were captured on one stream may run
+    side by side."""
+    if handle != torch._C._cuda_getCurrentRawStream(device):
+        # Made on the stream that uses it, whose order its memory's next use has to follow.
+        with torch.cuda.stream(torch.cuda.ExternalStream(handle, device)):
+            return _auto_workspace(device, handle)
+    capturing = torch.cuda.is_current_stream_capturing()
+    ws = None if capturing else _decode_workspaces.get((device, handle))
+    if ws is None:
         ws = torch.empty(rbs_decode_workspace_bytes() // 4, dtype=torch.float32, device=torch.device("cuda", device))
         if not capturing:
             _decode_workspaces[device, handle] = ws

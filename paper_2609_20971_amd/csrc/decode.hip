@@ -60,6 +60,12 @@ constexpr int64_t kCachedBytes = int64_t(16) << 20;
 // rows comes late (24 rows of 1 to 9000 keys 28.4 us, 1: 23.4, 2 to 8: 21.3; 300
 // rows of 10 to 600 keys 1: 33.7, 4: 30.3, 8: 32.8).
 constexpr int kRowCost = 4;
+// Rows are a wave's alone where no share is longer than kSoloShare, nor than
+// kSoloRatio times an average wave's.  A workgroup's / a wave's: 300 rows of 10 to
+// 100 FP8 keys, 4 KV heads, 18.3 / 14.9 us, 256 rows of 20 to 100, 8 / 8 heads, 20.7 /
+// 18.1, 300 of 100 to 300 FP8 keys, 64 / 8, 37.5 / 35.9; longer rows 300 of 700 to 800,
+// 64 / 8, 163 / 167; more different ones (a ratio of 3) 300 of 10 to 1000 64.9 / 73.9.
+constexpr int kSoloShare = 20, kSoloRatio = 2;
 // A join by single columns takes at most so many workgroups: one row of 20000 keys
 // 18.2 us and not 20.8, of 131000 57 and not 60; but 64 rows 72 and not 65.
 constexpr int kJoinThreads = 512, kFewJoins = 512;
@@ -100,16 +106,17 @@ __device__ __forceinline__ int share_of(int len) {
   return len > 0 ? (len - 1) / kTile<kFp8> + 1 + kRowCost : 0;
 }
 
-// first[row]: shares of the rows before it, first[n_rows]: of all; length[row].
-// Each thread sums n_rows / 256 rows, then a scan over the threads.
+// first[row]: shares of the rows before it, first[n_rows]: of all; length[row];
+// returns the longest share.  Each thread sums n_rows / 256 rows, then a scan over
+// the threads.
 template <bool kFp8>
-__device__ __forceinline__ void tile_offsets(const DecodeArgs& a, const int32_t* lens, int* first, int* length,
+__device__ __forceinline__ int tile_offsets(const DecodeArgs& a, const int32_t* lens, int* first, int* length,
                                              int* sums) {
   constexpr int kPer = kMaxRows / kThreads;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int per = (a.n_rows + kThreads - 1) / kThreads, row0 = t * per;
   const int64_t cap = (int64_t)a.max_pages << a.cache.page_shift;
-  int share[kPer], mine = 0;
+  int share[kPer], mine = 0, longest = 0;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) share[i] = 0;
 #pragma unroll
@@ -121,10 +128,17 @@ __device__ __forceinline__ void tile_offsets(const DecodeArgs& a, const int32_t*
       share[i] = share_of<kFp8>(clamped);
     }
     mine += share[i];
+    longest = max(longest, share[i]);
   }
   const int x = wave_scan(mine, [](int u, int v) { return u + v; });
-  if (lane == 63) sums[wave] = x;
+  longest = wave_scan(longest, [](int u, int v) { return max(u, v); });
+  if (lane == 63) {
+    sums[wave] = x;
+    sums[kWaves + wave] = longest;
+  }
   __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) longest = max(longest, sums[kWaves + w]);
   int before = x - mine;
 #pragma unroll
   for (int w = 0; w < kWaves - 1; ++w) before += w < wave ? sums[w] : 0;
@@ -136,6 +150,7 @@ __device__ __forceinline__ void tile_offsets(const DecodeArgs& a, const int32_t*
   }
   if (t == kThreads - 1) first[a.n_rows] = before;
   __syncthreads();
+  return __builtin_amdgcn_readfirstlane(longest);
 }
 
 // The workers that share T tiles: each has at least a tile for each wave.
@@ -387,7 +402,7 @@ __device__ __forceinline__ int row_from(const int* first, int n_rows, int x) {
 template <bool kFp8, bool kWhole>
 __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(DecodeArgs a, const int32_t* __restrict__ lens,
                                                                 const int32_t* __restrict__ page_table) {
-  __shared__ int first[kMaxRows + 1], length[kMaxRows], sums[kWaves];
+  __shared__ int first[kMaxRows + 1], length[kMaxRows], sums[2 * kWaves];
   __shared__ __align__(16) float acc[kWaves][kCols][kPad];
   __shared__ float ms[kWaves][kCols], ls[kWaves][kCols];
   const int lane = threadIdx.x & 63, c = lane >> 4, col = lane & 15;
@@ -397,13 +412,17 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(DecodeArgs a,
   const int g = unit / wk.tiles_of_cols, group = a.n_q_heads / a.n_kv_heads;
   const int head0 = g * group + (unit % wk.tiles_of_cols) * kCols;
   const int cols = min(kCols, (g + 1) * group - head0);
-  tile_offsets<kFp8>(a, lens, first, length, sums);
-  const int T = first[a.n_rows], W = workers_of(T, wk.workers);
-  int t = worker < W ? start_of(T, worker, W) : T, t_end = worker < W ? start_of(T, worker + 1, W) : T;
-  if (kWhole) {
-    t = first[row_from(first, a.n_rows, t)];
-    t_end = first[row_from(first, a.n_rows, t_end)];
+  const int longest = tile_offsets<kFp8>(a, lens, first, length, sums);
+  const int T = first[a.n_rows];
+  // Many short rows: each wave takes whole rows for itself, with nothing to join.
+  const bool solo = longest <= kSoloShare && (int64_t)longest * (kWaves * wk.workers) <= (int64_t)kSoloRatio * T;
+  const int W = solo ? kWaves * wk.workers : workers_of(T, wk.workers), id = solo ? kWaves * worker + wave : worker;
+  int t = id < W ? start_of(T, id, W) : T, t_end = id < W ? start_of(T, id + 1, W) : T;
+  if (kWhole || solo) {
+    t = __builtin_amdgcn_readfirstlane(first[row_from(first, a.n_rows, t)]);
+    t_end = __builtin_amdgcn_readfirstlane(first[row_from(first, a.n_rows, t_end)]);
   }
+  const int step = solo ? 1 : kWaves, offset = solo ? 0 : wave;
   const bool by_row = a.n_rows <= wk.workers;
   Shared shared{-1, 0, 0, 0};
 
@@ -439,14 +458,14 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(DecodeArgs a,
     int row, tile, end, len;  // end: of the row's share
   } next{-1, 0, 0, 0};
   // Moves the cursor to the wave's first tile in row r or after it: the wave takes
-  // tiles wave, wave + 4, .. of each row's share.
+  // tiles offset, offset + step, .. of each row's share.
   auto seek = [&](int r) __attribute__((always_inline)) {
     for (;; ++r) {
       if (r >= a.n_rows || first[r] >= t_end) {
         next.row = -1;
         return;
       }
-      const int x = max(first[r], t) + wave, to = min(first[r + 1] - kRowCost, t_end);
+      const int x = max(first[r], t) + offset, to = min(first[r + 1] - kRowCost, t_end);
       if (x < to) {
         next.row = __builtin_amdgcn_readfirstlane(r);
         next.tile = __builtin_amdgcn_readfirstlane(x - first[r]);
@@ -501,13 +520,30 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(DecodeArgs a,
     for (int i = 0; i < 8; ++i) s.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     while (next.row == r) {
       const int j = next.tile * kTile<kFp8>, len = next.len;
-      next.tile += kWaves;
+      next.tile += step;
       if (next.tile >= next.end) seek(r + 1);
       int64_t base[kSteps] = {};
       if (next.row >= 0) offsets(base);
       attend_tile<kFp8>(st, tile, q, scale_log2, j, len, next.row >= 0, base, s);
     }
     s.l = over_rows(s.l, [](float a, float b) { return a + b; });
+
+    if (solo) {
+      if (col < cols) {
+        const float f = v_scale / s.l;
+        uint16_t* out = a.O + (head0 + col) * a.q_head + r * a.q_tok + 32 * c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          *reinterpret_cast<uint4*>(out + 8 * e) =
+              make_uint4(two_bf16(s.o[0][e] * f, s.o[1][e] * f), two_bf16(s.o[2][e] * f, s.o[3][e] * f),
+                         two_bf16(s.o[4][e] * f, s.o[5][e] * f), two_bf16(s.o[6][e] * f, s.o[7][e] * f));
+        if (c == 0 && a.lse != nullptr)
+          a.lse[(int64_t)(head0 + col) * a.n_rows + r] = (s.m + __log2f(s.l)) * 0.69314718055994531f;
+      }
+      if (!kWhole && by_row && lane == 0) shared_rows(a)[r * wk.units + unit] = Shared{-1, 0, 0, 0};
+      at = first[r + 1];
+      continue;
+    }
 
     // The four waves' states joined.
     if (c == 0) {

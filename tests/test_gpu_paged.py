@@ -382,7 +382,7 @@ def _check_decode(c, O, lse, scale, untouched=None):
     return worst
 
 
-def _run_decode(c, scale=0.0, q_layout="tokens", with_lse=True, **more):
+def _run_decode(c, scale=0.0, q_layout="tokens", with_lse=True, ready=False, **more):
     q = c["q"].cuda()
     if q_layout == "tokens":
         Q = q.transpose(0, 1)
@@ -394,7 +394,12 @@ def _run_decode(c, scale=0.0, q_layout="tokens", with_lse=True, **more):
     O.fill_(math.nan)
     lse = torch.full((c["hq"], c["n"]), math.nan, device="cuda") if with_lse else None
     shape = rbs.make_shape(c["n"], c["hq"], c["hkv"], 64)
-    got = rbs.rbs_paged_decode(shape, Q, c["cache"], c["table"].cuda(), _ints(c["lens"]), scale, O=O, lse=lse, **more)
+    table, lens = c["table"].cuda(), _ints(c["lens"])
+    if ready:  # the call goes to another stream than the one that made its tensors
+        torch.cuda.synchronize()
+    got = rbs.rbs_paged_decode(shape, Q, c["cache"], table, lens, scale, O=O, lse=lse, **more)
+    if ready:
+        torch.cuda.synchronize()
     assert got is O
     return O, lse
 
@@ -418,6 +423,15 @@ DECODE = [
     ([9000, 2, 4097, 0, 12345], 8, 2, 16, False, "heads", "tokens", 0.0),
     ([9000, 2, 4097, 0, 12345], 8, 2, 128, True, "heads", "tokens", 0.0),
     ([65537], 4, 4, 256, False, "tokens", "tokens", 0.0),
+    ([(i * 53) % 260 for i in range(700)], 16, 8, 16, False, "heads", "tokens", 0.0),    # a wave to a row
+    ([(i * 53) % 500 - 1 for i in range(700)], 14, 2, 32, True, "heads", "qkv", 0.0),
+    ([(i * 53) % 90 for i in range(600)] + [1500], 8, 8, 64, False, "tokens", "tokens", 0.0),  # and one long row
+    ([150] * 520 + [2500] * 3, 16, 1, 16, False, "heads", "tokens", 0.0),                # more rows than workers
+    ([768] * 3, 8, 1, 256, False, "heads", "tokens", 0.0),
+    ([769, 1, 768], 8, 1, 16, False, "heads", "tokens", 0.0),
+    ([4000] * 70 + [1], 8, 2, 64, True, "heads", "tokens", 0.0),                          # past the caches
+    ([5000] * 8 + [0, 33], 16, 4, 16, False, "tokens", "tokens", 0.0),
+    ([512, 3000], 512, 512, 16, False, "heads", "tokens", 0.0),                           # as many units as workers
     ([150001], 8, 1, 64, False, "heads", "tokens", 0.0),
 ]
 
@@ -493,6 +507,10 @@ def test_decode_on_a_side_stream_and_own_workspace():
     s.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(s):
         got = _run_decode(c)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    s.wait_stream(torch.cuda.current_stream())
+    got = _run_decode(c, stream=s, ready=True)  # given by name, from another current stream
     torch.cuda.synchronize()
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     ws = torch.full((rbs.rbs_decode_workspace_bytes() // 4,), math.nan, device="cuda")
