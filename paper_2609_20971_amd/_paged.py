@@ -91,13 +91,20 @@ def _on(device: int, stream, call, *args):
         return call(*args, _handle(device, stream))
 
 
-def _same_gpu(t, *named) -> int:
-    """L._on_gpu of the named tensors, of which t is one, short where all is well."""
-    dev = t.get_device()
-    for _, x in named:
-        if x is not None and (x.get_device() != dev or dev < 0):
-            return L._on_gpu(*named)
-    return dev
+def _elsewhere(dev: int, *tensors) -> bool:
+    """Whether one of the tensors (None skipped) is not on GPU dev, or dev is none."""
+    for x in tensors:
+        if x is not None and x.get_device() != dev:
+            return True
+    return dev < 0
+
+
+def _strided(shape, q, kv=None):
+    """L._with_strides, short where the shape leaves the strides to the tensors."""
+    if shape.q_stride_head == shape.q_stride_tok == shape.kv_stride_head == shape.kv_stride_tok == 0:
+        return L.rbs_shape(shape.n_tokens, shape.n_q_heads, shape.n_kv_heads, shape.head_dim, shape.block_size, *q,
+                           *((0, 0) if kv is None else kv))
+    return L._with_strides(shape, q=q, kv=kv)
 
 
 def _one_dimensional(name, t, dtype, n=None):
@@ -363,16 +370,18 @@ def rbs_qk_norm_rope(shape: L.rbs_shape, rope: Rope, Q, K, positions, V=None, ca
         L._heads_tokens("Q_out", Q_out, hq, n, d)
     if K_out is not None:
         L._heads_tokens("K_out", K_out, hkv, n, d)
-    dev = _same_gpu(Q, ("Q", Q), ("K", K), ("positions", positions), ("V", V if cache is not None else None),
-                    ("slots", slots if cache is not None else None), ("cache.K", None if cache is None else cache.K),
-                    ("Q_out", Q_out), ("K_out", K_out))
+    dev = Q.get_device()
+    if _elsewhere(dev, K, positions, Q_out, K_out) or (cache is not None and (
+            cache.device != dev or _elsewhere(dev, V, slots))):
+        L._on_gpu(("Q", Q), ("K", K), ("positions", positions), ("Q_out", Q_out), ("K_out", K_out),
+                  *(() if cache is None else (("V", V), ("slots", slots), ("cache.K", cache.K))))
     if rope.device is not None and rope.device != dev:
         raise ValueError(f"rope is on cuda:{rope.device}, the other arguments on cuda:{dev}")
     if Q_out is None:
         Q_out = torch.empty_like(Q)  # Q's order of strides, without the gaps of a fused projection's view
     if K_out is None and keep_k:
         K_out = torch.empty_like(K)
-    sh = L._with_strides(shape, q=qs, kv=ks)
+    sh = _strided(shape, qs, ks)
     out = L.rbs_shape(n, hq, hkv, d, shape.block_size, *Q_out.stride()[:2],
                       *(ks if K_out is None else K_out.stride()[:2]))
     L._check("rbs_qk_norm_rope", _on(dev, stream, L.load().rbs_qk_norm_rope, sh, out, rope.c, Q.data_ptr(),
@@ -422,8 +431,10 @@ def rbs_paged_decode(shape: L.rbs_shape, Q, cache: PagedCache, page_table, seq_l
         L._check_out(O, Q)
     if lse is not None:
         L._check_tensor("lse", lse, torch.float32, (hq, n))
-    dev = _same_gpu(Q, ("cache.K", cache.K), ("Q", Q), ("page_table", page_table), ("seq_lens", seq_lens), ("O", O),
-                    ("lse", lse))
+    dev = Q.get_device()
+    if cache.device != dev or _elsewhere(dev, page_table, seq_lens, O, lse):
+        L._on_gpu(("cache.K", cache.K), ("Q", Q), ("page_table", page_table), ("seq_lens", seq_lens), ("O", O),
+                  ("lse", lse))
     if O is None:
         O = torch.empty_like(Q)
         if O.stride() != Q.stride():
@@ -435,7 +446,7 @@ def rbs_paged_decode(shape: L.rbs_shape, Q, cache: PagedCache, page_table, seq_l
         raise ValueError("workspace must be AUTO or a contiguous tensor on the inputs' GPU")
     elif workspace.numel() * workspace.element_size() < rbs_decode_workspace_bytes():
         raise ValueError("workspace is smaller than rbs_decode_workspace_bytes()")
-    L._check("rbs_paged_decode", _on(dev, stream, _decode, L._with_strides(shape, q=qs), cache, Q, page_table, seq_lens,
+    L._check("rbs_paged_decode", _on(dev, stream, _decode, _strided(shape, qs), cache, Q, page_table, seq_lens,
                                      softmax_scale, O, lse, workspace, dev))
     return O
 
