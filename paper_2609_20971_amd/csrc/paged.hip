@@ -61,6 +61,14 @@ __global__ __launch_bounds__(kPageThreads) void pages_extend_kernel(PagesArgs a,
   int add[kRowsPerThread], need[kRowsPerThread], page_of[kOne ? kRowsPerThread : 1];
   int tokens = 0, pages = 0;
   bool too_long = false;
+  // This workgroup's share of the new pages, before it is known how many there are.
+  constexpr int kTaken = kOne ? 1 : kFillTokens / kPageThreads;
+  int taken[kTaken];
+  if (!kOne) {
+#pragma unroll
+    for (int i = 0; i < kTaken; ++i)
+      taken[i] = a.free_pages[max(min(max(n_free, 0), a.n_pages) - 1 - ((int)blockIdx.x * kFillTokens + i * kPageThreads + t), 0)];
+  }
 #pragma unroll
   for (int i = 0; i < kRowsPerThread; ++i) add[i] = need[i] = 0;
 #pragma unroll
@@ -68,10 +76,9 @@ __global__ __launch_bounds__(kPageThreads) void pages_extend_kernel(PagesArgs a,
     const int row = row0 + i;
     if (i >= per) break;
     if (row < a.n_rows) {
-      const int len = a.seq_lens[row];
+      const int len = a.seq_lens[row], more = kOne ? 1 : max(a.new_tokens[row], 0);
       length[row] = len;
       if (len >= 0) {
-        const int more = kOne ? 1 : max(a.new_tokens[row], 0);
         if (kOne) page_of[i] = a.page_table[(int64_t)row * a.max_pages + min(len >> shift, a.max_pages - 1)];
         const int64_t held = ((int64_t)len + places) >> shift;
         const int64_t after = ((int64_t)len + more + places) >> shift;
@@ -127,37 +134,46 @@ __global__ __launch_bounds__(kPageThreads) void pages_extend_kernel(PagesArgs a,
            tok += kPageThreads)
         a.positions[tok] = a.slots[tok] = -1;
     } else {
-      if (ok) {
-        for (int k = begin + t; k < min(begin + kFillTokens, all_pages); k += kPageThreads) {
-          const int row = seq_of(first_page, a.n_rows, k);
-          const int at = ((length[row] + places) >> shift) + k - first_page[row];
-          a.page_table[(int64_t)row * a.max_pages + at] = a.free_pages[n_free - 1 - k];
+      // Four tokens a thread: where each one's page number stands, then all four loads
+      // at once (tokens with none read the stack's first entry, for nothing).
+      const int tok = begin + 4 * t;
+      int pos[4];
+      const int32_t* page_at[4];
+      int row = ok ? seq_of(first_token, a.n_rows, min(tok, max(all_tokens - 1, 0))) : 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        pos[i] = -1;
+        page_at[i] = a.free_pages;
+        if (ok && tok + i < all_tokens) {
+          while (first_token[row + 1] <= tok + i) ++row;
+          pos[i] = length[row] + tok + i - first_token[row];
+          const int at = pos[i] >> shift, held = (length[row] + places) >> shift;
+          page_at[i] = at < held ? a.page_table + (int64_t)row * a.max_pages + at
+                                 : a.free_pages + (n_free - 1 - (first_page[row] + at - held));
         }
       }
-      const int tok = begin + 4 * t;
-      if (tok < a.max_tokens) {
-        int pos[4], slot[4];
-        int row = ok ? seq_of(first_token, a.n_rows, min(tok, max(all_tokens - 1, 0))) : 0;
+      int slot[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          pos[i] = slot[i] = -1;
-          if (ok && tok + i < all_tokens) {
-            while (first_token[row + 1] <= tok + i) ++row;
-            pos[i] = length[row] + tok + i - first_token[row];
-            const int at = pos[i] >> shift, held = (length[row] + places) >> shift;
-            const int p = at < held ? a.page_table[(int64_t)row * a.max_pages + at]
-                                    : a.free_pages[n_free - 1 - (first_page[row] + at - held)];
-            slot[i] = (p << shift) + (pos[i] & places);
-          }
+      for (int i = 0; i < 4; ++i) slot[i] = *page_at[i];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) slot[i] = pos[i] < 0 ? -1 : (slot[i] << shift) + (pos[i] & places);
+      if (tok + 4 <= a.max_tokens) {
+        *reinterpret_cast<int4*>(a.positions + tok) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+        *reinterpret_cast<int4*>(a.slots + tok) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+      } else {
+        for (int i = 0; i < 4 && tok + i < a.max_tokens; ++i) {
+          a.positions[tok + i] = pos[i];
+          a.slots[tok + i] = slot[i];
         }
-        if (tok + 4 <= a.max_tokens) {
-          *reinterpret_cast<int4*>(a.positions + tok) = make_int4(pos[0], pos[1], pos[2], pos[3]);
-          *reinterpret_cast<int4*>(a.slots + tok) = make_int4(slot[0], slot[1], slot[2], slot[3]);
-        } else {
-          for (int i = 0; i < 4 && tok + i < a.max_tokens; ++i) {
-            a.positions[tok + i] = pos[i];
-            a.slots[tok + i] = slot[i];
-          }
+      }
+      if (ok) {
+#pragma unroll
+        for (int i = 0; i < kTaken; ++i) {
+          const int k = begin + i * kPageThreads + t;
+          if (k >= all_pages) break;
+          const int row = seq_of(first_page, a.n_rows, k);
+          const int at = ((length[row] + places) >> shift) + k - first_page[row];
+          a.page_table[(int64_t)row * a.max_pages + at] = taken[i];
         }
       }
     }
