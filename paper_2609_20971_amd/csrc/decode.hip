@@ -9,7 +9,7 @@
 //   ones, of the next row too, as soon as an operand has been used.
 // - S^T = K Q^T and O^T = V^T P^T in 16x16x32 products with the (up to 16) query
 //   heads of a KV head as columns.  Lane l holds column l % 16 of S, keys
-//   4 (l / 16) + r of each 16, which is what the second product takes as its
+//   4 (l / 16) + r of each 16 (FP8: another four), which is what the second product takes as its
 //   right operand if V's rows come in the same order: P never leaves its lane.
 //   V's operand needs eight keys of one element; a lane reads eight elements of
 //   eight keys (16 lanes: whole rows) and regroups them with byte permutes.
@@ -196,11 +196,23 @@ struct State {
 template <bool kFp8>
 struct Tile {
   static constexpr int kSteps = kTile<kFp8> / 16;
-  uint4 k[kSteps][kFp8 ? 2 : 4];  // of 16 keys, lane l % 16's
-  uint4 v[kSteps][kFp8 ? 2 : 4];  // of 16 keys, 4 (l / 16) + r, elements 8 (l % 16) .. (FP8: two of them in 16 bytes)
+  // Of 16 keys, with m = l % 16, c = l / 16.  bf16: key m, elements 32 x + 8 c ..;
+  // FP8: key 8 x + m / 2, elements 64 (m % 2) + 16 c ..: eight lanes to a row of 128
+  // bytes (in pieces of 64 200 rows of 300 to 2000 keys took 7% longer).
+  uint4 k[kSteps][kFp8 ? 2 : 4];
+  // bf16: key 4 c + x, elements 8 m ..; FP8: key 8 x + 2 c + m % 2, elements 16 (m / 2)
+  // .., of which half is for the lane next to it: in loads of 8 bytes, each for its
+  // own lane, a long read past the caches took 193 us and not 134.
+  uint4 v[kSteps][kFp8 ? 2 : 4];
 };
 
-// 16 (8) bytes of K or V; kOnce: without a place in the caches.
+// Which of 16 keys a lane's logit (and weight) u is of, 0 <= u < 4.
+template <bool kFp8>
+__device__ __forceinline__ int key_of(int c, int u) {
+  return kFp8 ? 8 * (u >> 1) + 2 * c + (u & 1) : 4 * c + u;
+}
+
+// 16 bytes of K or V; kOnce: without a place in the caches.
 template <bool kOnce>
 __device__ __forceinline__ uint4 load16(const char* p) {
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -208,12 +220,10 @@ __device__ __forceinline__ uint4 load16(const char* p) {
   const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
   return make_uint4(v.x, v.y, v.z, v.w);
 }
-template <bool kOnce>
-__device__ __forceinline__ uint2 load8(const char* p) {
-  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-  if (!kOnce) return *reinterpret_cast<const uint2*>(p);
-  const u32x2 v = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
-  return make_uint2(v.x, v.y);
+
+// The other lane's of two next to each other.
+__device__ __forceinline__ uint32_t neighbour(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xb1, 0xf, 0xf, false);  // quad_perm [1, 0, 3, 2]
 }
 
 template <bool kFp8>
@@ -245,29 +255,16 @@ struct Stream {
 #pragma unroll
     for (int h = 0; h < Tile<kFp8>::kSteps; ++h)
 #pragma unroll
-      for (int s = 0; s < (kFp8 ? 2 : 4); ++s) t.k[h][s] = load16<kOnce>(K + base[h] + k_off + 64 * s);
+      for (int x = 0; x < (kFp8 ? 2 : 4); ++x)
+        t.k[h][x] = load16<kOnce>(K + base[h] + k_off + x * (kFp8 ? 8 * tok_bytes : 64));
   }
   template <bool kOnce>
   __device__ __forceinline__ void load_v_as(Tile<kFp8>& t, const int64_t* base) const {
 #pragma unroll
     for (int h = 0; h < Tile<kFp8>::kSteps; ++h)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const char* p = V + base[h] + v_off + r * tok_bytes;
-        if (kFp8) {
-          const uint2 w = load8<kOnce>(p);
-          uint4& d = t.v[h][r >> 1];
-          if (r & 1) {
-            d.z = w.x;
-            d.w = w.y;
-          } else {
-            d.x = w.x;
-            d.y = w.y;
-          }
-        } else {
-          t.v[h][r] = load16<kOnce>(p);
-        }
-      }
+      for (int x = 0; x < (kFp8 ? 2 : 4); ++x)
+        t.v[h][x] = load16<kOnce>(V + base[h] + v_off + x * (kFp8 ? 8 : 1) * tok_bytes);
   }
 };
 
@@ -279,17 +276,26 @@ __device__ __forceinline__ void attend_tile(const Stream<kFp8>& st, Tile<kFp8>& 
                                             State& s) {
   constexpr int kSteps = Tile<kFp8>::kSteps;
   const int c = (threadIdx.x & 63) >> 4;
+  const bool odd = threadIdx.x & 1;
   f32x4 sc[kSteps];
 #pragma unroll
   for (int h = 0; h < kSteps; ++h) {
-    sc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (kFp8) {
+      // Rows 2 n and 2 n + 1 of the operand are the two halves of key n: the halves of
+      // q with it in turn, of which every other row counts.
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        sc[h] = mfma16(widen(tile.k[h][x].x, tile.k[h][x].y), q[2 * x], sc[h]);
-        sc[h] = mfma16(widen(tile.k[h][x].z, tile.k[h][x].w), q[2 * x + 1], sc[h]);
+        const uint4 k0 = widen(tile.k[h][x].x, tile.k[h][x].y), k1 = widen(tile.k[h][x].z, tile.k[h][x].w);
+        f32x4 lo{0.f, 0.f, 0.f, 0.f}, hi{0.f, 0.f, 0.f, 0.f};
+        lo = mfma16(k0, q[0], lo);
+        hi = mfma16(k0, q[2], hi);
+        lo = mfma16(k1, q[1], lo);
+        hi = mfma16(k1, q[3], hi);
+        sc[h][2 * x] = lo[0] + hi[1];
+        sc[h][2 * x + 1] = lo[2] + hi[3];
       }
     } else {
+      sc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int x = 0; x < 4; ++x) sc[h] = mfma16(tile.k[h][x], q[x], sc[h]);
     }
@@ -303,7 +309,7 @@ __device__ __forceinline__ void attend_tile(const Stream<kFp8>& st, Tile<kFp8>& 
   if (partial) {
 #pragma unroll
     for (int e = 0; e < 4 * kSteps; ++e)
-      if (j + 16 * (e >> 2) + 4 * c + (e & 3) >= len) x[e] = -INFINITY;
+      if (j + 16 * (e >> 2) + key_of<kFp8>(c, e & 3) >= len) x[e] = -INFINITY;
   }
   float top = x[0];
 #pragma unroll
@@ -333,17 +339,23 @@ __device__ __forceinline__ void attend_tile(const Stream<kFp8>& st, Tile<kFp8>& 
     const uint4 p_hi = make_uint4(hi[0], hi[1], hi[2], hi[3]), p_lo = make_uint4(lo[0], lo[1], lo[2], lo[3]);
     uint4 v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int h = 2 * b + (e >> 2), r = e & 3;
-      if (kFp8)
-        v[e] = (r & 1) ? widen(tile.v[h][r / 2].z, tile.v[h][r / 2].w) : widen(tile.v[h][r / 2].x, tile.v[h][r / 2].y);
-      else
-        v[e] = tile.v[h][r];
+    for (int e = 0; e < 8; e += 2) {
+      const int h = 2 * b + (e >> 2);
+      if (kFp8) {
+        const uint4& w = tile.v[h][(e >> 1) & 1];
+        // (Every lane gives and takes: not inside a condition on the lane.)
+        const uint32_t nx = neighbour(w.x), ny = neighbour(w.y), nz = neighbour(w.z), nw = neighbour(w.w);
+        v[e] = widen(odd ? nz : w.x, odd ? nw : w.y);
+        v[e + 1] = widen(odd ? w.z : nx, odd ? w.w : ny);
+      } else {
+        v[e] = tile.v[h][e & 3];
+        v[e + 1] = tile.v[h][(e & 3) + 1];
+      }
     }
     if (partial) {  // places past the row's length may hold anything, NaN too
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const bool in = j + 32 * b + 16 * (e >> 2) + 4 * c + (e & 3) < len;
+        const bool in = j + 32 * b + 16 * (e >> 2) + key_of<kFp8>(c, e & 3) < len;
         v[e].x = in ? v[e].x : 0u;
         v[e].y = in ? v[e].y : 0u;
         v[e].z = in ? v[e].z : 0u;
@@ -445,8 +457,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(DecodeArgs a,
   st.n_pages = a.cache.n_pages;
   st.shift = a.cache.page_shift;
   st.once = wk.tiles_of_cols == 1 && (int64_t)T * wk.units * (kTile<kFp8> * 2 * kHeadDim * kBytes) >= kCachedBytes;
-  st.k_off = col * st.tok_bytes + 16 * c;
-  st.v_off = 4 * c * st.tok_bytes + 8 * kBytes * col;
+  st.k_off = kFp8 ? (col >> 1) * st.tok_bytes + 64 * (col & 1) + 16 * c : col * st.tok_bytes + 16 * c;
+  st.v_off = kFp8 ? (2 * c + (col & 1)) * st.tok_bytes + 16 * (col >> 1) : 4 * c * st.tok_bytes + 16 * col;
   float scale_log2 = a.scale * kLog2e;
   if (kFp8 && a.cache.amax[g] > 0.f) scale_log2 *= a.cache.amax[g] / 448.f;
   const float v_scale = value_scale<kFp8>(a, g);
@@ -505,7 +517,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(DecodeArgs a,
     uint4 q[4];
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-      // Elements that the K operand's lane holds: 32 x + 8 c, FP8 64 (x / 2) + 16 c + 8 (x % 2).
+      // Elements that the K operand's lane holds.
       const int d = kFp8 ? 64 * (x >> 1) + 16 * c + 8 * (x & 1) : 32 * x + 8 * c;
       q[x] = make_uint4(0u, 0u, 0u, 0u);
       if (col < cols) q[x] = *reinterpret_cast<const uint4*>(a.Q + (head0 + col) * a.q_head + r * a.q_tok + d);
