@@ -9,6 +9,7 @@
 #include <atomic>
 
 #include "../../include/rbs.h"
+#include "paged.hpp"
 #include "rbs_launch.hpp"
 
 namespace {

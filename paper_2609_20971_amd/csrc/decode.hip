@@ -24,8 +24,7 @@
 // matrix core as two bf16 parts (the value and what its rounding left), off by
 // 2^-16 together: in one part they would be off by half as much as the result's
 // own rounding, and the second product costs nothing here.
-#include "rbs_device.hpp"
-#include "rbs_launch.hpp"
+#include "paged.hpp"
 
 namespace rbs {
 
@@ -79,12 +78,6 @@ struct Shared {
   int last;   // and its last
   int slot;   // the first one's part, 0 or 1 (the others': 0)
 };
-
-__device__ __forceinline__ uint32_t two_bf16(float a, float b) {
-  typedef __bf16 bf16x2 __attribute__((__vector_size__(2 * sizeof(__bf16))));
-  const bf16x2 v = {(__bf16)a, (__bf16)b};
-  return __builtin_bit_cast(uint32_t, v);
-}
 
 struct Work {
   int units, tiles_of_cols, workers;  // KV heads x column tiles; workers of a unit

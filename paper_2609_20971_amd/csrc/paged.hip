@@ -1,8 +1,7 @@
 // Around a paged key-value cache: pages and slots of a batch's new tokens, pages
 // given back, and queries and keys normed, rotated and put into the cache.
 #include "../../include/rbs.h"
-#include "rbs_device.hpp"
-#include "rbs_launch.hpp"
+#include "paged.hpp"
 
 namespace rbs {
 
@@ -324,13 +323,6 @@ __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
-// Two fp32 to bf16 (nearest even) in one word.
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-  typedef __bf16 bf16x2 __attribute__((__vector_size__(2 * sizeof(__bf16))));
-  const bf16x2 v = {(__bf16)a, (__bf16)b};
-  return __builtin_bit_cast(uint32_t, v);
-}
-
 // E4M3 codes of four values times scale, saturating at +-448 (NaN stays NaN).
 __device__ __forceinline__ uint32_t pack_e4m3(const float* x, float scale) {
   float y[4];
@@ -464,7 +456,7 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a, 
       }
       uint32_t b[kRun];
 #pragma unroll
-      for (int e = 0; e < kRun; ++e) b[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
+      for (int e = 0; e < kRun; ++e) b[e] = two_bf16(x[2 * e], x[2 * e + 1]);
       if (is_v) {  // (as it came: a NaN keeps its bits)
 #pragma unroll
         for (int e = 0; e < kRun; ++e) b[e] = w[u][e];

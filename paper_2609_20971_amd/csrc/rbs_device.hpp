@@ -65,20 +65,6 @@ __device__ __forceinline__ float wave_extreme(float x) {
   const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return pick(__uint_as_float(r32[0]), __uint_as_float(r32[1]));
 }
-// x combined over the lanes up to and with this one (op: associative, 0 its
-// neutral element): within each row of 16 lanes, then the last lane of row 0 (2)
-// onto row 1 (3), then that of the first two rows onto the others.  A lane or row
-// with no source takes 0.
-template <typename Op>
-__device__ __forceinline__ int wave_scan(int x, Op op) {
-  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));  // row_shr 1
-  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));  // row_shr 2
-  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));  // row_shr 4
-  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));  // row_shr 8
-  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));  // row_bcast 15
-  return op(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));  // row_bcast 31
-}
-
 __device__ __forceinline__ float wave_max(float x) { return wave_extreme<true>(x); }
 __device__ __forceinline__ float wave_min(float x) { return wave_extreme<false>(x); }
 

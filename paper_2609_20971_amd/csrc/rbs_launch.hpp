@@ -382,75 +382,4 @@ hipError_t launch_attention_varlen(const AttnArgs& a, const SeqTable& t, hipStre
 hipError_t launch_dense_indices_varlen(int n_q_heads, const SeqTable& t, int32_t* counts, int32_t* indices,
                                        hipStream_t s);
 
-// ---- Paged cache (paged.hip, decode.hip).
-
-// K and V of a paged cache: element (page, head, place, j) at page * page + ...
-struct CacheView {
-  void* K;
-  void* V;
-  const float* amax;  // null: bf16
-  int64_t page, head, tok;
-  int n_pages, page_shift;
-};
-
-struct PagesArgs {
-  int n_rows, max_pages, n_pages, page_shift;
-  int32_t* page_table;
-  const int32_t* free_pages;
-  const int32_t* seq_lens;
-  const int32_t* new_tokens;  // null: one each
-  const int32_t* n_free;
-  int max_tokens;
-  int32_t* seq_lens_out;
-  int32_t* n_free_out;
-  int32_t* cu_tokens;
-  int32_t* positions;
-  int32_t* slots;
-  int32_t* status;
-};
-
-struct RopeArgs {
-  const uint16_t* Q;
-  const uint16_t* K;
-  const uint16_t* V;
-  Strides in, out;  // out.kv_*: K_out
-  int n_tokens, n_q_heads, n_kv_heads;
-  const uint16_t* q_weight;
-  const uint16_t* k_weight;
-  const float* inv_freq;
-  int rot_dim;
-  bool interleaved;
-  float eps, factor;
-  const int32_t* positions;
-  const int32_t* slots;
-  uint16_t* Q_out;
-  uint16_t* K_out;  // null: not kept
-  bool cached;
-  CacheView cache;
-};
-
-struct DecodeArgs {
-  const uint16_t* Q;
-  int64_t q_head, q_tok;  // Q and O
-  int n_rows, n_q_heads, n_kv_heads;
-  CacheView cache;
-  const int32_t* page_table;
-  int max_pages;
-  const int32_t* seq_lens;
-  float scale;
-  uint16_t* O;
-  float* lse;
-  float* workspace;
-};
-
-constexpr int kMaxRows = 4096;  // rows of a page table
-
-hipError_t launch_pages_extend(const PagesArgs& a, hipStream_t s);
-hipError_t launch_pages_release(int n_rows, int max_pages, int n_pages, int page_shift, const int32_t* page_table,
-                                int32_t* free_pages, const int32_t* released, int32_t* seq_lens, int32_t* n_free,
-                                int32_t* status, hipStream_t s);
-hipError_t launch_qk_norm_rope(const RopeArgs& a, hipStream_t s);
-size_t decode_workspace_bytes();
-hipError_t launch_paged_decode(const DecodeArgs& a, hipStream_t s);
-
 }  // namespace rbs
