@@ -530,8 +530,9 @@ size_t rbs_decode_workspace_bytes(void);
  * unused row (negative length): its O and lse are left as they were.
  * page_table int32 [n_tokens][max_pages], seq_lens int32 [n_tokens], with
  * n_tokens * (max_pages * page_size / 32 + 8) < 2^31.  Both are trusted like the
- * prefill's lists: page numbers are clamped to the cache and lengths to the table, so that no access leaves the buffers.  Places past a row's
- * length may hold anything; an infinity in a value that is attended may give NaN.
+ * prefill's lists: page numbers are clamped to the cache and lengths to the
+ * table, so that no access leaves the buffers.  Places past a row's length may
+ * hold anything; an infinity in a value that is attended may give NaN.
  */
 int rbs_paged_decode(const rbs_shape* shape, const rbs_cache* cache, const void* Q, const int32_t* page_table,
                      int32_t max_pages, const int32_t* seq_lens, float softmax_scale, void* O, float* lse,

@@ -404,8 +404,13 @@ def _auto_workspace(device: int, handle: int) -> torch.Tensor:
     side by side."""
     if handle != torch._C._cuda_getCurrentRawStream(device):
         # Made on the stream that uses it, whose order its memory's next use has to follow.
-        with torch.cuda.stream(torch.cuda.ExternalStream(handle, device)):
-            return _auto_workspace(device, handle)
+        own = torch.cuda.ExternalStream(handle, device) if handle else torch.cuda.default_stream(device)
+        with torch.cuda.stream(own):
+            return _workspace_of(device, handle)
+    return _workspace_of(device, handle)
+
+
+def _workspace_of(device: int, handle: int) -> torch.Tensor:
     capturing = torch.cuda.is_current_stream_capturing()
     ws = None if capturing else _decode_workspaces.get((device, handle))
     if ws is None:

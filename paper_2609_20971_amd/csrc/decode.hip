@@ -5,25 +5,27 @@
 // where the card has 300).  So everything is arranged for loads in flight:
 //
 // - K and V go from memory to registers as matrix operands, with no LDS and no
-//   barrier in the loop; a wave streams 32 keys at a time (64 in FP8) and asks for the next
-//   ones, of the next row too, as soon as an operand has been used.
+//   barrier in the loop; a wave streams 32 keys at a time (64 in FP8) and asks for
+//   the next ones, of the next row too, as soon as an operand has been used.
 // - S^T = K Q^T and O^T = V^T P^T in 16x16x32 products with the (up to 16) query
-//   heads of a KV head as columns.  Lane l holds column l % 16 of S, keys
-//   4 (l / 16) + r of each 16 (FP8: another four), which is what the second product takes as its
-//   right operand if V's rows come in the same order: P never leaves its lane.
-//   V's operand needs eight keys of one element; a lane reads eight elements of
-//   eight keys (16 lanes: whole rows) and regroups them with byte permutes.
+//   heads of a KV head as columns.  Lane l holds column l % 16 of S and four keys
+//   of each 16 (key_of), which is what the second product takes as its right
+//   operand if V's rows come in the same order: P never leaves its lane.  V's
+//   operand needs eight keys of one element; a lane has eight elements of eight
+//   keys (16 lanes: whole rows) and regroups them with byte permutes.
 // - The keys of all rows together are dealt out evenly: a tile is 32 (64) keys of
 //   one row, and worker w of a KV head takes tiles [T w / W, T (w + 1) / W) of
 //   the T tiles of all rows, its four waves every fourth of them.  Lengths are on
-//   the GPU, so that every workgroup sums them up for itself.  A row that several workers share is left in parts
-//   (maximum, sum, weighted values in fp32) that a second launch joins, in the
-//   order of the workers: the result depends on the lengths alone.
+//   the GPU, so that every workgroup sums them up for itself.  A row that several
+//   workers share is left in parts (maximum, sum, weighted values in fp32) that a
+//   second launch joins, in the order of the workers: results do not depend on
+//   which workgroup comes first.
 //
 // The exponentials' sum and the products are in fp32.  The weights go to the
 // matrix core as two bf16 parts (the value and what its rounding left), off by
-// 2^-16 together: in one part they would be off by half as much as the result's
-// own rounding, and the second product costs nothing here.
+// 2^-16 together: in one part they would add about as much error as the result's
+// own rounding, and the second product costs nothing here (160.3 us without it,
+// 161.2 with it, 32 rows of 9000 to 16000 FP8 keys, 64 / 8 heads).
 #include "paged.hpp"
 
 namespace rbs {
@@ -35,8 +37,8 @@ constexpr int kWaves = kThreads / 64;
 // Keys of one row that a wave takes at a time: 16 KB of K and V in either type.
 template <bool kFp8>
 constexpr int kTile = kFp8 ? 64 : 32;
-constexpr int kCols = 16;                  // query heads of a unit
-constexpr int kWorkers = 512;             // workgroups of a launch: two on each of 256 compute units
+constexpr int kCols = 16;      // query heads of a unit
+constexpr int kWorkers = 512;  // workgroups of a launch: two on each of 256 compute units
 constexpr int kPartFloats = kCols * kHeadDim + 2 * kCols;  // weighted values, maxima, sums
 // Rows that the table holds up to so many keys of are a worker's alone, and there
 // is no second launch (4 us, and 3.7 us of the calling thread).  In parts / whole,
@@ -44,7 +46,7 @@ constexpr int kPartFloats = kCols * kHeadDim + 2 * kCols;  // weighted values, m
 // 13.5; 64 rows of 200 to 500 18.9 / 16.5, to 1000 20.8 / 22.6; called one by one
 // 700 12.4 / 11.1.
 constexpr int kWholeKeys = 768;
-constexpr int kPad = kHeadDim + 4;                         // floats between LDS rows (banks)
+constexpr int kPad = kHeadDim + 4;  // floats between LDS rows (banks)
 // A launch that reads more than this of K and V reads them past the caches: what
 // it would leave there is gone before the next step reads it, and making room
 // costs, most where the caches hold what others wrote.  Cached / past them, after a
@@ -405,8 +407,8 @@ __device__ __forceinline__ int row_from(const int* first, int n_rows, int x) {
 
 // kWhole: a row is one worker's, so that there is nothing to join.
 template <bool kFp8, bool kWhole>
-__global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(DecodeArgs a, const int32_t* __restrict__ lens,
-                                                                const int32_t* __restrict__ page_table) {
+__global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
+    DecodeArgs a, const int32_t* __restrict__ lens, const int32_t* __restrict__ page_table) {
   __shared__ int first[kMaxRows + 1], length[kMaxRows], sums[2 * kWaves];
   __shared__ __align__(16) float acc[kWaves][kCols][kPad];
   __shared__ float ms[kWaves][kCols], ls[kWaves][kCols];
@@ -478,11 +480,13 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(DecodeArgs a,
         next.len = __builtin_amdgcn_readfirstlane(length[next.row]);
         return;
       }
+      if (first[r + 1] == first[r]) r = seq_of(first, a.n_rows, first[r]) - 1;  // past all the empty rows here
     }
   };
   auto offsets = [&](int64_t* base) __attribute__((always_inline)) {
     const int32_t* table = page_table + (int64_t)__builtin_amdgcn_readfirstlane(next.row) * a.max_pages;
-    const int len = __builtin_amdgcn_readfirstlane(next.len), j = __builtin_amdgcn_readfirstlane(next.tile * kTile<kFp8>);
+    const int len = __builtin_amdgcn_readfirstlane(next.len);
+    const int j = __builtin_amdgcn_readfirstlane(next.tile * kTile<kFp8>);
 #pragma unroll
     for (int h = 0; h < kSteps; ++h) base[h] = st.at(table, len, j + 16 * h);
   };
@@ -498,7 +502,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(DecodeArgs a,
   int at = t;  // the first tile that is still to do
   bool is_first = true;
   while (at < t_end) {
-    while (first[row + 1] <= at) ++row;
+    if (first[row + 1] <= at && first[++row + 1] <= at) row = seq_of(first, a.n_rows, at);
     const int r = __builtin_amdgcn_readfirstlane(row);
     const int last = first[r + 1] - kRowCost;  // past the row's last tile
     if (at >= last) {

@@ -65,8 +65,10 @@ __global__ __launch_bounds__(kPageThreads) void pages_extend_kernel(PagesArgs a,
   int taken[kTaken];
   if (!kOne) {
 #pragma unroll
-    for (int i = 0; i < kTaken; ++i)
-      taken[i] = a.free_pages[max(min(max(n_free, 0), a.n_pages) - 1 - ((int)blockIdx.x * kFillTokens + i * kPageThreads + t), 0)];
+    for (int i = 0; i < kTaken; ++i) {
+      const int k = (int)blockIdx.x * kFillTokens + i * kPageThreads + t;
+      taken[i] = a.free_pages[max(min(max(n_free, 0), a.n_pages) - 1 - k, 0)];
+    }
   }
 #pragma unroll
   for (int i = 0; i < kRowsPerThread; ++i) add[i] = need[i] = 0;
@@ -106,7 +108,8 @@ __global__ __launch_bounds__(kPageThreads) void pages_extend_kernel(PagesArgs a,
     first_token[a.n_rows] = all_tokens;
     first_page[a.n_rows] = all_pages;
   }
-  const int status = (all_pages > max(n_free, 0) ? RBS_PAGES_FEW : 0) | (__syncthreads_or(too_long) ? RBS_PAGES_ROW : 0) |
+  const int status = (all_pages > max(n_free, 0) ? RBS_PAGES_FEW : 0) |
+                     (__syncthreads_or(too_long) ? RBS_PAGES_ROW : 0) |
                      (all_tokens > a.max_tokens ? RBS_PAGES_TOKENS : 0) |
                      (n_free < 0 || n_free > a.n_pages ? RBS_PAGES_STACK : 0);
   const bool ok = status == 0;
@@ -144,7 +147,8 @@ __global__ __launch_bounds__(kPageThreads) void pages_extend_kernel(PagesArgs a,
         pos[i] = -1;
         page_at[i] = a.free_pages;
         if (ok && tok + i < all_tokens) {
-          while (first_token[row + 1] <= tok + i) ++row;
+          if (first_token[row + 1] <= tok + i && first_token[++row + 1] <= tok + i)
+            row = seq_of(first_token, a.n_rows, tok + i);  // (many rows may take none)
           pos[i] = length[row] + tok + i - first_token[row];
           const int at = pos[i] >> shift, held = (length[row] + places) >> shift;
           page_at[i] = at < held ? a.page_table + (int64_t)row * a.max_pages + at
@@ -462,7 +466,8 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a, 
         for (int e = 0; e < kRun; ++e) b[e] = w[u][e];
       }
       uint16_t* dst = is_q ? a.Q_out + head * a.out.q_head + tok * a.out.q_tok
-                           : is_v || a.K_out == nullptr ? nullptr : a.K_out + head * a.out.kv_head + tok * a.out.kv_tok;
+                           : is_v || a.K_out == nullptr ? nullptr
+                                                        : a.K_out + head * a.out.kv_head + tok * a.out.kv_tok;
       if (dst != nullptr) {
         store_words<kRun / 2, kOnce>(dst + lo, b);
         store_words<kRun / 2, kOnce>(dst + hi, b + kRun / 2);

@@ -53,6 +53,7 @@ EXTEND = [
     ([1] * 1025, None, 16, 1, 0, 1),                            # two rows a thread
     ([(37 * i) % 300 - 1 for i in range(4096)], None, 128, 3, 9, 0),
     ([(37 * i) % 300 for i in range(3000)], [(11 * i) % 7 - 1 for i in range(3000)], 256, 2, 1, 11),
+    ([9] * 4096, [3] + [0] * 2000 + [1] + [0] * 2093 + [2500], 64, 41, 4, 6),               # few rows take tokens
 ]
 
 
@@ -431,6 +432,8 @@ DECODE = [
     ([769, 1, 768], 8, 1, 16, False, "heads", "tokens", 0.0),
     ([4000] * 70 + [1], 8, 2, 64, True, "heads", "tokens", 0.0),                          # past the caches
     ([5000] * 8 + [0, 33], 16, 4, 16, False, "tokens", "tokens", 0.0),
+    ([70] + [0] * 2000 + [-1] * 2000 + [3000, 33], 8, 2, 16, False, "heads", "tokens", 0.0),  # few rows used
+    ([0] * 50 + [20] * 3 + [-1] * 900 + [40] * 2, 4, 1, 32, True, "heads", "tokens", 0.0),
     ([512, 3000], 512, 512, 16, False, "heads", "tokens", 0.0),                           # as many units as workers
     ([150001], 8, 1, 64, False, "heads", "tokens", 0.0),
 ]
@@ -511,6 +514,10 @@ def test_decode_on_a_side_stream_and_own_workspace():
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     s.wait_stream(torch.cuda.current_stream())
     got = _run_decode(c, stream=s, ready=True)  # given by name, from another current stream
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    with torch.cuda.stream(s):
+        got = _run_decode(c, stream=torch.cuda.default_stream(), ready=True)
     torch.cuda.synchronize()
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     ws = torch.full((rbs.rbs_decode_workspace_bytes() // 4,), math.nan, device="cuda")
