@@ -99,6 +99,20 @@ def _elsewhere(dev: int, *tensors) -> bool:
     return dev < 0
 
 
+def _rows(name, t, sizes):
+    """The strides of a bf16 (head, token, dimension) tensor of these sizes."""
+    if isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.shape == sizes:
+        strides = t.stride()
+        if strides[2] == 1:
+            return strides[:2]
+    return L._heads_tokens(name, t, *sizes)
+
+
+def _int_row(name, t, n):
+    if not (isinstance(t, torch.Tensor) and t.dtype is torch.int32 and t.shape == (n,) and t.is_contiguous()):
+        L._check_tensor(name, t, torch.int32, (n,))
+
+
 def _strided(shape, q, kv=None):
     """L._with_strides, short where the shape leaves the strides to the tensors."""
     if shape.q_stride_head == shape.q_stride_tok == shape.kv_stride_head == shape.kv_stride_tok == 0:
@@ -355,21 +369,21 @@ def rbs_qk_norm_rope(shape: L.rbs_shape, rope: Rope, Q, K, positions, V=None, ca
     if not isinstance(rope, Rope):
         raise ValueError("rope must be a Rope")
     hq, hkv, n, d = shape.n_q_heads, shape.n_kv_heads, shape.n_tokens, shape.head_dim
-    qs = L._heads_tokens("Q", Q, hq, n, d)
-    ks = L._heads_tokens("K", K, hkv, n, d)
-    L._check_tensor("positions", positions, torch.int32, (n,))
+    q_sizes, k_sizes = (hq, n, d), (hkv, n, d)
+    qs, ks = _rows("Q", Q, q_sizes), _rows("K", K, k_sizes)
+    _int_row("positions", positions, n)
     if cache is not None:
         if not isinstance(cache, PagedCache):
             raise ValueError("cache must be a PagedCache")
         if V is None or slots is None:
             raise ValueError("a cache needs V and slots")
-        if L._heads_tokens("V", V, hkv, n, d) != ks:
+        if _rows("V", V, k_sizes) != ks:
             raise ValueError(f"V strides {V.stride()[:2]} differ from K strides {ks}; the library takes one pair")
-        L._check_tensor("slots", slots, torch.int32, (n,))
+        _int_row("slots", slots, n)
     if Q_out is not None:
-        L._heads_tokens("Q_out", Q_out, hq, n, d)
+        _rows("Q_out", Q_out, q_sizes)
     if K_out is not None:
-        L._heads_tokens("K_out", K_out, hkv, n, d)
+        _rows("K_out", K_out, k_sizes)
     dev = Q.get_device()
     if _elsewhere(dev, K, positions, Q_out, K_out) or (cache is not None and (
             cache.device != dev or _elsewhere(dev, V, slots))):
@@ -425,13 +439,13 @@ def rbs_paged_decode(shape: L.rbs_shape, Q, cache: PagedCache, page_table, seq_l
     """Attention of one new token per row over the row's cached tokens; returns O
     (bf16, Q's sizes and strides).  Q: (head, row, dimension)."""
     hq, n, d = shape.n_q_heads, shape.n_tokens, shape.head_dim
-    qs = L._heads_tokens("Q", Q, hq, n, d)
+    qs = _rows("Q", Q, (hq, n, d))
     if not isinstance(cache, PagedCache):
         raise ValueError("cache must be a PagedCache")
     if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
         raise ValueError("page_table must be an [n_rows][max_pages] tensor")
     L._check_tensor("page_table", page_table, torch.int32, (n, page_table.shape[1]))
-    L._check_tensor("seq_lens", seq_lens, torch.int32, (n,))
+    _int_row("seq_lens", seq_lens, n)
     if O is not None:
         L._check_out(O, Q)
     if lse is not None:
