@@ -40,12 +40,14 @@ constexpr int kTile = kFp8 ? 64 : 32;
 constexpr int kCols = 16;      // query heads of a unit
 constexpr int kWorkers = 512;  // workgroups of a launch: two on each of 256 compute units
 constexpr int kPartFloats = kCols * kHeadDim + 2 * kCols;  // weighted values, maxima, sums
-// Rows that the table holds up to so many keys of are a worker's alone, and there
-// is no second launch (4 us, and 3.7 us of the calling thread).  In parts / whole,
-// the GPU's time alone: one row of 500 keys 9.9 / 9.2, 700 9.8 / 11.0, 1000 10.3 /
-// 13.5; 64 rows of 200 to 500 18.9 / 16.5, to 1000 20.8 / 22.6; called one by one
-// 700 12.4 / 11.1.
-constexpr int kWholeKeys = 768;
+// Rows of which the table holds at most so many tiles are a worker's alone, and there
+// is no second launch.  In parts / whole, the GPU's time: one row of 384 keys 9.7 /
+// 8.0 us, 64 rows of 200 to 256 15.6 / 14.2, to 384 16.2 / 16.7, to 500 17.4 / 19.4;
+// FP8, 64 rows of 100 to 700 keys 16.4 / 16.0.
+constexpr int kWholeTiles = 12;
+// For few workgroups the launch that it saves (3 us of the calling thread) counts for
+// more: one row of 700 keys on the GPU 9.5 / 11.1, called one by one 12.5 / 11.2.
+constexpr int kWholeKeysOfFew = 768, kFewWhole = 8;
 constexpr int kPad = kHeadDim + 4;  // floats between LDS rows (banks)
 // A launch that reads more than this of K and V reads them past the caches: what
 // it would leave there is gone before the next step reads it, and making room
@@ -68,8 +70,11 @@ constexpr int kRowCost = 4;
 // 64 / 8, 163 / 167; more different ones (a ratio of 3) 300 of 10 to 1000 64.9 / 73.9.
 constexpr int kSoloShare = 20, kSoloRatio = 2;
 // A join by single columns takes at most so many workgroups: one row of 20000 keys
-// 18.2 us and not 20.8, of 131000 57 and not 60; but 64 rows 72 and not 65.
-constexpr int kJoinThreads = 512, kFewJoins = 512;
+// 18.2 us and not 20.8, of 131000 57 and not 60, 24 rows of 28 / 4 heads 20.6 and
+// not 21.5; but 16 rows of 64 / 8 heads 29.9 and not 29.2, 64 rows of 32 / 4 72 and not
+// 65.  Threads of a join's workgroup, 256 / 512 / 1024: one row of 2000 keys 9.5 /
+// 10.9 / 12.4, 200 of 300 to 2000 41.9 / 43.3 / 46.3, one of 131000 50.1 / 50.1 / 51.5.
+constexpr int kJoinThreads = 256, kFewJoins = 768;
 
 // What the worker that has a row's first tile leaves for the join, at the
 // workspace's end: one for each row and unit, or where there are more rows than
@@ -687,7 +692,8 @@ hipError_t launch(const DecodeArgs& a, hipStream_t s) {
   const Work wk = work_of_heads(a.n_q_heads, a.n_kv_heads);
   const int group = a.n_q_heads / a.n_kv_heads, cols = group < kCols ? group : kCols;
   const dim3 grid(wk.units * wk.workers);
-  if (((int64_t)a.max_pages << a.cache.page_shift) <= kWholeKeys) {
+  const int64_t most = (int64_t)a.max_pages << a.cache.page_shift;  // keys of a row
+  if (most <= kWholeTiles * kTile<kFp8> || (most <= kWholeKeysOfFew && a.n_rows * wk.units <= kFewWhole)) {
     hipLaunchKernelGGL((paged_decode_kernel<kFp8, true>), grid, dim3(kThreads), 0, s, a, a.seq_lens, a.page_table);
     return hipGetLastError();
   }

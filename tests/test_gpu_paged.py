@@ -428,6 +428,9 @@ DECODE = [
     ([(i * 53) % 500 - 1 for i in range(700)], 14, 2, 32, True, "heads", "qkv", 0.0),
     ([(i * 53) % 90 for i in range(600)] + [1500], 8, 8, 64, False, "tokens", "tokens", 0.0),  # and one long row
     ([150] * 520 + [2500] * 3, 16, 1, 16, False, "heads", "tokens", 0.0),                # more rows than workers
+    ([384, 383, 1] * 5, 8, 2, 32, False, "heads", "tokens", 0.0),                         # one launch up to here
+    ([385, 383, 1] * 5, 8, 2, 16, False, "heads", "tokens", 0.0),
+    ([768, 700, 0] * 5, 8, 2, 16, True, "heads", "tokens", 0.0),
     ([768] * 3, 8, 1, 256, False, "heads", "tokens", 0.0),
     ([769, 1, 768], 8, 1, 16, False, "heads", "tokens", 0.0),
     ([4000] * 70 + [1], 8, 2, 64, True, "heads", "tokens", 0.0),                          # past the caches
