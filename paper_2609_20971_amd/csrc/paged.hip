@@ -313,9 +313,9 @@ constexpr int kRopeWaves = kRopeThreads / 64;
 // MB) 12.4 cached in runs of four, 14.9 in runs of eight, 17.0 past the caches as
 // well; 96 of 64 / 8 3.9 and 4.3.
 constexpr int64_t kRopeCachedBytes = int64_t(64) << 20;
-// Waves that a call of few tokens is spread over, a token's rows in several parts:
-// 512 tokens of 32 / 4 heads 2048 5.2 us, 4096 4.6, 8192 4.6; 3001 of 28 / 4 2048
-// 13.0, 4096 14.9, 8192 15.8 (runs of eight).
+// Waves that a call of few tokens is spread over, a token's rows in several parts.
+// 2048 / 4096 / 8192: 512 tokens of 32 / 4 heads 5.2 / 4.9 / 4.9 us, 1500 10.8 / 10.1 /
+// 10.4, 3001 of 28 / 4 13.4 / 12.5 / 13.1, 2000 of 8 / 1 5.1 / 5.7 / 5.7.
 constexpr int kRopeSpread = 4096;
 
 template <int kLanes>

@@ -96,6 +96,9 @@ def _run_extend(lens, new, page, columns, pool, max_tokens, in_place, want_statu
     ([0, 2**31 - 1], [2**31 - 1, 2**31 - 1], 16, 4, 9, 17, 9, 7),   # lengths and counts past every limit
     ([3, 5], None, 16, 2, 4, 2, 5, 8),                              # a stack larger than the pool
     ([3, 5], None, 16, 2, 4, 2, -1, 8),
+    ([1, -1, 1, 1], None, 16, 2, 9, 2, None, 4),                    # a token each, and room for two
+    ([32, 1], None, 16, 2, 9, 2, None, 2),                          # a full row
+    ([16] * 1100, None, 16, 2, 2199, 1100, None, 1),                # two workgroups
     ([0] * 50, [1000] * 50, 16, 63, 50 * 63 - 1, 50000, None, 1),   # refused by each of several workgroups
     ([2**31 - 1] * 4096, [2**31 - 1] * 4096, 256, 1, 1, 1, 1, 7),
 ])
@@ -504,6 +507,39 @@ def test_decode_pages_past_32_bits():
     rbs.rbs_qk_norm_rope(rbs.make_shape(4, hq, hkv, 64), rbs.Rope(None), Q, Kn, _ints([1, 2, 3, 4]), V=Vn,
                          cache=far["cache"], slots=slots)
     assert torch.equal(K[-1, :, 255], Kn[:, 0]) and torch.equal(V[-3, :, 0], Vn[:, 1]) and torch.equal(V[0, :, 7], Vn[:, 2])
+
+
+@pytest.mark.parametrize("order", ["heads", "tokens"])
+def test_keys_and_values_in_one_buffer(order):
+    """[n_pages][2][..]: written by the norm and rotation call, read by the attention."""
+    n, hq, hkv, page, pool = 40, 8, 2, 16, 7
+    inner = (hkv, page) if order == "heads" else (page, hkv)
+    both = torch.full((pool, 2, *inner, D), math.nan, dtype=torch.bfloat16, device="cuda")
+    K, V = (both[:, i] if order == "heads" else both[:, i].transpose(1, 2) for i in range(2))
+    cache = rbs.PagedCache(K, V)
+    Q, Kn, Vn = _qkv(n, hq, hkv, 31)
+    table = torch.tensor([[5, 0, 3]], dtype=torch.int32)
+    at = torch.arange(n)
+    slots = (table[0, at // page] * page + at % page).to(torch.int32)
+    shape = rbs.make_shape(n, hq, hkv, 64)
+    q, k = rbs.rbs_qk_norm_rope(shape, rbs.Rope(rbs.rope_frequencies()[0]), Q, Kn, at.to(torch.int32).cuda(), V=Vn,
+                                cache=cache, slots=slots.cuda())
+    last = q[:, -1:]
+    lse = torch.empty(hq, 1, device="cuda")
+    O = rbs.rbs_paged_decode(rbs.make_shape(1, hq, hkv, 64), last, cache, table.cuda(), _ints([n]), lse=lse)
+    o, l, o_tol, l_tol = R.attend(last[:, 0].cpu().double(), k.cpu().double(), Vn.cpu().double(), 1 / math.sqrt(D))
+    assert bool(((O[:, 0].cpu().double() - o).abs() <= o_tol).all())
+    assert bool(((lse[:, 0].cpu().double() - l).abs() <= l_tol).all())
+    assert bool(both[[1, 2, 4, 6]].isnan().all())
+
+
+def test_decode_with_heads_of_scale_one():
+    """amax 0: the codes stand for themselves."""
+    c = _decode_case([300, 40], 4, 2, 16, True, "heads", 99)
+    c["amax"][0] = c["amax"][3] = 0.0
+    c["cache"].amax.copy_(c["amax"])
+    O, lse = _run_decode(c, 0.01)
+    _check_decode(c, O, lse, 0.01)
 
 
 def test_decode_on_a_side_stream_and_own_workspace():
