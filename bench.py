@@ -78,6 +78,11 @@ def parse():
     p.add_argument("--fp8", action="store_true",
                    help="instead of the benchmark line: the attention stage on FP8 (E4M3) inputs over the same "
                         "lists, against the bf16 attention and the FP8 dense path, plus the packing time")
+    p.add_argument("--serve", type=int, default=0,
+                   help="instead of the benchmark line: a prompt of the workload's length from a projection's output "
+                        "(pages, norm and rotation, sparse prefill), then decode steps of this many requests with "
+                        "that much in their paged cache")
+    p.add_argument("--serve-fp8", action="store_true", help="the serving mode's cache in FP8 (E4M3)")
     p.add_argument("--layer-sweep", type=int, default=0,
                    help="instead of the benchmark line: this many layers of the 128K layer schedule "
                         "(per-layer key noise and needle counts), per-layer density and times, sparse vs "
@@ -274,6 +279,8 @@ def main():
         return layer_sweep(args)
     if args.fp8:
         return fp8_bench(args)
+    if args.serve:
+        return serve_bench(args)
     if args.unit_rates:
         print(json.dumps(unit_rates()), flush=True)
         return
@@ -940,6 +947,96 @@ def fp8_bench(args):
         "attn_fp8_tflops": round(tf_f8, 1), "attn_fp8_mfma_frac": round(tf_f8 / PEAK_FP8_TFLOPS, 4),
         "dense_fp8_ms": round(t_f8d, 3), "dense_fp8_tflops": round(tf_f8d, 1),
         "dense_fp8_mfma_frac": round(tf_f8d / PEAK_FP8_TFLOPS, 4),
+    }), flush=True)
+
+
+def serve_bench(args):
+    """One layer of a serving stack: a prompt's QKV projection output (random
+    values) gets its pages, is normed, rotated and cached, and goes through the
+    sparse prefill; then decode steps of args.serve requests, each with a cached
+    prompt of that length, replayed as one graph a step.  One JSON line."""
+    import numpy as np
+    import torch
+
+    import paper_2609_20971_amd as rbs
+    from synth import workload
+
+    w = workload(args.workload or "qwen3-30b-a3b-128k")
+    dev = torch.device("cuda", 0)
+    torch.cuda.set_device(0)
+    n, hq, hkv, d, page, rows, steps = w.seq_len, w.n_q_heads, w.n_kv_heads, 128, 64, args.serve, max(1, args.steps)
+    gen = torch.Generator(device=dev).manual_seed(w.seed)
+
+    def project(tokens):
+        qkv = torch.randn(tokens, hq + 2 * hkv, d, generator=gen, device=dev, dtype=torch.bfloat16).transpose(0, 1)
+        return qkv[:hq], qkv[hq:hq + hkv], qkv[hq + hkv:]
+
+    per_row = -(-(n + steps + 2) // page)
+    pages = rbs.Pages.allocate(rows, per_row, rows * per_row, page, dev)
+    amax = torch.full((2 * hkv,), 6.0, device=dev) if args.serve_fp8 else None
+    cache = rbs.PagedCache.allocate(rows * per_row, page, hkv, amax=amax, device=dev)
+    ones = torch.ones(d, dtype=torch.bfloat16, device=dev)
+    inv_freq, factor = rbs.rope_frequencies(device=dev)
+    rope = rbs.Rope(inv_freq, ones, ones, factor=factor)
+    shape = rbs.make_shape(n, hq, hkv, w.block_size)
+
+    def one_prompt(row, Q, K, V):
+        counts = torch.zeros(rows, dtype=torch.int32, device=dev)
+        counts[row] = n
+        pages.seq_lens[row] = 0
+        marks = _events(torch, 4)
+        marks[0].record()
+        step = rbs.rbs_pages_extend(pages, counts, n)
+        marks[1].record()
+        rbs.rbs_qk_norm_rope(shape, rope, Q, K, step.positions, V=V, cache=cache, slots=step.slots, Q_out=Q, K_out=K)
+        marks[2].record()
+        stats = rbs.rbs_block_stats(shape, K)
+        rbs.rbs_select_attend(shape, Q, K, V, stats, w.tau_base, w.tau_rescue, w.n_sink, w.n_local, w.n_recent)
+        marks[3].record()
+        torch.cuda.synchronize()
+        if int(step.status.item()) != 0:
+            raise RuntimeError(f"rbs_pages_extend: status {int(step.status.item())}")
+        return [a.elapsed_time(b) for a, b in zip(marks, marks[1:])]
+
+    times = [one_prompt(row, *project(n)) for row in range(rows)]
+    pages_ms, rope_ms, prefill_ms = (float(np.median(x)) for x in zip(*(times[1:] or times)))
+
+    Q, K, V = project(rows)
+    rows_shape = rbs.make_shape(rows, hq, hkv, w.block_size)
+    out = rbs.PageStep.allocate(pages, rows)
+
+    def decode():
+        step = rbs.rbs_pages_extend(pages, step=out)
+        q, _ = rbs.rbs_qk_norm_rope(rows_shape, rope, Q, K, step.positions, V=V, cache=cache, slots=step.slots,
+                                    keep_k=False)
+        return rbs.rbs_paged_decode(rows_shape, q, cache, pages.page_table, step.seq_lens)
+
+    decode()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        decode()
+    marks = _events(torch, steps + 1)
+    marks[0].record()
+    for k in range(steps):
+        graph.replay()
+        marks[k + 1].record()
+    torch.cuda.synchronize()
+    if int(out.status.item()) != 0:
+        raise RuntimeError(f"rbs_pages_extend: status {int(out.status.item())}")
+    step_us = 1e3 * float(np.median([a.elapsed_time(b) for a, b in zip(marks, marks[1:])]))
+    read = rows * (n + steps // 2) * hkv * d * 2 * (1 if args.serve_fp8 else 2)
+    _log(f"[serve] prompt: pages {pages_ms:.3f} ms, norm and rotation {rope_ms:.3f} ms, prefill {prefill_ms:.3f} ms; "
+         f"decode of {rows} rows {step_us:.1f} us ({read / step_us / 1e3:.0f} GB/s of keys and values)")
+    print(json.dumps({
+        "mode": "serve", "workload": w.name, "data": "synthetic", "rows": rows, "steps": steps,
+        "cache": "fp8 e4m3" if args.serve_fp8 else "bf16", "page_size": page,
+        "prompt_pages_ms": round(pages_ms, 4), "prompt_norm_rope_ms": round(rope_ms, 4),
+        "prompt_prefill_ms": round(prefill_ms, 4), "decode_step_us": round(step_us, 2),
+        "decode_kv_gbps": round(read / step_us / 1e3, 1),
+        "decode_tokens_per_s": round(rows / step_us * 1e6, 1),
     }), flush=True)
 
 
