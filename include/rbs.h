@@ -514,7 +514,9 @@ int rbs_qk_norm_rope(const rbs_shape* in, const rbs_shape* out, const rbs_rope* 
 
 /* Workspace of rbs_paged_decode, 16-byte aligned; contents on entry are ignored.
  * Calls that share one must be ordered, like those that share an output: a
- * captured graph that may run beside another call needs one of its own. */
+ * captured graph that may run beside another call needs one of its own, and so
+ * does a host thread that may call while another does (a call is two launches,
+ * and on one stream too another thread's launch may come between them). */
 size_t rbs_decode_workspace_bytes(void);
 
 /*

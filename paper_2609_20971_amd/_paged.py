@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import threading
 from dataclasses import dataclass, field
 
 import torch
@@ -404,7 +405,7 @@ def rbs_qk_norm_rope(shape: L.rbs_shape, rope: Rope, Q, K, positions, V=None, ca
     return Q_out, K_out
 
 
-_decode_workspaces: dict = {}
+_decode_workspaces = threading.local()  # attributes of its own for every thread
 
 
 def rbs_decode_workspace_bytes() -> int:
@@ -412,10 +413,11 @@ def rbs_decode_workspace_bytes() -> int:
 
 
 def _auto_workspace(device: int, handle: int) -> torch.Tensor:
-    """The workspace of a (device, stream): calls on one stream are ordered, so
-    they may share it.  While the stream is being captured, a new one, which
-    belongs to the graph's memory: graphs that were captured on one stream may run
-    side by side."""
+    """The workspace of a (device, stream) and of this thread: a thread's calls on
+    one stream are ordered, so they may share it.  Those of two threads are not: a
+    call is two launches, and the other thread's may come between them.  While the
+    stream is being captured, a new one, which belongs to the graph's memory:
+    graphs that were captured on one stream may run side by side."""
     if handle != torch._C._cuda_getCurrentRawStream(device):
         # Made on the stream that uses it, whose order its memory's next use has to follow.
         own = torch.cuda.ExternalStream(handle, device) if handle else torch.cuda.default_stream(device)
@@ -426,11 +428,12 @@ def _auto_workspace(device: int, handle: int) -> torch.Tensor:
 
 def _workspace_of(device: int, handle: int) -> torch.Tensor:
     capturing = torch.cuda.is_current_stream_capturing()
-    ws = None if capturing else _decode_workspaces.get((device, handle))
+    held = _decode_workspaces.__dict__  # (freed with the thread; its memory's next use on the stream is ordered)
+    ws = None if capturing else held.get((device, handle))
     if ws is None:
         ws = torch.empty(rbs_decode_workspace_bytes() // 4, dtype=torch.float32, device=torch.device("cuda", device))
         if not capturing:
-            _decode_workspaces[device, handle] = ws
+            held[device, handle] = ws
     return ws
 
 

@@ -271,3 +271,27 @@ def test_rope_frequencies():
                 dict(scaling="parts", fast=1.0, slow=2.0)):
         with pytest.raises(ValueError):
             rbs.rope_frequencies(**bad, device="cpu")
+
+
+def test_threads_have_decode_workspaces_of_their_own(monkeypatch):
+    """A call is two launches over the workspace: two threads' calls on one stream may interleave."""
+    import threading
+
+    from paper_2609_20971_amd import _paged
+    empty = torch.empty
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: empty(*a, **dict(k, device="cpu")))
+    got = {}
+
+    def ask(name):
+        got[name] = [_paged._workspace_of(0, 77), _paged._workspace_of(0, 77), _paged._workspace_of(0, 78)]
+
+    threads = [threading.Thread(target=ask, args=(i,)) for i in range(3)]
+    for t in threads:
+        t.start()
+        t.join()
+    ask("here")
+    for a, again, other in got.values():
+        assert a is again and a is not other
+        assert a.numel() * 4 >= rbs.rbs_decode_workspace_bytes()
+    assert len({x.data_ptr() for three in got.values() for x in three}) == 2 * len(got)

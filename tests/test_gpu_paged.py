@@ -736,3 +736,39 @@ def test_captured_steps_side_by_side():
             assert servers[i].pages.seq_lens.tolist() == [x + k + 1 for x in servers[i].lens0]
         c = _decode_case([3000, 5], hq, hkv, page, False, "heads", 400 + k)
         _check_decode(c, *_run_decode(c), 1 / math.sqrt(D))
+
+
+# ------------------------------------------------------------------ threads
+
+def test_threads_that_decode_on_one_stream():
+    """Rows in parts (two launches a call), calls of three threads between each other."""
+    import threading
+    cases = [_decode_case(lens, 8, 2, 16, False, "heads", 500 + k)
+             for k, lens in enumerate(([3000, 900, 0, 2100], [4000], [1500] * 30))]
+    want = [_run_decode(c) for c in cases]
+    held = [(c["q"].cuda().transpose(0, 1), c["table"].cuda(), _ints(c["lens"])) for c in cases]
+    torch.cuda.synchronize()
+    got, failed, start = [[] for _ in cases], [], threading.Barrier(len(cases))
+
+    def calls(k):
+        try:
+            c, (Q, table, lens) = cases[k], held[k]
+            shape = rbs.make_shape(c["n"], c["hq"], c["hkv"], 64)
+            start.wait()
+            for _ in range(60):
+                lse = torch.empty(c["hq"], c["n"], device="cuda")
+                got[k].append((rbs.rbs_paged_decode(shape, Q, c["cache"], table, lens, lse=lse), lse))
+        except Exception as e:  # (shown below: a thread's own traceback is not the test's)
+            failed.append(e)
+
+    threads = [threading.Thread(target=calls, args=(k,)) for k in range(len(cases))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failed, failed
+    for k, (o, l) in enumerate(want):
+        assert len(got[k]) == 60
+        for O, lse in got[k]:
+            assert torch.equal(O, o) and torch.equal(lse, l)
