@@ -1009,7 +1009,7 @@ def serve_bench(args):
         step = rbs.rbs_pages_extend(pages, step=out)
         q, _ = rbs.rbs_qk_norm_rope(rows_shape, rope, Q, K, step.positions, V=V, cache=cache, slots=step.slots,
                                     keep_k=False)
-        return rbs.rbs_paged_decode(rows_shape, q, cache, pages.page_table, step.seq_lens)
+        return rbs.rbs_paged_decode(rows_shape, q, cache, pages.page_table, step.seq_lens, cu_tokens=step.cu_tokens)
 
     decode()
     side = torch.cuda.Stream()

@@ -29,7 +29,8 @@
  *   rbs_qk_norm_rope    per-head norm and rotary position of queries and keys
  *                       (the form the stages above take them in), keys and
  *                       values put into the cache in the same pass
- *   rbs_paged_decode    attention of one new token per row over the cache
+ *   rbs_paged_decode,   attention of one new token per row over the cache, the
+ *   rbs_paged_decode_packed   queries by row or packed as rbs_pages_extend packs them
  *
  * Conventions shared by every call
  *   - Tensors live in device memory.  Q, K, V and O are indexed by (head,
@@ -512,7 +513,7 @@ int rbs_qk_norm_rope(const rbs_shape* in, const rbs_shape* out, const rbs_rope* 
                      const void* V, const int32_t* positions, void* Q_out, void* K_out, const rbs_cache* cache,
                      const int32_t* slots, void* stream);
 
-/* Workspace of rbs_paged_decode, 16-byte aligned; contents on entry are ignored.
+/* Workspace of rbs_paged_decode and _packed, 16-byte aligned; contents on entry are ignored.
  * Calls that share one must be ordered, like those that share an output: a
  * captured graph that may run beside another call needs one of its own, and so
  * does a host thread that may call while another does (a call is two launches,
@@ -539,6 +540,23 @@ size_t rbs_decode_workspace_bytes(void);
 int rbs_paged_decode(const rbs_shape* shape, const rbs_cache* cache, const void* Q, const int32_t* page_table,
                      int32_t max_pages, const int32_t* seq_lens, float softmax_scale, void* O, float* lse,
                      void* workspace, void* stream);
+
+/*
+ * The same for a batch's tokens as rbs_pages_extend packs them and
+ * rbs_qk_norm_rope leaves them: row after row, none of unused rows, so that a
+ * row's token is found by cu_tokens (int32 [n_rows + 1], as that call writes it).
+ * shape: n_tokens tokens of Q and O, those behind the last one of a padded batch
+ * included (up to RBS_MAX_NEW_TOKENS); lse: NULL or [H_q][n_tokens]; page_table
+ * [n_rows][max_pages], seq_lens [n_rows], n_rows up to RBS_MAX_ROWS.
+ * The query of row s is its last new token's, cu_tokens[s + 1] - 1, which attends
+ * over the row's first seq_lens[s] tokens; O and lse go to the same token.  Rows
+ * without a new token are skipped, and O and lse of tokens that are no row's last
+ * are left as they were.  A row whose offsets fall outside 0 .. n_tokens is one
+ * without a token.
+ */
+int rbs_paged_decode_packed(const rbs_shape* shape, const rbs_cache* cache, const void* Q, const int32_t* cu_tokens,
+                            int32_t n_rows, const int32_t* page_table, int32_t max_pages, const int32_t* seq_lens,
+                            float softmax_scale, void* O, float* lse, void* workspace, void* stream);
 
 /* Static description of a status code. */
 const char* rbs_status_str(int status);

@@ -15,7 +15,7 @@ and around a paged key-value cache (the tokens that follow a prompt):
     pages = Pages.allocate(n_rows, max_pages, n_pages, page_size); cache = PagedCache.allocate(n_pages, page_size, H_kv)
     step = rbs_pages_extend(pages, new_tokens, max_tokens)             # pages, positions, slots of new tokens
     Q, K = rbs_qk_norm_rope(shape, rope, Q, K, step.positions, V=V, cache=cache, slots=step.slots)
-    O = rbs_paged_decode(shape, Q, cache, pages.page_table, step.seq_lens)   # one new token per row
+    O = rbs_paged_decode(shape, Q, cache, pages.page_table, step.seq_lens, cu_tokens=step.cu_tokens)
     rbs_pages_release(pages, released)                                 # finished rows
 """
 

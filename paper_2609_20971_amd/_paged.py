@@ -76,6 +76,8 @@ def declare(lib):
     lib.rbs_decode_workspace_bytes.restype = SZ
     lib.rbs_paged_decode.argtypes = [SP, ctypes.POINTER(rbs_cache), P, P, I32, P, F32, P, P, P, P]
     lib.rbs_paged_decode.restype = ctypes.c_int
+    lib.rbs_paged_decode_packed.argtypes = [SP, ctypes.POINTER(rbs_cache), P, P, I32, P, I32, P, F32, P, P, P, P]
+    lib.rbs_paged_decode_packed.restype = ctypes.c_int
 
 
 def _handle(device: int, stream):
@@ -438,25 +440,31 @@ def _workspace_of(device: int, handle: int) -> torch.Tensor:
 
 
 def rbs_paged_decode(shape: L.rbs_shape, Q, cache: PagedCache, page_table, seq_lens, softmax_scale: float = 0.0,
-                     O=None, lse=None, stream=None, workspace=L.AUTO):
+                     O=None, lse=None, stream=None, workspace=L.AUTO, cu_tokens=None):
     """Attention of one new token per row over the row's cached tokens; returns O
-    (bf16, Q's sizes and strides).  Q: (head, row, dimension)."""
+    (bf16, Q's sizes and strides).  Q: (head, row, dimension), a query for every
+    row; or with cu_tokens, those of rbs_pages_extend's step, (head, token,
+    dimension) as the step's tokens are packed: none of unused rows, and any behind
+    the last one left alone."""
     hq, n, d = shape.n_q_heads, shape.n_tokens, shape.head_dim
     qs = _rows("Q", Q, (hq, n, d))
     if not isinstance(cache, PagedCache):
         raise ValueError("cache must be a PagedCache")
     if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
         raise ValueError("page_table must be an [n_rows][max_pages] tensor")
-    L._check_tensor("page_table", page_table, torch.int32, (n, page_table.shape[1]))
-    _int_row("seq_lens", seq_lens, n)
+    rows = n if cu_tokens is None else page_table.shape[0]
+    L._check_tensor("page_table", page_table, torch.int32, (rows, page_table.shape[1]))
+    _int_row("seq_lens", seq_lens, rows)
+    if cu_tokens is not None:
+        _int_row("cu_tokens", cu_tokens, rows + 1)
     if O is not None:
         L._check_out(O, Q)
     if lse is not None:
         L._check_tensor("lse", lse, torch.float32, (hq, n))
     dev = Q.get_device()
-    if cache.device != dev or _elsewhere(dev, page_table, seq_lens, O, lse):
+    if cache.device != dev or _elsewhere(dev, page_table, seq_lens, O, lse, cu_tokens):
         L._on_gpu(("cache.K", cache.K), ("Q", Q), ("page_table", page_table), ("seq_lens", seq_lens), ("O", O),
-                  ("lse", lse))
+                  ("lse", lse), ("cu_tokens", cu_tokens))
     if O is None:
         O = torch.empty_like(Q)
         if O.stride() != Q.stride():
@@ -469,13 +477,16 @@ def rbs_paged_decode(shape: L.rbs_shape, Q, cache: PagedCache, page_table, seq_l
     elif workspace.numel() * workspace.element_size() < rbs_decode_workspace_bytes():
         raise ValueError("workspace is smaller than rbs_decode_workspace_bytes()")
     L._check("rbs_paged_decode", _on(dev, stream, _decode, _strided(shape, qs), cache, Q, page_table, seq_lens,
-                                     softmax_scale, O, lse, workspace, dev))
+                                     softmax_scale, O, lse, workspace, cu_tokens, dev))
     return O
 
 
-def _decode(shape, cache, Q, page_table, seq_lens, softmax_scale, O, lse, workspace, dev, s):
+def _decode(shape, cache, Q, page_table, seq_lens, softmax_scale, O, lse, workspace, cu_tokens, dev, s):
     # (With the inputs' device current, which tells whether its stream is being captured.)
     ws = _auto_workspace(dev, s) if isinstance(workspace, str) else workspace
-    return L.load().rbs_paged_decode(shape, cache.c, Q.data_ptr(), page_table.data_ptr(), page_table.shape[1],
-                                     seq_lens.data_ptr(), float(softmax_scale), O.data_ptr(), L._ptr(lse),
-                                     ws.data_ptr(), s)
+    rest = (page_table.data_ptr(), page_table.shape[1], seq_lens.data_ptr(), float(softmax_scale), O.data_ptr(),
+            L._ptr(lse), ws.data_ptr(), s)
+    if cu_tokens is None:
+        return L.load().rbs_paged_decode(shape, cache.c, Q.data_ptr(), *rest)
+    return L.load().rbs_paged_decode_packed(shape, cache.c, Q.data_ptr(), cu_tokens.data_ptr(), page_table.shape[0],
+                                            *rest)

@@ -860,12 +860,16 @@ int rbs_qk_norm_rope(const rbs_shape* in, const rbs_shape* out, const rbs_rope* 
 
 size_t rbs_decode_workspace_bytes(void) { return rbs::decode_workspace_bytes(); }
 
-int rbs_paged_decode(const rbs_shape* shape, const rbs_cache* cache, const void* Q, const int32_t* page_table,
-                     int32_t max_pages, const int32_t* seq_lens, float softmax_scale, void* O, float* lse,
-                     void* workspace, void* stream) {
-  int rc = check_heads(shape, RBS_MAX_ROWS);
-  if (rc != RBS_OK) return rc;
+// packed: rows take their tokens by cu_tokens; otherwise the shape's tokens are the rows.
+static int paged_decode(const rbs_shape* shape, const rbs_cache* cache, const void* Q, bool packed,
+                        const int32_t* cu_tokens, int32_t n_rows, const int32_t* page_table, int32_t max_pages,
+                        const int32_t* seq_lens, float softmax_scale, void* O, float* lse, void* workspace,
+                        void* stream) {
   static_assert(RBS_MAX_ROWS == rbs::kMaxRows, "rows of a page table");
+  int rc = check_heads(shape, packed ? RBS_MAX_NEW_TOKENS : RBS_MAX_ROWS);
+  if (rc != RBS_OK) return rc;
+  if (!packed) n_rows = shape->n_tokens;
+  if (n_rows < 1 || n_rows > RBS_MAX_ROWS) return RBS_ERR_SHAPE;
   rbs::DecodeArgs a{};
   if ((rc = resolve_strides(shape->q_stride_head, shape->q_stride_tok, shape->n_q_heads, shape->n_tokens, &a.q_head,
                             &a.q_tok)) != RBS_OK)
@@ -874,25 +878,42 @@ int rbs_paged_decode(const rbs_shape* shape, const rbs_cache* cache, const void*
   if (cache->n_kv_heads != shape->n_kv_heads || max_pages < 1 || max_pages > (INT32_MAX >> a.cache.page_shift))
     return RBS_ERR_SHAPE;
   // The shares of all rows are counted in 32 bits.
-  if (shape->n_tokens * ((((int64_t)max_pages << a.cache.page_shift) >> 5) + 8) > INT32_MAX) return RBS_ERR_SHAPE;
-  if (Q == nullptr || page_table == nullptr || seq_lens == nullptr || O == nullptr || workspace == nullptr)
+  if (n_rows * ((((int64_t)max_pages << a.cache.page_shift) >> 5) + 8) > INT32_MAX) return RBS_ERR_SHAPE;
+  if (Q == nullptr || page_table == nullptr || seq_lens == nullptr || O == nullptr || workspace == nullptr ||
+      (packed && cu_tokens == nullptr))
     return RBS_ERR_NULL;
   if (!(softmax_scale == softmax_scale) || isinf(softmax_scale)) return RBS_ERR_ARG;
   if (!aligned16(Q) || !aligned16(page_table) || !aligned16(seq_lens) || !aligned16(O) || !aligned16(lse) ||
-      !aligned16(workspace))
+      !aligned16(workspace) || !aligned16(cu_tokens))
     return RBS_ERR_ALIGN;
   a.Q = static_cast<const uint16_t*>(Q);
-  a.n_rows = shape->n_tokens;
+  a.n_tokens = shape->n_tokens;
+  a.n_rows = n_rows;
   a.n_q_heads = shape->n_q_heads;
   a.n_kv_heads = shape->n_kv_heads;
   a.page_table = page_table;
   a.max_pages = max_pages;
   a.seq_lens = seq_lens;
+  a.cu_tokens = packed ? cu_tokens : nullptr;
   a.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)shape->head_dim);
   a.O = static_cast<uint16_t*>(O);
   a.lse = lse;
   a.workspace = static_cast<float*>(workspace);
   return finish(rbs::launch_paged_decode(a, static_cast<hipStream_t>(stream)), stream);
+}
+
+int rbs_paged_decode(const rbs_shape* shape, const rbs_cache* cache, const void* Q, const int32_t* page_table,
+                     int32_t max_pages, const int32_t* seq_lens, float softmax_scale, void* O, float* lse,
+                     void* workspace, void* stream) {
+  return paged_decode(shape, cache, Q, false, nullptr, 0, page_table, max_pages, seq_lens, softmax_scale, O, lse,
+                      workspace, stream);
+}
+
+int rbs_paged_decode_packed(const rbs_shape* shape, const rbs_cache* cache, const void* Q, const int32_t* cu_tokens,
+                            int32_t n_rows, const int32_t* page_table, int32_t max_pages, const int32_t* seq_lens,
+                            float softmax_scale, void* O, float* lse, void* workspace, void* stream) {
+  return paged_decode(shape, cache, Q, true, cu_tokens, n_rows, page_table, max_pages, seq_lens, softmax_scale, O,
+                      lse, workspace, stream);
 }
 
 const char* rbs_status_str(int status) {

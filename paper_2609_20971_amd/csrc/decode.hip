@@ -13,6 +13,9 @@
 //   operand if V's rows come in the same order: P never leaves its lane.  V's
 //   operand needs eight keys of one element; a lane has eight elements of eight
 //   keys (16 lanes: whole rows) and regroups them with byte permutes.
+// - A row's place in Q, O and lse is its number, or its last new token's where those
+//   are packed: one scalar load as the row starts, and rows without one are skipped
+//   like unused ones when the lengths are read.
 // - The keys of all rows together are dealt out evenly: a tile is 32 (64) keys of
 //   one row, and worker w of a KV head takes tiles [T w / W, T (w + 1) / W) of
 //   the T tiles of all rows, its four waves every fourth of them.  Lengths are on
@@ -99,6 +102,17 @@ __host__ __device__ inline Work work_of_heads(int n_q_heads, int n_kv_heads) {
   return w;
 }
 
+// The row's place in Q, O and lse (of a row that has one).
+__device__ __forceinline__ int token_of(const int32_t* cu_tokens, int row) {
+  return cu_tokens == nullptr ? row : cu_tokens[row + 1] - 1;
+}
+// Whether it has one.  Offsets are trusted like the page table: tokens outside Q are no row's.
+__device__ __forceinline__ bool has_token(const int32_t* cu_tokens, int n_tokens, int row) {
+  if (cu_tokens == nullptr) return true;
+  const int begin = cu_tokens[row], end = cu_tokens[row + 1];
+  return end > max(begin, 0) && end <= n_tokens;
+}
+
 // A row's share in the dealing out: its tiles, and kRowCost more for what it
 // costs to start and end a row.
 template <bool kFp8>
@@ -106,12 +120,12 @@ __device__ __forceinline__ int share_of(int len) {
   return len > 0 ? (len - 1) / kTile<kFp8> + 1 + kRowCost : 0;
 }
 
-// first[row]: shares of the rows before it, first[n_rows]: of all; length[row];
-// returns the longest share.  Each thread sums n_rows / 256 rows, then a scan over
+// first[row]: shares of the rows before it, first[n_rows]: of all; length[row] (-1:
+// a row to leave alone); returns the longest share.  Each thread sums n_rows / 256 rows, then a scan over
 // the threads.
 template <bool kFp8>
-__device__ __forceinline__ int tile_offsets(const DecodeArgs& a, const int32_t* lens, int* first, int* length,
-                                             int* sums) {
+__device__ __forceinline__ int tile_offsets(const DecodeArgs& a, const int32_t* lens, const int32_t* cu_tokens,
+                                             int* first, int* length, int* sums) {
   constexpr int kPer = kMaxRows / kThreads;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int per = (a.n_rows + kThreads - 1) / kThreads, row0 = t * per;
@@ -123,7 +137,8 @@ __device__ __forceinline__ int tile_offsets(const DecodeArgs& a, const int32_t* 
   for (int i = 0; i < kPer; ++i) {
     if (i >= per) break;
     if (row0 + i < a.n_rows) {
-      const int len = lens[row0 + i], clamped = (int)(len < cap ? len : cap);
+      const int len = lens[row0 + i];
+      const int clamped = has_token(cu_tokens, a.n_tokens, row0 + i) ? (int)(len < cap ? len : cap) : -1;
       length[row0 + i] = clamped;
       share[i] = share_of<kFp8>(clamped);
     }
@@ -377,15 +392,15 @@ __device__ __forceinline__ void attend_tile(const Stream<kFp8>& st, Tile<kFp8>& 
   if (more) st.load_v(tile, next);
 }
 
-// The result of one column of a row: o holds 8 elements from 8 part on of the
+// The result of one column of a token: o holds 8 elements from 8 part on of the
 // sum of weighted values, l the sum of weights in units of 2^m.
-__device__ __forceinline__ void write_row(const DecodeArgs& a, int row, int head, int part, const float* o, float m,
-                                          float l, float v_scale) {
+__device__ __forceinline__ void write_token(const DecodeArgs& a, int tok, int head, int part, const float* o,
+                                            float m, float l, float v_scale) {
   const float f = v_scale / l;
   const uint4 w = make_uint4(two_bf16(o[0] * f, o[1] * f), two_bf16(o[2] * f, o[3] * f),
                              two_bf16(o[4] * f, o[5] * f), two_bf16(o[6] * f, o[7] * f));
-  *reinterpret_cast<uint4*>(a.O + head * a.q_head + row * a.q_tok + 8 * part) = w;
-  if (part == 0 && a.lse != nullptr) a.lse[(int64_t)head * a.n_rows + row] = (m + __log2f(l)) * 0.69314718055994531f;
+  *reinterpret_cast<uint4*>(a.O + head * a.q_head + tok * a.q_tok + 8 * part) = w;
+  if (part == 0 && a.lse != nullptr) a.lse[(int64_t)head * a.n_tokens + tok] = (m + __log2f(l)) * 0.69314718055994531f;
 }
 
 template <bool kFp8>
@@ -413,7 +428,8 @@ __device__ __forceinline__ int row_from(const int* first, int n_rows, int x) {
 // kWhole: a row is one worker's, so that there is nothing to join.
 template <bool kFp8, bool kWhole>
 __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
-    DecodeArgs a, const int32_t* __restrict__ lens, const int32_t* __restrict__ page_table) {
+    DecodeArgs a, const int32_t* __restrict__ lens, const int32_t* __restrict__ page_table,
+    const int32_t* __restrict__ cu_tokens) {
   __shared__ int first[kMaxRows + 1], length[kMaxRows], sums[2 * kWaves];
   __shared__ __align__(16) float acc[kWaves][kCols][kPad];
   __shared__ float ms[kWaves][kCols], ls[kWaves][kCols];
@@ -424,7 +440,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
   const int g = unit / wk.tiles_of_cols, group = a.n_q_heads / a.n_kv_heads;
   const int head0 = g * group + (unit % wk.tiles_of_cols) * kCols;
   const int cols = min(kCols, (g + 1) * group - head0);
-  const int longest = tile_offsets<kFp8>(a, lens, first, length, sums);
+  const int longest = tile_offsets<kFp8>(a, lens, cu_tokens, first, length, sums);
   const int T = first[a.n_rows];
   // Many short rows: each wave takes whole rows for itself, with nothing to join.
   const bool solo = longest <= kSoloShare && (int64_t)longest * (kWaves * wk.workers) <= (int64_t)kSoloRatio * T;
@@ -441,11 +457,12 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
   // Empty rows: zeros, and -inf.
   for (int row = worker; row < a.n_rows; row += wk.workers) {
     if (length[row] != 0) continue;
+    const int tok = token_of(cu_tokens, row);
     for (int x = threadIdx.x; x < cols * (kHeadDim / 8); x += kThreads)
-      *reinterpret_cast<uint4*>(a.O + (head0 + x / 16) * a.q_head + row * a.q_tok + 8 * (x % 16)) =
+      *reinterpret_cast<uint4*>(a.O + (head0 + x / 16) * a.q_head + tok * a.q_tok + 8 * (x % 16)) =
           make_uint4(0u, 0u, 0u, 0u);
     if (a.lse != nullptr && (int)threadIdx.x < cols)
-      a.lse[(int64_t)(head0 + threadIdx.x) * a.n_rows + row] = -INFINITY;
+      a.lse[(int64_t)(head0 + threadIdx.x) * a.n_tokens + tok] = -INFINITY;
   }
 
   constexpr int kBytes = kFp8 ? 1 : 2, kSteps = Tile<kFp8>::kSteps;
@@ -516,13 +533,14 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
     }
     const int stop = min(last, t_end);
     const bool begins = at == first[r], whole = begins && stop == last;
+    const int tok = token_of(cu_tokens, r);
     uint4 q[4];
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       // Elements that the K operand's lane holds.
       const int d = kFp8 ? 64 * (x >> 1) + 16 * c + 8 * (x & 1) : 32 * x + 8 * c;
       q[x] = make_uint4(0u, 0u, 0u, 0u);
-      if (col < cols) q[x] = *reinterpret_cast<const uint4*>(a.Q + (head0 + col) * a.q_head + r * a.q_tok + d);
+      if (col < cols) q[x] = *reinterpret_cast<const uint4*>(a.Q + (head0 + col) * a.q_head + tok * a.q_tok + d);
     }
     // Waited for here: in the loop the wait for the first Q would be one for the
     // values on their way as well, at every tile.
@@ -545,14 +563,14 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
     if (solo) {
       if (col < cols) {
         const float f = v_scale / s.l;
-        uint16_t* out = a.O + (head0 + col) * a.q_head + r * a.q_tok + 32 * c;
+        uint16_t* out = a.O + (head0 + col) * a.q_head + tok * a.q_tok + 32 * c;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           *reinterpret_cast<uint4*>(out + 8 * e) =
               make_uint4(two_bf16(s.o[0][e] * f, s.o[1][e] * f), two_bf16(s.o[2][e] * f, s.o[3][e] * f),
                          two_bf16(s.o[4][e] * f, s.o[5][e] * f), two_bf16(s.o[6][e] * f, s.o[7][e] * f));
         if (c == 0 && a.lse != nullptr)
-          a.lse[(int64_t)(head0 + col) * a.n_rows + r] = (s.m + __log2f(s.l)) * 0.69314718055994531f;
+          a.lse[(int64_t)(head0 + col) * a.n_tokens + tok] = (s.m + __log2f(s.l)) * 0.69314718055994531f;
       }
       if (!kWhole && by_row && lane == 0) shared_rows(a)[r * wk.units + unit] = Shared{-1, 0, 0, 0};
       at = first[r + 1];
@@ -587,7 +605,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
         o[4] += y.x * f; o[5] += y.y * f; o[6] += y.z * f; o[7] += y.w * f;
       }
       if (kWhole || whole) {
-        write_row(a, r, head0 + hc, part, o, m, l, v_scale);
+        write_token(a, tok, head0 + hc, part, o, m, l, v_scale);
       } else {
         float* slot = a.workspace + (size_t)(2 * blockIdx.x + (is_first ? 0 : 1)) * kPartFloats;
         *reinterpret_cast<float4*>(slot + hc * kHeadDim + 8 * part) = make_float4(o[0], o[1], o[2], o[3]);
@@ -623,8 +641,10 @@ __global__ __launch_bounds__(kJoinThreads) void paged_decode_join_kernel(DecodeA
   const bool by_row = a.n_rows <= wk.workers;
   const int unit = blockIdx.x % wk.units;
   const Shared shared = shared_rows(a)[blockIdx.x];
-  const int len = by_row ? a.seq_lens[blockIdx.x / wk.units] : 1;
-  if (len <= 0 || shared.row < 0) return;  // (a row of no length is no worker's)
+  const int row = blockIdx.x / wk.units;
+  // (A row of no length or no token is no worker's: there is no record of it.)
+  if (by_row && (a.seq_lens[row] <= 0 || !has_token(a.cu_tokens, a.n_tokens, row))) return;
+  if (shared.row < 0) return;
   const int wa = shared.first;
   const int g = unit / wk.tiles_of_cols, group = a.n_q_heads / a.n_kv_heads;
   const int head0 = g * group + (unit % wk.tiles_of_cols) * kCols;
@@ -684,7 +704,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_decode_join_kernel(DecodeA
 #pragma unroll
     for (int e = 0; e < 8; ++e) out[e] += acc[hc + i * cols][8 * part + e] * f;
   }
-  write_row(a, shared.row, head0 + col0 + hc, part, out, top, sum, value_scale<kFp8>(a, g));
+  write_token(a, token_of(a.cu_tokens, shared.row), head0 + col0 + hc, part, out, top, sum, value_scale<kFp8>(a, g));
 }
 
 template <bool kFp8>
@@ -694,10 +714,12 @@ hipError_t launch(const DecodeArgs& a, hipStream_t s) {
   const dim3 grid(wk.units * wk.workers);
   const int64_t most = (int64_t)a.max_pages << a.cache.page_shift;  // keys of a row
   if (most <= kWholeTiles * kTile<kFp8> || (most <= kWholeKeysOfFew && a.n_rows * wk.units <= kFewWhole)) {
-    hipLaunchKernelGGL((paged_decode_kernel<kFp8, true>), grid, dim3(kThreads), 0, s, a, a.seq_lens, a.page_table);
+    hipLaunchKernelGGL((paged_decode_kernel<kFp8, true>), grid, dim3(kThreads), 0, s, a, a.seq_lens, a.page_table,
+                       a.cu_tokens);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((paged_decode_kernel<kFp8, false>), grid, dim3(kThreads), 0, s, a, a.seq_lens, a.page_table);
+  hipLaunchKernelGGL((paged_decode_kernel<kFp8, false>), grid, dim3(kThreads), 0, s, a, a.seq_lens, a.page_table,
+                       a.cu_tokens);
   const int joins = wk.units * (a.n_rows < wk.workers ? a.n_rows : wk.workers);
   if (joins * cols <= kFewJoins)
     hipLaunchKernelGGL((paged_decode_join_kernel<kFp8, 1>), dim3(joins, cols), dim3(kJoinThreads), 0, s, a);

@@ -55,11 +55,13 @@ struct RopeArgs {
 struct DecodeArgs {
   const uint16_t* Q;
   int64_t q_head, q_tok;  // Q and O
+  int n_tokens;           // of Q, O and lse
   int n_rows, n_q_heads, n_kv_heads;
   CacheView cache;
   const int32_t* page_table;
   int max_pages;
   const int32_t* seq_lens;
+  const int32_t* cu_tokens;  // row s's token is cu_tokens[s + 1] - 1; null: s
   float scale;
   uint16_t* O;
   float* lse;

@@ -295,3 +295,52 @@ def test_threads_have_decode_workspaces_of_their_own(monkeypatch):
         assert a is again and a is not other
         assert a.numel() * 4 >= rbs.rbs_decode_workspace_bytes()
     assert len({x.data_ptr() for three in got.values() for x in three}) == 2 * len(got)
+
+
+# ------------------------------------------------------------------ packed queries
+
+def _packed(shape=None, cache=None, **over):
+    shape = rbs.make_shape(10, 4, 2, 64) if shape is None else shape
+    a = dict(Q=FAKE, cu_tokens=FAKE, n_rows=5, page_table=FAKE, max_pages=4, seq_lens=FAKE, scale=0.0, O=FAKE, lse=FAKE,
+             workspace=FAKE)
+    a.update(over)
+    return _lib().rbs_paged_decode_packed(shape, _cache() if cache is None else cache, *a.values(), None)
+
+
+@pytest.mark.parametrize("over,code", CACHE_BAD)
+def test_packed_cache_validation(over, code):
+    assert _packed(cache=_cache(**over)) == code
+
+
+def test_packed_arguments():
+    for name in ("Q", "cu_tokens", "page_table", "seq_lens", "O", "workspace"):
+        assert _packed(**{name: None}) == 1, name
+    for name in ("Q", "cu_tokens", "page_table", "seq_lens", "O", "workspace", "lse"):
+        assert _packed(**{name: MIS}) == 5, name
+    for bad in (0, -1, 4097):
+        assert _packed(n_rows=bad) == 2
+    # More tokens than a table has rows, up to a step's; the tiles are counted over the rows.
+    assert _packed(shape=rbs.make_shape(1 << 24, 4, 2, 64), n_rows=4096, Q=None) == OK_PAST
+    assert _packed(shape=rbs.make_shape((1 << 24) + 1, 4, 2, 64)) == 2
+    assert _packed(n_rows=4096, max_pages=2**20) == 2
+    assert _packed(shape=rbs.make_shape(4096, 4, 2, 64), n_rows=1, max_pages=2**20, Q=None) == OK_PAST
+    for bad in (math.nan, math.inf):
+        assert _packed(scale=bad) == 4
+    assert _lib().rbs_paged_decode_packed(None, _cache(), FAKE, FAKE, 5, FAKE, 4, FAKE, 0.0, FAKE, None, FAKE, None) == 1
+
+
+def test_packed_binding_checks():
+    shape = rbs.make_shape(10, 4, 2, 64)
+    cache = object.__new__(rbs.PagedCache)
+    object.__setattr__(cache, "device", -1)
+    object.__setattr__(cache, "K", _bf(4, 2, 16, 128))
+    table, lens, cu = _i32(6, 3), _i32(6), _i32(7)
+    for t, s, c, message in [
+        (table, lens, cu.long(), "cu_tokens must be torch.int32"),
+        (table, lens, cu[:6], "cu_tokens must have shape"),
+        (table, _i32(10), cu, "seq_lens must have shape"),
+        (table, lens, None, "page_table must have shape"),
+        (table, lens, cu, "must be on a GPU"),
+    ]:
+        with pytest.raises(ValueError, match=message):
+            rbs.rbs_paged_decode(shape, _bf(4, 10, 128), cache, t, s, cu_tokens=c)

@@ -772,3 +772,157 @@ def test_threads_that_decode_on_one_stream():
         assert len(got[k]) == 60
         for O, lse in got[k]:
             assert torch.equal(O, o) and torch.equal(lse, l)
+
+
+# ------------------------------------------------------------------ queries packed row after row
+
+def _run_packed(c, new, behind, scale=0.0, cu=None):
+    """Random queries for every token of a batch in which row s has new[s] (unused rows: none); O and lse, the
+    token of each row that has one, and those queries."""
+    add = [max(0, a) if n >= 0 else 0 for n, a in zip(c["lens"], new)]
+    at = [0]
+    for a in add:
+        at.append(at[-1] + a)
+    n = max(1, at[-1] + behind)
+    Q = (torch.randn(n, c["hq"], D, generator=_gen(len(c["lens"]) + n)) * 1.5).to(torch.bfloat16)
+    Qd = Q.cuda().transpose(0, 1)
+    O = torch.full_like(Qd, math.nan)
+    lse = torch.full((c["hq"], n), math.nan, device="cuda")
+    got = rbs.rbs_paged_decode(rbs.make_shape(n, c["hq"], c["hkv"], 64), Qd, c["cache"], c["table"].cuda(),
+                               _ints(c["lens"]), scale, O=O, lse=lse, cu_tokens=_ints(at if cu is None else cu))
+    assert got is O
+    return O, lse, {row: at[row + 1] - 1 for row, a in enumerate(add) if a > 0}, Q
+
+
+def _check_packed(c, O, lse, token, Q, scale):
+    K, V = _values(c, "K"), _values(c, "V")
+    for row, t in token.items():
+        n = c["lens"][row]
+        k, v = (R.gather(x, c["table"][row], n, c["page"]) for x in (K, V))
+        o, l, o_tol, l_tol = R.attend(Q[t].double(), k, v, scale)
+        assert bool(((O[:, t].cpu().double() - o).abs() <= o_tol).all()), f"row {row} of length {n}, token {t}"
+        got = lse[:, t].cpu().double()
+        assert bool(((got - l).abs() <= l_tol).all()) if n > 0 else bool((got == -math.inf).all())
+    others = [t for t in range(O.shape[1]) if t not in token.values()]
+    assert bool(O[:, others].isnan().all()) and bool(lse[:, others].isnan().all()), "other tokens were written"
+
+
+PACKED = [
+    # lengths, new tokens, tokens behind the last, heads, page, fp8, columns to spare
+    ([-1, 5], [1, 1], 0, 2, 1, 16, False, 1),
+    ([-1, -1], [1, 1], 3, 2, 1, 16, False, 1),                                    # no token at all
+    ([70, -1, 33, 0, -1, 200], [1] * 6, 2, 8, 2, 16, False, 0),                    # one launch
+    ([70, -1, 33, 0, -1, 200], [1] * 6, 2, 8, 2, 16, True, 0),
+    ([3000, -1, 900, 40, -1, 5000, 17], [1, 1, 0, 1, 1, 1, 1], 1, 28, 4, 16, False, 60),   # rows in parts, one with none
+    ([3000, -1, 900, 40, -1, 5000, 17], [3, 1, 0, 800, 1, 1, 17], 5, 28, 4, 32, True, 0),   # a last token each
+    ([-1, 9000, -1], [1, 1, 1], 0, 8, 1, 64, False, 300),                                   # a wide table
+    ([(i * 53) % 90 - 1 for i in range(700)], [1 - (i % 7 == 3) for i in range(700)], 9, 16, 8, 16, False, 0),
+    ([(i * 53) % 1500 - 1 if i % 4 else -1 for i in range(300)], [1] * 300, 75, 8, 2, 32, True, 0),
+    ([(i * 53) % 700 - 1 if i % 3 else -1 for i in range(90)], [1] * 90, 0, 64, 32, 16, False, 0),   # fewer workers than rows
+    ([2000, -1, 10], [1, 1, 1], 0, 34, 2, 16, False, 0),                                    # 17 heads to a KV head
+    ([-1] * 3000 + [600, 2], [1] * 3002, 40, 4, 2, 16, False, 0),
+]
+
+
+@pytest.mark.parametrize("k", range(len(PACKED)))
+def test_decode_of_packed_queries(k):
+    lens, new, behind, hq, hkv, page, fp8, spare = PACKED[k]
+    _say(f"[packed] {len(lens)} rows, heads {hq}/{hkv}, page {page}, fp8 {fp8}")
+    c = _decode_case(lens, hq, hkv, page, fp8, "heads", 600 + k, spare_columns=spare)
+    _check_packed(c, *_run_packed(c, new, behind, 0.1), 0.1)
+
+
+def test_packed_queries_with_a_row_each_are_those_by_row():
+    """Every row used: token t is row t's, and the two forms give the same bits."""
+    c = _decode_case([300, 4000, 1, 77, 2500], 8, 2, 16, False, "heads", 640)
+    O, lse = _run_decode(c)
+    Q = c["q"].cuda().transpose(0, 1)
+    l2 = torch.empty_like(lse)
+    O2 = rbs.rbs_paged_decode(rbs.make_shape(5, 8, 2, 64), Q, c["cache"], c["table"].cuda(), _ints(c["lens"]), lse=l2,
+                              cu_tokens=_ints([0, 1, 2, 3, 4, 5]))
+    assert torch.equal(O2, O) and torch.equal(l2, lse)
+
+
+def test_packed_offsets_outside_the_tokens():
+    """Rows whose offsets fall outside the queries have no token; nothing is read or written there."""
+    c = _decode_case([3000, 40, 500, 20, 900], 8, 2, 16, False, "heads", 641)
+    cu = [-5, 0, 1, 2**31 - 1, -2**31, 2]   # rows 1 and 4 have tokens 0 and 1 of three
+    O, lse, _, Q = _run_packed(c, [1, 1, 1, 0, 0], 0, cu=cu)
+    _check_packed(c, O, lse, {1: 0, 4: 1}, Q, 1 / math.sqrt(D))
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_steps_with_unused_rows(fp8):
+    """The three calls chained with rows unused, admitted and released between them, before used ones too: nothing is
+    read back for the next call, and captured steps equal the eager ones."""
+    hq, hkv, page, rows, steps = 8, 2, 16, 6, 7
+    rope, _, _ = _layer(9, hq, hkv)
+    amax = torch.full((2 * hkv,), 7.0).cuda() if fp8 else None
+    shape = rbs.make_shape(rows, hq, hkv, 64)
+    inputs = [_qkv(rows, hq, hkv, 700 + k) for k in range(steps)]
+    now = [torch.empty_like(x) for x in inputs[0]]  # what the graph reads
+
+    class Server:
+        def __init__(self):
+            self.pages = rbs.Pages.allocate(rows, 400, 500, page)
+            self.cache = _cache(500, hkv, page, fp8, "heads", amax, fill=0xFF)  # NaN everywhere
+            self.out = rbs.PageStep.allocate(self.pages, rows)
+            self.O = torch.full((rows, hq, D), math.nan, dtype=torch.bfloat16, device="cuda").transpose(0, 1)
+            self.lse = torch.full((hq, rows), math.nan, device="cuda")
+            for row, n in ((1, 1000), (3, 40)):  # prompts in rows 1 and 3; rows 0, 2, 4 and 5 unused
+                self.pages.seq_lens[row] = 0
+                Q, K, V = _qkv(n, hq, hkv, 720 + row)
+                counts = torch.zeros(rows, dtype=torch.int32, device="cuda")
+                counts[row] = n
+                s = rbs.rbs_pages_extend(self.pages, counts, n)
+                rbs.rbs_qk_norm_rope(rbs.make_shape(n, hq, hkv, 64), rope, Q, K, s.positions, V=V, cache=self.cache,
+                                     slots=s.slots, keep_k=False)
+
+        def between(self, k):
+            if k == 2:
+                self.pages.seq_lens[5] = 0
+            if k == 3:
+                self.pages.seq_lens[0] = 0
+            if k == 5:
+                rbs.rbs_pages_release(self.pages, _ints([0, 1, 0, 0, 0, 0]))
+
+        def step(self):
+            Q, K, V = now
+            o = rbs.rbs_pages_extend(self.pages, step=self.out)
+            self.q, _ = rbs.rbs_qk_norm_rope(shape, rope, Q, K, o.positions, V=V, cache=self.cache, slots=o.slots,
+                                             keep_k=False)
+            return rbs.rbs_paged_decode(shape, self.q, self.cache, self.pages.page_table, o.seq_lens, O=self.O,
+                                        lse=self.lse, cu_tokens=o.cu_tokens)
+
+    eager, want = Server(), []
+    used_at = [[1, 3], [1, 3], [1, 3, 5], [0, 1, 3, 5], [0, 1, 3, 5], [0, 3, 5], [0, 3, 5]]
+    for k in range(steps):
+        eager.between(k)
+        for a, b in zip(now, inputs[k]):
+            a.copy_(b)
+        eager.step()
+        lens, used = eager.pages.seq_lens.tolist(), used_at[k]
+        assert [r for r in range(rows) if lens[r] >= 0] == used and eager.out.status.tolist() == [0]
+        table, (kc, vc) = eager.pages.page_table.cpu(), (x.cpu() for x in (eager.cache.K, eager.cache.V))
+        for t, row in enumerate(used):
+            held = [R.gather(x, table[row], lens[row], page) for x in (kc, vc)]
+            held = [R.e4m3_values(x) * 7.0 / 448 if fp8 else x.double() for x in held]
+            o, l, o_tol, l_tol = R.attend(eager.q[:, t].cpu().double(), *held, 1 / math.sqrt(D))
+            assert bool(((eager.O[:, t].cpu().double() - o).abs() <= o_tol).all()), f"step {k}, row {row}"
+            assert bool(((eager.lse[:, t].cpu().double() - l).abs() <= l_tol).all())
+        want.append((eager.O.clone(), eager.lse.clone()))
+    captured = Server()
+    for a, b in zip(now, inputs[0]):
+        a.copy_(b)
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        captured.step()
+    for k in range(steps):
+        captured.between(k)
+        for a, b in zip(now, inputs[k]):
+            a.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        n = len(used_at[k])
+        assert torch.equal(captured.O[:, :n], want[k][0][:, :n]) and torch.equal(captured.lse[:, :n], want[k][1][:, :n])
