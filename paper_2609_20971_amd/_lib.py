@@ -259,9 +259,14 @@ def _on_gpu(*named) -> int:
 
 def _heads_tokens(name: str, t, n_heads: int, n_tokens: int, head_dim: int):
     """A bf16 (head, token, dimension) tensor of any strides with a contiguous
-    last dimension; returns its (head stride, token stride)."""
+    last dimension; returns its (head stride, token stride).  An expanded tensor
+    is refused: to the library a stride of 0 means the dense layout, which would
+    reach past the tensor's storage."""
     _check_tensor(name, t, torch.bfloat16, (n_heads, n_tokens, head_dim), contiguous=False)
-    return t.stride()[:2]
+    strides = t.stride()[:2]
+    if (strides[0] == 0 and n_heads > 1) or (strides[1] == 0 and n_tokens > 1):
+        raise ValueError(f"{name} is expanded (strides {tuple(t.stride())}); the library takes no stride of 0")
+    return strides
 
 
 def _with_strides(shape: rbs_shape, q=None, kv=None) -> rbs_shape:

@@ -106,7 +106,7 @@ def _rows(name, t, sizes):
     """The strides of a bf16 (head, token, dimension) tensor of these sizes."""
     if isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.shape == sizes:
         strides = t.stride()
-        if strides[2] == 1:
+        if strides[2] == 1 and strides[0] and strides[1]:
             return strides[:2]
     return L._heads_tokens(name, t, *sizes)
 

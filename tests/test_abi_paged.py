@@ -344,3 +344,46 @@ def test_packed_binding_checks():
     ]:
         with pytest.raises(ValueError, match=message):
             rbs.rbs_paged_decode(shape, _bf(4, 10, 128), cache, t, s, cu_tokens=c)
+
+
+# ------------------------------------------------------------------ expanded tensors
+
+def _expanded(h, n, over):
+    """A bf16 [h][n][128] tensor that repeats its storage over the heads or over the tokens."""
+    return (_bf(1, n, 128) if over == "heads" else _bf(h, 1, 128)).expand(h, n, 128)
+
+
+@pytest.mark.parametrize("over", ["heads", "tokens"])
+def test_expanded_tensors_are_refused(over):
+    """Their stride of 0 would stand for the dense layout in the library, past the end of their storage."""
+    shape, pos = rbs.make_shape(10, 4, 2, 64), _i32(10)
+    Q, K, rope = _bf(4, 10, 128), _bf(2, 10, 128), rbs.Rope(None)
+    cache = object.__new__(rbs.PagedCache)
+    q, k = _expanded(4, 10, over), _expanded(2, 10, over)
+    for args, more, name in [
+        ((q, K, pos), {}, "Q"), ((Q, k, pos), {}, "K"), ((Q, k, pos), dict(V=k, cache=cache, slots=pos), "K"),
+        ((Q, K, pos), dict(V=k, cache=cache, slots=pos), "V"), ((Q, K, pos), dict(Q_out=q), "Q_out"),
+        ((Q, K, pos), dict(K_out=k), "K_out"),
+    ]:
+        with pytest.raises(ValueError, match=f"^{name} is expanded"):
+            rbs.rbs_qk_norm_rope(shape, rope, *args, **more)
+    for O in (None, q):
+        with pytest.raises(ValueError, match="^Q is expanded"):
+            rbs.rbs_paged_decode(shape, q, cache, _i32(10, 3), pos, O=O)
+    with pytest.raises(ValueError, match="O strides"):
+        rbs.rbs_paged_decode(shape, Q, cache, _i32(10, 3), pos, O=q)
+    # The prefill's calls take their strides from the tensors as well.
+    counts, indices = _i32(4, 1), _i32(4, 1)
+    for args, name in [((q, K, K), "Q"), ((Q, k, k), "K"), ((Q, K, k), "V")]:
+        with pytest.raises(ValueError, match=f"^{name} is expanded"):
+            rbs.rbs_sparse_prefill(shape, *args, counts, indices, workspace=None)
+    with pytest.raises(ValueError, match="^K is expanded"):
+        rbs.rbs_block_stats(shape, k)
+
+
+def test_one_head_or_token_may_have_any_stride():
+    """(What it is stays unused: the checks after this one are reached.)"""
+    shape = rbs.make_shape(1, 1, 1, 64)
+    x = _bf(128).as_strided((1, 1, 128), (0, 0, 1))
+    with pytest.raises(ValueError, match="must be on a GPU"):
+        rbs.rbs_qk_norm_rope(shape, rbs.Rope(None), x, x, _i32(1))
