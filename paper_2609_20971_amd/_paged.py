@@ -5,6 +5,11 @@ rotation's weights) sit in objects that check them once, when made, and keep
 their C structs: a decode step's calls are short, and the checks of all of
 their tensors would take longer than the kernels.  The tensors that change from
 call to call are checked at every call, as in the other calls.
+
+stream: where a call goes, the current stream by default.  What a call makes
+itself (outputs that are not given, the workspace) is that stream's memory, which
+nothing else uses before the stream's earlier work is done; outputs may be dropped
+once the current stream's work that uses them has been queued.
 """
 
 from __future__ import annotations
@@ -92,6 +97,24 @@ def _on(device: int, stream, call, *args):
         return call(*args, _handle(device, stream))
     with torch.cuda.device(device):
         return call(*args, _handle(device, stream))
+
+
+def _own(device: int, handle: int):
+    """With the stream of that handle current."""
+    return torch.cuda.stream(torch.cuda.ExternalStream(handle, device) if handle else torch.cuda.default_stream(device))
+
+
+def _made(device: int, stream, make, *args):
+    """make(*args): an output (a tensor or a PageStep) of a call on `stream`, as that
+    stream's memory, which the current one will use as well."""
+    if stream is None or _handle(device, stream) == torch._C._cuda_getCurrentRawStream(device):
+        return make(*args)
+    current = torch.cuda.current_stream(device)
+    with _own(device, _handle(device, stream)):
+        out = make(*args)
+    for t in (out.cu_tokens, out.positions, out.slots, out.status) if isinstance(out, PageStep) else (out,):
+        t.record_stream(current)
+    return out
 
 
 def _elsewhere(dev: int, *tensors) -> bool:
@@ -270,7 +293,7 @@ def rbs_pages_extend(pages: Pages, new_tokens=None, max_tokens: int | None = Non
         if new_tokens.get_device() != pages.device:
             L._on_gpu(("page_table", pages.page_table), ("new_tokens", new_tokens))
     if step is None:
-        step = PageStep.allocate(pages, pages.n_rows if max_tokens is None else max_tokens)
+        step = _made(pages.device, stream, PageStep.allocate, pages, pages.n_rows if max_tokens is None else max_tokens)
     else:
         if not isinstance(step, PageStep):
             raise ValueError("step must be a PageStep")
@@ -296,7 +319,7 @@ def rbs_pages_release(pages: Pages, released, status=None, stream=None) -> torch
         L._check_tensor("status", status, torch.int32, (1,))
     L._on_gpu(("page_table", pages.page_table), ("released", released), ("status", status))
     if status is None:
-        status = torch.empty(1, dtype=torch.int32, device=pages.page_table.device)
+        status = _made(pages.device, stream, pages.n_free.new_empty, 1)
     L._check("rbs_pages_release", _on(pages.device, stream, L.load().rbs_pages_release, pages.c, released.data_ptr(),
                                       *pages.state, status.data_ptr()))
     return status
@@ -395,9 +418,10 @@ def rbs_qk_norm_rope(shape: L.rbs_shape, rope: Rope, Q, K, positions, V=None, ca
     if rope.device is not None and rope.device != dev:
         raise ValueError(f"rope is on cuda:{rope.device}, the other arguments on cuda:{dev}")
     if Q_out is None:
-        Q_out = torch.empty_like(Q)  # Q's order of strides, without the gaps of a fused projection's view
+        # (Q's order of strides, without the gaps of a fused projection's view.)
+        Q_out = _made(dev, stream, torch.empty_like, Q)
     if K_out is None and keep_k:
-        K_out = torch.empty_like(K)
+        K_out = _made(dev, stream, torch.empty_like, K)
     sh = _strided(shape, qs, ks)
     out = L.rbs_shape(n, hq, hkv, d, shape.block_size, *Q_out.stride()[:2],
                       *(ks if K_out is None else K_out.stride()[:2]))
@@ -422,8 +446,7 @@ def _auto_workspace(device: int, handle: int) -> torch.Tensor:
     graphs that were captured on one stream may run side by side."""
     if handle != torch._C._cuda_getCurrentRawStream(device):
         # Made on the stream that uses it, whose order its memory's next use has to follow.
-        own = torch.cuda.ExternalStream(handle, device) if handle else torch.cuda.default_stream(device)
-        with torch.cuda.stream(own):
+        with _own(device, handle):
             return _workspace_of(device, handle)
     return _workspace_of(device, handle)
 
@@ -466,9 +489,9 @@ def rbs_paged_decode(shape: L.rbs_shape, Q, cache: PagedCache, page_table, seq_l
         L._on_gpu(("cache.K", cache.K), ("Q", Q), ("page_table", page_table), ("seq_lens", seq_lens), ("O", O),
                   ("lse", lse), ("cu_tokens", cu_tokens))
     if O is None:
-        O = torch.empty_like(Q)
+        O = _made(dev, stream, torch.empty_like, Q)
         if O.stride() != Q.stride():
-            O = L._like_q(Q)
+            O = _made(dev, stream, L._like_q, Q)
     if isinstance(workspace, str):
         if workspace != L.AUTO:
             raise ValueError(f"workspace must be AUTO or a tensor, not {workspace!r}")

@@ -926,3 +926,43 @@ def test_steps_with_unused_rows(fp8):
         torch.cuda.synchronize()
         n = len(used_at[k])
         assert torch.equal(captured.O[:, :n], want[k][0][:, :n]) and torch.equal(captured.lse[:, :n], want[k][1][:, :n])
+
+
+# ------------------------------------------------------------------ streams given by name
+
+def _memory_of(t):
+    """Handle of the stream whose memory a tensor is."""
+    for s in torch.cuda.memory_snapshot():
+        if s["address"] <= t.data_ptr() < s["address"] + s["total_size"]:
+            return s["stream"]
+    raise AssertionError("not torch's memory")
+
+
+@pytest.mark.parametrize("which", ["side", "default", "current"])
+def test_outputs_are_the_memory_of_the_calls_stream(which):
+    """What a call on a stream given by name makes itself: memory of another stream may still be in use there."""
+    hq, hkv, page, rows = 8, 2, 16, 3
+    side = torch.cuda.Stream()
+    stream = dict(side=side, default=torch.cuda.default_stream(), current=None)[which]
+    here = side if which == "default" else torch.cuda.default_stream()
+    handle = here.cuda_stream if stream is None else stream.cuda_stream
+    c = _decode_case([300, 40, 2000], hq, hkv, page, False, "heads", 650)
+    shape, rope = rbs.make_shape(rows, hq, hkv, 64), rbs.Rope(rbs.rope_frequencies()[0])
+    pages = rbs.Pages.allocate(rows, 9, 20, page)
+    pages.seq_lens.zero_()
+    Q, K, V = _qkv(rows, hq, hkv, 651)
+    cache, lens, table = _cache(20, hkv, page, False), _ints(c["lens"]), c["table"].cuda()
+    released = _ints([1, 0, 1])
+    queries = c["q"].cuda().transpose(0, 1)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(here):
+        step = rbs.rbs_pages_extend(pages, stream=stream)
+        q, k = rbs.rbs_qk_norm_rope(shape, rope, Q, K, step.positions, V=V, cache=cache, slots=step.slots, stream=stream)
+        O = rbs.rbs_paged_decode(shape, queries, c["cache"], table, lens, stream=stream)
+        status = rbs.rbs_pages_release(pages, released, stream=stream)
+    torch.cuda.synchronize()
+    for t in (step.cu_tokens, step.positions, step.slots, step.status, q, k, O, status):
+        assert _memory_of(t) == handle
+    assert step.seq_lens is pages.seq_lens and pages.seq_lens.tolist() == [-1, 1, -1] and status.tolist() == [0]
+    assert torch.equal(cache.K[:3, :, 0].transpose(0, 1), k[:, :])
+    _check_decode(c, O, None, 1 / math.sqrt(D))
