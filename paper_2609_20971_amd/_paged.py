@@ -403,8 +403,10 @@ def rbs_qk_norm_rope(shape: L.rbs_shape, rope: Rope, Q, K, positions, V=None, ca
             raise ValueError("cache must be a PagedCache")
         if V is None or slots is None:
             raise ValueError("a cache needs V and slots")
-        if _rows("V", V, k_sizes) != ks:
-            raise ValueError(f"V strides {V.stride()[:2]} differ from K strides {ks}; the library takes one pair")
+        vs = _rows("V", V, k_sizes)
+        # (A stride over one head or one token is never used.)
+        if vs != ks and ((vs[0] != ks[0] and hkv > 1) or (vs[1] != ks[1] and n > 1)):
+            raise ValueError(f"V strides {vs} differ from K strides {ks}; the library takes one pair")
         _int_row("slots", slots, n)
     if Q_out is not None:
         _rows("Q_out", Q_out, q_sizes)

@@ -387,3 +387,19 @@ def test_one_head_or_token_may_have_any_stride():
     x = _bf(128).as_strided((1, 1, 128), (0, 0, 1))
     with pytest.raises(ValueError, match="must be on a GPU"):
         rbs.rbs_qk_norm_rope(shape, rbs.Rope(None), x, x, _i32(1))
+
+
+def test_strides_over_one_head_or_token_need_not_agree():
+    """K and V of one token (or KV head) from buffers of different layouts: only a missing GPU is left to refuse."""
+    cache = object.__new__(rbs.PagedCache)
+    for n, hkv, K, V, message in [
+        (1, 2, _bf(2, 1, 128), _bf(1, 2 * 128 + 512)[:, :256].view(1, 2, 128).transpose(0, 1), "must be on a GPU"),
+        (10, 1, _bf(1, 10, 128), _bf(3, 10, 128)[:1].as_strided((1, 10, 128), (7 * 1280, 128, 1)), "must be on a GPU"),
+        (2, 2, _bf(2, 2, 128), _bf(2, 2, 128).transpose(0, 1), "differ from K strides"),
+        (10, 1, _bf(1, 10, 128), _bf(10, 2, 128)[:, :1].transpose(0, 1), "differ from K strides"),
+    ]:
+        Q, pos = _bf(4, n, 128), _i32(n)
+        object.__setattr__(cache, "device", -1)
+        object.__setattr__(cache, "K", _bf(4, hkv, 16, 128))
+        with pytest.raises(ValueError, match=message):
+            rbs.rbs_qk_norm_rope(rbs.make_shape(n, 4, hkv, 64), rbs.Rope(None), Q, K, pos, V=V, cache=cache, slots=pos)

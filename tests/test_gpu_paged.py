@@ -966,3 +966,20 @@ def test_outputs_are_the_memory_of_the_calls_stream(which):
     assert step.seq_lens is pages.seq_lens and pages.seq_lens.tolist() == [-1, 1, -1] and status.tolist() == [0]
     assert torch.equal(cache.K[:3, :, 0].transpose(0, 1), k[:, :])
     _check_decode(c, O, None, 1 / math.sqrt(D))
+
+
+@pytest.mark.parametrize("n,hkv", [(1, 2), (5, 1)])
+def test_values_of_another_layout(n, hkv):
+    """One token, or one KV head: V's stride over it is not K's, and not used."""
+    hq, page = 4, 16
+    Q, K, V = _qkv(n, hq, hkv, 660, "heads")
+    far = torch.zeros(hkv + 2, n + 3, D, dtype=torch.bfloat16, device="cuda")
+    V2 = far[:hkv, :n] if n == 1 else far[:hkv].as_strided((1, n, D), (9 * far.stride(0), D, 1))
+    V2.copy_(V)
+    if n == 1:  # (head, token, dimension) of a buffer whose tokens are far apart
+        V2 = V2.transpose(0, 1).contiguous().transpose(0, 1)
+        K = K.as_strided((hkv, 1, D), (D, D, 1))
+    assert V2.stride() != K.stride()
+    cache, slots = _cache(2, hkv, page, False), torch.arange(n, dtype=torch.int32, device="cuda") + 3
+    rbs.rbs_qk_norm_rope(rbs.make_shape(n, hq, hkv, 64), rbs.Rope(None), Q, K, slots, V=V2, cache=cache, slots=slots)
+    assert torch.equal(cache.V[0, :, 3:3 + n], V) and torch.equal(cache.K[0, :, 3:3 + n], K)
