@@ -158,7 +158,8 @@ int64_t rbs_index_capacity(int32_t n_blocks);
  * The call resets the queues itself (with a kernel on `stream`, no memset):
  * contents on entry are ignored and undefined afterwards.  The workspace is
  * written by the call like an output, so calls that share one must be
- * ordered (the same stream, or events between streams). */
+ * ordered (the same stream, or events between streams), and since a call is two
+ * launches, host threads that share one must not be inside a call at once. */
 #define RBS_ATTN_WORKSPACE_BYTES 256
 size_t rbs_attention_workspace_bytes(void);
 

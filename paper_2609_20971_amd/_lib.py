@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import threading
 from dataclasses import dataclass
 
 import torch
@@ -171,10 +172,13 @@ def _stream(stream) -> int | None:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
 
-# Attention workspace argument: AUTO takes one cached per (device, stream) --
-# calls on one stream are ordered, so they may share it (a stream handle that
-# is destroyed and handed out again while work is pending would share it
-# with that work; torch's pooled streams are never destroyed) --; None asks
+# Attention workspace argument: AUTO takes one cached per (device, stream, host
+# thread) -- a thread's calls on one stream are ordered, so they may share it (a
+# stream handle that is destroyed and handed out again while work is pending
+# would share it with that work; torch's pooled streams are never destroyed);
+# another thread's launches may come between a call's reset of the queues and
+# its attention, and a thread that got the number of one that has ended comes
+# after all of its calls --; None asks
 # for the one-workgroup-per-item launch; a device tensor of at least
 # rbs_attention_workspace_bytes() bytes is used as given.  Its contents do not
 # matter: every call resets the queues on its own stream.
@@ -185,7 +189,7 @@ _workspaces: dict = {}
 def attention_workspace(device, stream=None) -> torch.Tensor:
     device = torch.device(device)
     index = device.index if device.index is not None else torch.cuda.current_device()
-    key = (index, _stream(stream))
+    key = (index, _stream(stream), threading.get_ident())
     ws = _workspaces.get(key)
     if ws is None:
         n = int(load().rbs_attention_workspace_bytes())

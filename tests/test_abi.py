@@ -454,3 +454,29 @@ def test_binding_strides_come_from_the_tensors():
     shape.q_stride_tok = 384
     with pytest.raises(ValueError, match="disagrees"):
         rbs._lib._with_strides(shape, q=(128, 512))
+
+
+def test_threads_have_attention_workspaces_of_their_own(monkeypatch):
+    """A call resets its queues and then takes them: two launches, between which another thread's may come."""
+    import threading
+
+    import torch
+    from paper_2609_20971_amd import _lib as L
+    _lib()
+    empty, got = torch.empty, []
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: empty(*a, **dict(k, device="cpu")))
+    monkeypatch.setattr(L, "_workspaces", {})
+
+    def ask():
+        a = L.attention_workspace("cuda:0", 77)
+        assert L.attention_workspace("cuda:0", 77) is a and L.attention_workspace("cuda:0", 78) is not a
+        got.append(a)
+        here.wait()  # (both threads alive: their numbers differ)
+
+    here = threading.Barrier(2)
+    threads = [threading.Thread(target=ask) for _ in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert len(got) == 2 and got[0] is not got[1]

@@ -314,3 +314,36 @@ def test_persistent_attention_replays_from_a_graph():
         assert torch.equal(lse, ref[1]), f"replay {rep}: lse differs"
         eager = _attend(shape, Q, K, V, counts, indices, ws)  # the same workspace, between replays
         _assert_same(eager, ref, f"eager call after replay {rep}")
+
+
+def test_threads_that_attend_on_one_stream():
+    """Calls of two threads between each other, each with the binding's workspace."""
+    import threading
+
+    import torch
+    w = WORKLOADS["tiny-2k"].with_(name="queue-threads", seq_len=_past_the_line(128, 16), n_q_heads=16, n_kv_heads=4,
+                                   block_size=128, seed=77)
+    _say(f"[queue] two threads, N={w.seq_len}")
+    args = [_setup(w), _setup(w, dense=True)]
+    want = [_attend(*a, None) for a in args]
+    torch.cuda.synchronize()
+    got, failed, start = [[], []], [], threading.Barrier(2)
+
+    def calls(k):
+        try:
+            start.wait()
+            for _ in range(12):
+                got[k].append(_attend(*args[k], "auto"))
+        except Exception as e:  # (shown below: a thread's own traceback is not the test's)
+            failed.append(e)
+
+    threads = [threading.Thread(target=calls, args=(k,)) for k in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed, failed
+    for k in range(2):
+        assert len(got[k]) == 12
+        for i, one in enumerate(got[k]):
+            _assert_same(want[k], one, f"thread {k}, call {i}")
