@@ -983,3 +983,64 @@ def test_values_of_another_layout(n, hkv):
     cache, slots = _cache(2, hkv, page, False), torch.arange(n, dtype=torch.int32, device="cuda") + 3
     rbs.rbs_qk_norm_rope(rbs.make_shape(n, hq, hkv, 64), rbs.Rope(None), Q, K, slots, V=V2, cache=cache, slots=slots)
     assert torch.equal(cache.V[0, :, 3:3 + n], V) and torch.equal(cache.K[0, :, 3:3 + n], K)
+
+
+# ------------------------------------------------------------------ every key once
+
+LONG = [
+    # lengths, heads, page, fp8, with the log-sum-exp of the longest row known to a key
+    ([150001], 8, 1, 64, False),                          # parts of 512 workers, joined by single columns
+    ([150001], 8, 1, 64, True),
+    ([150001] + [700] * 30, 32, 4, 16, False),             # four columns a join
+    ([150001] + [700] * 30, 32, 4, 32, True),
+    ([700] * 9 + [40000] + [5] * 10, 64, 32, 128, False),  # fewer workers than rows: a record for each worker
+    ([700] * 9 + [40000] + [5] * 10, 64, 32, 128, True),
+    ([50000, 33, 49999], 34, 2, 256, False),               # 17 heads to a KV head
+]
+
+
+@pytest.mark.parametrize("k", range(len(LONG)))
+def test_every_key_counts_once(k):
+    """Keys of 0, so that every weight is 1: the log-sum-exp is ln n, to less than one key more or less would make,
+    and values that mark their tile of 32 (FP8: 64) keys in one element each, so that a tile (a part) that is lost or
+    counted twice shows in that element.
+
+    Sums of ones and of marks are whole numbers below 2^24, exact in fp32 in any order.  lse = log2(n) ln 2: the
+    logarithm to 2 of its steps (2^-19 each from 16 on), the product and its constant to half a step each: 4.1e-6
+    for 150001 keys (one key: 6.7e-6).  O = count / n: a division, a product and bf16, half a step of bf16 and 4 of
+    fp32."""
+    lens, hq, hkv, page, fp8 = LONG[k]
+    _say(f"[once] {len(lens)} rows, heads {hq}/{hkv}, page {page}, fp8 {fp8}")
+    tile, n = 64 if fp8 else 32, len(lens)
+    held = [-(-x // page) for x in lens]
+    pool = sum(held)
+    order = torch.randperm(pool, generator=_gen(670 + k)).to(torch.int32)
+    table = torch.full((n, max(held) + 1), -1, dtype=torch.int32)
+    at = 0
+    for row, h in enumerate(held):
+        table[row, :h] = order[at:at + h]
+        at += h
+    one = 0x38 if fp8 else 1.0
+    kind = torch.uint8 if fp8 else torch.bfloat16
+    K = torch.zeros(pool, hkv, page, D, dtype=kind, device="cuda")
+    V = torch.zeros_like(K)
+    want = torch.zeros(n, D, dtype=torch.float64)
+    for row, x in enumerate(lens):
+        j = torch.arange(x)
+        mark = (j // tile) % D
+        want[row] = torch.bincount(mark, minlength=D).double() / x
+        V[table[row, j // page].long().cuda(), :, (j % page).cuda(), mark.cuda()] = one
+    cache = rbs.PagedCache(K, V, torch.full((2 * hkv,), 448.0, device="cuda") if fp8 else None)
+    Q = torch.randn(n, hq, D, generator=_gen(k)).to(torch.bfloat16).cuda().transpose(0, 1)
+    lse = torch.full((hq, n), math.nan, device="cuda")
+    O = rbs.rbs_paged_decode(rbs.make_shape(n, hq, hkv, 64), Q, cache, table.cuda(), _ints(lens), lse=lse)
+    for row, x in enumerate(lens):
+        o = O[:, row].cpu().double()
+        err = (o - want[row]).abs()
+        assert bool((err <= want[row] * (R.HALF_BF16 + 4 * R.U32)).all()), f"row {row}: a tile's mark"
+        exact = math.log(x)
+        step = 2.0 ** -23 * 2.0 ** math.floor(math.log2(max(math.log2(x), 1e-30)))
+        tol = 2 * step * math.log(2) + 2 * R.U32 * exact
+        assert tol < 0.75 * (math.log(x + 1) - exact)
+        off = (lse[:, row].cpu().double() - exact).abs()
+        assert bool((off <= tol).all()), f"row {row}: {float(off.max()):.3g} of {tol:.3g}"
