@@ -1151,24 +1151,28 @@ def layer_sweep(args):
     }), flush=True)
 
 
-# Sources each kernel is built from, with the build script (it holds per-source
-# compiler flags); their joint hash identifies the kernel in the committed
-# rocprofv3 summaries.  The attention calls run the persistent (queue) kernels.
+# Sources each kernel is built from; their hash, with the compiler flags of the
+# first one, identifies the kernel in the committed rocprofv3 summaries.  The
+# attention calls run the persistent (queue) kernels.
 KERNEL_SOURCES = {
-    "stats_kernel": ["stats.hip", "rbs_device.hpp", "rbs_launch.hpp", "../build.py"],
-    "quantile_kernel": ["stats.hip", "rbs_device.hpp", "rbs_launch.hpp", "../build.py"],
-    "select_kernel": ["select.hip", "rbs_device.hpp", "rbs_launch.hpp", "../build.py"],
-    "attn_queue_kernel": ["attn.hip", "attend_block.hpp", "rbs_device.hpp", "rbs_launch.hpp", "../build.py"],
-    "attn_fp8_queue_kernel": ["fp8.hip", "attend_block.hpp", "rbs_device.hpp", "rbs_launch.hpp", "../build.py"],
+    "stats_kernel": ["stats.hip", "rbs_device.hpp", "rbs_launch.hpp"],
+    "quantile_kernel": ["stats.hip", "rbs_device.hpp", "rbs_launch.hpp"],
+    "select_kernel": ["select.hip", "rbs_device.hpp", "rbs_launch.hpp"],
+    "attn_queue_kernel": ["attn.hip", "attend_block.hpp", "rbs_device.hpp", "rbs_launch.hpp"],
+    "attn_fp8_queue_kernel": ["fp8.hip", "attend_block.hpp", "rbs_device.hpp", "rbs_launch.hpp"],
 }
 
 
 def source_sha(kernel: str) -> str:
     import hashlib
+
+    from paper_2609_20971_amd import build
     h = hashlib.sha256()
     for src in KERNEL_SOURCES[kernel]:
         with open(os.path.join(ROOT, "paper_2609_20971_amd", "csrc", src), "rb") as f:
             h.update(f.read())
+    flags = build.FLAGS[:build.FLAGS.index("-I")]  # (then the include folder, wherever the tree lies)
+    h.update("\n".join([*flags, *build.EXTRA_FLAGS.get(KERNEL_SOURCES[kernel][0], [])]).encode())
     return h.hexdigest()[:16]
 
 

@@ -104,3 +104,24 @@ def test_unit_rate_summary_reads_the_probe_cases(monkeypatch, tmp_path):
     assert r["mfma_cycles_with_softmax_mix"] == 47.5
     assert r["lds_read_bytes_per_clk_per_cu"] == {"ds_read_b128": 256.0, "ds_read_b64_tr_b16": 256.0}
     assert r["block_loop_mfma_busy"] == {"free_running": 0.75}
+
+
+def test_profile_summaries_are_of_the_current_kernels(monkeypatch):
+    """A summary's hash is that of its kernel's sources and flags; files that the kernel is not built from, such as
+    another source in the library's list, leave it as it is."""
+    from paper_2609_20971_amd import build
+    found = 0
+    for path in sorted((ROOT / "profiles").glob("*.md")):
+        lines = [x for x in path.read_text().splitlines() if x.startswith("source_sha: ")]
+        kernel = next((k for k in bench.KERNEL_SOURCES if path.name.startswith(k + "_")), None)
+        assert bool(lines) == (kernel is not None), path.name
+        if lines:
+            found += 1
+            assert lines == [f"source_sha: {bench.source_sha(kernel)}"], path.name
+    assert found >= len(bench.KERNEL_SOURCES)
+    before = bench.source_sha("select_kernel"), bench.source_sha("stats_kernel")
+    monkeypatch.setattr(build, "SOURCES", build.SOURCES + ["other.hip"])
+    monkeypatch.setitem(build.EXTRA_FLAGS, "other.hip", ["-O1"])
+    assert (bench.source_sha("select_kernel"), bench.source_sha("stats_kernel")) == before
+    monkeypatch.setitem(build.EXTRA_FLAGS, "select.hip", ["-O1"])
+    assert bench.source_sha("select_kernel") != before[0] and bench.source_sha("stats_kernel") == before[1]
