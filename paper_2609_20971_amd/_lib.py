@@ -172,6 +172,33 @@ def _stream(stream) -> int | None:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
 
+def _own(device: int, handle: int):
+    """With the stream of that handle current."""
+    return torch.cuda.stream(torch.cuda.ExternalStream(handle, device) if handle else torch.cuda.default_stream(device))
+
+
+def _made(device, stream, make, *args):
+    """make(*args): an output (a tensor, several, or an object that holds some) of a
+    call on `stream`, as that stream's memory: the current stream's may still be in
+    use there when the call writes, or again before it has.  The current stream is
+    noted as one that will use it as well."""
+    if stream is None:
+        return make(*args)
+    device = torch.device(device)
+    if device.type != "cuda":  # (refused by the call's checks)
+        return make(*args)
+    index, handle = device.index if device.index is not None else torch.cuda.current_device(), _stream(stream)
+    current = torch.cuda.current_stream(index)
+    if handle == current.cuda_stream:
+        return make(*args)
+    with _own(index, handle):
+        out = make(*args)
+    for t in (out,) if isinstance(out, torch.Tensor) else out if isinstance(out, tuple) else vars(out).values():
+        if isinstance(t, torch.Tensor):
+            t.record_stream(current)
+    return out
+
+
 # Attention workspace argument: AUTO takes one cached per (device, stream, host
 # thread) -- a thread's calls on one stream are ordered, so they may share it (a
 # stream handle that is destroyed and handed out again while work is pending
@@ -193,7 +220,7 @@ def attention_workspace(device, stream=None) -> torch.Tensor:
     ws = _workspaces.get(key)
     if ws is None:
         n = int(load().rbs_attention_workspace_bytes())
-        ws = torch.empty(n // 4, dtype=torch.int32, device=torch.device("cuda", index))
+        ws = _made(index, stream, lambda: torch.empty(n // 4, dtype=torch.int32, device=torch.device("cuda", index)))
         _workspaces[key] = ws
     return ws
 
@@ -393,7 +420,7 @@ def rbs_block_stats(shape: rbs_shape, K: torch.Tensor, stats: BlockStats | None 
     """Stage 1: centroids, radii, radius quantiles and beta of every key block."""
     kvs = _check_kv(shape, K)
     if stats is None:
-        stats = BlockStats.allocate(shape, K.device)
+        stats = _made(K.device, stream, BlockStats.allocate, shape, K.device)
     _on_gpu(("K", K), *_check_stats(shape, stats))
     sh = _with_strides(shape, kv=kvs)
     c = stats.as_c()
@@ -447,7 +474,7 @@ def rbs_block_box(shape: rbs_shape, K: torch.Tensor, box: BoxStats | None = None
     """Coordinate-wise key box of every block (centre, half-width)."""
     kvs = _check_kv(shape, K)
     if box is None:
-        box = BoxStats.allocate(shape, K.device)
+        box = _made(K.device, stream, BoxStats.allocate, shape, K.device)
     _on_gpu(("K", K), *_check_box(shape, box))
     sh = _with_strides(shape, kv=kvs)
     c = box.as_c()
@@ -465,7 +492,7 @@ def rbs_select_variant(shape: rbs_shape, Q: torch.Tensor, stats: BlockStats, sel
     if box is not None:
         named += _check_box(shape, box)
     if counts is None or indices is None:
-        counts, indices = allocate_lists(shape, Q.device)
+        counts, indices = _made(Q.device, stream, allocate_lists, shape, Q.device)
     _check_lists(shape, counts, indices)
     _on_gpu(("Q", Q), *named, ("counts", counts), ("indices", indices))
     sh = _with_strides(shape, q=qs)
@@ -490,7 +517,7 @@ def rbs_select(shape: rbs_shape, Q: torch.Tensor, stats: BlockStats, tau_base: f
     qs = _check_q(shape, Q)
     named = _check_stats(shape, stats, need_fp32=False)
     if counts is None or indices is None:
-        counts, indices = allocate_lists(shape, Q.device)
+        counts, indices = _made(Q.device, stream, allocate_lists, shape, Q.device)
     _check_lists(shape, counts, indices)
     _on_gpu(("Q", Q), *named, ("counts", counts), ("indices", indices))
     sh = _with_strides(shape, q=qs)
@@ -512,7 +539,7 @@ def rbs_sparse_prefill(shape: rbs_shape, Q, K, V, counts, indices, softmax_scale
     _check_lse(shape, lse)
     _on_gpu(("Q", Q), ("K", K), ("V", V), ("counts", counts), ("indices", indices), ("O", O), ("lse", lse))
     if O is None:
-        O = _like_q(Q)
+        O = _made(Q.device, stream, _like_q, Q)
     ws = _workspace(workspace, Q.device, stream)
     sh = _with_strides(shape, q=qs, kv=kvs)
     _check("rbs_sparse_prefill", load().rbs_sparse_prefill(ctypes.byref(sh), _ptr(Q), _ptr(K), _ptr(V),
@@ -546,7 +573,7 @@ def rbs_select_attend(shape: rbs_shape, Q, K, V, stats: BlockStats, tau_base: fl
     kvs = _check_kv(shape, K, V)
     named = _check_stats(shape, stats, need_fp32=False)
     if counts is None or indices is None:
-        counts, indices = allocate_lists(shape, Q.device)
+        counts, indices = _made(Q.device, stream, allocate_lists, shape, Q.device)
     _check_lists(shape, counts, indices)
     if O is not None:
         _check_out(O, Q)
@@ -554,7 +581,7 @@ def rbs_select_attend(shape: rbs_shape, Q, K, V, stats: BlockStats, tau_base: fl
     _on_gpu(("Q", Q), ("K", K), ("V", V), *named, ("counts", counts), ("indices", indices), ("O", O),
             ("lse", lse))
     if O is None:
-        O = _like_q(Q)
+        O = _made(Q.device, stream, _like_q, Q)
     c = stats.as_c()
     ws = _workspace(workspace, Q.device, stream)
     sh = _with_strides(shape, q=qs, kv=kvs)
@@ -568,7 +595,7 @@ def rbs_select_attend(shape: rbs_shape, Q, K, V, stats: BlockStats, tau_base: fl
 def rbs_dense_indices(shape: rbs_shape, counts=None, indices=None, stream=None, device="cuda"):
     """Full causal lists: the dense path through the same attention kernel."""
     if counts is None or indices is None:
-        counts, indices = allocate_lists(shape, device)
+        counts, indices = _made(device, stream, allocate_lists, shape, device)
     _check_lists(shape, counts, indices)
     _on_gpu(("counts", counts), ("indices", indices))
     _check("rbs_dense_indices", load().rbs_dense_indices(ctypes.byref(shape), _ptr(counts), _ptr(indices),
@@ -648,7 +675,7 @@ def rbs_block_stats_varlen(shape: rbs_shape, batch: Batch, K: torch.Tensor, stat
     """Stage 1 for every sequence of a batch (one launch)."""
     kvs = _check_kv(shape, K)
     if stats is None:
-        stats = allocate_stats_varlen(shape, batch, K.device)
+        stats = _made(K.device, stream, allocate_stats_varlen, shape, batch, K.device)
     _on_gpu(("K", K), *_check_stats(shape, stats, n_blocks_total=rbs_varlen_blocks(shape, batch),
                                     n_seqs=batch.n_seqs, summary_bytes=rbs_varlen_summary_bytes(shape, batch)))
     sh = _with_strides(shape, kv=kvs)
@@ -667,7 +694,7 @@ def rbs_select_varlen(shape: rbs_shape, batch: Batch, Q: torch.Tensor, stats: Bl
     named = _check_stats(shape, stats, n_blocks_total=m, n_seqs=batch.n_seqs,
                          summary_bytes=rbs_varlen_summary_bytes(shape, batch), need_fp32=False)
     if counts is None or indices is None:
-        counts, indices = allocate_lists_varlen(shape, batch, Q.device)
+        counts, indices = _made(Q.device, stream, allocate_lists_varlen, shape, batch, Q.device)
     _check_lists(shape, counts, indices, n_blocks_total=m, capacity=cap)
     _on_gpu(("Q", Q), *named, ("counts", counts), ("indices", indices))
     sh = _with_strides(shape, q=qs)
@@ -690,7 +717,7 @@ def rbs_sparse_prefill_varlen(shape: rbs_shape, batch: Batch, Q, K, V, counts, i
     _check_lse(shape, lse)
     _on_gpu(("Q", Q), ("K", K), ("V", V), ("counts", counts), ("indices", indices), ("O", O), ("lse", lse))
     if O is None:
-        O = _like_q(Q)
+        O = _made(Q.device, stream, _like_q, Q)
     ws = _workspace(workspace, Q.device, stream)
     sh = _with_strides(shape, q=qs, kv=kvs)
     _check("rbs_sparse_prefill_varlen", load().rbs_sparse_prefill_varlen(
@@ -703,7 +730,7 @@ def rbs_dense_indices_varlen(shape: rbs_shape, batch: Batch, counts=None, indice
                              device="cuda"):
     """Full causal lists of every sequence of a batch."""
     if counts is None or indices is None:
-        counts, indices = allocate_lists_varlen(shape, batch, device)
+        counts, indices = _made(device, stream, allocate_lists_varlen, shape, batch, device)
     _check_lists(shape, counts, indices, n_blocks_total=rbs_varlen_blocks(shape, batch),
                  capacity=rbs_varlen_index_capacity(shape, batch))
     _on_gpu(("counts", counts), ("indices", indices))
@@ -773,7 +800,7 @@ def rbs_fp8_pack(shape: rbs_shape, Q, K, V, f8: Fp8Inputs, stream=None) -> Fp8In
 def rbs_fp8_prepare(shape: rbs_shape, Q, K, V, f8: Fp8Inputs | None = None, stream=None) -> Fp8Inputs:
     """amax then pack: the E4M3 inputs of rbs_sparse_prefill_fp8."""
     if f8 is None:
-        f8 = allocate_fp8(shape, Q.device)
+        f8 = _made(Q.device, stream, allocate_fp8, shape, Q.device)
     rbs_fp8_amax(shape, Q, K, V, f8.amax, stream)
     return rbs_fp8_pack(shape, Q, K, V, f8, stream)
 
@@ -784,8 +811,8 @@ def rbs_sparse_prefill_fp8(shape: rbs_shape, f8: Fp8Inputs, counts, indices, sof
     named = _check_fp8(shape, f8)
     _check_lists(shape, counts, indices)
     if O is None:
-        O = torch.empty((shape.n_q_heads, shape.n_tokens, shape.head_dim), dtype=torch.bfloat16,
-                        device=f8.Q8.device)
+        O = _made(f8.Q8.device, stream, lambda: torch.empty(
+            (shape.n_q_heads, shape.n_tokens, shape.head_dim), dtype=torch.bfloat16, device=f8.Q8.device))
     qs = _heads_tokens("O", O, shape.n_q_heads, shape.n_tokens, shape.head_dim)
     _check_lse(shape, lse)
     _on_gpu(*named, ("counts", counts), ("indices", indices), ("O", O), ("lse", lse))

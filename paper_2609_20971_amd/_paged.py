@@ -99,24 +99,6 @@ def _on(device: int, stream, call, *args):
         return call(*args, _handle(device, stream))
 
 
-def _own(device: int, handle: int):
-    """With the stream of that handle current."""
-    return torch.cuda.stream(torch.cuda.ExternalStream(handle, device) if handle else torch.cuda.default_stream(device))
-
-
-def _made(device: int, stream, make, *args):
-    """make(*args): an output (a tensor or a PageStep) of a call on `stream`, as that
-    stream's memory, which the current one will use as well."""
-    if stream is None or _handle(device, stream) == torch._C._cuda_getCurrentRawStream(device):
-        return make(*args)
-    current = torch.cuda.current_stream(device)
-    with _own(device, _handle(device, stream)):
-        out = make(*args)
-    for t in (out.cu_tokens, out.positions, out.slots, out.status) if isinstance(out, PageStep) else (out,):
-        t.record_stream(current)
-    return out
-
-
 def _elsewhere(dev: int, *tensors) -> bool:
     """Whether one of the tensors (None skipped) is not on GPU dev, or dev is none."""
     for x in tensors:
@@ -293,7 +275,7 @@ def rbs_pages_extend(pages: Pages, new_tokens=None, max_tokens: int | None = Non
         if new_tokens.get_device() != pages.device:
             L._on_gpu(("page_table", pages.page_table), ("new_tokens", new_tokens))
     if step is None:
-        step = _made(pages.device, stream, PageStep.allocate, pages, pages.n_rows if max_tokens is None else max_tokens)
+        step = L._made(pages.device, stream, PageStep.allocate, pages, pages.n_rows if max_tokens is None else max_tokens)
     else:
         if not isinstance(step, PageStep):
             raise ValueError("step must be a PageStep")
@@ -319,7 +301,7 @@ def rbs_pages_release(pages: Pages, released, status=None, stream=None) -> torch
         L._check_tensor("status", status, torch.int32, (1,))
     L._on_gpu(("page_table", pages.page_table), ("released", released), ("status", status))
     if status is None:
-        status = _made(pages.device, stream, pages.n_free.new_empty, 1)
+        status = L._made(pages.device, stream, pages.n_free.new_empty, 1)
     L._check("rbs_pages_release", _on(pages.device, stream, L.load().rbs_pages_release, pages.c, released.data_ptr(),
                                       *pages.state, status.data_ptr()))
     return status
@@ -421,9 +403,9 @@ def rbs_qk_norm_rope(shape: L.rbs_shape, rope: Rope, Q, K, positions, V=None, ca
         raise ValueError(f"rope is on cuda:{rope.device}, the other arguments on cuda:{dev}")
     if Q_out is None:
         # (Q's order of strides, without the gaps of a fused projection's view.)
-        Q_out = _made(dev, stream, torch.empty_like, Q)
+        Q_out = L._made(dev, stream, torch.empty_like, Q)
     if K_out is None and keep_k:
-        K_out = _made(dev, stream, torch.empty_like, K)
+        K_out = L._made(dev, stream, torch.empty_like, K)
     sh = _strided(shape, qs, ks)
     out = L.rbs_shape(n, hq, hkv, d, shape.block_size, *Q_out.stride()[:2],
                       *(ks if K_out is None else K_out.stride()[:2]))
@@ -448,7 +430,7 @@ def _auto_workspace(device: int, handle: int) -> torch.Tensor:
     graphs that were captured on one stream may run side by side."""
     if handle != torch._C._cuda_getCurrentRawStream(device):
         # Made on the stream that uses it, whose order its memory's next use has to follow.
-        with _own(device, handle):
+        with L._own(device, handle):
             return _workspace_of(device, handle)
     return _workspace_of(device, handle)
 
@@ -491,9 +473,9 @@ def rbs_paged_decode(shape: L.rbs_shape, Q, cache: PagedCache, page_table, seq_l
         L._on_gpu(("cache.K", cache.K), ("Q", Q), ("page_table", page_table), ("seq_lens", seq_lens), ("O", O),
                   ("lse", lse), ("cu_tokens", cu_tokens))
     if O is None:
-        O = _made(dev, stream, torch.empty_like, Q)
+        O = L._made(dev, stream, torch.empty_like, Q)
         if O.stride() != Q.stride():
-            O = _made(dev, stream, L._like_q, Q)
+            O = L._made(dev, stream, L._like_q, Q)
     if isinstance(workspace, str):
         if workspace != L.AUTO:
             raise ValueError(f"workspace must be AUTO or a tensor, not {workspace!r}")

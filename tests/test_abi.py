@@ -466,6 +466,7 @@ def test_threads_have_attention_workspaces_of_their_own(monkeypatch):
     empty, got = torch.empty, []
     monkeypatch.setattr(torch, "empty", lambda *a, **k: empty(*a, **dict(k, device="cpu")))
     monkeypatch.setattr(L, "_workspaces", {})
+    monkeypatch.setattr(L, "_made", lambda device, stream, make: make())  # (on no stream: there is no GPU)
 
     def ask():
         a = L.attention_workspace("cuda:0", 77)
@@ -473,7 +474,7 @@ def test_threads_have_attention_workspaces_of_their_own(monkeypatch):
         got.append(a)
         here.wait()  # (both threads alive: their numbers differ)
 
-    here = threading.Barrier(2)
+    here = threading.Barrier(2, timeout=30)
     threads = [threading.Thread(target=ask) for _ in range(2)]
     for t in threads:
         t.start()
