@@ -457,7 +457,8 @@ enum {
  *               n_free are passed on unchanged, cu_tokens is 0 and positions
  *               and slots are -1
  * seq_lens_out may be seq_lens and n_free_out may be n_free (one extra launch
- * then, where max_tokens is large); no other two buffers may overlap.
+ * then, where max_tokens is large, so that host threads that extend the same
+ * pages have to take turns); no other two buffers may overlap.
  * All int32, device memory.  free_pages is only read.
  * Errors: RBS_ERR_NULL, RBS_ERR_SHAPE (counts and sizes), RBS_ERR_UNSUPPORTED
  * (page size), RBS_ERR_ALIGN.

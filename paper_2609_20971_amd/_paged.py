@@ -187,7 +187,8 @@ class Pages:
     """The bookkeeping of a cache's pages (int32 device tensors): the page table
     [n_rows][max_pages], the stack of free pages [n_pages] and how many it
     holds [1], the rows' lengths [n_rows] (negative: unused; a request is
-    admitted to a row by setting its length to 0)."""
+    admitted to a row by setting its length to 0).  Calls that change them are
+    ordered by the caller: threads that share a Pages take turns."""
     page_table: torch.Tensor
     free_pages: torch.Tensor
     n_free: torch.Tensor
@@ -343,7 +344,8 @@ def rope_frequencies(rot_dim: int = 128, base: float = 1.0e6, scaling: str | Non
       "parts"   by how many turns a pair makes over the original context: at
                 least `fast` turns, kept; at most `slow`, divided by scale; in
                 between, interpolated linearly over the pair's index; factor
-                0.1 ln(scale) + 1 on queries and keys each
+                0.1 ln(scale) + 1 on queries and keys each (YaRN, Peng et al. 2023,
+                Sec. 3.2 and 3.4, with whole indices as the ends of the interpolation)
     """
     if rot_dim < 2 or rot_dim % 2 != 0 or not base > 1 or not scale >= 1:
         raise ValueError("rot_dim must be even and positive, base past 1, scale at least 1")
