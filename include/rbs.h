@@ -29,6 +29,8 @@
  *   rbs_qk_norm_rope    per-head norm and rotary position of queries and keys
  *                       (the form the stages above take them in), keys and
  *                       values put into the cache in the same pass
+ *   rbs_cache_write,    keys and values quantised into the cache (FP8, 4 bits),
+ *   rbs_cache_read      and rows of it as bf16 again
  *   rbs_paged_decode,   attention of one new token per row over the cache, the
  *   rbs_paged_decode_packed   queries by row or packed as rbs_pages_extend packs them
  *
@@ -389,7 +391,7 @@ int rbs_dense_indices_varlen(const rbs_shape* shape, const rbs_batch* batch, int
  * Row lengths live on the GPU (seq_lens): 0 is an empty row, a negative length
  * an unused one, which every call leaves as it is.
  */
-enum { RBS_CACHE_BF16 = 0, RBS_CACHE_FP8 = 1 };
+enum { RBS_CACHE_BF16 = 0, RBS_CACHE_FP8 = 1, RBS_CACHE_FP4 = 4 };
 
 #define RBS_MAX_ROWS 4096 /* rows of a page table */
 
@@ -405,6 +407,15 @@ enum { RBS_CACHE_BF16 = 0, RBS_CACHE_FP8 = 1 };
  *                   code = E4M3(x * (448 / amax)), values past amax saturating;
  *                   amax fp32 [2 H_kv], K heads then V heads (the tail of
  *                   rbs_fp8_amax's array, kept while the cache is in use; 0: scale 1)
+ *   RBS_CACHE_FP4   E2M1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign), two to a
+ *                   byte, the even element low, over a power of two for each 32
+ *                   elements of a row: element x (as counted by the strides, which
+ *                   are multiples of 128 here) in byte x / 2 of K or V, the scale of
+ *                   elements x .. x + 31 in byte x / 32 of K_scale or V_scale, b for
+ *                   2^(b - 127), 255 for 32 NaN.  Written from bf16: the least power
+ *                   of two (from 2^-126) that takes the 32's largest magnitude under
+ *                   7, and the nearest code (ties to even); a NaN or an infinity
+ *                   makes its 32 elements NaN.  68 bytes a row of 128.
  */
 typedef struct {
   int32_t n_pages;     /* n_pages * page_size < 2^31 */
@@ -418,6 +429,8 @@ typedef struct {
   void* K;
   void* V;
   const float* amax;   /* RBS_CACHE_FP8 only */
+  void* K_scale;       /* RBS_CACHE_FP4 only (not read otherwise) */
+  void* V_scale;
 } rbs_cache;
 
 /*
@@ -506,7 +519,7 @@ typedef struct {
  *   to bf16.  Q_out may be Q and K_out may be K with the same strides;
  *   otherwise outputs and inputs do not overlap.  K_out may be NULL.
  *   cache NULL: no cache.  Otherwise the key (rounded to the cache's type from
- *   fp32) and V's row go to slots[t] (int32 [n_tokens]); a slot outside the
+ *   fp32; FP4: from bf16, as K_out has it) and V's row go to slots[t] (int32 [n_tokens]); a slot outside the
  *   cache (-1) writes none.  Tokens with a slot of their own each.
  * Tokens with a negative position are left out: nothing of theirs is written.
  * V and slots are read only with a cache.
@@ -514,6 +527,30 @@ typedef struct {
 int rbs_qk_norm_rope(const rbs_shape* in, const rbs_shape* out, const rbs_rope* rope, const void* Q, const void* K,
                      const void* V, const int32_t* positions, void* Q_out, void* K_out, const rbs_cache* cache,
                      const int32_t* slots, void* stream);
+
+/*
+ * Keys and values into the cache as they are: token t's rows of K and V (bf16) go
+ * to slots[t] (int32 [n_tokens]) in the cache's type; a slot outside the cache
+ * (-1) writes none.  Tokens with a slot of their own each.
+ * shape: sizes (n_tokens up to RBS_MAX_NEW_TOKENS, H_kv; H_q a multiple of it up to
+ * 512, any block_size) and K's strides (kv_*).  v_shape: NULL, or a shape of the
+ * same sizes with V's strides (kv_*).
+ */
+int rbs_cache_write(const rbs_shape* shape, const rbs_shape* v_shape, const void* K, const void* V,
+                    const rbs_cache* cache, const int32_t* slots, void* stream);
+
+/*
+ * Cached keys and values as bf16, rows packed one after another: token t of
+ * cu_tokens[s] .. cu_tokens[s + 1] - 1 (int32 [n_rows + 1], from 0, ascending) is row
+ * s's at position starts[s] + t - cu_tokens[s] (int32 [n_rows], any alignment to
+ * pages; NULL: from 0).  K, V (head, token, dimension) with the strides kv_* of
+ * shape, whose n_tokens (up to RBS_MAX_NEW_TOKENS) tokens they hold.  BF16 and FP4
+ * values come exactly, FP8 ones rounded once.  Tokens that are no row's, and
+ * positions outside the row's page table, are left as they were.  page_table int32
+ * [n_rows][max_pages], trusted like rbs_paged_decode's; lengths are not looked at.
+ */
+int rbs_cache_read(const rbs_shape* shape, const rbs_cache* cache, const int32_t* cu_tokens, const int32_t* starts,
+                   int32_t n_rows, const int32_t* page_table, int32_t max_pages, void* K, void* V, void* stream);
 
 /* Workspace of rbs_paged_decode and _packed, 16-byte aligned; contents on entry are ignored.
  * Calls that share one must be ordered, like those that share an output: a

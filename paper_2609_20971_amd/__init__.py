@@ -71,6 +71,7 @@ from ._lib import (  # noqa: F401
 )
 from ._paged import (  # noqa: F401
     RBS_CACHE_BF16,
+    RBS_CACHE_FP4,
     RBS_CACHE_FP8,
     RBS_MAX_ROWS,
     RBS_PAGES_FEW,
@@ -82,6 +83,8 @@ from ._paged import (  # noqa: F401
     PageStep,
     Rope,
     rbs_cache,
+    rbs_cache_read,
+    rbs_cache_write,
     rbs_decode_workspace_bytes,
     rbs_paged_decode,
     rbs_pages,

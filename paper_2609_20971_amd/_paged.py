@@ -23,7 +23,7 @@ import torch
 
 from . import _lib as L
 
-RBS_CACHE_BF16, RBS_CACHE_FP8 = 0, 1
+RBS_CACHE_BF16, RBS_CACHE_FP8, RBS_CACHE_FP4 = 0, 1, 4
 RBS_PAGES_FEW, RBS_PAGES_ROW, RBS_PAGES_TOKENS, RBS_PAGES_STACK = 1, 2, 4, 8
 RBS_MAX_ROWS = 4096
 
@@ -41,6 +41,8 @@ class rbs_cache(ctypes.Structure):
         ("K", ctypes.c_void_p),
         ("V", ctypes.c_void_p),
         ("amax", ctypes.c_void_p),
+        ("K_scale", ctypes.c_void_p),
+        ("V_scale", ctypes.c_void_p),
     ]
 
 
@@ -77,6 +79,10 @@ def declare(lib):
     lib.rbs_pages_release.restype = ctypes.c_int
     lib.rbs_qk_norm_rope.argtypes = [SP, SP, ctypes.POINTER(rbs_rope), P, P, P, P, P, P, ctypes.POINTER(rbs_cache), P, P]
     lib.rbs_qk_norm_rope.restype = ctypes.c_int
+    lib.rbs_cache_write.argtypes = [SP, SP, P, P, ctypes.POINTER(rbs_cache), P, P]
+    lib.rbs_cache_write.restype = ctypes.c_int
+    lib.rbs_cache_read.argtypes = [SP, ctypes.POINTER(rbs_cache), P, P, I32, P, I32, P, P, P]
+    lib.rbs_cache_read.restype = ctypes.c_int
     lib.rbs_decode_workspace_bytes.argtypes = []
     lib.rbs_decode_workspace_bytes.restype = SZ
     lib.rbs_paged_decode.argtypes = [SP, ctypes.POINTER(rbs_cache), P, P, I32, P, F32, P, P, P, P]
@@ -140,41 +146,61 @@ class PagedCache:
     """Keys and values of a paged cache: K and V [n_pages][H_kv][page_size][d]
     views of any strides the library takes (for [n_pages][page_size][H_kv][d]
     buffers, their transpose(1, 2)), bf16, or uint8 E4M3 codes with amax (fp32
-    [2 H_kv]: the magnitudes of each K head, then each V head, that map to 448)."""
+    [2 H_kv]: the magnitudes of each K head, then each V head, that map to 448), or
+    uint8 E2M1 codes [n_pages][H_kv][page_size][d / 2] with K_scale and V_scale
+    (uint8 [n_pages][H_kv][page_size][d / 32], the same layout as the codes)."""
     K: torch.Tensor
     V: torch.Tensor
     amax: torch.Tensor | None = None
+    K_scale: torch.Tensor | None = None
+    V_scale: torch.Tensor | None = None
     c: rbs_cache = field(init=False, repr=False)
     device: int = field(init=False, repr=False)
 
     def __post_init__(self):
-        K, V = self.K, self.V
+        K, V, fp4 = self.K, self.V, self.K_scale is not None or self.V_scale is not None
         if not isinstance(K, torch.Tensor) or K.dim() != 4:
             raise ValueError("K must be a [n_pages][H_kv][page_size][d] tensor")
-        dtype = torch.bfloat16 if self.amax is None else torch.uint8
+        if fp4 and self.amax is not None:
+            raise ValueError("a cache has amax (FP8) or scales (FP4), not both")
+        dtype = torch.bfloat16 if self.amax is None and not fp4 else torch.uint8
         L._check_tensor("K", K, dtype, tuple(K.shape), contiguous=False)
         L._check_tensor("V", V, dtype, tuple(K.shape), contiguous=False)
         if V.stride() != K.stride():
             raise ValueError(f"V strides {V.stride()} differ from K strides {K.stride()}; the library takes one set")
         n_pages, hkv, page_size, d = K.shape
+        d *= 2 if fp4 else 1
         if self.amax is not None:
             L._check_tensor("amax", self.amax, torch.float32, (2 * hkv,))
-        s = K.stride()
+        s = tuple(x * (2 if fp4 else 1) for x in K.stride())  # in elements
         if K.numel() == 0 or min(s[i] for i in range(3) if K.shape[i] > 1 or i == 2) < d:
-            raise ValueError(f"K's places overlap or it holds none (shape {tuple(K.shape)}, strides {s})")
-        dev = L._on_gpu(("K", K), ("V", V), ("amax", self.amax))
+            raise ValueError(f"K's places overlap or it holds none (shape {tuple(K.shape)}, strides {K.stride()})")
+        if fp4:
+            for name in ("K_scale", "V_scale"):
+                t = getattr(self, name)
+                L._check_tensor(name, t, torch.uint8, (n_pages, hkv, page_size, d // 32), contiguous=False)
+                if any(32 * t.stride(i) != s[i] for i in range(3) if t.shape[i] > 1 or i == 2):
+                    raise ValueError(f"{name} strides {t.stride()} are not 1/16 of K's {K.stride()}")
+        dev = L._on_gpu(("K", K), ("V", V), ("amax", self.amax), ("K_scale", self.K_scale), ("V_scale", self.V_scale))
         # A dimension of one page or head has no stride of its own.
         page, head = (s[i] if K.shape[i] > 1 else n for i, n in ((0, hkv * page_size * d), (1, page_size * d)))
-        c = rbs_cache(n_pages, page_size, hkv, d, RBS_CACHE_BF16 if self.amax is None else RBS_CACHE_FP8, page, head,
-                      s[2], K.data_ptr(), V.data_ptr(), L._ptr(self.amax))
+        format = RBS_CACHE_FP4 if fp4 else RBS_CACHE_BF16 if self.amax is None else RBS_CACHE_FP8
+        c = rbs_cache(n_pages, page_size, hkv, d, format, page, head, s[2], K.data_ptr(), V.data_ptr(),
+                      L._ptr(self.amax), L._ptr(self.K_scale), L._ptr(self.V_scale))
         object.__setattr__(self, "c", c)
         object.__setattr__(self, "device", dev)
 
     @classmethod
     def allocate(cls, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int = 128, amax=None,
-                 device="cuda") -> "PagedCache":
+                 device="cuda", fp4: bool = False) -> "PagedCache":
+        """bf16; with amax FP8; with fp4 4 bits."""
+        shape = (n_pages, n_kv_heads, page_size)
+        if fp4:
+            u8 = dict(dtype=torch.uint8, device=device)
+            K, K_scale = torch.empty((*shape, head_dim // 2), **u8), torch.empty((*shape, head_dim // 32), **u8)
+            return cls(K, torch.empty_like(K), amax, K_scale, torch.empty_like(K_scale))
         dtype = torch.bfloat16 if amax is None else torch.uint8
-        K = torch.empty((n_pages, n_kv_heads, page_size, head_dim), dtype=dtype, device=device)
+        K = torch.empty((*shape, head_dim), dtype=dtype, device=device)
         return cls(K, torch.empty_like(K), amax)
 
     @property
@@ -415,6 +441,74 @@ def rbs_qk_norm_rope(shape: L.rbs_shape, rope: Rope, Q, K, positions, V=None, ca
                                      K.data_ptr(), L._ptr(V), positions.data_ptr(), Q_out.data_ptr(), L._ptr(K_out),
                                      None if cache is None else cache.c, L._ptr(slots)))
     return Q_out, K_out
+
+
+def rbs_cache_write(shape: L.rbs_shape, K, V, cache: PagedCache, slots, stream=None) -> PagedCache:
+    """Rows of K and V (bf16, (head, token, dimension) tensors of any strides) into the
+    cache at `slots`, in its type; returns the cache."""
+    sizes = (shape.n_kv_heads, shape.n_tokens, shape.head_dim)
+    ks, vs = _rows("K", K, sizes), _rows("V", V, sizes)
+    if not isinstance(cache, PagedCache):
+        raise ValueError("cache must be a PagedCache")
+    _int_row("slots", slots, shape.n_tokens)
+    dev = K.get_device()
+    if cache.device != dev or _elsewhere(dev, V, slots):
+        L._on_gpu(("cache.K", cache.K), ("K", K), ("V", V), ("slots", slots))
+    v_shape = None
+    if vs != ks:
+        v_shape = L.rbs_shape(shape.n_tokens, shape.n_q_heads, shape.n_kv_heads, shape.head_dim, shape.block_size, 0, 0, *vs)
+    L._check("rbs_cache_write", _on(dev, stream, L.load().rbs_cache_write, _kv_strided(shape, ks), v_shape, K.data_ptr(),
+                                    V.data_ptr(), cache.c, slots.data_ptr()))
+    return cache
+
+
+def rbs_cache_read(shape: L.rbs_shape, cache: PagedCache, page_table, cu_tokens, starts=None, K=None, V=None,
+                   stream=None):
+    """Cached rows as bf16, packed: tokens cu_tokens[row] .. of the (head, token, dimension)
+    tensors K and V are the row's from position starts[row] on (None: 0).  Returns (K, V), by default
+    new ones, dense; tokens that are no row's are left as they were."""
+    hkv, n, d = shape.n_kv_heads, shape.n_tokens, shape.head_dim
+    if not isinstance(cache, PagedCache):
+        raise ValueError("cache must be a PagedCache")
+    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+        raise ValueError("page_table must be an [n_rows][max_pages] tensor")
+    rows = page_table.shape[0]
+    L._check_tensor("page_table", page_table, torch.int32, (rows, page_table.shape[1]))
+    _int_row("cu_tokens", cu_tokens, rows + 1)
+    if starts is not None:
+        _int_row("starts", starts, rows)
+    if (K is None) != (V is None):
+        raise ValueError("K and V are given together or not at all")
+    dev = cache.device
+    if K is None:
+        if _elsewhere(dev, page_table, cu_tokens, starts):
+            L._on_gpu(("cache.K", cache.K), ("page_table", page_table), ("cu_tokens", cu_tokens), ("starts", starts))
+        K, V = L._made(dev, stream, _pair, cache.K, (hkv, n, d))
+        strides = (n * d, d)
+    else:
+        strides = _rows("K", K, (hkv, n, d))
+        vs = _rows("V", V, (hkv, n, d))
+        if vs != strides and ((vs[0] != strides[0] and hkv > 1) or (vs[1] != strides[1] and n > 1)):
+            raise ValueError(f"V strides {vs} differ from K strides {strides}; the library takes one pair")
+        if _elsewhere(dev, K, V, page_table, cu_tokens, starts):
+            L._on_gpu(("cache.K", cache.K), ("K", K), ("V", V), ("page_table", page_table), ("cu_tokens", cu_tokens),
+                      ("starts", starts))
+    L._check("rbs_cache_read", _on(dev, stream, L.load().rbs_cache_read, _kv_strided(shape, strides), cache.c,
+                                   cu_tokens.data_ptr(), L._ptr(starts), rows, page_table.data_ptr(),
+                                   page_table.shape[1], K.data_ptr(), V.data_ptr()))
+    return K, V
+
+
+def _pair(like, sizes):
+    K = torch.empty(sizes, dtype=torch.bfloat16, device=like.device)
+    return K, torch.empty_like(K)
+
+
+def _kv_strided(shape, kv):
+    """As _strided, for calls that take no Q."""
+    if shape.kv_stride_head == shape.kv_stride_tok == 0:
+        return L.rbs_shape(shape.n_tokens, shape.n_q_heads, shape.n_kv_heads, shape.head_dim, shape.block_size, 0, 0, *kv)
+    return L._with_strides(shape, kv=kv)
 
 
 _decode_workspaces = threading.local()  # attributes of its own for every thread

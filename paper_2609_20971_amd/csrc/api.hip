@@ -176,23 +176,32 @@ int check_cache(const rbs_cache* c, rbs::CacheView* out) {
   if (c == nullptr) return RBS_ERR_NULL;
   const int shift = page_shift_of(c->page_size);
   if (c->head_dim != 128 || shift < 0) return RBS_ERR_UNSUPPORTED;
-  if (c->format != RBS_CACHE_BF16 && c->format != RBS_CACHE_FP8) return RBS_ERR_ARG;
+  if (c->format != RBS_CACHE_BF16 && c->format != RBS_CACHE_FP8 && c->format != RBS_CACHE_FP4) return RBS_ERR_ARG;
+  static_assert(RBS_CACHE_BF16 == rbs::kCacheBf16 && RBS_CACHE_FP8 == rbs::kCacheFp8 &&
+                    RBS_CACHE_FP4 == rbs::kCacheFp4, "cache formats");
+  const bool fp4 = c->format == RBS_CACHE_FP4;
   if (c->n_kv_heads < 1 || c->n_pages < 1 || c->n_pages > (INT32_MAX >> shift)) return RBS_ERR_SHAPE;
   rbs::CacheView v{};
   v.tok = c->stride_tok == 0 ? 128 : c->stride_tok;
   v.head = c->stride_head == 0 ? (int64_t)c->page_size * 128 : c->stride_head;
   v.page = c->stride_page == 0 ? (int64_t)c->n_kv_heads * c->page_size * 128 : c->stride_page;
-  if (v.tok < 128 || v.head < 128 || v.page < 128 || v.tok % 16 != 0 || v.head % 16 != 0 || v.page % 16 != 0)
+  const int unit = fp4 ? 128 : 16;  // (a row's four scales are one word)
+  if (v.tok < 128 || v.head < 128 || v.page < 128 || v.tok % unit != 0 || v.head % unit != 0 || v.page % unit != 0)
     return RBS_ERR_SHAPE;
   // The largest offset (in bytes) has to fit 63 bits, and a place's inside its page the kernels' 31.
   if (v.tok > INT32_MAX / 1024 || v.head > (int64_t(1) << 40) || v.page > (int64_t(1) << 60) / c->n_pages)
     return RBS_ERR_SHAPE;
   if (c->K == nullptr || c->V == nullptr || (c->format == RBS_CACHE_FP8 && c->amax == nullptr)) return RBS_ERR_NULL;
-  if (!aligned16(c->K) || !aligned16(c->V) || (c->format == RBS_CACHE_FP8 && !aligned16(c->amax)))
+  if (fp4 && (c->K_scale == nullptr || c->V_scale == nullptr)) return RBS_ERR_NULL;
+  if (!aligned16(c->K) || !aligned16(c->V) || (c->format == RBS_CACHE_FP8 && !aligned16(c->amax)) ||
+      (fp4 && (!aligned16(c->K_scale) || !aligned16(c->V_scale))))
     return RBS_ERR_ALIGN;
+  v.format = c->format;
   v.K = c->K;
   v.V = c->V;
   v.amax = c->format == RBS_CACHE_FP8 ? c->amax : nullptr;
+  v.K_scale = fp4 ? c->K_scale : nullptr;
+  v.V_scale = fp4 ? c->V_scale : nullptr;
   v.n_pages = c->n_pages;
   v.page_shift = shift;
   *out = v;
@@ -856,6 +865,65 @@ int rbs_qk_norm_rope(const rbs_shape* in, const rbs_shape* out, const rbs_rope* 
   a.Q_out = static_cast<uint16_t*>(Q_out);
   a.K_out = static_cast<uint16_t*>(K_out);
   return finish(rbs::launch_qk_norm_rope(a, static_cast<hipStream_t>(stream)), stream);
+}
+
+int rbs_cache_write(const rbs_shape* shape, const rbs_shape* v_shape, const void* K, const void* V,
+                    const rbs_cache* cache, const int32_t* slots, void* stream) {
+  int rc = check_heads(shape, RBS_MAX_NEW_TOKENS);
+  if (rc != RBS_OK) return rc;
+  rbs::MoveArgs a{};
+  if ((rc = resolve_strides(shape->kv_stride_head, shape->kv_stride_tok, shape->n_kv_heads, shape->n_tokens, &a.k_head,
+                            &a.k_tok)) != RBS_OK)
+    return rc;
+  a.v_head = a.k_head;
+  a.v_tok = a.k_tok;
+  if (v_shape != nullptr) {
+    if (v_shape->n_tokens != shape->n_tokens || v_shape->n_kv_heads != shape->n_kv_heads ||
+        v_shape->head_dim != shape->head_dim)
+      return RBS_ERR_SHAPE;
+    if ((rc = resolve_strides(v_shape->kv_stride_head, v_shape->kv_stride_tok, shape->n_kv_heads, shape->n_tokens,
+                              &a.v_head, &a.v_tok)) != RBS_OK)
+      return rc;
+  }
+  if ((rc = check_cache(cache, &a.cache)) != RBS_OK) return rc;
+  if (cache->n_kv_heads != shape->n_kv_heads) return RBS_ERR_SHAPE;
+  if (K == nullptr || V == nullptr || slots == nullptr) return RBS_ERR_NULL;
+  if (!aligned16(K) || !aligned16(V) || !aligned16(slots)) return RBS_ERR_ALIGN;
+  a.K = static_cast<uint16_t*>(const_cast<void*>(K));
+  a.V = static_cast<uint16_t*>(const_cast<void*>(V));
+  a.n_tokens = shape->n_tokens;
+  a.n_kv_heads = shape->n_kv_heads;
+  a.slots = slots;
+  return finish(rbs::launch_cache_write(a, static_cast<hipStream_t>(stream)), stream);
+}
+
+int rbs_cache_read(const rbs_shape* shape, const rbs_cache* cache, const int32_t* cu_tokens, const int32_t* starts,
+                   int32_t n_rows, const int32_t* page_table, int32_t max_pages, void* K, void* V, void* stream) {
+  int rc = check_heads(shape, RBS_MAX_NEW_TOKENS);
+  if (rc != RBS_OK) return rc;
+  if (n_rows < 1 || n_rows > RBS_MAX_ROWS) return RBS_ERR_SHAPE;
+  rbs::MoveArgs a{};
+  if ((rc = resolve_strides(shape->kv_stride_head, shape->kv_stride_tok, shape->n_kv_heads, shape->n_tokens, &a.k_head,
+                            &a.k_tok)) != RBS_OK)
+    return rc;
+  if ((rc = check_cache(cache, &a.cache)) != RBS_OK) return rc;
+  if (cache->n_kv_heads != shape->n_kv_heads || max_pages < 1 || max_pages > (INT32_MAX >> a.cache.page_shift))
+    return RBS_ERR_SHAPE;
+  if (cu_tokens == nullptr || page_table == nullptr || K == nullptr || V == nullptr) return RBS_ERR_NULL;
+  if (!aligned16(cu_tokens) || !aligned16(starts) || !aligned16(page_table) || !aligned16(K) || !aligned16(V))
+    return RBS_ERR_ALIGN;
+  a.K = static_cast<uint16_t*>(K);
+  a.V = static_cast<uint16_t*>(V);
+  a.v_head = a.k_head;
+  a.v_tok = a.k_tok;
+  a.n_tokens = shape->n_tokens;
+  a.n_kv_heads = shape->n_kv_heads;
+  a.cu_tokens = cu_tokens;
+  a.starts = starts;
+  a.n_rows = n_rows;
+  a.max_pages = max_pages;
+  a.page_table = page_table;
+  return finish(rbs::launch_cache_read(a, static_cast<hipStream_t>(stream)), stream);
 }
 
 size_t rbs_decode_workspace_bytes(void) { return rbs::decode_workspace_bytes(); }

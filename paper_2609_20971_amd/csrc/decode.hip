@@ -37,9 +37,18 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-// Keys of one row that a wave takes at a time: 16 KB of K and V in either type.
-template <bool kFp8>
-constexpr int kTile = kFp8 ? 64 : 32;
+template <int kFmt>
+constexpr bool is_fp8 = kFmt == kCacheFp8;
+template <int kFmt>
+constexpr bool is_fp4 = kFmt == kCacheFp4;
+// Keys of one row that a wave takes at a time: 16 KB of K and V in bf16 and FP8, 8.5 in FP4.
+template <int kFmt>
+constexpr int kTile = kFmt == kCacheBf16 ? 32 : 64;
+// Bytes of a head row of K or V: the codes, and with an FP4 row's four scales.
+template <int kFmt>
+constexpr int kCodeBytes = is_fp4<kFmt> ? kHeadDim / 2 : is_fp8<kFmt> ? kHeadDim : 2 * kHeadDim;
+template <int kFmt>
+constexpr int kRowBytes = kCodeBytes<kFmt> + (is_fp4<kFmt> ? kHeadDim / 32 : 0);
 constexpr int kCols = 16;      // query heads of a unit
 constexpr int kWorkers = 512;  // workgroups of a launch: two on each of 256 compute units
 constexpr int kPartFloats = kCols * kHeadDim + 2 * kCols;  // weighted values, maxima, sums
@@ -115,15 +124,15 @@ __device__ __forceinline__ bool has_token(const int32_t* cu_tokens, int n_tokens
 
 // A row's share in the dealing out: its tiles, and kRowCost more for what it
 // costs to start and end a row.
-template <bool kFp8>
+template <int kFmt>
 __device__ __forceinline__ int share_of(int len) {
-  return len > 0 ? (len - 1) / kTile<kFp8> + 1 + kRowCost : 0;
+  return len > 0 ? (len - 1) / kTile<kFmt> + 1 + kRowCost : 0;
 }
 
 // first[row]: shares of the rows before it, first[n_rows]: of all; length[row] (-1:
 // a row to leave alone); returns the longest share.  Each thread sums n_rows / 256 rows, then a scan over
 // the threads.
-template <bool kFp8>
+template <int kFmt>
 __device__ __forceinline__ int tile_offsets(const DecodeArgs& a, const int32_t* lens, const int32_t* cu_tokens,
                                              int* first, int* length, int* sums) {
   constexpr int kPer = kMaxRows / kThreads;
@@ -140,7 +149,7 @@ __device__ __forceinline__ int tile_offsets(const DecodeArgs& a, const int32_t* 
       const int len = lens[row0 + i];
       const int clamped = has_token(cu_tokens, a.n_tokens, row0 + i) ? (int)(len < cap ? len : cap) : -1;
       length[row0 + i] = clamped;
-      share[i] = share_of<kFp8>(clamped);
+      share[i] = share_of<kFmt>(clamped);
     }
     mine += share[i];
     longest = max(longest, share[i]);
@@ -208,23 +217,34 @@ struct State {
   f32x4 o[8];
 };
 
-template <bool kFp8>
+template <int kFmt>
 struct Tile {
-  static constexpr int kSteps = kTile<kFp8> / 16;
+  static constexpr int kSteps = kTile<kFmt> / 16;
   // Of 16 keys, with m = l % 16, c = l / 16.  bf16: key m, elements 32 x + 8 c ..;
   // FP8: key 8 x + m / 2, elements 64 (m % 2) + 16 c ..: eight lanes to a row of 128
   // bytes (in pieces of 64 200 rows of 300 to 2000 keys took 7% longer).
-  uint4 k[kSteps][kFp8 ? 2 : 4];
+  uint4 k[kSteps][is_fp8<kFmt> ? 2 : 4];
   // bf16: key 4 c + x, elements 8 m ..; FP8: key 8 x + 2 c + m % 2, elements 16 (m / 2)
   // .., of which half is for the lane next to it: in loads of 8 bytes, each for its
   // own lane, a long read past the caches took 193 us and not 134.
-  uint4 v[kSteps][kFp8 ? 2 : 4];
+  uint4 v[kSteps][is_fp8<kFmt> ? 2 : 4];
+};
+
+// FP4, of 16 keys: each load of the wave takes whole runs of memory (1 KB of K, 256
+// bytes of V), and each scale is a byte of its own: 64 bytes for the wave.
+template <>
+struct Tile<kCacheFp4> {
+  static constexpr int kSteps = kTile<kCacheFp4> / 16;
+  uint4 k[kSteps];         // key 4 (m % 4) + m / 4, elements 32 c ..: a matrix operand's row and block as they are
+  int k_scale[kSteps];     // of these 32 elements
+  uint32_t v[kSteps][4];   // key 4 x + c, elements 8 m ..
+  int v_scale[kSteps];     // of key 4 (m % 4) + c, elements 32 (m / 4) ..: what the four lanes of a quad need, one each
 };
 
 // Which of 16 keys a lane's logit (and weight) u is of, 0 <= u < 4.
-template <bool kFp8>
+template <int kFmt>
 __device__ __forceinline__ int key_of(int c, int u) {
-  return kFp8 ? 8 * (u >> 1) + 2 * c + (u & 1) : 4 * c + u;
+  return is_fp4<kFmt> ? 4 * u + c : is_fp8<kFmt> ? 8 * (u >> 1) + 2 * c + (u & 1) : 4 * c + u;
 }
 
 // 16 bytes of K or V; kOnce: without a place in the caches.
@@ -236,15 +256,36 @@ __device__ __forceinline__ uint4 load16(const char* p) {
   return make_uint4(v.x, v.y, v.z, v.w);
 }
 
+template <bool kOnce>
+__device__ __forceinline__ uint32_t load4(const char* p) {
+  return kOnce ? __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p)) : *reinterpret_cast<const uint32_t*>(p);
+}
+template <bool kOnce>
+__device__ __forceinline__ int load1(const char* p) {
+  return kOnce ? __builtin_nontemporal_load(reinterpret_cast<const uint8_t*>(p)) : *reinterpret_cast<const uint8_t*>(p);
+}
+
 // The other lane's of two next to each other.
 __device__ __forceinline__ uint32_t neighbour(uint32_t x) {
   return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xb1, 0xf, 0xf, false);  // quad_perm [1, 0, 3, 2]
 }
 
-template <bool kFp8>
+// Lane u's of the lane's four.
+__device__ __forceinline__ uint32_t of_quad(uint32_t x, int u) {
+  const int i = (int)x;
+  return (uint32_t)(u == 0   ? __builtin_amdgcn_update_dpp(0, i, 0x00, 0xf, 0xf, false)  // quad_perm [u, u, u, u]
+                    : u == 1 ? __builtin_amdgcn_update_dpp(0, i, 0x55, 0xf, 0xf, false)
+                    : u == 2 ? __builtin_amdgcn_update_dpp(0, i, 0xaa, 0xf, 0xf, false)
+                             : __builtin_amdgcn_update_dpp(0, i, 0xff, 0xf, 0xf, false));
+}
+
+template <int kFmt>
 struct Stream {
   const char* K;  // this KV head's
   const char* V;
+  const char* K_scale;  // FP4: the scale of 32 elements at byte x of the codes is byte x / 16
+  const char* V_scale;
+  uint32_t ks_off, vs_off;
   int64_t page_bytes;
   int tok_bytes, n_pages, shift;
   uint32_t k_off, v_off;  // this lane's, within 16 keys
@@ -257,45 +298,130 @@ struct Stream {
     const int page = min(max(table[__builtin_amdgcn_readfirstlane(min(j0, len - 1) >> shift)], 0), n_pages - 1);
     return page * page_bytes + (int64_t)(j0 & ((1 << shift) - 1)) * tok_bytes;
   }
-  __device__ __forceinline__ void load_k(Tile<kFp8>& t, const int64_t* base) const {
+  __device__ __forceinline__ void load_k(Tile<kFmt>& t, const int64_t* base) const {
     if (once) load_k_as<true>(t, base);
     else load_k_as<false>(t, base);
   }
-  __device__ __forceinline__ void load_v(Tile<kFp8>& t, const int64_t* base) const {
+  __device__ __forceinline__ void load_v(Tile<kFmt>& t, const int64_t* base) const {
     if (once) load_v_as<true>(t, base);
     else load_v_as<false>(t, base);
   }
   template <bool kOnce>
-  __device__ __forceinline__ void load_k_as(Tile<kFp8>& t, const int64_t* base) const {
+  __device__ __forceinline__ void load_k_as(Tile<kFmt>& t, const int64_t* base) const {
 #pragma unroll
-    for (int h = 0; h < Tile<kFp8>::kSteps; ++h)
+    for (int h = 0; h < Tile<kFmt>::kSteps; ++h) {
+      if constexpr (is_fp4<kFmt>) {
+        t.k[h] = load16<kOnce>(K + base[h] + k_off);
+        t.k_scale[h] = load1<kOnce>(K_scale + (base[h] >> 4) + ks_off);
+      } else {
 #pragma unroll
-      for (int x = 0; x < (kFp8 ? 2 : 4); ++x)
-        t.k[h][x] = load16<kOnce>(K + base[h] + k_off + x * (kFp8 ? 8 * tok_bytes : 64));
+        for (int x = 0; x < (is_fp8<kFmt> ? 2 : 4); ++x)
+          t.k[h][x] = load16<kOnce>(K + base[h] + k_off + x * (is_fp8<kFmt> ? 8 * tok_bytes : 64));
+      }
+    }
   }
   template <bool kOnce>
-  __device__ __forceinline__ void load_v_as(Tile<kFp8>& t, const int64_t* base) const {
+  __device__ __forceinline__ void load_v_as(Tile<kFmt>& t, const int64_t* base) const {
 #pragma unroll
-    for (int h = 0; h < Tile<kFp8>::kSteps; ++h)
+    for (int h = 0; h < Tile<kFmt>::kSteps; ++h) {
+      if constexpr (is_fp4<kFmt>) {
 #pragma unroll
-      for (int x = 0; x < (kFp8 ? 2 : 4); ++x)
-        t.v[h][x] = load16<kOnce>(V + base[h] + v_off + x * (kFp8 ? 8 : 1) * tok_bytes);
+        for (int x = 0; x < 4; ++x) t.v[h][x] = load4<kOnce>(V + base[h] + v_off + 4 * x * tok_bytes);
+        t.v_scale[h] = load1<kOnce>(V_scale + (base[h] >> 4) + vs_off);
+      } else {
+#pragma unroll
+        for (int x = 0; x < (is_fp8<kFmt> ? 2 : 4); ++x)
+          t.v[h][x] = load16<kOnce>(V + base[h] + v_off + x * (is_fp8<kFmt> ? 8 : 1) * tok_bytes);
+      }
+    }
   }
 };
 
+// A wave's 16 queries as the right operand of K's products: q, and for FP4 keys
+// what multiplies its two halves.
+template <int kFmt>
+struct Queries {
+  uint4 q[4];
+};
+
+// FP4 keys go to the matrix core as they are, codes and scales, which takes queries
+// in 8 bits: two E4M3 numbers each (the value and 16 times what its rounding left),
+// over a power of two for the whole row.  A bf16 has 8 significant bits and each of
+// the two takes 4 of them, so that nothing is lost but below 2^-22 of the row's
+// largest magnitude (where E4M3 is subnormal: half a step, 2^-10, over 16, of
+// the 2^8 that the largest reaches).
+template <>
+struct Queries<kCacheFp4> {
+  i32x8 hi, lo;
+  int hi_scale, lo_scale;
+};
+
+// From the lane's elements 16 c .. + 15 (q[0], q[1]) and 64 + 16 c .. + 15 (q[2], q[3])
+// of its column, in the order in which the 8-bit operand holds them.
+__device__ __forceinline__ Queries<kCacheFp4> split_queries(const uint4* q) {
+  Queries<kCacheFp4> out;
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t w = word_of(q[i >> 2], i & 3);
+    top = max(top, max(w & 0x7fffu, (w >> 16) & 0x7fffu));
+  }
+  top = __float_as_uint(over_rows(__uint_as_float(top), [](float a, float b) {
+    return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));
+  }));
+  const uint32_t e = min(max(top >> 7, 12u), 254u);  // biased exponent of the largest magnitude
+  const float f = __uint_as_float((261u - e) << 23);  // takes it to 2^7 .. 2^8
+  const bool bad = (top >> 7) == 255u;                // NaN or an infinity: every logit NaN
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float y[4];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint32_t w = word_of(q[i >> 1], 2 * (i & 1) + k);
+      y[2 * k] = bf16_lo(w) * f;
+      y[2 * k + 1] = bf16_hi(w) * f;
+    }
+    int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], hi, true);
+    y[0] -= __builtin_amdgcn_cvt_f32_fp8(hi, 0);
+    y[1] -= __builtin_amdgcn_cvt_f32_fp8(hi, 1);
+    y[2] -= __builtin_amdgcn_cvt_f32_fp8(hi, 2);
+    y[3] -= __builtin_amdgcn_cvt_f32_fp8(hi, 3);
+    int lo = __builtin_amdgcn_cvt_pk_fp8_f32(16.f * y[0], 16.f * y[1], 0, false);
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(16.f * y[2], 16.f * y[3], lo, true);
+    out.hi[i] = bad ? 0x7f7f7f7f : hi;
+    out.lo[i] = bad ? 0 : lo;
+  }
+  out.hi_scale = (int)e - 7;
+  out.lo_scale = (int)e - 11;
+  return out;
+}
+
+// 16 keys of 128 elements times 16 queries, all of it in one product: K in E2M1 with
+// a scale for each 32 elements.
+__device__ __forceinline__ f32x4 mfma_fp4(const uint4& k, int k_scale, const i32x8& q, int q_scale, const f32x4& c) {
+  const i32x8 a = {(int)k.x, (int)k.y, (int)k.z, (int)k.w, 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q, c, 4, 0, 0, k_scale, 0, q_scale);  // E2M1 by E4M3
+}
+
 // One tile from key j on added to a wave's state; `next` gives the offsets of the
 // tile to ask for (more: whether there is one).
-template <bool kFp8>
-__device__ __forceinline__ void attend_tile(const Stream<kFp8>& st, Tile<kFp8>& tile, const uint4* q,
+template <int kFmt>
+__device__ __forceinline__ void attend_tile(const Stream<kFmt>& st, Tile<kFmt>& tile, const Queries<kFmt>& queries,
                                             float scale_log2, int j, int len, bool more, const int64_t* next,
                                             State& s) {
-  constexpr int kSteps = Tile<kFp8>::kSteps;
+  constexpr int kSteps = Tile<kFmt>::kSteps;
   const int c = (threadIdx.x & 63) >> 4;
   const bool odd = threadIdx.x & 1;
   f32x4 sc[kSteps];
 #pragma unroll
   for (int h = 0; h < kSteps; ++h) {
-    if (kFp8) {
+    if constexpr (is_fp4<kFmt>) {
+      sc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+      sc[h] = mfma_fp4(tile.k[h], tile.k_scale[h], queries.lo, queries.lo_scale, sc[h]);
+      sc[h] = mfma_fp4(tile.k[h], tile.k_scale[h], queries.hi, queries.hi_scale, sc[h]);
+    } else if constexpr (is_fp8<kFmt>) {
+      const uint4* q = queries.q;
       // Rows 2 n and 2 n + 1 of the operand are the two halves of key n: the halves of
       // q with it in turn, of which every other row counts.
 #pragma unroll
@@ -312,19 +438,19 @@ __device__ __forceinline__ void attend_tile(const Stream<kFp8>& st, Tile<kFp8>& 
     } else {
       sc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int x = 0; x < 4; ++x) sc[h] = mfma16(tile.k[h][x], q[x], sc[h]);
+      for (int x = 0; x < 4; ++x) sc[h] = mfma16(tile.k[h][x], queries.q[x], sc[h]);
     }
   }
   if (more) st.load_k(tile, next);
 
-  const bool partial = j + kTile<kFp8> > len;
+  const bool partial = j + kTile<kFmt> > len;
   float x[4 * kSteps];
 #pragma unroll
   for (int e = 0; e < 4 * kSteps; ++e) x[e] = sc[e >> 2][e & 3] * scale_log2;
   if (partial) {
 #pragma unroll
     for (int e = 0; e < 4 * kSteps; ++e)
-      if (j + 16 * (e >> 2) + key_of<kFp8>(c, e & 3) >= len) x[e] = -INFINITY;
+      if (j + 16 * (e >> 2) + key_of<kFmt>(c, e & 3) >= len) x[e] = -INFINITY;
   }
   float top = x[0];
 #pragma unroll
@@ -356,7 +482,11 @@ __device__ __forceinline__ void attend_tile(const Stream<kFp8>& st, Tile<kFp8>& 
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
       const int h = 2 * b + (e >> 2);
-      if (kFp8) {
+      if constexpr (is_fp4<kFmt>) {
+        const uint32_t scales = (uint32_t)tile.v_scale[h] << 23;
+        v[e] = widen_e2m1(tile.v[h][e & 3], of_quad(scales, e & 3));
+        v[e + 1] = widen_e2m1(tile.v[h][(e & 3) + 1], of_quad(scales, (e & 3) + 1));
+      } else if constexpr (is_fp8<kFmt>) {
         const uint4& w = tile.v[h][(e >> 1) & 1];
         // (Every lane gives and takes: not inside a condition on the lane.)
         const uint32_t nx = neighbour(w.x), ny = neighbour(w.y), nz = neighbour(w.z), nw = neighbour(w.w);
@@ -370,7 +500,7 @@ __device__ __forceinline__ void attend_tile(const Stream<kFp8>& st, Tile<kFp8>& 
     if (partial) {  // places past the row's length may hold anything, NaN too
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const bool in = j + 32 * b + 16 * (e >> 2) + key_of<kFp8>(c, e & 3) < len;
+        const bool in = j + 32 * b + 16 * (e >> 2) + key_of<kFmt>(c, e & 3) < len;
         v[e].x = in ? v[e].x : 0u;
         v[e].y = in ? v[e].y : 0u;
         v[e].z = in ? v[e].z : 0u;
@@ -403,9 +533,9 @@ __device__ __forceinline__ void write_token(const DecodeArgs& a, int tok, int he
   if (part == 0 && a.lse != nullptr) a.lse[(int64_t)head * a.n_tokens + tok] = (m + __log2f(l)) * 0.69314718055994531f;
 }
 
-template <bool kFp8>
+template <int kFmt>
 __device__ __forceinline__ float value_scale(const DecodeArgs& a, int g) {
-  if (!kFp8) return 1.f;
+  if (!is_fp8<kFmt>) return 1.f;
   const float m = a.cache.amax[a.n_kv_heads + g];
   return m > 0.f ? m / 448.f : 1.f;
 }
@@ -426,7 +556,7 @@ __device__ __forceinline__ int row_from(const int* first, int n_rows, int x) {
 }
 
 // kWhole: a row is one worker's, so that there is nothing to join.
-template <bool kFp8, bool kWhole>
+template <int kFmt, bool kWhole>
 __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
     DecodeArgs a, const int32_t* __restrict__ lens, const int32_t* __restrict__ page_table,
     const int32_t* __restrict__ cu_tokens) {
@@ -440,7 +570,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
   const int g = unit / wk.tiles_of_cols, group = a.n_q_heads / a.n_kv_heads;
   const int head0 = g * group + (unit % wk.tiles_of_cols) * kCols;
   const int cols = min(kCols, (g + 1) * group - head0);
-  const int longest = tile_offsets<kFp8>(a, lens, cu_tokens, first, length, sums);
+  const int longest = tile_offsets<kFmt>(a, lens, cu_tokens, first, length, sums);
   const int T = first[a.n_rows];
   // Many short rows: each wave takes whole rows for itself, with nothing to join.
   const bool solo = longest <= kSoloShare && (int64_t)longest * (kWaves * wk.workers) <= (int64_t)kSoloRatio * T;
@@ -465,20 +595,30 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
       a.lse[(int64_t)(head0 + threadIdx.x) * a.n_tokens + tok] = -INFINITY;
   }
 
-  constexpr int kBytes = kFp8 ? 1 : 2, kSteps = Tile<kFp8>::kSteps;
-  Stream<kFp8> st;
-  st.K = static_cast<const char*>(a.cache.K) + g * a.cache.head * kBytes;
-  st.V = static_cast<const char*>(a.cache.V) + g * a.cache.head * kBytes;
-  st.page_bytes = a.cache.page * kBytes;
-  st.tok_bytes = (int)a.cache.tok * kBytes;
+  constexpr int kSteps = Tile<kFmt>::kSteps;
+  // Bytes of so many elements.
+  auto bytes = [](int64_t x) __attribute__((always_inline)) { return x * kCodeBytes<kFmt> / kHeadDim; };
+  Stream<kFmt> st;
+  st.K = static_cast<const char*>(a.cache.K) + bytes(g * a.cache.head);
+  st.V = static_cast<const char*>(a.cache.V) + bytes(g * a.cache.head);
+  st.page_bytes = bytes(a.cache.page);
+  st.tok_bytes = (int)bytes(a.cache.tok);
   st.n_pages = a.cache.n_pages;
   st.shift = a.cache.page_shift;
-  st.once = wk.tiles_of_cols == 1 && (int64_t)T * wk.units * (kTile<kFp8> * 2 * kHeadDim * kBytes) >= kCachedBytes;
-  st.k_off = kFp8 ? (col >> 1) * st.tok_bytes + 64 * (col & 1) + 16 * c : col * st.tok_bytes + 16 * c;
-  st.v_off = kFp8 ? (2 * c + (col & 1)) * st.tok_bytes + 16 * (col >> 1) : 4 * c * st.tok_bytes + 16 * col;
+  st.once = wk.tiles_of_cols == 1 && (int64_t)T * wk.units * (kTile<kFmt> * 2 * kRowBytes<kFmt>) >= kCachedBytes;
+  st.k_off = is_fp8<kFmt> ? (col >> 1) * st.tok_bytes + 64 * (col & 1) + 16 * c : col * st.tok_bytes + 16 * c;
+  st.v_off = is_fp8<kFmt> ? (2 * c + (col & 1)) * st.tok_bytes + 16 * (col >> 1) : 4 * c * st.tok_bytes + 16 * col;
+  if constexpr (is_fp4<kFmt>) {
+    st.K_scale = static_cast<const char*>(a.cache.K_scale) + g * a.cache.head / 32;
+    st.V_scale = static_cast<const char*>(a.cache.V_scale) + g * a.cache.head / 32;
+    st.k_off = (4 * (col & 3) + (col >> 2)) * st.tok_bytes + 16 * c;
+    st.v_off = c * st.tok_bytes + 4 * col;
+    st.ks_off = (4 * (col & 3) + (col >> 2)) * (st.tok_bytes >> 4) + c;
+    st.vs_off = (4 * (col & 3) + c) * (st.tok_bytes >> 4) + (col >> 2);
+  }
   float scale_log2 = a.scale * kLog2e;
-  if (kFp8 && a.cache.amax[g] > 0.f) scale_log2 *= a.cache.amax[g] / 448.f;
-  const float v_scale = value_scale<kFp8>(a, g);
+  if (is_fp8<kFmt> && a.cache.amax[g] > 0.f) scale_log2 *= a.cache.amax[g] / 448.f;
+  const float v_scale = value_scale<kFmt>(a, g);
 
   // The wave's next tile: tile `tile` of row `row` (-1: none), of `len` keys.  It
   // runs ahead of the rows below by one tile, whose keys and values are on their
@@ -508,12 +648,12 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
   auto offsets = [&](int64_t* base) __attribute__((always_inline)) {
     const int32_t* table = page_table + (int64_t)__builtin_amdgcn_readfirstlane(next.row) * a.max_pages;
     const int len = __builtin_amdgcn_readfirstlane(next.len);
-    const int j = __builtin_amdgcn_readfirstlane(next.tile * kTile<kFp8>);
+    const int j = __builtin_amdgcn_readfirstlane(next.tile * kTile<kFmt>);
 #pragma unroll
     for (int h = 0; h < kSteps; ++h) base[h] = st.at(table, len, j + 16 * h);
   };
   int row = t < t_end ? seq_of(first, a.n_rows, t) : 0;
-  Tile<kFp8> tile;
+  Tile<kFmt> tile;
   if (t < t_end) seek(row);
   if (next.row >= 0) {
     int64_t base[kSteps];
@@ -538,25 +678,32 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       // Elements that the K operand's lane holds.
-      const int d = kFp8 ? 64 * (x >> 1) + 16 * c + 8 * (x & 1) : 32 * x + 8 * c;
+      const int d = kFmt != kCacheBf16 ? 64 * (x >> 1) + 16 * c + 8 * (x & 1) : 32 * x + 8 * c;
       q[x] = make_uint4(0u, 0u, 0u, 0u);
       if (col < cols) q[x] = *reinterpret_cast<const uint4*>(a.Q + (head0 + col) * a.q_head + tok * a.q_tok + d);
     }
     // Waited for here: in the loop the wait for the first Q would be one for the
     // values on their way as well, at every tile.
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+    Queries<kFmt> queries;
+    if constexpr (is_fp4<kFmt>) {
+      queries = split_queries(q);
+    } else {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) queries.q[x] = q[x];
+    }
     State s;
     s.m = -INFINITY;
     s.l = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) s.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     while (next.row == r) {
-      const int j = next.tile * kTile<kFp8>, len = next.len;
+      const int j = next.tile * kTile<kFmt>, len = next.len;
       next.tile += step;
       if (next.tile >= next.end) seek(r + 1);
       int64_t base[kSteps] = {};
       if (next.row >= 0) offsets(base);
-      attend_tile<kFp8>(st, tile, q, scale_log2, j, len, next.row >= 0, base, s);
+      attend_tile<kFmt>(st, tile, queries, scale_log2, j, len, next.row >= 0, base, s);
     }
     s.l = over_rows(s.l, [](float a, float b) { return a + b; });
 
@@ -632,7 +779,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
 // loads are in flight at a time (a row of 128K keys has 128 parts).  One column to
 // a workgroup where that makes few of them, otherwise four: most workgroups of a
 // large batch find nothing to join.
-template <bool kFp8, int kJoinCols>
+template <int kFmt, int kJoinCols>
 __global__ __launch_bounds__(kJoinThreads) void paged_decode_join_kernel(DecodeArgs a) {
   constexpr int kSets = kJoinThreads / 16, kBatch = kJoinCols == 1 ? 4 : 8;
   __shared__ __align__(16) float acc[kSets][kPad];
@@ -704,27 +851,27 @@ __global__ __launch_bounds__(kJoinThreads) void paged_decode_join_kernel(DecodeA
 #pragma unroll
     for (int e = 0; e < 8; ++e) out[e] += acc[hc + i * cols][8 * part + e] * f;
   }
-  write_token(a, token_of(a.cu_tokens, shared.row), head0 + col0 + hc, part, out, top, sum, value_scale<kFp8>(a, g));
+  write_token(a, token_of(a.cu_tokens, shared.row), head0 + col0 + hc, part, out, top, sum, value_scale<kFmt>(a, g));
 }
 
-template <bool kFp8>
+template <int kFmt>
 hipError_t launch(const DecodeArgs& a, hipStream_t s) {
   const Work wk = work_of_heads(a.n_q_heads, a.n_kv_heads);
   const int group = a.n_q_heads / a.n_kv_heads, cols = group < kCols ? group : kCols;
   const dim3 grid(wk.units * wk.workers);
   const int64_t most = (int64_t)a.max_pages << a.cache.page_shift;  // keys of a row
-  if (most <= kWholeTiles * kTile<kFp8> || (most <= kWholeKeysOfFew && a.n_rows * wk.units <= kFewWhole)) {
-    hipLaunchKernelGGL((paged_decode_kernel<kFp8, true>), grid, dim3(kThreads), 0, s, a, a.seq_lens, a.page_table,
+  if (most <= kWholeTiles * kTile<kFmt> || (most <= kWholeKeysOfFew && a.n_rows * wk.units <= kFewWhole)) {
+    hipLaunchKernelGGL((paged_decode_kernel<kFmt, true>), grid, dim3(kThreads), 0, s, a, a.seq_lens, a.page_table,
                        a.cu_tokens);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((paged_decode_kernel<kFp8, false>), grid, dim3(kThreads), 0, s, a, a.seq_lens, a.page_table,
+  hipLaunchKernelGGL((paged_decode_kernel<kFmt, false>), grid, dim3(kThreads), 0, s, a, a.seq_lens, a.page_table,
                        a.cu_tokens);
   const int joins = wk.units * (a.n_rows < wk.workers ? a.n_rows : wk.workers);
   if (joins * cols <= kFewJoins)
-    hipLaunchKernelGGL((paged_decode_join_kernel<kFp8, 1>), dim3(joins, cols), dim3(kJoinThreads), 0, s, a);
+    hipLaunchKernelGGL((paged_decode_join_kernel<kFmt, 1>), dim3(joins, cols), dim3(kJoinThreads), 0, s, a);
   else
-    hipLaunchKernelGGL((paged_decode_join_kernel<kFp8, 4>), dim3(joins, (cols + 3) / 4), dim3(kJoinThreads), 0, s, a);
+    hipLaunchKernelGGL((paged_decode_join_kernel<kFmt, 4>), dim3(joins, (cols + 3) / 4), dim3(kJoinThreads), 0, s, a);
   return hipGetLastError();
 }
 
@@ -735,7 +882,12 @@ hipError_t launch(const DecodeArgs& a, hipStream_t s) {
 size_t decode_workspace_bytes() { return sizeof(float) * 2 * kWorkers * kPartFloats + kWorkers * sizeof(Shared); }
 
 hipError_t launch_paged_decode(const DecodeArgs& a, hipStream_t s) {
-  return a.cache.amax != nullptr ? launch<true>(a, s) : launch<false>(a, s);
+  switch (a.cache.format) {
+    case kCacheBf16: return launch<kCacheBf16>(a, s);
+    case kCacheFp8: return launch<kCacheFp8>(a, s);
+    case kCacheFp4: return launch<kCacheFp4>(a, s);
+    default: return hipErrorInvalidValue;
+  }
 }
 
 }  // namespace rbs

@@ -327,34 +327,34 @@ __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
-// E4M3 codes of four values times scale, saturating at +-448 (NaN stays NaN).
-__device__ __forceinline__ uint32_t pack_e4m3(const float* x, float scale) {
-  float y[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    y[i] = x[i] * scale;
-    y[i] = y[i] > 448.f ? 448.f : y[i] < -448.f ? -448.f : y[i];
-  }
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-  return __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+// The largest of each half word over the lanes of a row, in all of them.
+template <int kLanes>
+__device__ __forceinline__ uint32_t row_top(uint32_t x) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  auto top = [](uint32_t a, int b) __attribute__((always_inline)) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+  };
+  x = top(x, __builtin_amdgcn_update_dpp(0, (int)x, 0xb1, 0xf, 0xf, false));   // as in row_sum
+  x = top(x, __builtin_amdgcn_update_dpp(0, (int)x, 0x4e, 0xf, 0xf, false));
+  x = top(x, __builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, false));
+  if (kLanes == 16) x = top(x, __builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, false));
+  return x;
 }
 
-// kWords words between memory and registers; kOnce: with no place in the caches.
-template <int kWords, bool kOnce>
-__device__ __forceinline__ void load_words(const void* p, uint32_t* w) {
-  typedef uint32_t Vec __attribute__((ext_vector_type(kWords)));
-  const Vec v = kOnce ? __builtin_nontemporal_load(static_cast<const Vec*>(p)) : *static_cast<const Vec*>(p);
+// The largest magnitude (bits of bf16) of a run.
+template <int kWords>
+__device__ __forceinline__ uint32_t run_top(const uint32_t* w) {
+  uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < kWords; ++i) w[i] = v[i];
+  for (int e = 0; e < kWords; ++e) top = max(top, max(w[e] & 0x7fffu, (w[e] >> 16) & 0x7fffu));
+  return top;
 }
-template <int kWords, bool kOnce>
-__device__ __forceinline__ void store_words(void* p, const uint32_t* w) {
-  typedef uint32_t Vec __attribute__((ext_vector_type(kWords)));
-  Vec v;
-#pragma unroll
-  for (int i = 0; i < kWords; ++i) v[i] = w[i];
-  if (kOnce) __builtin_nontemporal_store(v, static_cast<Vec*>(p));
-  else *static_cast<Vec*>(p) = v;
+
+// E2M1 codes of a run of eight elements, or of four in the low half.
+template <int kWords>
+__device__ __forceinline__ uint32_t pack_run(const uint32_t* w, uint32_t scale) {
+  const uint32_t x[4] = {w[0], w[1], kWords == 4 ? w[kWords - 2] : 0u, kWords == 4 ? w[kWords - 1] : 0u};
+  return pack_e2m1(x, scale);
 }
 
 template <int kLanes, bool kInterleaved, bool kOnce>
@@ -475,7 +475,36 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a, 
       if (!is_q && cached) {
         const int64_t at = place + head * a.cache.head;
         void* base = is_v ? a.cache.V : a.cache.K;
-        if (a.cache.amax == nullptr) {
+        if (a.cache.format == kCacheFp4) {
+          // Of the row as it is written to K_out, in bf16.  A run lies within one
+          // block of 32 elements; the four blocks' largest go round the row's lanes in
+          // two words.
+          constexpr int kWords = kRun / 2;
+          const uint32_t lo_top = run_top<kWords>(b), hi_top = run_top<kWords>(b + kWords);
+          const int lo_block = lo >> 5, hi_block = hi >> 5;
+          uint32_t tops[2];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const uint32_t even = max(lo_block == 2 * x ? lo_top : 0u, hi_block == 2 * x ? hi_top : 0u);
+            const uint32_t odd = max(lo_block == 2 * x + 1 ? lo_top : 0u, hi_block == 2 * x + 1 ? hi_top : 0u);
+            tops[x] = row_top<kLanes>(even | odd << 16);
+          }
+          uint32_t scales = 0;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) scales |= fp4_scale((tops[x >> 1] >> (16 * (x & 1))) & 0x7fffu) << (8 * x);
+          const uint32_t lo_codes = pack_run<kWords>(b, (scales >> (8 * lo_block)) & 255u);
+          const uint32_t hi_codes = pack_run<kWords>(b + kWords, (scales >> (8 * hi_block)) & 255u);
+          uint8_t* codes = static_cast<uint8_t*>(base) + (at >> 1);
+          if (kRun == 8) {
+            *reinterpret_cast<uint32_t*>(codes + (lo >> 1)) = lo_codes;
+            *reinterpret_cast<uint32_t*>(codes + (hi >> 1)) = hi_codes;
+          } else {
+            *reinterpret_cast<uint16_t*>(codes + (lo >> 1)) = (uint16_t)lo_codes;
+            *reinterpret_cast<uint16_t*>(codes + (hi >> 1)) = (uint16_t)hi_codes;
+          }
+          if (i == 0)
+            *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(is_v ? a.cache.V_scale : a.cache.K_scale) + (at >> 5)) = scales;
+        } else if (a.cache.format == kCacheBf16) {
           store_words<kRun / 2, kOnce>(static_cast<uint16_t*>(base) + at + lo, b);
           store_words<kRun / 2, kOnce>(static_cast<uint16_t*>(base) + at + hi, b + kRun / 2);
         } else {
