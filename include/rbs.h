@@ -33,6 +33,7 @@
  *   rbs_cache_read      and rows of it as bf16 again
  *   rbs_paged_decode,   attention of one new token per row over the cache, the
  *   rbs_paged_decode_packed   queries by row or packed as rbs_pages_extend packs them
+ *   rbs_paged_prefill   attention of all new tokens of each row over the cache, causal
  *
  * Conventions shared by every call
  *   - Tensors live in device memory.  Q, K, V and O are indexed by (head,
@@ -596,6 +597,36 @@ int rbs_paged_decode(const rbs_shape* shape, const rbs_cache* cache, const void*
 int rbs_paged_decode_packed(const rbs_shape* shape, const rbs_cache* cache, const void* Q, const int32_t* cu_tokens,
                             int32_t n_rows, const int32_t* page_table, int32_t max_pages, const int32_t* seq_lens,
                             float softmax_scale, void* O, float* lse, void* workspace, void* stream);
+
+/* Workspace of rbs_paged_prefill, 16-byte aligned; shared as the decode calls'. */
+size_t rbs_prefill_workspace_bytes(void);
+
+/*
+ * Attention of all new tokens of a batch over the rows' cached tokens (their own keys
+ * and values among them): whole prompts, parts of a prompt after what is cached
+ * already, drafted tokens to be checked, single tokens, in any mixture.  Tokens are
+ * packed as rbs_pages_extend packs them: row s has tokens cu_tokens[s] ..
+ * cu_tokens[s + 1] - 1 of Q (a of them; int32 [n_rows + 1], ascending), which are the
+ * last ones of its first seq_lens[s] cached tokens.  For query head h of token i of the row
+ *   O = sum_j softmax_j(q . k_j * scale) v_j over j = 0 .. seq_lens[s] - a + i
+ * with fp32 sums, the weights rounded once to bf16 (and summed as such), rounded
+ * to bf16.  What later tokens hold, infinities and NaN too, does not reach a token's
+ * result; an infinity in a value that is attended may give NaN.
+ * shape: n_tokens tokens of Q and O, those behind the last one of a padded batch
+ * included (up to RBS_MAX_NEW_TOKENS), H_q (up to 512) and H_kv heads, strides of Q
+ * and O (any block_size; kv strides are not used).  softmax_scale <= 0 selects
+ * 1/sqrt(d).  lse: NULL or fp32 [H_q][n_tokens], natural log.  A token before its
+ * row's first key (more new tokens than seq_lens[s]): O = 0, lse = -inf.  Rows that are
+ * unused (a negative length) or have no new token are skipped, and O and lse of tokens
+ * that are no row's are left as they were.  A row whose offsets fall outside 0 ..
+ * n_tokens is one without tokens; where offsets descend anywhere, no row has any.
+ * page_table int32 [n_rows][max_pages], seq_lens int32 [n_rows], trusted like
+ * rbs_paged_decode's.  Results do not depend on timing; those of a row may differ in their
+ * last bits with the rows beside it, whose lengths decide how a row is divided.
+ */
+int rbs_paged_prefill(const rbs_shape* shape, const rbs_cache* cache, const void* Q, const int32_t* cu_tokens,
+                      int32_t n_rows, const int32_t* page_table, int32_t max_pages, const int32_t* seq_lens,
+                      float softmax_scale, void* O, float* lse, void* workspace, void* stream);
 
 /* Static description of a status code. */
 const char* rbs_status_str(int status);

@@ -87,9 +87,11 @@ from ._paged import (  # noqa: F401
     rbs_cache_write,
     rbs_decode_workspace_bytes,
     rbs_paged_decode,
+    rbs_paged_prefill,
     rbs_pages,
     rbs_pages_extend,
     rbs_pages_release,
+    rbs_prefill_workspace_bytes,
     rbs_qk_norm_rope,
     rbs_rope,
     rope_frequencies,

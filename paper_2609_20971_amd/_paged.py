@@ -89,6 +89,10 @@ def declare(lib):
     lib.rbs_paged_decode.restype = ctypes.c_int
     lib.rbs_paged_decode_packed.argtypes = [SP, ctypes.POINTER(rbs_cache), P, P, I32, P, I32, P, F32, P, P, P, P]
     lib.rbs_paged_decode_packed.restype = ctypes.c_int
+    lib.rbs_prefill_workspace_bytes.argtypes = []
+    lib.rbs_prefill_workspace_bytes.restype = SZ
+    lib.rbs_paged_prefill.argtypes = [SP, ctypes.POINTER(rbs_cache), P, P, I32, P, I32, P, F32, P, P, P, P]
+    lib.rbs_paged_prefill.restype = ctypes.c_int
 
 
 def _handle(device: int, stream):
@@ -511,15 +515,19 @@ def _kv_strided(shape, kv):
     return L._with_strides(shape, kv=kv)
 
 
-_decode_workspaces = threading.local()  # attributes of its own for every thread
+_workspaces = threading.local()  # attributes of its own for every thread
 
 
 def rbs_decode_workspace_bytes() -> int:
     return int(L.load().rbs_decode_workspace_bytes())
 
 
-def _auto_workspace(device: int, handle: int) -> torch.Tensor:
-    """The workspace of a (device, stream) and of this thread: a thread's calls on
+def rbs_prefill_workspace_bytes() -> int:
+    return int(L.load().rbs_prefill_workspace_bytes())
+
+
+def _auto_workspace(device: int, handle: int, size=rbs_decode_workspace_bytes) -> torch.Tensor:
+    """The workspace (of size() bytes) of a (device, stream) and of this thread: a thread's calls on
     one stream are ordered, so they may share it.  Those of two threads are not: a
     call is two launches, and the other thread's may come between them.  While the
     stream is being captured, a new one, which belongs to the graph's memory:
@@ -527,18 +535,18 @@ def _auto_workspace(device: int, handle: int) -> torch.Tensor:
     if handle != torch._C._cuda_getCurrentRawStream(device):
         # Made on the stream that uses it, whose order its memory's next use has to follow.
         with L._own(device, handle):
-            return _workspace_of(device, handle)
-    return _workspace_of(device, handle)
+            return _workspace_of(device, handle, size)
+    return _workspace_of(device, handle, size)
 
 
-def _workspace_of(device: int, handle: int) -> torch.Tensor:
+def _workspace_of(device: int, handle: int, size=rbs_decode_workspace_bytes) -> torch.Tensor:
     capturing = torch.cuda.is_current_stream_capturing()
-    held = _decode_workspaces.__dict__  # (freed with the thread; its memory's next use on the stream is ordered)
-    ws = None if capturing else held.get((device, handle))
+    held = _workspaces.__dict__  # (freed with the thread; its memory's next use on the stream is ordered)
+    ws = None if capturing else held.get((device, handle, size))
     if ws is None:
-        ws = torch.empty(rbs_decode_workspace_bytes() // 4, dtype=torch.float32, device=torch.device("cuda", device))
+        ws = torch.empty(size() // 4, dtype=torch.float32, device=torch.device("cuda", device))
         if not capturing:
-            held[device, handle] = ws
+            held[device, handle, size] = ws
     return ws
 
 
@@ -569,16 +577,8 @@ def rbs_paged_decode(shape: L.rbs_shape, Q, cache: PagedCache, page_table, seq_l
         L._on_gpu(("cache.K", cache.K), ("Q", Q), ("page_table", page_table), ("seq_lens", seq_lens), ("O", O),
                   ("lse", lse), ("cu_tokens", cu_tokens))
     if O is None:
-        O = L._made(dev, stream, torch.empty_like, Q)
-        if O.stride() != Q.stride():
-            O = L._made(dev, stream, L._like_q, Q)
-    if isinstance(workspace, str):
-        if workspace != L.AUTO:
-            raise ValueError(f"workspace must be AUTO or a tensor, not {workspace!r}")
-    elif not isinstance(workspace, torch.Tensor) or workspace.get_device() != dev or not workspace.is_contiguous():
-        raise ValueError("workspace must be AUTO or a contiguous tensor on the inputs' GPU")
-    elif workspace.numel() * workspace.element_size() < rbs_decode_workspace_bytes():
-        raise ValueError("workspace is smaller than rbs_decode_workspace_bytes()")
+        O = _out_like(Q, dev, stream)
+    _check_workspace(workspace, dev, rbs_decode_workspace_bytes)
     L._check("rbs_paged_decode", _on(dev, stream, _decode, _strided(shape, qs), cache, Q, page_table, seq_lens,
                                      softmax_scale, O, lse, workspace, cu_tokens, dev))
     return O
@@ -593,3 +593,57 @@ def _decode(shape, cache, Q, page_table, seq_lens, softmax_scale, O, lse, worksp
         return L.load().rbs_paged_decode(shape, cache.c, Q.data_ptr(), *rest)
     return L.load().rbs_paged_decode_packed(shape, cache.c, Q.data_ptr(), cu_tokens.data_ptr(), page_table.shape[0],
                                             *rest)
+
+
+def _out_like(Q, dev, stream):
+    O = L._made(dev, stream, torch.empty_like, Q)
+    return O if O.stride() == Q.stride() else L._made(dev, stream, L._like_q, Q)
+
+
+def _check_workspace(workspace, dev, size):
+    if isinstance(workspace, str):
+        if workspace != L.AUTO:
+            raise ValueError(f"workspace must be AUTO or a tensor, not {workspace!r}")
+    elif not isinstance(workspace, torch.Tensor) or workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be AUTO or a contiguous tensor on the inputs' GPU")
+    elif workspace.numel() * workspace.element_size() < size():
+        raise ValueError(f"workspace is smaller than {size.__name__}()")
+
+
+def rbs_paged_prefill(shape: L.rbs_shape, Q, cache: PagedCache, page_table, seq_lens, cu_tokens,
+                      softmax_scale: float = 0.0, O=None, lse=None, stream=None, workspace=L.AUTO):
+    """Attention of all new tokens of a batch over the rows' cached tokens, each over those up
+    to itself; returns O (bf16, Q's sizes and strides).  Q: (head, token, dimension), packed as
+    rbs_pages_extend's step packs its tokens: row's from cu_tokens[row] on, the last ones of its
+    first seq_lens[row] cached ones.  Tokens of no row are left alone."""
+    hq, n, d = shape.n_q_heads, shape.n_tokens, shape.head_dim
+    qs = _rows("Q", Q, (hq, n, d))
+    if not isinstance(cache, PagedCache):
+        raise ValueError("cache must be a PagedCache")
+    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+        raise ValueError("page_table must be an [n_rows][max_pages] tensor")
+    rows = page_table.shape[0]
+    L._check_tensor("page_table", page_table, torch.int32, (rows, page_table.shape[1]))
+    _int_row("seq_lens", seq_lens, rows)
+    _int_row("cu_tokens", cu_tokens, rows + 1)
+    if O is not None:
+        L._check_out(O, Q)
+    if lse is not None:
+        L._check_tensor("lse", lse, torch.float32, (hq, n))
+    dev = Q.get_device()
+    if cache.device != dev or _elsewhere(dev, page_table, seq_lens, cu_tokens, O, lse):
+        L._on_gpu(("cache.K", cache.K), ("Q", Q), ("page_table", page_table), ("seq_lens", seq_lens),
+                  ("cu_tokens", cu_tokens), ("O", O), ("lse", lse))
+    if O is None:
+        O = _out_like(Q, dev, stream)
+    _check_workspace(workspace, dev, rbs_prefill_workspace_bytes)
+    L._check("rbs_paged_prefill", _on(dev, stream, _prefill, _strided(shape, qs), cache, Q, page_table, seq_lens,
+                                      cu_tokens, softmax_scale, O, lse, workspace, dev))
+    return O
+
+
+def _prefill(shape, cache, Q, page_table, seq_lens, cu_tokens, softmax_scale, O, lse, workspace, dev, s):
+    ws = _auto_workspace(dev, s, rbs_prefill_workspace_bytes) if isinstance(workspace, str) else workspace
+    return L.load().rbs_paged_prefill(shape, cache.c, Q.data_ptr(), cu_tokens.data_ptr(), page_table.shape[0],
+                                      page_table.data_ptr(), page_table.shape[1], seq_lens.data_ptr(),
+                                      float(softmax_scale), O.data_ptr(), L._ptr(lse), ws.data_ptr(), s)

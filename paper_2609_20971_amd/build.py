@@ -15,7 +15,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "librbs.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
-SOURCES = ["api.hip", "stats.hip", "select.hip", "attn.hip", "fp8.hip", "paged.hip", "cache.hip", "decode.hip"]
+SOURCES = ["api.hip", "stats.hip", "select.hip", "attn.hip", "fp8.hip", "paged.hip", "cache.hip", "decode.hip",
+           "prefill.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

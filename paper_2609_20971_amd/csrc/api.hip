@@ -984,6 +984,44 @@ int rbs_paged_decode_packed(const rbs_shape* shape, const rbs_cache* cache, cons
                       lse, workspace, stream);
 }
 
+size_t rbs_prefill_workspace_bytes(void) { return rbs::prefill_workspace_bytes(); }
+
+int rbs_paged_prefill(const rbs_shape* shape, const rbs_cache* cache, const void* Q, const int32_t* cu_tokens,
+                      int32_t n_rows, const int32_t* page_table, int32_t max_pages, const int32_t* seq_lens,
+                      float softmax_scale, void* O, float* lse, void* workspace, void* stream) {
+  int rc = check_heads(shape, RBS_MAX_NEW_TOKENS);
+  if (rc != RBS_OK) return rc;
+  if (n_rows < 1 || n_rows > RBS_MAX_ROWS) return RBS_ERR_SHAPE;
+  rbs::PrefillArgs a{};
+  if ((rc = resolve_strides(shape->q_stride_head, shape->q_stride_tok, shape->n_q_heads, shape->n_tokens, &a.q_head,
+                            &a.q_tok)) != RBS_OK)
+    return rc;
+  if ((rc = check_cache(cache, &a.cache)) != RBS_OK) return rc;
+  if (cache->n_kv_heads != shape->n_kv_heads || max_pages < 1 || max_pages > (INT32_MAX >> a.cache.page_shift))
+    return RBS_ERR_SHAPE;
+  if (Q == nullptr || cu_tokens == nullptr || page_table == nullptr || seq_lens == nullptr || O == nullptr ||
+      workspace == nullptr)
+    return RBS_ERR_NULL;
+  if (!(softmax_scale == softmax_scale) || isinf(softmax_scale)) return RBS_ERR_ARG;
+  if (!aligned16(Q) || !aligned16(cu_tokens) || !aligned16(page_table) || !aligned16(seq_lens) || !aligned16(O) ||
+      !aligned16(lse) || !aligned16(workspace))
+    return RBS_ERR_ALIGN;
+  a.Q = static_cast<const uint16_t*>(Q);
+  a.n_tokens = shape->n_tokens;
+  a.n_rows = n_rows;
+  a.n_q_heads = shape->n_q_heads;
+  a.n_kv_heads = shape->n_kv_heads;
+  a.page_table = page_table;
+  a.max_pages = max_pages;
+  a.seq_lens = seq_lens;
+  a.cu_tokens = cu_tokens;
+  a.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)shape->head_dim);
+  a.O = static_cast<uint16_t*>(O);
+  a.lse = lse;
+  a.workspace = static_cast<float*>(workspace);
+  return finish(rbs::launch_paged_prefill(a, static_cast<hipStream_t>(stream)), stream);
+}
+
 const char* rbs_status_str(int status) {
   switch (status) {
     case RBS_OK: return "ok";

@@ -87,6 +87,23 @@ struct DecodeArgs {
   float* workspace;
 };
 
+// rbs_paged_prefill: as above, every new token of a row a query.
+struct PrefillArgs {
+  const uint16_t* Q;
+  int64_t q_head, q_tok;  // Q and O
+  int n_tokens;           // of Q, O and lse
+  int n_rows, n_q_heads, n_kv_heads;
+  CacheView cache;
+  const int32_t* page_table;
+  int max_pages;
+  const int32_t* seq_lens;
+  const int32_t* cu_tokens;
+  float scale;
+  uint16_t* O;
+  float* lse;
+  float* workspace;
+};
+
 constexpr int kMaxRows = 4096;  // rows of a page table
 
 hipError_t launch_pages_extend(const PagesArgs& a, hipStream_t s);
@@ -98,6 +115,8 @@ hipError_t launch_cache_write(const MoveArgs& a, hipStream_t s);
 hipError_t launch_cache_read(const MoveArgs& a, hipStream_t s);
 size_t decode_workspace_bytes();
 hipError_t launch_paged_decode(const DecodeArgs& a, hipStream_t s);
+size_t prefill_workspace_bytes();
+hipError_t launch_paged_prefill(const PrefillArgs& a, hipStream_t s);
 
 // x combined over the lanes up to and with this one (op: associative, 0 its
 // neutral element): within each row of 16 lanes, then the last lane of row 0 (2)
