@@ -20,12 +20,15 @@
 // read of K and V for few queries.
 //
 // Sums are in fp32.  The weights go to the second product rounded once to bf16, and
-// the denominator sums what goes there (on the matrix core), so that their common error cancels.
+// the denominator sums what goes there (on the matrix core), so that their common error
+// cancels; the log-sum-exp, where it is asked for, has a sum of the weights before that.
 //
 // Work: unit u of a KV head is a tile, or where there are few tiles a piece of one,
 // of at most P blocks of keys; pieces leave maximum, sum and weighted values in fp32,
 // which a second launch joins in the order of the keys.  Lengths are on the GPU, so
 // that every workgroup finds the units for itself.
+#include <type_traits>
+
 #include "attend_block.hpp"
 #include "paged.hpp"
 
@@ -37,10 +40,20 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kBlock = 128;                      // queries of a tile, keys of a block
 constexpr int kUnits = 1024;                     // pieces of a call whose tiles are split
-constexpr int kPartFloats = kBlock * kHeadDim + 2 * kBlock;  // weighted values, maxima, sums
+constexpr int kPartFloats = kBlock * kHeadDim + 3 * kBlock;  // weighted values, maxima, sums of rounded and exact weights
 constexpr int kMost = 1 << 29;                   // counts stop here
 
 __device__ __forceinline__ int capped_add(int a, int b) { return min(a + b, kMost); }
+
+// The rows, as kernel arguments of their own (scalar loads: a vector load of a page
+// number would have to be waited for together with the copies on their way).
+struct Rows {
+  const int32_t* page_table;
+  const int32_t* seq_lens;
+  const int32_t* cu_tokens;
+};
+#define RBS_ROWS_ARGS \
+  const int32_t *__restrict__ page_table, const int32_t *__restrict__ seq_lens, const int32_t *__restrict__ cu_tokens
 
 struct RowWork {
   int tiles;   // 0: nothing to do
@@ -70,7 +83,7 @@ struct Plan {
 // most `piece` blocks to a unit; returns it.  Of the pieces that make at most `room`
 // units the smallest is taken, from below (a count over the rows for each try, four
 // at once); where there are as many tiles as that, whole tiles.
-__device__ __forceinline__ int plan_units(const PrefillArgs& a, int room, const Plan& plan) {
+__device__ __forceinline__ int plan_units(const PrefillArgs& a, const Rows& rows, int room, const Plan& plan) {
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, group = a.n_q_heads / a.n_kv_heads;
   const int per = (a.n_rows + kThreads - 1) / kThreads;  // a thread's rows, one after another
   const int row0 = min(t * per, a.n_rows), row1 = min(row0 + per, a.n_rows);
@@ -79,9 +92,9 @@ __device__ __forceinline__ int plan_units(const PrefillArgs& a, int room, const 
   float blocks = 0.f;  // (within 2^-12)
   bool descends = false;
   for (int r = row0; r < row1; ++r) {
-    const int begin = a.cu_tokens[r], end = a.cu_tokens[r + 1];
+    const int begin = rows.cu_tokens[r], end = rows.cu_tokens[r + 1];
     descends |= end < begin;
-    const RowWork w = work_of_row(a, group, begin, end, a.seq_lens[r]);
+    const RowWork w = work_of_row(a, group, begin, end, rows.seq_lens[r]);
     plan.tiles[r] = w.tiles;
     plan.blocks[r] = w.blocks;
     tiles = capped_add(tiles, w.tiles);
@@ -179,14 +192,14 @@ struct Unit {
   int tile, part, parts;        // of the row; of the tile
 };
 
-__device__ __forceinline__ Unit unit_of(const PrefillArgs& a, const int* first, int piece, int u) {
+__device__ __forceinline__ Unit unit_of(const PrefillArgs& a, const Rows& rows, const int* first, int piece, int u) {
   const int group = a.n_q_heads / a.n_kv_heads;
   Unit n;
   n.row = __builtin_amdgcn_readfirstlane(seq_of(first, a.n_rows, u));
   const int local = __builtin_amdgcn_readfirstlane(u - first[n.row]);
-  n.begin = a.cu_tokens[n.row];
-  n.tokens = a.cu_tokens[n.row + 1] - n.begin;
-  n.len = a.seq_lens[n.row];
+  n.begin = rows.cu_tokens[n.row];
+  n.tokens = rows.cu_tokens[n.row + 1] - n.begin;
+  n.len = rows.seq_lens[n.row];
   const RowWork w = work_of_row(a, group, n.begin, n.begin + n.tokens, n.len);
   const int tiles = max(w.tiles, 1);
   n.parts = piece == INT_MAX ? 1 : (w.blocks + piece - 1) / piece;
@@ -296,7 +309,7 @@ __device__ __forceinline__ float head_factor(const PrefillArgs& a, int head) {
 
 // The result of a query: 64 of its elements in a lane.
 __device__ __forceinline__ void write_query(const PrefillArgs& a, int head, int tok, int half, const f32x16* o, float m,
-                                            float l, float v_factor) {
+                                            float l, float l_exact, float v_factor) {
   const float inv = l > 0.f ? v_factor / l : l == 0.f ? 0.f : __builtin_nanf("");
   uint16_t* row = a.O + head * a.q_head + tok * a.q_tok;
 #pragma unroll
@@ -307,7 +320,7 @@ __device__ __forceinline__ void write_query(const PrefillArgs& a, int head, int 
           make_uint2(two_bf16(o[dt][4 * rq] * inv, o[dt][4 * rq + 1] * inv),
                      two_bf16(o[dt][4 * rq + 2] * inv, o[dt][4 * rq + 3] * inv));
   if (a.lse != nullptr && half == 0)
-    a.lse[(int64_t)head * a.n_tokens + tok] = l == 0.f ? -INFINITY : (m + log2f(l)) / kLog2e;
+    a.lse[(int64_t)head * a.n_tokens + tok] = l_exact == 0.f ? -INFINITY : (m + log2f(l_exact)) / kLog2e;
 }
 
 // What the workgroup's tiles in LDS are.
@@ -338,43 +351,41 @@ __device__ __forceinline__ void take_out(const Tiles& t, int limit, f32x16* o, i
   }
 }
 
-template <int kFmt>
-__device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Unit& n, int piece, int g, const Tiles& t,
+template <int kFmt, bool kLse>
+__device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& rows, const Unit& n, int piece, int g, const Tiles& t,
                                             float* slot) {
   constexpr int KT = kBlock / 32;
+  constexpr bool kCopied = kFmt == kCacheBf16;  // straight to LDS
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, l32 = lane & 31;
   const int group = a.n_q_heads / a.n_kv_heads;
   const int64_t queries = (int64_t)n.tokens * group, x0 = (int64_t)n.tile * kBlock;
-  const int64_t x = x0 + 32 * wave + l32;
-  const bool ok = x < queries;
-  const int i = (int)((ok ? x : queries - 1) / group);  // the lane's token
-  const int head = g * group + (int)((ok ? x : queries - 1) - (int64_t)i * group), tok = n.begin + i;
   const int64_t cap = (int64_t)a.max_pages << a.cache.page_shift;
-  const int before = n.len - n.tokens;                 // position of the row's first new token
+  const int before = n.len - n.tokens;  // position of the row's first new token
   const int held = (int)min((int64_t)n.len, cap);
-  const int last = min(before + i, held - 1);          // the lane's last key
-  const int64_t x1 = min(x0 + kBlock, queries) - 1;
-  const int tile_last = min(before + (int)(x1 / group), held - 1);
-  const int tile_first_last = min(before + (int)(x0 / group), held - 1);  // the first query's
+  const int tile_last = min(before + (int)((min(x0 + kBlock, queries) - 1) / group), held - 1);
+  const int first_last = min(before + (int)(x0 / group), held - 1);  // the last key of the tile's first query
   const int blocks = tile_last < 0 ? 0 : tile_last / kBlock + 1;
   const int b0 = piece == INT_MAX ? 0 : n.part * piece;
   const int b1 = piece == INT_MAX ? blocks : min(blocks, b0 + piece);
-  const bool works = x0 + 32 * wave < queries;         // (the wave has a query)
+  const int plain = min(b1, (first_last + 1) / kBlock);  // blocks before it are attended whole
 
+  // The lane's query (past the row's last one: that one, and not written).
+  const int64_t x = x0 + 32 * wave + l32;
+  const bool ok = x < queries;
+  const int i = (int)((ok ? x : queries - 1) / group);
+  const int head = g * group + (int)((ok ? x : queries - 1) - (int64_t)i * group), tok = n.begin + i;
+  const int last = min(before + i, held - 1);  // its last key
   bf16x8 q[8];
   {
     const uint16_t* row = a.Q + head * a.q_head + tok * a.q_tok + 8 * half;
 #pragma unroll
-    for (int ks = 0; ks < 8; ++ks) {
-      const uint4 w = ok ? *reinterpret_cast<const uint4*>(row + 16 * ks) : make_uint4(0u, 0u, 0u, 0u);
-      q[ks] = __builtin_bit_cast(bf16x8, w);
-    }
+    for (int ks = 0; ks < 8; ++ks) q[ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(row + 16 * ks));
   }
   RBS_WAIT_VMCNT(0);  // (a wait for Q inside the loop would be one for the copies too)
 
   Pages<kFmt> pages;
-  pages.table = a.page_table + (int64_t)n.row * a.max_pages;
+  pages.table = rows.page_table + (int64_t)n.row * a.max_pages;
   pages.n_pages = a.cache.n_pages;
   pages.shift = a.cache.page_shift;
   pages.last_key = max(tile_last, 0);
@@ -387,7 +398,10 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Unit& n,
   const char* Vs = static_cast<const char*>(a.cache.V_scale) + g * a.cache.head / 32;
   const float scale_log2 = a.scale * kLog2e * head_factor<kFmt>(a, g);
 
-  // BF16: the wave copies keys 32 wave .. + 31 of a block, four at a time, straight to LDS.
+  // BF16: the wave copies keys 32 wave .. + 31 of a block, in eight copies of four.  A
+  // workgroup's copies all at once would hold its waves up at their issue, so that
+  // half of a tensor's go out as its tile becomes free and the others in pairs among the
+  // matrix and exponential steps.
   const uint32_t k_lds = __builtin_amdgcn_readfirstlane(lds_offset(t.k) + (uint32_t)wave * 8192u);
   const uint32_t v_lds = __builtin_amdgcn_readfirstlane(lds_offset(t.v) + (uint32_t)wave * 8192u);
   uint32_t k_off[4], v_off;
@@ -397,32 +411,41 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Unit& n,
     for (int j = 0; j < 4; ++j) k_off[j] = (uint32_t)(4 * j + l4) * pages.tok_bytes + 16u * (uint32_t)kswz(4 * j + l4, pc);
     v_off = (uint32_t)l4 * pages.tok_bytes + 16u * (uint32_t)vswz(l4, pc);
   }
-  auto copy = [&](int block, bool is_v) __attribute__((always_inline)) {
-    const char* base = is_v ? V : K;
-    const uint32_t lds = is_v ? v_lds : k_lds;
+  int64_t at_k[2], at_v[2];  // where the wave's two runs of 16 keys are, of the block whose K (V) is copied
+  auto find = [&](int block) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) at_k[h] = pages.at(block * kBlock + 32 * wave + 16 * h);
+  };
+  auto copy_pair = [&](bool is_v, int j) __attribute__((always_inline)) {  // copies j and j + 1 of 8
+    const int64_t* from = is_v ? at_v : at_k;
+#pragma unroll
+    for (int c = j; c < j + 2; ++c) {
+      const char* run = (is_v ? V : K) + from[c >> 2];
+      lds_dma16(is_v ? run + (size_t)(4 * (c & 3)) * pages.tok_bytes : run, is_v ? v_off : k_off[c & 3],
+                (is_v ? v_lds : k_lds) + 1024u * c);
+    }
+  };
+  // Half of a block's copies, or where the row's last key is among its keys or before them, all: past it, that one again.
+  auto copy_head = [&](int block, bool is_v) __attribute__((always_inline)) {
+    const int64_t* from = is_v ? at_v : at_k;
     const int j0 = block * kBlock + 32 * wave;
     if (j0 + 31 <= pages.last_key) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const char* from = base + pages.at(j0 + 16 * h);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          lds_dma16(is_v ? from + (size_t)(4 * j) * pages.tok_bytes : from, is_v ? v_off : k_off[j],
-                    lds + (uint32_t)(4096 * h + 1024 * j));
-      }
-    } else {  // past the row's last key: that one again
+      copy_pair(is_v, 0);
+      copy_pair(is_v, 2);
+    } else {
 #pragma unroll 1
       for (int c = 0; c < 8; ++c) {
         const int j16 = j0 + 16 * (c >> 2), r = 4 * (c & 3) + (lane >> 4);
         const int top = pages.last_key - min(j16, pages.last_key & ~15);
-        const int from = j16 > pages.last_key ? top : min(r, top);
-        const int piece_of = is_v ? vswz(r, lane & 15) : kswz(r, lane & 15);
-        lds_dma16(base + pages.at(j16), (uint32_t)from * pages.tok_bytes + 16u * (uint32_t)piece_of,
-                  lds + (uint32_t)(1024 * c));
+        const int row = j16 > pages.last_key ? top : min(r, top);
+        const int at = is_v ? vswz(r, lane & 15) : kswz(r, lane & 15);
+        lds_dma16((is_v ? V : K) + from[c >> 2], (uint32_t)row * pages.tok_bytes + 16u * (uint32_t)at,
+                  (is_v ? v_lds : k_lds) + 1024u * c);
       }
     }
   };
-  Staged<kFmt == kCacheBf16 ? kCacheFp8 : kFmt> k_next, v_next;
+  auto has_rest = [&](int block) __attribute__((always_inline)) { return block * kBlock + 32 * wave + 31 <= pages.last_key; };
+  Staged<kCopied ? kCacheFp8 : kFmt> k_next, v_next;
 
   const int vq = (lane & 15) >> 2;
   const int vsub = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
@@ -437,96 +460,129 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Unit& n,
   }
   f32x4 lacc{};
   auto l_of = [&]() __attribute__((always_inline)) { return ((lane >> 4) & 1) ? lacc[1] : lacc[0]; };
+  float l_exact = 0.f;  // this half wave's, of the weights before their rounding
   bool is_nan = false;  // the lane's query has a weight that is NaN
   f32x16 o[4];
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt) o[dt] = f32x16{};
   float m = -INFINITY;
 
-  if (b0 < b1) {
-    if constexpr (kFmt == kCacheBf16) {
-      copy(b0, false);
-      copy(b0, true);
-    } else {
-      k_next.load(pages, K, Ks, b0);
-      v_next.load(pages, V, Vs, b0);
-    }
-  }
-  for (int b = b0; b < b1; ++b) {
+  auto attend = [&](auto masked_of, int b) __attribute__((always_inline)) {
+    constexpr bool masked = decltype(masked_of)::value;
     const bool more = b + 1 < b1;
-    const bool masked = b * kBlock + kBlock - 1 > tile_first_last;
-    if constexpr (kFmt == kCacheBf16) {
-      RBS_WAIT_VMCNT(8);  // this block's K; its V may still be on its way
+    if constexpr (kCopied) {
+      RBS_WAIT_VMCNT(4);  // this block's K; its V may still be on its way
     } else {
       k_next.store(t.k, false);
     }
     __syncthreads();
-    if constexpr (kFmt != kCacheBf16)
+    const bool v_rest = kCopied && b > b0 && has_rest(b);
+    if (kCopied && more) find(b + 1);
+    if constexpr (!kCopied)
       if (more) k_next.load(pages, K, Ks, b + 1);
 
     f32x16 s[KT];
-    if (works) {
 #pragma unroll
-      for (int mt = 0; mt < KT; ++mt) {
-        s[mt] = f32x16{};
-        const int row = 32 * mt + l32;
-        const unsigned char* krow = t.k + row * 256;
+    for (int mt = 0; mt < KT; ++mt) {
+      s[mt] = f32x16{};
+      const int row = 32 * mt + l32;
+      const unsigned char* krow = t.k + row * 256;
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) {
-          const uint4 w = *reinterpret_cast<const uint4*>(krow + 16 * kswz(row, 2 * ks + half));
-          s[mt] = mfma_bf16(__builtin_bit_cast(bf16x8, w), q[ks], s[mt]);
-        }
+      for (int ks = 0; ks < 8; ++ks) {
+        const uint4 w = *reinterpret_cast<const uint4*>(krow + 16 * kswz(row, 2 * ks + half));
+        s[mt] = mfma_bf16(__builtin_bit_cast(bf16x8, w), q[ks], s[mt]);
+      }
+      if (kCopied && mt < 2) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (v_rest) copy_pair(true, 4 + 2 * mt);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     __syncthreads();  // every wave is done with this K
-    if constexpr (kFmt == kCacheBf16)
-      if (more) copy(b + 1, false);
+    const bool k_rest = kCopied && more && has_rest(b + 1);
+    if constexpr (kCopied)
+      if (more) copy_head(b + 1, false);
     const int limit = last - b * kBlock;  // the lane's last key in this block
-    if (works) {
-      if (masked) {
+    if constexpr (masked) {
 #pragma unroll
-        for (int mt = 0; mt < KT; ++mt) {
-          const int lim = limit - 32 * mt - 4 * half;
+      for (int mt = 0; mt < KT; ++mt) {
+        const int lim = limit - 32 * mt - 4 * half;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            s[mt][r] = (8 * (r >> 2) + (r & 3)) > lim ? -INFINITY : s[mt][r];
-            __builtin_amdgcn_sched_barrier(0);  // (64 compares' masks at once would not fit the scalar registers)
-          }
+        for (int r = 0; r < 16; ++r) {
+          s[mt][r] = (8 * (r >> 2) + (r & 3)) > lim ? -INFINITY : s[mt][r];
+          __builtin_amdgcn_sched_barrier(0);  // (64 compares' masks at once would not fit the scalar registers)
         }
       }
-      float top = -INFINITY;
-#pragma unroll
-      for (int mt = 0; mt < KT; ++mt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[mt][r]);
-      top = half_max(top) * scale_log2;
-      if (__any(top > m + kRescaleSlack)) {
-        // (Each query for itself: its result does not depend on the wave's others.)
-        const float m_new = top > m + kRescaleSlack ? top : m;
-        const float f = m_new == m ? 1.f : fast_exp2(m - m_new);
-        m = m_new;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) lacc[e] *= f;
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[dt][r] *= f;
-      }
-      const float shift = m == -INFINITY ? 0.f : m;
-#pragma unroll
-      for (int mt = 0; mt < KT; ++mt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[mt][r] = fast_exp2(fmaf(s[mt][r], scale_log2, -shift));
     }
-    if constexpr (kFmt == kCacheBf16) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int mt = 0; mt < KT; ++mt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[mt][r]);
+    top = half_max(top) * scale_log2;
+    if (__any(top > m + kRescaleSlack)) {
+      // (Each query for itself: its result does not depend on the wave's others.)
+      const float m_new = top > m + kRescaleSlack ? top : m;
+      const float f = m_new == m ? 1.f : fast_exp2(m - m_new);
+      m = m_new;
+      l_exact *= f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) lacc[e] *= f;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[dt][r] *= f;
+    }
+    const float shift = m == -INFINITY ? 0.f : m;
+    bf16x8 p[kBlock / 16];
+#pragma unroll
+    for (int mt = 0; mt < KT; ++mt) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[mt][r] = fast_exp2(fmaf(s[mt][r], scale_log2, -shift));
+      if (kLse) {
+        float sum[4] = {};
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum[r & 3] += s[mt][r];
+        l_exact += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) p[2 * mt + (e >> 3)][e & 7] = (__bf16)s[mt][e];
+      if (kCopied && mt < 2) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (k_rest) copy_pair(false, 4 + 2 * mt);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    const f32x4 lacc_before = lacc;
+#pragma unroll
+    for (int c = 0; c < kBlock / 16; ++c) lacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lsel, p[c], lacc, 0, 0, 0);
+    if (__any(l_of() != l_of())) {
+      // That product has two queries to a column, one of them times 0: a query with a
+      // NaN takes no part in it.
+#pragma unroll
+      for (int c = 0; c < kBlock / 16; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) is_nan |= (float)p[c][e] != (float)p[c][e];
+      is_nan = half_max(is_nan ? 1.f : 0.f) > 0.f;
+      lacc = lacc_before;
+#pragma unroll 1
+      for (int again = 0; again < 1; ++again) {
+#pragma unroll
+        for (int c = 0; c < kBlock / 16; ++c) {
+          const bf16x8 z{};
+          lacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lsel, is_nan ? z : p[c], lacc, 0, 0, 0);
+        }
+      }
+    }
+    if constexpr (kCopied) {
       if (more) RBS_WAIT_VMCNT(8); else RBS_WAIT_VMCNT(0);  // this block's V
     } else {
       v_next.store(t.v, true);
     }
     __syncthreads();
-    if constexpr (kFmt != kCacheBf16)
+    if constexpr (!kCopied)
       if (more) v_next.load(pages, V, Vs, b + 1);
-    if (masked) {
+    if constexpr (masked) {
       // Does the block hold a value that is not finite?
       bool bad = false;
 #pragma unroll
@@ -548,7 +604,7 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Unit& n,
             if ((z[e] & 0x7f80u) == 0x7f80u || (z[e] & 0x7f800000u) == 0x7f800000u) t.bad[(tid + kThreads * k) >> 4] = 1;
         }
         __syncthreads();
-        if (works) take_out(t, min(limit, pages.last_key - b * kBlock), o, half);
+        take_out(t, limit, o, half);
         __syncthreads();
 #pragma unroll 1
         for (int k = 0; k < 8; ++k) {
@@ -563,55 +619,59 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Unit& n,
         __syncthreads();
       }
     }
-    if (works) {
-      const f32x4 lacc_before = lacc;
 #pragma unroll
-      for (int c = 0; c < kBlock / 16; ++c) {
-        bf16x8 p;
+    for (int c = 0; c < kBlock / 16; ++c) {
+      const int row0 = 16 * c + 4 * half + vq;
+      const unsigned char* v0 = t.v + row0 * 256 + vbyte;
+      const unsigned char* v1 = v0 + 8 * 256;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[c >> 1][8 * (c & 1) + e];
-        lacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lsel, p, lacc, 0, 0, 0);
-        const int row0 = 16 * c + 4 * half + vq;
-        const unsigned char* v0 = t.v + row0 * 256 + vbyte;
-        const unsigned char* v1 = v0 + 8 * 256;
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt) {
-          const int pc = 16 * vswz(row0, 4 * dt + vsub);
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(v0 + pc));
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(v1 + pc));
-          bf16x8 v;
-          __builtin_memcpy(&v, &lo, 8);
-          __builtin_memcpy(reinterpret_cast<unsigned char*>(&v) + 8, &hi, 8);
-          o[dt] = mfma_bf16(v, p, o[dt]);
-        }
-      }
-      if (__any(l_of() != l_of())) {
-        // The denominators' product has two queries to a column, one of them times 0: a
-        // query with a NaN takes no part in it.
-#pragma unroll
-        for (int mt = 0; mt < KT; ++mt)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) is_nan |= s[mt][r] != s[mt][r];
-        is_nan = half_max(is_nan ? 1.f : 0.f) > 0.f;
-        lacc = lacc_before;
-#pragma unroll
-        for (int c = 0; c < kBlock / 16; ++c) {
-          bf16x8 p;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) p[e] = (__bf16)(is_nan ? 0.f : s[c >> 1][8 * (c & 1) + e]);
-          lacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lsel, p, lacc, 0, 0, 0);
-        }
+      for (int dt = 0; dt < 4; ++dt) {
+        const int pc = 16 * vswz(row0, 4 * dt + vsub);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(v0 + pc));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(v1 + pc));
+        bf16x8 v;
+        __builtin_memcpy(&v, &lo, 8);
+        __builtin_memcpy(reinterpret_cast<unsigned char*>(&v) + 8, &hi, 8);
+        o[dt] = mfma_bf16(v, p[c], o[dt]);
       }
     }
     __syncthreads();  // every wave is done with this V
-    if constexpr (kFmt == kCacheBf16)
-      if (more) copy(b + 1, true);
-  }
+    if constexpr (kCopied) {
+      if (more) {
+        at_v[0] = at_k[0];
+        at_v[1] = at_k[1];
+        copy_head(b + 1, true);
+      }
+    }
+  };
 
-  if (!works) return;
+  if (b0 < b1) {
+    if constexpr (kCopied) {
+      find(b0);
+      at_v[0] = at_k[0];
+      at_v[1] = at_k[1];
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        copy_head(b0, v != 0);
+        if (has_rest(b0)) {
+          copy_pair(v != 0, 4);
+          copy_pair(v != 0, 6);
+        }
+      }
+    } else {
+      k_next.load(pages, K, Ks, b0);
+      v_next.load(pages, V, Vs, b0);
+    }
+  }
+  int b = b0;
+  for (; b < plain; ++b) attend(std::false_type{}, b);
+  for (; b < b1; ++b) attend(std::true_type{}, b);
+
+  if (x0 + 32 * wave >= queries) return;  // (no query of the wave's)
   const float l = is_nan ? __builtin_nanf("") : l_of();
+  if (kLse) l_exact = half_sum(l_exact);
   if (n.parts == 1) {
-    if (ok) write_query(a, head, tok, half, o, m, l, head_factor<kFmt>(a, a.n_kv_heads + g));
+    if (ok) write_query(a, head, tok, half, o, m, l, kLse ? l_exact : l, head_factor<kFmt>(a, a.n_kv_heads + g));
     return;
   }
   // A piece: every lane's 64 elements in runs of four, a KB for the wave at a time.
@@ -623,14 +683,18 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Unit& n,
                                                                         o[k >> 2][4 * (k & 3) + 2], o[k >> 2][4 * (k & 3) + 3]);
   }
   if (half == 0) {
-    slot[kBlock * kHeadDim + 32 * wave + l32] = m;
-    slot[kBlock * kHeadDim + kBlock + 32 * wave + l32] = l;
+    float* sums = slot + kBlock * kHeadDim + 32 * wave + l32;
+    sums[0] = m;
+    sums[kBlock] = l;
+    if (kLse) sums[2 * kBlock] = l_exact;
   }
 }
 
-template <int kFmt>
+template <int kFmt, bool kLse>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_prefill_kernel(PrefillArgs a,
-                                                                                                         int room) {
+                                                                                                         int room,
+                                                                                                         RBS_ROWS_ARGS) {
+  const Rows rows{page_table, seq_lens, cu_tokens};
   __shared__ __align__(1024) unsigned char tiles[2 * kBlock * 256];
   __shared__ int sums[4 * kWaves], bad[kBlock];
   const Tiles t{tiles, tiles + kBlock * 256, bad};
@@ -638,16 +702,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   int* first = reinterpret_cast<int*>(tiles);
   const Plan plan{first, first + kMaxRows + 1, first + 2 * kMaxRows + 1, sums};
   for (int b = blockIdx.x;; b += gridDim.x) {
-    const int piece = plan_units(a, room, plan);
+    const int piece = plan_units(a, rows, room, plan);
     const int units = __builtin_amdgcn_readfirstlane(first[a.n_rows]);
     const int bunch = bunch_of(units, a.n_kv_heads);
     if (b >= slots_of(units, a.n_kv_heads, bunch)) return;
     int g, i;
     slot_of(b, a.n_kv_heads, bunch, &g, &i);
     if (i < units) {
-      const Unit n = unit_of(a, first, piece, i);
+      const Unit n = unit_of(a, rows, first, piece, i);
       __syncthreads();  // every wave has read the offsets
-      attend_unit<kFmt>(a, n, piece, g, t, n.parts > 1 ? a.workspace + (size_t)(g * units + i) * kPartFloats : nullptr);
+      attend_unit<kFmt, kLse>(a, rows, n, piece, g, t, n.parts > 1 ? a.workspace + (size_t)(g * units + i) * kPartFloats : nullptr);
     }
     __syncthreads();  // the tiles are free
   }
@@ -655,9 +719,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 
 // Joins the pieces of the tiles: a wave to 32 queries and 32 of their elements.
 template <int kFmt>
-__global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArgs a, int room) {
-  __shared__ int first[kMaxRows + 1], rows[2 * kMaxRows], sums[4 * kWaves];
-  const int piece = plan_units(a, room, Plan{first, rows, rows + kMaxRows, sums});
+__global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArgs a, int room, RBS_ROWS_ARGS) {
+  const Rows rows{page_table, seq_lens, cu_tokens};
+  __shared__ int first[kMaxRows + 1], counts[2 * kMaxRows], sums[4 * kWaves];
+  const int piece = plan_units(a, rows, room, Plan{first, counts, counts + kMaxRows, sums});
   if (piece == INT_MAX) return;
   const int units = __builtin_amdgcn_readfirstlane(first[a.n_rows]);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -666,7 +731,7 @@ __global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArg
   // Workgroup (unit of all KV heads, 32 elements); only the first piece's of a tile stays.
   for (int b = blockIdx.x; b < units * a.n_kv_heads; b += gridDim.x) {
     const int g = b / units, i = b - g * units;
-    const Unit n = unit_of(a, first, piece, i);
+    const Unit n = unit_of(a, rows, first, piece, i);
     if (n.part != 0 || n.parts == 1) continue;
     const int tiles = (int)(((int64_t)n.tokens * group + kBlock - 1) / kBlock);
     const int64_t queries = (int64_t)n.tokens * group, x = (int64_t)n.tile * kBlock + 32 * wave + l32;
@@ -678,7 +743,7 @@ __global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArg
     float m = -INFINITY;
     for (int p = 0; p < n.parts; ++p) m = fmaxf(m, slots[p * step + at]);
     const float ref = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
+    float l = 0.f, l_exact = 0.f;
     f32x16 o{};
     constexpr int kBatch = 4;
     for (int p0 = 0; p0 < n.parts; p0 += kBatch) {
@@ -699,6 +764,7 @@ __global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArg
         if (p0 + k >= n.parts || pl[k] == 0.f) continue;
         const float f = fast_exp2(pm[k] - ref);
         l += pl[k] * f;
+        if (a.lse != nullptr) l_exact += slots[(p0 + k) * step + at + 2 * kBlock] * f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           o[4 * e] += w[k][e].x * f;
@@ -717,7 +783,7 @@ __global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArg
       *reinterpret_cast<uint2*>(row + 8 * e) = make_uint2(two_bf16(o[4 * e] * inv, o[4 * e + 1] * inv),
                                                           two_bf16(o[4 * e + 2] * inv, o[4 * e + 3] * inv));
     if (a.lse != nullptr && half == 0 && dt == 0)
-      a.lse[(int64_t)head * a.n_tokens + tok] = l == 0.f ? -INFINITY : (m + log2f(l)) / kLog2e;
+      a.lse[(int64_t)head * a.n_tokens + tok] = l_exact == 0.f ? -INFINITY : (m + log2f(l_exact)) / kLog2e;
   }
 }
 
@@ -732,8 +798,11 @@ hipError_t launch(const PrefillArgs& a, hipStream_t s) {
   const int room = split ? kUnits / 2 / a.n_kv_heads : 0;
   const int64_t slots = (split ? kUnits : units) + 64 + 8 * a.n_kv_heads;
   const int grid = (int)(slots < (1 << 20) ? slots : (1 << 20));
-  hipLaunchKernelGGL(paged_prefill_kernel<kFmt>, dim3(grid), dim3(kThreads), 0, s, a, room);
-  if (split) hipLaunchKernelGGL(paged_prefill_join_kernel<kFmt>, dim3(kUnits / 2, 4), dim3(kThreads), 0, s, a, room);
+  const auto kernel = a.lse != nullptr ? paged_prefill_kernel<kFmt, true> : paged_prefill_kernel<kFmt, false>;
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), 0, s, a, room, a.page_table, a.seq_lens, a.cu_tokens);
+  if (split)
+    hipLaunchKernelGGL(paged_prefill_join_kernel<kFmt>, dim3(kUnits / 2, 4), dim3(kThreads), 0, s, a, room, a.page_table,
+                       a.seq_lens, a.cu_tokens);
   return hipGetLastError();
 }
 
