@@ -613,9 +613,9 @@ size_t rbs_prefill_workspace_bytes(void);
  * to bf16.  What later tokens hold, infinities and NaN too, does not reach a token's
  * result; an infinity in a value that is attended may give NaN.
  * shape: n_tokens tokens of Q and O, those behind the last one of a padded batch
- * included (up to RBS_MAX_NEW_TOKENS), H_q (up to 512) and H_kv heads, strides of Q
- * and O (any block_size; kv strides are not used).  softmax_scale <= 0 selects
- * 1/sqrt(d).  lse: NULL or fp32 [H_q][n_tokens], natural log.  A token before its
+ * included (up to RBS_MAX_NEW_TOKENS), H_q (up to 512; n_tokens H_q up to 2^30) and
+ * H_kv heads, strides of Q and O (any block_size; kv strides are not used).  softmax_scale
+ * <= 0 selects 1/sqrt(d).  lse: NULL or fp32 [H_q][n_tokens], natural log.  A token before its
  * row's first key (more new tokens than seq_lens[s]): O = 0, lse = -inf.  Rows that are
  * unused (a negative length) or have no new token are skipped, and O and lse of tokens
  * that are no row's are left as they were.  A row whose offsets fall outside 0 ..

@@ -45,7 +45,7 @@ FLAGS = [
 # slower.
 _ILP = ["-mllvm", "-amdgpu-sched-strategy=iterative-ilp"]
 _VGPR = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
-EXTRA_FLAGS = {"select.hip": _VGPR, "attn.hip": _ILP, "decode.hip": _VGPR, "prefill.hip": _ILP}
+EXTRA_FLAGS = {"select.hip": _VGPR, "attn.hip": _ILP, "decode.hip": _VGPR}
 
 
 def _run(cmd):

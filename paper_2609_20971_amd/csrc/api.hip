@@ -992,6 +992,8 @@ int rbs_paged_prefill(const rbs_shape* shape, const rbs_cache* cache, const void
   int rc = check_heads(shape, RBS_MAX_NEW_TOKENS);
   if (rc != RBS_OK) return rc;
   if (n_rows < 1 || n_rows > RBS_MAX_ROWS) return RBS_ERR_SHAPE;
+  // (Workgroups of a launch: one for 128 queries, and a few for each row and head.)
+  if ((int64_t)shape->n_tokens * shape->n_q_heads > (int64_t(1) << 30)) return RBS_ERR_SHAPE;
   rbs::PrefillArgs a{};
   if ((rc = resolve_strides(shape->q_stride_head, shape->q_stride_tok, shape->n_q_heads, shape->n_tokens, &a.q_head,
                             &a.q_tok)) != RBS_OK)

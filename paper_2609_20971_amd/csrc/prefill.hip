@@ -38,9 +38,12 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kBlock = 128;                      // queries of a tile, keys of a block
+constexpr int kQueries = 128;                    // of a tile
+constexpr int kKeys = 64;                        // of a block
+constexpr int kBlockBytes = kKeys * 2 * kHeadDim;  // of K or V in LDS
 constexpr int kUnits = 1024;                     // pieces of a call whose tiles are split
-constexpr int kPartFloats = kBlock * kHeadDim + 3 * kBlock;  // weighted values, maxima, sums of rounded and exact weights
+constexpr int kPartFloats = kQueries * kHeadDim + 3 * kQueries;  // weighted values, maxima, sums of rounded and exact weights
+constexpr int kAhead = 4;                        // operands on their way from LDS
 constexpr int kMost = 1 << 29;                   // counts stop here
 
 __device__ __forceinline__ int capped_add(int a, int b) { return min(a + b, kMost); }
@@ -66,8 +69,8 @@ __device__ __forceinline__ RowWork work_of_row(const PrefillArgs& a, int group, 
   RowWork w{0, 1};
   if (len < 0 || begin < 0 || end <= begin || end > a.n_tokens) return w;
   const int64_t cap = (int64_t)a.max_pages << a.cache.page_shift;
-  w.tiles = (int)(((int64_t)(end - begin) * group + kBlock - 1) / kBlock);
-  w.blocks = max(1, (int)((min((int64_t)len, cap) + kBlock - 1) / kBlock));
+  w.tiles = (int)(((int64_t)(end - begin) * group + kQueries - 1) / kQueries);
+  w.blocks = max(1, (int)((min((int64_t)len, cap) + kKeys - 1) / kKeys));
   return w;
 }
 
@@ -222,16 +225,10 @@ __device__ __forceinline__ void slot_of(int b, int n_kv_heads, int bunch, int* g
 __device__ __forceinline__ int bunch_of(int units, int n_kv_heads) {
   return max(1, min(8, (int)min((int64_t)units * n_kv_heads / 64, (int64_t)8)));
 }
-__device__ __forceinline__ int slots_of(int units, int n_kv_heads, int bunch) {
-  const int64_t bunches = (int64_t)((units + bunch - 1) / bunch) * n_kv_heads;
-  return (int)min((bunches + 7) / 8 * 8 * bunch, (int64_t)INT_MAX);
-}
-
 template <int kFmt>
 constexpr int kCodeBytes = kFmt == kCacheFp4 ? kHeadDim / 2 : kFmt == kCacheFp8 ? kHeadDim : 2 * kHeadDim;
 
-// A row's keys in the cache, for one wave's share of a block's copies.
-template <int kFmt>
+// A row's keys in the cache.
 struct Pages {
   const int32_t* table;  // the row's
   int n_pages, shift, last_key;
@@ -245,58 +242,43 @@ struct Pages {
   }
 };
 
-// One tensor's block in registers on its way to LDS (FP8, FP4).
+// One tensor's block in registers on its way to LDS (FP8, FP4): of a wave 16 keys.
 template <int kFmt>
 struct Staged {
-  static constexpr int kLoads = kFmt == kCacheFp8 ? 4 : 2;
-  static constexpr int kRows = kFmt == kCacheFp8 ? 8 : 16;  // of one load of a wave
+  static constexpr int kLoads = kFmt == kCacheFp8 ? 2 : 1;
+  static constexpr int kRows = 16 / kLoads;  // of one load; 16 bytes to a lane
   uint4 codes[kLoads];
-  uint32_t scale[kLoads];
-  // Load k of the wave has rows kRows (wave + 4 k) ..; 16 bytes to a lane.
-  static __device__ __forceinline__ int row_of(int k) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    return kRows * (wave + kWaves * k) + lane / (64 / kRows);
-  }
-  __device__ __forceinline__ void load(const Pages<kFmt>& pages, const char* base, const char* scales, int block) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int piece = lane % (64 / kRows);
+  uint32_t scale;
+  // The wave's keys lie at `at`; past the row's last key, which is key `last` of them, that one again.
+  __device__ __forceinline__ void load(const char* base, const char* scales, int64_t at, uint32_t tok_bytes, int last) {
+    const int lane = threadIdx.x & 63, piece = lane % (64 / kRows);
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {
-      const int j0 = block * kBlock + kRows * (wave + kWaves * k), j16 = j0 & ~15;
-      const int64_t at = pages.at(j16);
-      // Keys past the row's last one: that one again.
-      const int last = pages.last_key - min(j16, pages.last_key & ~15);
-      const int r = j16 > pages.last_key ? last : min((j0 & 15) + lane / (64 / kRows), last);
-      codes[k] = *reinterpret_cast<const uint4*>(base + at + (uint32_t)r * pages.tok_bytes + 16u * piece);
-      if (kFmt == kCacheFp4) scale[k] = *reinterpret_cast<const uint8_t*>(scales + (at >> 4) + (uint32_t)r * (pages.tok_bytes >> 4) + piece);
+      const uint32_t r = (uint32_t)min(kRows * k + lane / (64 / kRows), last);
+      codes[k] = *reinterpret_cast<const uint4*>(base + at + r * tok_bytes + 16u * piece);
+      if (kFmt == kCacheFp4) scale = *reinterpret_cast<const uint8_t*>(scales + (at >> 4) + r * (tok_bytes >> 4) + piece);
     }
   }
-  __device__ __forceinline__ void store(unsigned char* lds, bool is_v) const {
-    const int piece = (threadIdx.x & 63) % (64 / kRows);
+  // Piece p (of 4) of the lane's elements to the block's row.
+  __device__ __forceinline__ void store(unsigned char* lds, bool is_v, int p) const {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, piece = lane % (64 / kRows);
+    constexpr int kPieces = kFmt == kCacheFp8 ? 2 : 4;  // of 16 bytes, of a load
+    const int k = p / kPieces, row = 16 * wave + kRows * k + lane / (64 / kRows), c = kPieces * piece + p % kPieces;
+    const uint32_t w[4] = {codes[k].x, codes[k].y, codes[k].z, codes[k].w};
+    uint4 v;
+    if constexpr (kFmt == kCacheFp8) {
+      uint32_t x[4];
 #pragma unroll
-    for (int k = 0; k < kLoads; ++k) {
-      const int row = row_of(k);
-      unsigned char* out = lds + row * 256;
-      const uint32_t w[4] = {codes[k].x, codes[k].y, codes[k].z, codes[k].w};
-      constexpr int kPieces = kFmt == kCacheFp8 ? 2 : 4;  // of 16 bytes
-#pragma unroll
-      for (int p = 0; p < kPieces; ++p) {
-        const int c = kPieces * piece + p;
-        uint4 v;
-        if constexpr (kFmt == kCacheFp8) {
-          uint32_t x[4];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            x[2 * e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w[2 * p + e], 1.f, false));
-            x[2 * e + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w[2 * p + e], 1.f, true));
-          }
-          v = make_uint4(x[0], x[1], x[2], x[3]);
-        } else {
-          v = widen_e2m1(w[p], scale[k] << 23);
-        }
-        *reinterpret_cast<uint4*>(out + 16 * (is_v ? vswz(row, c) : kswz(row, c))) = v;
+      for (int e = 0; e < 2; ++e) {
+        const int z = (int)w[2 * (p % kPieces) + e];
+        x[2 * e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(z, 1.f, false));
+        x[2 * e + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(z, 1.f, true));
       }
+      v = make_uint4(x[0], x[1], x[2], x[3]);
+    } else {
+      v = widen_e2m1(w[p], scale << 23);
     }
+    *reinterpret_cast<uint4*>(lds + row * 256 + 16 * (is_v ? vswz(row, c) : kswz(row, c))) = v;
   }
 };
 
@@ -323,68 +305,121 @@ __device__ __forceinline__ void write_query(const PrefillArgs& a, int head, int 
     a.lse[(int64_t)head * a.n_tokens + tok] = l_exact == 0.f ? -INFINITY : (m + log2f(l_exact)) / kLog2e;
 }
 
-// What the workgroup's tiles in LDS are.
+// x, of which the compiler knows nothing here: what is made of it is made where it is
+// used, and not kept in registers over the steps.
+template <typename T>
+__device__ __forceinline__ T anew(T x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+template <typename T>
+__device__ __forceinline__ T anew_s(T x) {
+  asm volatile("" : "+s"(x));
+  return x;
+}
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// The workgroup's LDS: two blocks of K and two of V, and
 struct Tiles {
   unsigned char* k;
   unsigned char* v;
-  int* bad;  // [kBlock]: the key's value is not finite
+  int* bad;  // [kKeys]: the key's value is not finite
 };
 
+__device__ __forceinline__ bool not_finite(uint32_t pair) {
+  return (pair & 0x7f80u) == 0x7f80u || (pair & 0x7f800000u) == 0x7f800000u;
+}
+
 // Masked blocks: a weight of 0 times a value that is not finite would be NaN, so
-// such values are taken out of the tile and added to the queries that attend them.
-// (Weights are positive, so the sum is the same whatever they are.)
-__device__ __forceinline__ void take_out(const Tiles& t, int limit, f32x16* o, int half) {
+// such values are taken out of the block and added to the queries that attend them.
+// (Weights are positive, so the sum is the same whatever they are.)  limit: the
+// lane's last key in the block.
+__device__ __forceinline__ void take_out(unsigned char* v, int* bad, int limit, f32x16* o) {
+  constexpr int kLoads = kBlockBytes / 16 / kThreads;
+  const int tid = anew((int)threadIdx.x), half = (tid & 63) >> 5;
+  bool any = false;
+#pragma unroll
+  for (int k = 0; k < kLoads; ++k) {
+    const uint4 w = *reinterpret_cast<const uint4*>(v + 16 * (tid + kThreads * k));
+    any |= not_finite(w.x) || not_finite(w.y) || not_finite(w.z) || not_finite(w.w);
+  }
+  if (!__syncthreads_or(any)) return;
+  if (tid < kKeys) bad[tid] = 0;
+  __syncthreads();
 #pragma unroll 1
-  for (int key = 0; key < kBlock; ++key) {
-    if (__builtin_amdgcn_readfirstlane(t.bad[key]) == 0) continue;
+  for (int k = 0; k < kLoads; ++k) {
+    const uint4 w = *reinterpret_cast<const uint4*>(v + 16 * (tid + kThreads * k));
+    if (not_finite(w.x) || not_finite(w.y) || not_finite(w.z) || not_finite(w.w)) bad[(tid + kThreads * k) >> 4] = 1;
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int key = 0; key < kKeys; ++key) {
+    if (__builtin_amdgcn_readfirstlane(bad[key]) == 0) continue;
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
       for (int rq = 0; rq < 4; ++rq) {
         const int d = 32 * dt + 8 * rq + 4 * half;
-        const uint2 w = *reinterpret_cast<const uint2*>(t.v + key * 256 + 16 * vswz(key, d >> 3) + 2 * (d & 7));
+        const uint2 w = *reinterpret_cast<const uint2*>(v + key * 256 + 16 * vswz(key, d >> 3) + 2 * (d & 7));
         const float x[4] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           if (key <= limit && !(fabsf(x[e]) < INFINITY)) o[dt][4 * rq + e] += x[e];
       }
   }
+  __syncthreads();
+#pragma unroll 1
+  for (int k = 0; k < 4 * kLoads; ++k) {
+    uint32_t* at = reinterpret_cast<uint32_t*>(v) + tid + kThreads * k;
+    uint32_t z = *at;
+    if ((z & 0x7f80u) == 0x7f80u) z &= 0xffff0000u;
+    if ((z & 0x7f800000u) == 0x7f800000u) z &= 0xffffu;
+    *at = z;
+  }
+  __syncthreads();
 }
 
+// The order of instructions is that of the source here.
+__device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
+
+// One unit.  A step takes a block of 64 keys: the first product of the next block
+// runs beside the exponentials of this one, and this one's second product beside
+// the next one's maximum, an instruction of each in turn, so that the matrix core
+// and the vector unit work at the same time.  One barrier to a step, at its start:
+// the next K and this V are there, and the buffers of this K and the last V are free
+// for the copies of the K after the next and the next V.
 template <int kFmt, bool kLse>
-__device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& rows, const Unit& n, int piece, int g, const Tiles& t,
-                                            float* slot) {
-  constexpr int KT = kBlock / 32;
+__device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& rows, const Unit& n, int piece, int g,
+                                            const Tiles& t, float* slot) {
   constexpr bool kCopied = kFmt == kCacheBf16;  // straight to LDS
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, l32 = lane & 31;
   const int group = a.n_q_heads / a.n_kv_heads;
-  const int64_t queries = (int64_t)n.tokens * group, x0 = (int64_t)n.tile * kBlock;
+  const int64_t queries = (int64_t)n.tokens * group, x0 = (int64_t)n.tile * kQueries;
   const int64_t cap = (int64_t)a.max_pages << a.cache.page_shift;
   const int before = n.len - n.tokens;  // position of the row's first new token
   const int held = (int)min((int64_t)n.len, cap);
-  const int tile_last = min(before + (int)((min(x0 + kBlock, queries) - 1) / group), held - 1);
+  const int tile_last = min(before + (int)((min(x0 + kQueries, queries) - 1) / group), held - 1);
   const int first_last = min(before + (int)(x0 / group), held - 1);  // the last key of the tile's first query
-  const int blocks = tile_last < 0 ? 0 : tile_last / kBlock + 1;
+  const int blocks = tile_last < 0 ? 0 : tile_last / kKeys + 1;
   const int b0 = piece == INT_MAX ? 0 : n.part * piece;
   const int b1 = piece == INT_MAX ? blocks : min(blocks, b0 + piece);
-  const int plain = min(b1, (first_last + 1) / kBlock);  // blocks before it are attended whole
+  const int plain = (first_last + 1) / kKeys;  // blocks before it are attended whole
 
   // The lane's query (past the row's last one: that one, and not written).
-  const int64_t x = x0 + 32 * wave + l32;
-  const bool ok = x < queries;
-  const int i = (int)((ok ? x : queries - 1) / group);
-  const int head = g * group + (int)((ok ? x : queries - 1) - (int64_t)i * group), tok = n.begin + i;
-  const int last = min(before + i, held - 1);  // its last key
+  int last;  // its last key
   bf16x8 q[8];
   {
+    const int64_t x = min(x0 + 32 * wave + l32, queries - 1);
+    const int i = (int)(x / group), head = g * group + (int)(x - (int64_t)i * group), tok = n.begin + i;
+    last = min(before + i, held - 1);
     const uint16_t* row = a.Q + head * a.q_head + tok * a.q_tok + 8 * half;
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) q[ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(row + 16 * ks));
   }
-  RBS_WAIT_VMCNT(0);  // (a wait for Q inside the loop would be one for the copies too)
 
-  Pages<kFmt> pages;
+  Pages pages;
   pages.table = rows.page_table + (int64_t)n.row * a.max_pages;
   pages.n_pages = a.cache.n_pages;
   pages.shift = a.cache.page_shift;
@@ -398,295 +433,288 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& ro
   const char* Vs = static_cast<const char*>(a.cache.V_scale) + g * a.cache.head / 32;
   const float scale_log2 = a.scale * kLog2e * head_factor<kFmt>(a, g);
 
-  // BF16: the wave copies keys 32 wave .. + 31 of a block, in eight copies of four.  A
-  // workgroup's copies all at once would hold its waves up at their issue, so that
-  // half of a tensor's go out as its tile becomes free and the others in pairs among the
-  // matrix and exponential steps.
-  const uint32_t k_lds = __builtin_amdgcn_readfirstlane(lds_offset(t.k) + (uint32_t)wave * 8192u);
-  const uint32_t v_lds = __builtin_amdgcn_readfirstlane(lds_offset(t.v) + (uint32_t)wave * 8192u);
-  uint32_t k_off[4], v_off;
-  {
-    const int l4 = lane >> 4, pc = lane & 15;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) k_off[j] = (uint32_t)(4 * j + l4) * pages.tok_bytes + 16u * (uint32_t)kswz(4 * j + l4, pc);
-    v_off = (uint32_t)l4 * pages.tok_bytes + 16u * (uint32_t)vswz(l4, pc);
-  }
-  int64_t at_k[2], at_v[2];  // where the wave's two runs of 16 keys are, of the block whose K (V) is copied
-  auto find = [&](int block) __attribute__((always_inline)) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) at_k[h] = pages.at(block * kBlock + 32 * wave + 16 * h);
+  // The wave moves keys 16 wave .. + 15 of each block (all in one page).
+  auto key0 = [&](int b) __attribute__((always_inline)) { return b * kKeys + 16 * wave; };
+  auto last_of = [&](int b) __attribute__((always_inline)) {  // the row's last key among them (15 if it is behind them)
+    const int j = key0(b);
+    return j > pages.last_key ? (pages.last_key & 15) : min(15, pages.last_key - j);
   };
-  auto copy_pair = [&](bool is_v, int j) __attribute__((always_inline)) {  // copies j and j + 1 of 8
-    const int64_t* from = is_v ? at_v : at_k;
+  // BF16: four copies of four keys each, straight to LDS; copies c and c + 1.  Offset of
+  // a lane in a run of 16 keys: row 4 c + lane / 16, piece lane % 16 as it is swizzled.
+  uint32_t k_lds = __builtin_amdgcn_readfirstlane(lds_offset(t.k) + (uint32_t)wave * 4096u);
+  uint32_t v_lds = __builtin_amdgcn_readfirstlane(lds_offset(t.v) + (uint32_t)wave * 4096u);
+  const uint32_t row_off = (uint32_t)(lane >> 4) * pages.tok_bytes;
+  const uint32_t k_piece = 16u * (uint32_t)kswz(lane >> 4, lane & 15), v_piece = 16u * (uint32_t)vswz(lane >> 4, lane & 15);
+  auto copy = [&](bool is_v, int buf, int64_t at, int c0) __attribute__((always_inline)) {
+    const char* run = (is_v ? V : K) + at;
+    const uint32_t row_off_ = anew(row_off), tok_bytes = anew_s(pages.tok_bytes);
+    const uint32_t lds = (is_v ? v_lds : k_lds) + (uint32_t)(buf * kBlockBytes);
 #pragma unroll
-    for (int c = j; c < j + 2; ++c) {
-      const char* run = (is_v ? V : K) + from[c >> 2];
-      lds_dma16(is_v ? run + (size_t)(4 * (c & 3)) * pages.tok_bytes : run, is_v ? v_off : k_off[c & 3],
-                (is_v ? v_lds : k_lds) + 1024u * c);
-    }
+    for (int c = c0; c < c0 + 2; ++c)
+      lds_dma16(run + (size_t)(4 * c) * tok_bytes, row_off_ + (is_v ? v_piece : k_piece ^ (64u * c)), lds + 1024u * c);
   };
-  // Half of a block's copies, or where the row's last key is among its keys or before them, all: past it, that one again.
-  auto copy_head = [&](int block, bool is_v) __attribute__((always_inline)) {
-    const int64_t* from = is_v ? at_v : at_k;
-    const int j0 = block * kBlock + 32 * wave;
-    if (j0 + 31 <= pages.last_key) {
-      copy_pair(is_v, 0);
-      copy_pair(is_v, 2);
-    } else {
+  // All four, where the row's last key may be among them or before them: past it, that one again.
+  auto copy_last = [&](bool is_v, int buf, int64_t at, int b) __attribute__((always_inline)) {
+    const char* run = (is_v ? V : K) + at;
+    const uint32_t lds = (is_v ? v_lds : k_lds) + (uint32_t)(buf * kBlockBytes);
+    const int top = last_of(b), l = anew(lane);
 #pragma unroll 1
-      for (int c = 0; c < 8; ++c) {
-        const int j16 = j0 + 16 * (c >> 2), r = 4 * (c & 3) + (lane >> 4);
-        const int top = pages.last_key - min(j16, pages.last_key & ~15);
-        const int row = j16 > pages.last_key ? top : min(r, top);
-        const int at = is_v ? vswz(r, lane & 15) : kswz(r, lane & 15);
-        lds_dma16((is_v ? V : K) + from[c >> 2], (uint32_t)row * pages.tok_bytes + 16u * (uint32_t)at,
-                  (is_v ? v_lds : k_lds) + 1024u * c);
-      }
+    for (int c = 0; c < 4; ++c) {
+      const int r = 4 * c + (l >> 4), piece_at = is_v ? vswz(r, l & 15) : kswz(r, l & 15);
+      lds_dma16(run, (uint32_t)min(r, top) * pages.tok_bytes + 16u * (uint32_t)piece_at, lds + 1024u * c);
     }
   };
-  auto has_rest = [&](int block) __attribute__((always_inline)) { return block * kBlock + 32 * wave + 31 <= pages.last_key; };
   Staged<kCopied ? kCacheFp8 : kFmt> k_next, v_next;
 
+  // Operands from LDS.  K: row 32 mt + l32, pieces 2 ks + half.  V (transposed): rows
+  // 16 c + 4 half + (lane % 16) / 4 (and + 8), elements 32 dt + 16 ((lane / 16) % 2) + 4 (lane % 4).
+  // (The swizzled offsets are made as they are used: kept, they would take twelve registers.)
   const int vq = (lane & 15) >> 2;
-  const int vsub = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-  const int vbyte = 8 * (lane & 1);
-  // Row m of the denominator's left operand takes the keys of lanes' halves of
-  // parity m % 2: lane l finds its query's sum in element (l / 16) % 2 (attend_block.hpp).
-  bf16x8 lsel;
-  {
-    const __bf16 one = (((lane >> 4) & 1) == (lane & 1)) ? (__bf16)1.0f : (__bf16)0.0f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) lsel[e] = one;
-  }
-  f32x4 lacc{};
-  auto l_of = [&]() __attribute__((always_inline)) { return ((lane >> 4) & 1) ? lacc[1] : lacc[0]; };
-  float l_exact = 0.f;  // this half wave's, of the weights before their rounding
-  bool is_nan = false;  // the lane's query has a weight that is NaN
+  uint32_t k_row = lds_offset(t.k) + (uint32_t)l32 * 256u, k_swz = 16u * (uint32_t)kswz(l32, half);
+  uint32_t v_row = lds_offset(t.v) + (uint32_t)(4 * half + vq) * 256u + 8u * (lane & 1);
+  uint32_t v_swz = 16u * (uint32_t)vswz(vq, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1));
+  typedef const __attribute__((address_space(3))) u32x4 lds_u32x4;
+  auto k_frag = [&](int buf, int f) __attribute__((always_inline)) {  // f = 2 ks + mt
+    const uint32_t at = k_row + (k_swz ^ (32u * (f >> 1)));
+    return __builtin_bit_cast(bf16x8, *(lds_u32x4*)(uintptr_t)(at + (uint32_t)(buf * kBlockBytes + (f & 1) * 8192)));
+  };
+  auto v_frag = [&](int buf, int f) __attribute__((always_inline)) {  // f = 4 c + dt
+    const uint32_t at = v_row + (v_swz ^ (64u * (f & 3))) + (uint32_t)(buf * kBlockBytes + (f >> 2) * 4096);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)at);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(at + 8 * 256));
+    bf16x8 v;
+    __builtin_memcpy(&v, &lo, 8);
+    __builtin_memcpy(reinterpret_cast<unsigned char*>(&v) + 8, &hi, 8);
+    return v;
+  };
+
+  float l = 0.f, l_exact = 0.f;  // this half wave's sums, of the weights as they are rounded and before it
   f32x16 o[4];
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt) o[dt] = f32x16{};
-  float m = -INFINITY;
+  float m = -INFINITY, shift = 0.f;  // the reference of the exponentials; shift: 0 where it is -inf
 
-  auto attend = [&](auto masked_of, int b) __attribute__((always_inline)) {
-    constexpr bool masked = decltype(masked_of)::value;
-    const bool more = b + 1 < b1;
-    if constexpr (kCopied) {
-      RBS_WAIT_VMCNT(4);  // this block's K; its V may still be on its way
-    } else {
-      k_next.store(t.k, false);
+  auto mask = [&](f32x16* s, int b) __attribute__((always_inline)) {
+    const int limit = anew(last) - b * kKeys;
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) {
+      const int lim = limit - 32 * mt - 4 * half;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[mt][r] = (8 * (r >> 2) + (r & 3)) > lim ? -INFINITY : s[mt][r];
     }
-    __syncthreads();
-    const bool v_rest = kCopied && b > b0 && has_rest(b);
-    if (kCopied && more) find(b + 1);
-    if constexpr (!kCopied)
-      if (more) k_next.load(pages, K, Ks, b + 1);
-
-    f32x16 s[KT];
-#pragma unroll
-    for (int mt = 0; mt < KT; ++mt) {
-      s[mt] = f32x16{};
-      const int row = 32 * mt + l32;
-      const unsigned char* krow = t.k + row * 256;
-#pragma unroll
-      for (int ks = 0; ks < 8; ++ks) {
-        const uint4 w = *reinterpret_cast<const uint4*>(krow + 16 * kswz(row, 2 * ks + half));
-        s[mt] = mfma_bf16(__builtin_bit_cast(bf16x8, w), q[ks], s[mt]);
-      }
-      if (kCopied && mt < 2) {
-        __builtin_amdgcn_sched_barrier(0);
-        if (v_rest) copy_pair(true, 4 + 2 * mt);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-    __syncthreads();  // every wave is done with this K
-    const bool k_rest = kCopied && more && has_rest(b + 1);
-    if constexpr (kCopied)
-      if (more) copy_head(b + 1, false);
-    const int limit = last - b * kBlock;  // the lane's last key in this block
-    if constexpr (masked) {
-#pragma unroll
-      for (int mt = 0; mt < KT; ++mt) {
-        const int lim = limit - 32 * mt - 4 * half;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[mt][r] = (8 * (r >> 2) + (r & 3)) > lim ? -INFINITY : s[mt][r];
-          __builtin_amdgcn_sched_barrier(0);  // (64 compares' masks at once would not fit the scalar registers)
-        }
-      }
-    }
+  };
+  auto top_of = [&](const f32x16* s) __attribute__((always_inline)) {
     float top = -INFINITY;
 #pragma unroll
-    for (int mt = 0; mt < KT; ++mt)
+    for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, s[mt][r]);
-    top = half_max(top) * scale_log2;
-    if (__any(top > m + kRescaleSlack)) {
-      // (Each query for itself: its result does not depend on the wave's others.)
-      const float m_new = top > m + kRescaleSlack ? top : m;
-      const float f = m_new == m ? 1.f : fast_exp2(m - m_new);
-      m = m_new;
-      l_exact *= f;
+    return top;
+  };
+  // The reference follows a maximum that exceeds it by much.  (Each query for itself:
+  // its result does not depend on the wave's others.)
+  auto follow = [&](float top) __attribute__((always_inline)) {
+    const float m_new = top > m + kRescaleSlack ? top : m;
+    const float f = m_new == m ? 1.f : fast_exp2(m - m_new);
+    m = m_new;
+    shift = m == -INFINITY ? 0.f : m;
+    l *= f;
+    l_exact *= f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) lacc[e] *= f;
+    for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-      for (int dt = 0; dt < 4; ++dt)
+      for (int r = 0; r < 16; ++r) o[dt][r] *= f;
+  };
+
+  int64_t at0, at1, at2;  // where the keys of blocks b + 1, b + 2 and b + 3 are
+  f32x16 s0[2], s1[2];
+  uint32_t pw[16];  // the weights, pairs in bf16
+  auto exponentials = [&](const f32x16* s, int j) __attribute__((always_inline)) {  // of pair j
+    const float e0 = fast_exp2(fmaf(s[j >> 3][2 * (j & 7)], scale_log2, -shift));
+    const float e1 = fast_exp2(fmaf(s[j >> 3][2 * (j & 7) + 1], scale_log2, -shift));
+    if (kLse) l_exact += e0 + e1;
+    pw[j] = two_bf16(e0, e1);
+    const uint32_t ones = 0x3f803f80u;
+    l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw[j]), __builtin_bit_cast(bf16x2, ones), l, false);
+  };
+  auto weights = [&](int c) __attribute__((always_inline)) {  // of 16 keys
+    return __builtin_bit_cast(bf16x8, make_uint4(pw[4 * c], pw[4 * c + 1], pw[4 * c + 2], pw[4 * c + 3]));
+  };
+  auto logits = [&](int buf, f32x16* s) __attribute__((always_inline)) {
+    bf16x8 f[kAhead];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[dt][r] *= f;
+    for (int k = 0; k < kAhead; ++k) f[k] = k_frag(buf, k);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      fence();
+      s[k & 1] = mfma_bf16(f[k % kAhead], q[k >> 1], k < 2 ? f32x16{} : s[k & 1]);
+      if (k + kAhead < 16) f[k % kAhead] = k_frag(buf, k + kAhead);
     }
-    const float shift = m == -INFINITY ? 0.f : m;
-    bf16x8 p[kBlock / 16];
-#pragma unroll
-    for (int mt = 0; mt < KT; ++mt) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[mt][r] = fast_exp2(fmaf(s[mt][r], scale_log2, -shift));
-      if (kLse) {
-        float sum[4] = {};
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sum[r & 3] += s[mt][r];
-        l_exact += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      }
-#pragma unroll
-      for (int e = 0; e < 16; ++e) p[2 * mt + (e >> 3)][e & 7] = (__bf16)s[mt][e];
-      if (kCopied && mt < 2) {
-        __builtin_amdgcn_sched_barrier(0);
-        if (k_rest) copy_pair(false, 4 + 2 * mt);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-    const f32x4 lacc_before = lacc;
-#pragma unroll
-    for (int c = 0; c < kBlock / 16; ++c) lacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lsel, p[c], lacc, 0, 0, 0);
-    if (__any(l_of() != l_of())) {
-      // That product has two queries to a column, one of them times 0: a query with a
-      // NaN takes no part in it.
-#pragma unroll
-      for (int c = 0; c < kBlock / 16; ++c)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) is_nan |= (float)p[c][e] != (float)p[c][e];
-      is_nan = half_max(is_nan ? 1.f : 0.f) > 0.f;
-      lacc = lacc_before;
-#pragma unroll 1
-      for (int again = 0; again < 1; ++again) {
-#pragma unroll
-        for (int c = 0; c < kBlock / 16; ++c) {
-          const bf16x8 z{};
-          lacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lsel, is_nan ? z : p[c], lacc, 0, 0, 0);
-        }
-      }
-    }
-    if constexpr (kCopied) {
-      if (more) RBS_WAIT_VMCNT(8); else RBS_WAIT_VMCNT(0);  // this block's V
-    } else {
-      v_next.store(t.v, true);
-    }
+    fence();
+  };
+  // A step of block b, in buffers kBuf: its logits in s, the next block's to s_next.
+  // For blocks attended whole that have at least four more behind them.
+  auto step = [&](auto buf_of, int b, const f32x16* s, f32x16* s_next) __attribute__((always_inline)) {
+    constexpr int kBuf = decltype(buf_of)::value;
+    if constexpr (kCopied) RBS_WAIT_VMCNT(0);
     __syncthreads();
-    if constexpr (!kCopied)
-      if (more) v_next.load(pages, V, Vs, b + 1);
-    if constexpr (masked) {
-      // Does the block hold a value that is not finite?
-      bool bad = false;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const uint4 w = *reinterpret_cast<const uint4*>(t.v + 16 * (tid + kThreads * k));
-        const uint32_t z[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) bad |= (z[e] & 0x7f80u) == 0x7f80u || (z[e] & 0x7f800000u) == 0x7f800000u;
+    // (Opaque: sums of these with constants are not kept in registers from step to step.)
+    asm volatile("" : "+v"(k_row), "+v"(v_row), "+s"(k_lds), "+s"(v_lds));
+    asm volatile("" : "+v"(k_swz), "+v"(v_swz));
+    const int64_t at_v = at0, at_k = at1;
+    at0 = at1;
+    at1 = at2;
+    at2 = pages.at(key0(b + 4));
+    // What goes to the free buffers, in four parts.
+    auto move = [&](int part) __attribute__((always_inline)) {
+      if constexpr (kCopied) {
+        if (part < 2) copy(false, kBuf, at_k, 2 * part);
+        else copy(true, kBuf ^ 1, at_v, 2 * (part - 2));
+      } else if (part < 2) {
+        k_next.store(t.k + kBuf * kBlockBytes, false, 2 * part);
+        k_next.store(t.k + kBuf * kBlockBytes, false, 2 * part + 1);
+        if (part == 1) k_next.load(K, Ks, at1, pages.tok_bytes, 15);
+      } else {
+        v_next.store(t.v + (kBuf ^ 1) * kBlockBytes, true, 2 * (part - 2));
+        v_next.store(t.v + (kBuf ^ 1) * kBlockBytes, true, 2 * (part - 2) + 1);
+        if (part == 3) v_next.load(V, Vs, at0, pages.tok_bytes, 15);
       }
-      if (__syncthreads_or(bad)) {
-        if (tid < kBlock) t.bad[tid] = 0;
-        __syncthreads();
-#pragma unroll 1
-        for (int k = 0; k < 8; ++k) {
-          const uint4 w = *reinterpret_cast<const uint4*>(t.v + 16 * (tid + kThreads * k));
-          const uint32_t z[4] = {w.x, w.y, w.z, w.w};
+    };
+    // First product of the next block; three quarters of the exponentials.
+    bf16x8 f[kAhead];
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if ((z[e] & 0x7f80u) == 0x7f80u || (z[e] & 0x7f800000u) == 0x7f800000u) t.bad[(tid + kThreads * k) >> 4] = 1;
-        }
-        __syncthreads();
-        take_out(t, limit, o, half);
-        __syncthreads();
-#pragma unroll 1
-        for (int k = 0; k < 8; ++k) {
-          uint32_t* at = reinterpret_cast<uint32_t*>(t.v + 16 * (tid + kThreads * k));
-          for (int e = 0; e < 4; ++e) {
-            uint32_t z = at[e];
-            if ((z & 0x7f80u) == 0x7f80u) z &= 0xffff0000u;
-            if ((z & 0x7f800000u) == 0x7f800000u) z &= 0xffffu;
-            at[e] = z;
-          }
-        }
-        __syncthreads();
-      }
+    for (int k = 0; k < kAhead; ++k) f[k] = k_frag(kBuf ^ 1, k);
+    fence();
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      s_next[k & 1] = mfma_bf16(f[k % kAhead], q[k >> 1], k < 2 ? f32x16{} : s_next[k & 1]);
+      if (k + kAhead < 16) f[k % kAhead] = k_frag(kBuf ^ 1, k + kAhead);
+      if ((k & 3) != 3) exponentials(s, 3 * (k >> 2) + (k & 3));
+      else move(k >> 2);
+      fence();
     }
+    // Second product of this block; the last exponentials, and the next block's maximum.
 #pragma unroll
-    for (int c = 0; c < kBlock / 16; ++c) {
-      const int row0 = 16 * c + 4 * half + vq;
-      const unsigned char* v0 = t.v + row0 * 256 + vbyte;
-      const unsigned char* v1 = v0 + 8 * 256;
+    for (int k = 0; k < kAhead; ++k) f[k] = v_frag(kBuf, k);
+    fence();
+    float top = -INFINITY;
 #pragma unroll
-      for (int dt = 0; dt < 4; ++dt) {
-        const int pc = 16 * vswz(row0, 4 * dt + vsub);
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(v0 + pc));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(v1 + pc));
-        bf16x8 v;
-        __builtin_memcpy(&v, &lo, 8);
-        __builtin_memcpy(reinterpret_cast<unsigned char*>(&v) + 8, &hi, 8);
-        o[dt] = mfma_bf16(v, p[c], o[dt]);
-      }
+    for (int k = 0; k < 16; ++k) {
+      o[k & 3] = mfma_bf16(f[k % kAhead], weights(k >> 2), o[k & 3]);
+      if (k + kAhead < 16) f[k % kAhead] = v_frag(kBuf, k + kAhead);
+      if (k < 8 && (k & 1) == 1) exponentials(s, 12 + (k >> 1));
+      if (k >= 8)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, s_next[(k >> 2) & 1][4 * (k & 3) + e]);
+      fence();
     }
-    __syncthreads();  // every wave is done with this V
+    top = half_max(top) * scale_log2;
+    if (__any(top > m + kRescaleSlack)) follow(top);
+  };
+  // Any other block, in buffers buf: its logits in s0, then the next one's.
+  auto step_of_any = [&](int buf, int b) __attribute__((always_inline)) {
+    const bool more = b + 1 < b1, more2 = b + 2 < b1;
+    if constexpr (kCopied) RBS_WAIT_VMCNT(0);
+    __syncthreads();
+    asm volatile("" : "+v"(k_row), "+v"(v_row), "+v"(k_swz), "+v"(v_swz));
     if constexpr (kCopied) {
-      if (more) {
-        at_v[0] = at_k[0];
-        at_v[1] = at_k[1];
-        copy_head(b + 1, true);
+      if (more2) copy_last(false, buf, at1, b + 2);
+      if (more) copy_last(true, buf ^ 1, at0, b + 1);
+    } else {
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        if (more2) k_next.store(t.k + buf * kBlockBytes, false, p);
+        if (more) v_next.store(t.v + (buf ^ 1) * kBlockBytes, true, p);
       }
+      if (b + 3 < b1) k_next.load(K, Ks, at2, pages.tok_bytes, last_of(b + 3));
+      if (more2) v_next.load(V, Vs, at1, pages.tok_bytes, last_of(b + 2));
     }
+    at0 = at1;
+    at1 = at2;
+    at2 = pages.at(key0(min(b + 4, b1)));
+    if (b >= plain) take_out(t.v + buf * kBlockBytes, t.bad, last - b * kKeys, o);
+    if (more) logits(buf ^ 1, s1);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) exponentials(s0, j);
+    bf16x8 f[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) f[k] = v_frag(buf, k);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      fence();
+      o[k & 3] = mfma_bf16(f[k % kAhead], weights(k >> 2), o[k & 3]);
+      if (k + kAhead < 16) f[k % kAhead] = v_frag(buf, k + kAhead);
+    }
+    fence();
+    if (!more) return;
+    if (b + 1 >= plain) mask(s1, b + 1);
+    const float top = half_max(top_of(s1)) * scale_log2;
+    if (__any(top > m + kRescaleSlack)) follow(top);
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) s0[mt] = s1[mt];
   };
 
   if (b0 < b1) {
+    const int64_t at = pages.at(key0(b0));
+    at0 = pages.at(key0(b0 + 1));
+    at1 = pages.at(key0(b0 + 2));
+    at2 = pages.at(key0(b0 + 3));
+    const bool two = b0 + 1 < b1;
     if constexpr (kCopied) {
-      find(b0);
-      at_v[0] = at_k[0];
-      at_v[1] = at_k[1];
-#pragma unroll
-      for (int v = 0; v < 2; ++v) {
-        copy_head(b0, v != 0);
-        if (has_rest(b0)) {
-          copy_pair(v != 0, 4);
-          copy_pair(v != 0, 6);
-        }
-      }
+      copy_last(false, 0, at, b0);
+      copy_last(true, 0, at, b0);
+      if (two) copy_last(false, 1, at0, b0 + 1);
+      RBS_WAIT_VMCNT(0);
     } else {
-      k_next.load(pages, K, Ks, b0);
-      v_next.load(pages, V, Vs, b0);
+      k_next.load(K, Ks, at, pages.tok_bytes, last_of(b0));
+      v_next.load(V, Vs, at, pages.tok_bytes, last_of(b0));
+      Staged<kFmt> second;
+      second.load(K, Ks, at0, pages.tok_bytes, last_of(b0 + 1));
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        k_next.store(t.k, false, p);
+        v_next.store(t.v, true, p);
+        second.store(t.k + kBlockBytes, false, p);
+      }
+      if (b0 + 2 < b1) k_next.load(K, Ks, at1, pages.tok_bytes, last_of(b0 + 2));
+      if (two) v_next.load(V, Vs, at0, pages.tok_bytes, last_of(b0 + 1));
     }
+    __syncthreads();
+    logits(0, s0);
+    if (b0 >= plain) mask(s0, b0);
+    follow(half_max(top_of(s0)) * scale_log2);
+    int b = b0;
+    for (; b + 2 < plain && b + 5 < b1; b += 2) {
+      step(std::integral_constant<int, 0>{}, b, s0, s1);
+      step(std::integral_constant<int, 1>{}, b + 1, s1, s0);
+    }
+    for (int buf = 0; b < b1; ++b, buf ^= 1) step_of_any(buf, b);
   }
-  int b = b0;
-  for (; b < plain; ++b) attend(std::false_type{}, b);
-  for (; b < b1; ++b) attend(std::true_type{}, b);
 
   if (x0 + 32 * wave >= queries) return;  // (no query of the wave's)
-  const float l = is_nan ? __builtin_nanf("") : l_of();
+  const int64_t x = x0 + 32 * wave + (anew(lane) & 31);
+  l = half_sum(l);
   if (kLse) l_exact = half_sum(l_exact);
   if (n.parts == 1) {
-    if (ok) write_query(a, head, tok, half, o, m, l, kLse ? l_exact : l, head_factor<kFmt>(a, a.n_kv_heads + g));
+    const int i = (int)(x / group), head = g * group + (int)(x - (int64_t)i * group);
+    if (x < queries)
+      write_query(a, head, n.begin + i, half, o, m, l, kLse ? l_exact : l, head_factor<kFmt>(a, a.n_kv_heads + g));
     return;
   }
   // A piece: every lane's 64 elements in runs of four, a KB for the wave at a time.
   if (b0 < b1) {
     float* out = slot + wave * 32 * kHeadDim;
+    const int lane = anew((int)threadIdx.x) & 63;
 #pragma unroll
     for (int k = 0; k < 16; ++k)
       *reinterpret_cast<float4*>(out + 4 * (64 * k + lane)) = make_float4(o[k >> 2][4 * (k & 3)], o[k >> 2][4 * (k & 3) + 1],
                                                                         o[k >> 2][4 * (k & 3) + 2], o[k >> 2][4 * (k & 3) + 3]);
   }
   if (half == 0) {
-    float* sums = slot + kBlock * kHeadDim + 32 * wave + l32;
+    float* sums = slot + kQueries * kHeadDim + 32 * wave + l32;
     sums[0] = m;
-    sums[kBlock] = l;
-    if (kLse) sums[2 * kBlock] = l_exact;
+    sums[kQueries] = l;
+    if (kLse) sums[2 * kQueries] = l_exact;
   }
 }
 
@@ -695,26 +723,21 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                                                                                                          int room,
                                                                                                          RBS_ROWS_ARGS) {
   const Rows rows{page_table, seq_lens, cu_tokens};
-  __shared__ __align__(1024) unsigned char tiles[2 * kBlock * 256];
-  __shared__ int sums[4 * kWaves], bad[kBlock];
-  const Tiles t{tiles, tiles + kBlock * 256, bad};
+  __shared__ __align__(1024) unsigned char tiles[4 * kBlockBytes];
+  __shared__ int sums[4 * kWaves], bad[kKeys];
+  const Tiles t{tiles, tiles + 2 * kBlockBytes, bad};
   static_assert(sizeof(int) * (3 * kMaxRows + 1) <= sizeof(tiles), "the plan lies where the tiles will be");
   int* first = reinterpret_cast<int*>(tiles);
   const Plan plan{first, first + kMaxRows + 1, first + 2 * kMaxRows + 1, sums};
-  for (int b = blockIdx.x;; b += gridDim.x) {
-    const int piece = plan_units(a, rows, room, plan);
-    const int units = __builtin_amdgcn_readfirstlane(first[a.n_rows]);
-    const int bunch = bunch_of(units, a.n_kv_heads);
-    if (b >= slots_of(units, a.n_kv_heads, bunch)) return;
-    int g, i;
-    slot_of(b, a.n_kv_heads, bunch, &g, &i);
-    if (i < units) {
-      const Unit n = unit_of(a, rows, first, piece, i);
-      __syncthreads();  // every wave has read the offsets
-      attend_unit<kFmt, kLse>(a, rows, n, piece, g, t, n.parts > 1 ? a.workspace + (size_t)(g * units + i) * kPartFloats : nullptr);
-    }
-    __syncthreads();  // the tiles are free
-  }
+  const int piece = plan_units(a, rows, room, plan);
+  const int units = __builtin_amdgcn_readfirstlane(first[a.n_rows]);
+  const int bunch = bunch_of(units, a.n_kv_heads);
+  int g, i;
+  slot_of(blockIdx.x, a.n_kv_heads, bunch, &g, &i);
+  if (i >= units) return;
+  const Unit n = unit_of(a, rows, first, piece, i);
+  __syncthreads();  // every wave has read the offsets
+  attend_unit<kFmt, kLse>(a, rows, n, piece, g, t, n.parts > 1 ? a.workspace + (size_t)(g * units + i) * kPartFloats : nullptr);
 }
 
 // Joins the pieces of the tiles: a wave to 32 queries and 32 of their elements.
@@ -733,13 +756,13 @@ __global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArg
     const int g = b / units, i = b - g * units;
     const Unit n = unit_of(a, rows, first, piece, i);
     if (n.part != 0 || n.parts == 1) continue;
-    const int tiles = (int)(((int64_t)n.tokens * group + kBlock - 1) / kBlock);
-    const int64_t queries = (int64_t)n.tokens * group, x = (int64_t)n.tile * kBlock + 32 * wave + l32;
+    const int tiles = (int)(((int64_t)n.tokens * group + kQueries - 1) / kQueries);
+    const int64_t queries = (int64_t)n.tokens * group, x = (int64_t)n.tile * kQueries + 32 * wave + l32;
     if (x - l32 >= queries) continue;
     const int dt = blockIdx.y;
     const float* slots = a.workspace + (size_t)b * kPartFloats;
     const size_t step = (size_t)tiles * kPartFloats;
-    const int at = kBlock * kHeadDim + 32 * wave + l32;
+    const int at = kQueries * kHeadDim + 32 * wave + l32;
     float m = -INFINITY;
     for (int p = 0; p < n.parts; ++p) m = fmaxf(m, slots[p * step + at]);
     const float ref = m == -INFINITY ? 0.f : m;
@@ -753,7 +776,7 @@ __global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArg
       for (int k = 0; k < kBatch; ++k) {
         const float* slot = slots + min(p0 + k, n.parts - 1) * step;
         pm[k] = slot[at];
-        pl[k] = slot[at + kBlock];
+        pl[k] = slot[at + kQueries];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           w[k][e] = *reinterpret_cast<const float4*>(slot + wave * 32 * kHeadDim + 4 * (64 * (4 * dt + e) + lane));
@@ -764,7 +787,7 @@ __global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArg
         if (p0 + k >= n.parts || pl[k] == 0.f) continue;
         const float f = fast_exp2(pm[k] - ref);
         l += pl[k] * f;
-        if (a.lse != nullptr) l_exact += slots[(p0 + k) * step + at + 2 * kBlock] * f;
+        if (a.lse != nullptr) l_exact += slots[(p0 + k) * step + at + 2 * kQueries] * f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           o[4 * e] += w[k][e].x * f;
@@ -790,14 +813,14 @@ __global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArg
 template <int kFmt>
 hipError_t launch(const PrefillArgs& a, hipStream_t s) {
   const int group = a.n_q_heads / a.n_kv_heads;
-  // At most so many tiles of a KV head (of offsets that ascend; others are gone through in turns).
-  const int64_t tiles = (int64_t)a.n_tokens * group / kBlock + (a.n_rows < a.n_tokens ? a.n_rows : a.n_tokens);
+  // At most so many tiles of a KV head.
+  const int64_t tiles = (int64_t)a.n_tokens * group / kQueries + (a.n_rows < a.n_tokens ? a.n_rows : a.n_tokens);
   const int64_t most = (int64_t)a.max_pages << a.cache.page_shift;  // keys of a row
   const int64_t units = tiles * a.n_kv_heads;
-  const bool split = units < kUnits / 2 && most > kBlock;
+  const bool split = units < kUnits / 2 && most > kKeys;
   const int room = split ? kUnits / 2 / a.n_kv_heads : 0;
-  const int64_t slots = (split ? kUnits : units) + 64 + 8 * a.n_kv_heads;
-  const int grid = (int)(slots < (1 << 20) ? slots : (1 << 20));
+  // (Bunches round up a head's units, and the XCDs' shares of them.)
+  const int grid = (int)((split ? kUnits : units) + 64 + 8 * a.n_kv_heads);
   const auto kernel = a.lse != nullptr ? paged_prefill_kernel<kFmt, true> : paged_prefill_kernel<kFmt, false>;
   hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), 0, s, a, room, a.page_table, a.seq_lens, a.cu_tokens);
   if (split)

@@ -67,7 +67,8 @@ def test_caches(over, code):
 
 
 def test_largest_sizes_pass():
-    assert _prefill(shape=rbs.make_shape(1 << 24, 4, 2, 64), n_rows=4096, max_pages=(1 << 27) - 1, Q=None) == NULL
+    assert _prefill(shape=rbs.make_shape(1 << 24, 64, 2, 64), n_rows=4096, max_pages=(1 << 27) - 1, Q=None) == NULL
+    assert _prefill(shape=rbs.make_shape(1 << 24, 66, 2, 64)) == SHAPE
 
 
 def test_binding_checks():
