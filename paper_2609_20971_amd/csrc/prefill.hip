@@ -43,7 +43,6 @@ constexpr int kKeys = 64;                        // of a block
 constexpr int kBlockBytes = kKeys * 2 * kHeadDim;  // of K or V in LDS
 constexpr int kUnits = 1024;                     // pieces of a call whose tiles are split
 constexpr int kPartFloats = kQueries * kHeadDim + 3 * kQueries;  // weighted values, maxima, sums of rounded and exact weights
-constexpr int kAhead = 4;                        // operands on their way from LDS
 constexpr int kMost = 1 << 29;                   // counts stop here
 
 __device__ __forceinline__ int capped_add(int a, int b) { return min(a + b, kMost); }
@@ -236,7 +235,7 @@ struct Pages {
   uint32_t tok_bytes;
   // Byte offset of 16 keys from j0 (a multiple of 16) on, of the last ones where j0 is past them.
   __device__ __forceinline__ int64_t at(int j0) const {
-    const int j = __builtin_amdgcn_readfirstlane(min(j0, last_key & ~15));
+    const int j = min(j0, last_key & ~15);
     const int page = min(max(table[j >> shift], 0), n_pages - 1);
     return page * page_bytes + (int64_t)(j & ((1 << shift) - 1)) * tok_bytes;
   }
@@ -393,6 +392,7 @@ template <int kFmt, bool kLse>
 __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& rows, const Unit& n, int piece, int g,
                                             const Tiles& t, float* slot) {
   constexpr bool kCopied = kFmt == kCacheBf16;  // straight to LDS
+  constexpr int kAhead = kCopied ? 4 : 3;       // operands on their way from LDS
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, l32 = lane & 31;
   const int group = a.n_q_heads / a.n_kv_heads;
@@ -433,7 +433,9 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& ro
   const char* Vs = static_cast<const char*>(a.cache.V_scale) + g * a.cache.head / 32;
   const float scale_log2 = a.scale * kLog2e * head_factor<kFmt>(a, g);
 
-  // The wave moves keys 16 wave .. + 15 of each block (all in one page).
+  // The wave moves keys 16 wave .. + 15 of each block (all in one page).  Lane i holds
+  // where those of block window + i are: a page number's load, waited for once in 64
+  // blocks, would otherwise be one in every step.
   auto key0 = [&](int b) __attribute__((always_inline)) { return b * kKeys + 16 * wave; };
   auto last_of = [&](int b) __attribute__((always_inline)) {  // the row's last key among them (15 if it is behind them)
     const int j = key0(b);
@@ -468,18 +470,20 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& ro
 
   // Operands from LDS.  K: row 32 mt + l32, pieces 2 ks + half.  V (transposed): rows
   // 16 c + 4 half + (lane % 16) / 4 (and + 8), elements 32 dt + 16 ((lane / 16) % 2) + 4 (lane % 4).
-  // (The swizzled offsets are made as they are used: kept, they would take twelve registers.)
   const int vq = (lane & 15) >> 2;
-  uint32_t k_row = lds_offset(t.k) + (uint32_t)l32 * 256u, k_swz = 16u * (uint32_t)kswz(l32, half);
-  uint32_t v_row = lds_offset(t.v) + (uint32_t)(4 * half + vq) * 256u + 8u * (lane & 1);
-  uint32_t v_swz = 16u * (uint32_t)vswz(vq, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1));
+  uint32_t k_at[8], v_at[4];
+#pragma unroll
+  for (int ks = 0; ks < 8; ++ks) k_at[ks] = lds_offset(t.k) + (uint32_t)l32 * 256u + 16u * (uint32_t)kswz(l32, 2 * ks + half);
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+    v_at[dt] = lds_offset(t.v) + (uint32_t)(4 * half + vq) * 256u + 8u * (lane & 1) +
+               16u * (uint32_t)vswz(vq, 4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1));
   typedef const __attribute__((address_space(3))) u32x4 lds_u32x4;
   auto k_frag = [&](int buf, int f) __attribute__((always_inline)) {  // f = 2 ks + mt
-    const uint32_t at = k_row + (k_swz ^ (32u * (f >> 1)));
-    return __builtin_bit_cast(bf16x8, *(lds_u32x4*)(uintptr_t)(at + (uint32_t)(buf * kBlockBytes + (f & 1) * 8192)));
+    return __builtin_bit_cast(bf16x8, *(lds_u32x4*)(uintptr_t)(k_at[f >> 1] + (uint32_t)(buf * kBlockBytes + (f & 1) * 8192)));
   };
   auto v_frag = [&](int buf, int f) __attribute__((always_inline)) {  // f = 4 c + dt
-    const uint32_t at = v_row + (v_swz ^ (64u * (f & 3))) + (uint32_t)(buf * kBlockBytes + (f >> 2) * 4096);
+    const uint32_t at = v_at[f & 3] + (uint32_t)(buf * kBlockBytes + (f >> 2) * 4096);
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)at);
     const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(at + 8 * 256));
     bf16x8 v;
@@ -526,16 +530,31 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& ro
       for (int r = 0; r < 16; ++r) o[dt][r] *= f;
   };
 
-  int64_t at0, at1, at2;  // where the keys of blocks b + 1, b + 2 and b + 3 are
+  int window = 0;
+  int64_t places = 0;
+  auto look_up = [&](int b) __attribute__((always_inline)) {  // from block b on
+    window = b;
+    places = pages.at(key0(b + lane));
+  };
+  auto place_of = [&](int b) __attribute__((always_inline)) {  // called with ascending b
+    if (b >= window + 64) look_up(b);
+    const int lo = __builtin_amdgcn_readlane((int)(uint32_t)places, b - window);
+    const int hi = __builtin_amdgcn_readlane((int)(places >> 32), b - window);
+    return (int64_t)((uint64_t)(uint32_t)hi << 32 | (uint32_t)lo);
+  };
+  constexpr int kLead = kCopied ? 2 : 3;  // blocks that the loads of K are ahead; those of V are one behind them
+  int64_t at_v;                           // where the keys of the block whose V comes next are
   f32x16 s0[2], s1[2];
   uint32_t pw[16];  // the weights, pairs in bf16
-  auto exponentials = [&](const f32x16* s, int j) __attribute__((always_inline)) {  // of pair j
-    const float e0 = fast_exp2(fmaf(s[j >> 3][2 * (j & 7)], scale_log2, -shift));
-    const float e1 = fast_exp2(fmaf(s[j >> 3][2 * (j & 7) + 1], scale_log2, -shift));
+  auto weigh = [&](int j, float e0, float e1) __attribute__((always_inline)) {  // pair j
     if (kLse) l_exact += e0 + e1;
     pw[j] = two_bf16(e0, e1);
     const uint32_t ones = 0x3f803f80u;
     l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw[j]), __builtin_bit_cast(bf16x2, ones), l, false);
+  };
+  auto exponentials = [&](const f32x16* s, int j) __attribute__((always_inline)) {  // of pair j
+    weigh(j, fast_exp2(fmaf(s[j >> 3][2 * (j & 7)], scale_log2, -shift)),
+          fast_exp2(fmaf(s[j >> 3][2 * (j & 7) + 1], scale_log2, -shift)));
   };
   auto weights = [&](int c) __attribute__((always_inline)) {  // of 16 keys
     return __builtin_bit_cast(bf16x8, make_uint4(pw[4 * c], pw[4 * c + 1], pw[4 * c + 2], pw[4 * c + 3]));
@@ -559,25 +578,36 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& ro
     if constexpr (kCopied) RBS_WAIT_VMCNT(0);
     __syncthreads();
     // (Opaque: sums of these with constants are not kept in registers from step to step.)
-    asm volatile("" : "+v"(k_row), "+v"(v_row), "+s"(k_lds), "+s"(v_lds));
-    asm volatile("" : "+v"(k_swz), "+v"(v_swz));
-    const int64_t at_v = at0, at_k = at1;
-    at0 = at1;
-    at1 = at2;
-    at2 = pages.at(key0(b + 4));
+    asm volatile("" : "+s"(k_lds), "+s"(v_lds));  // (sums of these with constants are not kept from step to step)
+    const int64_t at = at_v, at_k = place_of(b + kLead);
+    at_v = at_k;
     // What goes to the free buffers, in four parts.
     auto move = [&](int part) __attribute__((always_inline)) {
       if constexpr (kCopied) {
         if (part < 2) copy(false, kBuf, at_k, 2 * part);
-        else copy(true, kBuf ^ 1, at_v, 2 * (part - 2));
+        else copy(true, kBuf ^ 1, at, 2 * (part - 2));
       } else if (part < 2) {
         k_next.store(t.k + kBuf * kBlockBytes, false, 2 * part);
         k_next.store(t.k + kBuf * kBlockBytes, false, 2 * part + 1);
-        if (part == 1) k_next.load(K, Ks, at1, pages.tok_bytes, 15);
+        if (part == 1) k_next.load(K, Ks, at_k, pages.tok_bytes, 15);
       } else {
         v_next.store(t.v + (kBuf ^ 1) * kBlockBytes, true, 2 * (part - 2));
         v_next.store(t.v + (kBuf ^ 1) * kBlockBytes, true, 2 * (part - 2) + 1);
-        if (part == 3) v_next.load(V, Vs, at0, pages.tok_bytes, 15);
+        if (part == 3) v_next.load(V, Vs, at, pages.tok_bytes, 15);
+      }
+    };
+    // The exponentials in three stages, a stage of three pairs at a time: none waits for
+    // the one before it.
+    float arg[2], exp[2];
+    auto stage = [&](int j) __attribute__((always_inline)) {
+      if (j >= 2 && j < 18) weigh(j - 2, exp[0], exp[1]);
+      if (j >= 1 && j < 17) {
+        exp[0] = fast_exp2(arg[0]);
+        exp[1] = fast_exp2(arg[1]);
+      }
+      if (j < 16) {
+        arg[0] = fmaf(s[j >> 3][2 * (j & 7)], scale_log2, -shift);
+        arg[1] = fmaf(s[j >> 3][2 * (j & 7) + 1], scale_log2, -shift);
       }
     };
     // First product of the next block; three quarters of the exponentials.
@@ -588,22 +618,19 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& ro
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
       s_next[k & 1] = mfma_bf16(f[k % kAhead], q[k >> 1], k < 2 ? f32x16{} : s_next[k & 1]);
-      if (k + kAhead < 16) f[k % kAhead] = k_frag(kBuf ^ 1, k + kAhead);
-      if ((k & 3) != 3) exponentials(s, 3 * (k >> 2) + (k & 3));
+      f[k % kAhead] = k + kAhead < 16 ? k_frag(kBuf ^ 1, k + kAhead) : v_frag(kBuf, k + kAhead - 16);
+      if ((k & 3) != 3) stage(3 * (k >> 2) + (k & 3));
       else move(k >> 2);
       fence();
     }
     // Second product of this block; the last exponentials, and the next block's maximum.
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) f[k] = v_frag(kBuf, k);
-    fence();
     float top = -INFINITY;
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
-      o[k & 3] = mfma_bf16(f[k % kAhead], weights(k >> 2), o[k & 3]);
-      if (k + kAhead < 16) f[k % kAhead] = v_frag(kBuf, k + kAhead);
-      if (k < 8 && (k & 1) == 1) exponentials(s, 12 + (k >> 1));
-      if (k >= 8)
+      o[k & 3] = mfma_bf16(f[(k + 16) % kAhead], weights(k >> 2), o[k & 3]);
+      if (k + kAhead < 16) f[(k + 16) % kAhead] = v_frag(kBuf, k + kAhead);
+      if (k < 6) stage(12 + k);
+      else if (k >= 8)
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = fmaxf(top, s_next[(k >> 2) & 1][4 * (k & 3) + e]);
       fence();
@@ -616,22 +643,20 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& ro
     const bool more = b + 1 < b1, more2 = b + 2 < b1;
     if constexpr (kCopied) RBS_WAIT_VMCNT(0);
     __syncthreads();
-    asm volatile("" : "+v"(k_row), "+v"(v_row), "+v"(k_swz), "+v"(v_swz));
+    const int64_t at = at_v, at_k = place_of(b + kLead);
+    at_v = at_k;
     if constexpr (kCopied) {
-      if (more2) copy_last(false, buf, at1, b + 2);
-      if (more) copy_last(true, buf ^ 1, at0, b + 1);
+      if (more2) copy_last(false, buf, at_k, b + 2);
+      if (more) copy_last(true, buf ^ 1, at, b + 1);
     } else {
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
         if (more2) k_next.store(t.k + buf * kBlockBytes, false, p);
         if (more) v_next.store(t.v + (buf ^ 1) * kBlockBytes, true, p);
       }
-      if (b + 3 < b1) k_next.load(K, Ks, at2, pages.tok_bytes, last_of(b + 3));
-      if (more2) v_next.load(V, Vs, at1, pages.tok_bytes, last_of(b + 2));
+      if (b + 3 < b1) k_next.load(K, Ks, at_k, pages.tok_bytes, last_of(b + 3));
+      if (more2) v_next.load(V, Vs, at, pages.tok_bytes, last_of(b + 2));
     }
-    at0 = at1;
-    at1 = at2;
-    at2 = pages.at(key0(min(b + 4, b1)));
     if (b >= plain) take_out(t.v + buf * kBlockBytes, t.bad, last - b * kKeys, o);
     if (more) logits(buf ^ 1, s1);
 #pragma unroll
@@ -655,29 +680,29 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& ro
   };
 
   if (b0 < b1) {
-    const int64_t at = pages.at(key0(b0));
-    at0 = pages.at(key0(b0 + 1));
-    at1 = pages.at(key0(b0 + 2));
-    at2 = pages.at(key0(b0 + 3));
+    look_up(b0);
+    const int64_t at = place_of(b0), at1 = place_of(b0 + 1);
     const bool two = b0 + 1 < b1;
     if constexpr (kCopied) {
       copy_last(false, 0, at, b0);
       copy_last(true, 0, at, b0);
-      if (two) copy_last(false, 1, at0, b0 + 1);
+      if (two) copy_last(false, 1, at1, b0 + 1);
+      at_v = at1;
       RBS_WAIT_VMCNT(0);
     } else {
       k_next.load(K, Ks, at, pages.tok_bytes, last_of(b0));
       v_next.load(V, Vs, at, pages.tok_bytes, last_of(b0));
       Staged<kFmt> second;
-      second.load(K, Ks, at0, pages.tok_bytes, last_of(b0 + 1));
+      second.load(K, Ks, at1, pages.tok_bytes, last_of(b0 + 1));
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
         k_next.store(t.k, false, p);
         v_next.store(t.v, true, p);
         second.store(t.k + kBlockBytes, false, p);
       }
-      if (b0 + 2 < b1) k_next.load(K, Ks, at1, pages.tok_bytes, last_of(b0 + 2));
-      if (two) v_next.load(V, Vs, at0, pages.tok_bytes, last_of(b0 + 1));
+      at_v = place_of(b0 + 2);
+      if (b0 + 2 < b1) k_next.load(K, Ks, at_v, pages.tok_bytes, last_of(b0 + 2));
+      if (two) v_next.load(V, Vs, at1, pages.tok_bytes, last_of(b0 + 1));
     }
     __syncthreads();
     logits(0, s0);
