@@ -73,141 +73,190 @@ __device__ __forceinline__ RowWork work_of_row(const PrefillArgs& a, int group, 
   return w;
 }
 
-// Where a workgroup keeps its plan.
-struct Plan {
-  int* first;   // [n_rows + 1]
-  int* tiles;   // [n_rows], a thread's rows for itself
-  int* blocks;
-  int* sums;    // [4 kWaves]
-};
+// What is to do, found by every workgroup for itself.  A KV head's units are numbered
+// row after row; of a row by pieces, so that neighbours read the same keys, and of a
+// piece by tiles, those with most keys first.
+//
+// The pieces: at most so many blocks to a unit that there are at most `room` units, the
+// smallest such number, tried from below four at a time (a count over the rows for
+// each); where there are as many tiles as that, whole tiles.
+__device__ __forceinline__ int pieces_of(int blocks, int piece) {
+  return piece == INT_MAX ? 1 : (blocks + piece - 1) / piece;
+}
 
-// The units of a KV head: first[row] of them before the row, first[n_rows] in all, at
-// most `piece` blocks to a unit; returns it.  Of the pieces that make at most `room`
-// units the smallest is taken, from below (a count over the rows for each try, four
-// at once); where there are as many tiles as that, whole tiles.
-__device__ __forceinline__ int plan_units(const PrefillArgs& a, const Rows& rows, int room, const Plan& plan) {
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, group = a.n_q_heads / a.n_kv_heads;
-  const int per = (a.n_rows + kThreads - 1) / kThreads;  // a thread's rows, one after another
-  const int row0 = min(t * per, a.n_rows), row1 = min(row0 + per, a.n_rows);
-  int* sums = plan.sums;
-  int tiles = 0;
-  float blocks = 0.f;  // (within 2^-12)
-  bool descends = false;
-  for (int r = row0; r < row1; ++r) {
-    const int begin = rows.cu_tokens[r], end = rows.cu_tokens[r + 1];
-    descends |= end < begin;
-    const RowWork w = work_of_row(a, group, begin, end, rows.seq_lens[r]);
-    plan.tiles[r] = w.tiles;
-    plan.blocks[r] = w.blocks;
-    tiles = capped_add(tiles, w.tiles);
-    blocks += (float)w.tiles * w.blocks;
-  }
-  if (__syncthreads_or(descends)) {  // no offsets: rows may lie over each other
-    for (int r = t; r <= a.n_rows; r += kThreads) plan.first[r] = 0;
-    __syncthreads();
-    return INT_MAX;
-  }
-  int piece = INT_MAX;
-  if (room > 0) {
-    // All tiles and all blocks.
-    const int all = wave_scan(tiles, capped_add);
-    for (int m = 1; m < 64; m *= 2) blocks += wave_xor_f(blocks, m);
-    if (lane == 63) {
-      sums[wave] = all;
-      sums[kWaves + wave] = __float_as_int(blocks);
-    }
-    __syncthreads();
-    int T = 0;
-    float B = 0.f;
-#pragma unroll
-    for (int v = 0; v < kWaves; ++v) {
-      T = capped_add(T, sums[v]);
-      B += __int_as_float(sums[kWaves + v]);
-    }
-    __syncthreads();
-    T = __builtin_amdgcn_readfirstlane(T);
-    if (T > 0 && T < room) {
-      // (All the blocks over all the room: nothing smaller will do.  With a tile's last
-      // piece as good as empty the second is enough.)
-      const int least = __builtin_amdgcn_readfirstlane(max((int)fminf(B * 0.999f / room, (float)kMost), 1));
-      const int enough = __builtin_amdgcn_readfirstlane((int)fminf(B * 1.001f / (room - T), (float)kMost) + 1);
-      piece = enough;
-      for (int p0 = least; p0 < enough && p0 < least + 8; p0 += 4) {
-        int units[4] = {};
-        for (int r = row0; r < row1; ++r) {
-          const int n = plan.tiles[r], m = plan.blocks[r];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) units[k] = capped_add(units[k], n * ((m + p0 + k - 1) / (p0 + k)));
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int x = wave_scan(units[k], capped_add);
-          if (lane == 63) sums[k * kWaves + wave] = x;
-        }
-        __syncthreads();
-        int found = 0;
-#pragma unroll
-        for (int k = 3; k >= 0; --k) {
-          int U = 0;
-#pragma unroll
-          for (int v = 0; v < kWaves; ++v) U = capped_add(U, sums[k * kWaves + v]);
-          if (U <= room) found = p0 + k;
-        }
-        __syncthreads();
-        found = __builtin_amdgcn_readfirstlane(found);
-        if (found > 0) {
-          piece = found;
-          break;
-        }
-      }
-    }
-  }
-  if (piece != INT_MAX) {
-    tiles = 0;
-    for (int r = row0; r < row1; ++r) {
-      const int n = plan.tiles[r] * ((plan.blocks[r] + piece - 1) / piece);
-      plan.tiles[r] = n;
-      tiles = capped_add(tiles, n);
-    }
-  }
-  const int x = wave_scan(tiles, capped_add);
-  if (lane == 63) sums[wave] = x;
-  __syncthreads();
-  int before = __builtin_amdgcn_update_dpp(0, x, 0x138, 0xf, 0xf, false), all = 0;  // wave_shr 1
-#pragma unroll
-  for (int v = 0; v < kWaves; ++v) {
-    if (v == wave) before = capped_add(before, all);
-    all = capped_add(all, sums[v]);
-  }
-  for (int r = row0; r < row1; ++r) {
-    plan.first[r] = before;
-    before = capped_add(before, plan.tiles[r]);
-  }
-  if (t == 0) plan.first[a.n_rows] = all;
-  __syncthreads();
-  return piece;
+// The numbers to try, given all tiles and all blocks of them (within 2^-12).
+struct Tries {
+  int least, enough;  // nothing smaller will do; with each tile's last piece as good as empty this will
+};
+__device__ __forceinline__ Tries tries_of(int tiles, float blocks, int room) {
+  Tries t;
+  t.least = __builtin_amdgcn_readfirstlane(max((int)fminf(blocks * 0.999f / room, (float)kMost), 1));
+  t.enough = __builtin_amdgcn_readfirstlane((int)fminf(blocks * 1.001f / (room - tiles), (float)kMost) + 1);
+  return t;
 }
 
 // A tile, or a piece of one.
 struct Unit {
   int row, begin, tokens, len;  // the row's first token in Q, how many, and its cached tokens
   int tile, part, parts;        // of the row; of the tile
+  int tiles, first;             // the row's tiles and its first unit
 };
 
-__device__ __forceinline__ Unit unit_of(const PrefillArgs& a, const Rows& rows, const int* first, int piece, int u) {
-  const int group = a.n_q_heads / a.n_kv_heads;
-  Unit n;
-  n.row = __builtin_amdgcn_readfirstlane(seq_of(first, a.n_rows, u));
-  const int local = __builtin_amdgcn_readfirstlane(u - first[n.row]);
-  n.begin = rows.cu_tokens[n.row];
-  n.tokens = rows.cu_tokens[n.row + 1] - n.begin;
-  n.len = rows.seq_lens[n.row];
-  const RowWork w = work_of_row(a, group, n.begin, n.begin + n.tokens, n.len);
-  const int tiles = max(w.tiles, 1);
-  n.parts = piece == INT_MAX ? 1 : (w.blocks + piece - 1) / piece;
-  // The same keys for neighbours; the tiles with most keys first.
+// Up to 64 rows: a row to a lane, every wave for itself, with one load's wait and no
+// barrier.
+struct WavePlan {
+  int begin, tokens, len;
+  RowWork w;
+  int tile_end, unit_end;  // of this row, counted over the rows up to it
+  int piece, units, tiles;
+
+  __device__ __forceinline__ void make(const PrefillArgs& a, const Rows& rows, int room, void*) {
+    const int r = threadIdx.x & 63, group = a.n_q_heads / a.n_kv_heads, at = min(r, a.n_rows - 1);
+    const int end = rows.cu_tokens[at + 1];
+    begin = rows.cu_tokens[at];
+    len = rows.seq_lens[at];
+    w = work_of_row(a, group, begin, end, len);
+    if (r >= a.n_rows || __any(end < begin)) w.tiles = 0;  // (descending offsets are none: rows may lie over each other)
+    tokens = end - begin;
+    tile_end = wave_scan(w.tiles, capped_add);
+    tiles = __builtin_amdgcn_readlane(tile_end, 63);
+    piece = INT_MAX;
+    if (tiles > 0 && tiles < room) {
+      float blocks = (float)w.tiles * w.blocks;
+      for (int m = 1; m < 64; m *= 2) blocks += wave_xor_f(blocks, m);
+      const Tries t = tries_of(tiles, blocks, room);
+      piece = t.enough;
+      for (int p0 = t.least; piece == t.enough && p0 < t.enough && p0 < t.least + 8; p0 += 4)
+#pragma unroll
+        for (int k = 3; k >= 0; --k) {
+          const int n = wave_scan(w.tiles * pieces_of(w.blocks, p0 + k), capped_add);
+          if (__builtin_amdgcn_readlane(n, 63) <= room) piece = p0 + k;
+        }
+    }
+    unit_end = wave_scan(w.tiles * pieces_of(w.blocks, piece), capped_add);
+    units = __builtin_amdgcn_readlane(unit_end, 63);
+  }
+  // The row of unit (or of tile) x of the KV head.
+  __device__ __forceinline__ Unit row_of(const Rows&, int x, bool is_tile) const {
+    Unit n;
+    n.row = (int)__builtin_ctzll(__ballot((is_tile ? tile_end : unit_end) > x));
+    n.begin = __builtin_amdgcn_readlane(begin, n.row);
+    n.tokens = __builtin_amdgcn_readlane(tokens, n.row);
+    n.len = __builtin_amdgcn_readlane(len, n.row);
+    n.tiles = __builtin_amdgcn_readlane(w.tiles, n.row);
+    n.parts = pieces_of(__builtin_amdgcn_readlane(w.blocks, n.row), piece);
+    n.first = __builtin_amdgcn_readlane(unit_end, n.row) - n.tiles * n.parts;
+    n.part = 0;
+    n.tile = is_tile ? x - (__builtin_amdgcn_readlane(tile_end, n.row) - n.tiles) : 0;
+    return n;
+  }
+};
+
+// Any number of rows: in LDS, a thread's rows one after another.
+struct RowsPlan {
+  struct Shared {
+    int tiles[kMaxRows], blocks[kMaxRows], first_tile[kMaxRows + 1], first_unit[kMaxRows + 1], sums[4 * kWaves];
+  };
+  Shared* s;
+  int piece, units, tiles;
+
+  // The sum over the threads before this one, and over all.
+  __device__ __forceinline__ int before(int mine, int* all) const {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = wave_scan(mine, capped_add);
+    __syncthreads();  // (the last sums have been read)
+    if (lane == 63) s->sums[wave] = x;
+    __syncthreads();
+    int sum = __builtin_amdgcn_update_dpp(0, x, 0x138, 0xf, 0xf, false);  // wave_shr 1
+    *all = 0;
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) {
+      if (v == wave) sum = capped_add(sum, *all);
+      *all = capped_add(*all, s->sums[v]);
+    }
+    *all = __builtin_amdgcn_readfirstlane(*all);
+    return sum;
+  }
+  __device__ __forceinline__ void make(const PrefillArgs& a, const Rows& rows, int room, void* shared) {
+    s = static_cast<Shared*>(shared);
+    const int t = threadIdx.x, group = a.n_q_heads / a.n_kv_heads;
+    const int per = (a.n_rows + kThreads - 1) / kThreads;
+    const int row0 = min(t * per, a.n_rows), row1 = min(row0 + per, a.n_rows);
+    int mine = 0;
+    float blocks = 0.f;
+    bool descends = false;
+    for (int r = row0; r < row1; ++r) {
+      const int begin = rows.cu_tokens[r], end = rows.cu_tokens[r + 1];
+      descends |= end < begin;
+      const RowWork w = work_of_row(a, group, begin, end, rows.seq_lens[r]);
+      s->tiles[r] = w.tiles;
+      s->blocks[r] = w.blocks;
+      mine = capped_add(mine, w.tiles);
+      blocks += (float)w.tiles * w.blocks;
+    }
+    if (__syncthreads_or(descends)) {
+      for (int r = row0; r < row1; ++r) s->tiles[r] = 0;
+      mine = 0;
+    }
+    int sum = before(mine, &tiles);
+    for (int r = row0; r < row1; ++r) {
+      s->first_tile[r] = sum;
+      sum = capped_add(sum, s->tiles[r]);
+    }
+    if (t == 0) s->first_tile[a.n_rows] = tiles;
+    piece = INT_MAX;
+    if (tiles > 0 && tiles < room) {
+      for (int m = 1; m < 64; m *= 2) blocks += wave_xor_f(blocks, m);
+      __syncthreads();
+      if ((t & 63) == 0) s->sums[t >> 6] = __float_as_int(blocks);
+      __syncthreads();
+      blocks = 0.f;
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) blocks += __int_as_float(s->sums[v]);
+      const Tries tr = tries_of(tiles, blocks, room);
+      piece = tr.enough;
+      for (int p = tr.least; p < tr.enough && p < tr.least + 8; ++p) {
+        int n = 0, all;
+        for (int r = row0; r < row1; ++r) n = capped_add(n, s->tiles[r] * pieces_of(s->blocks[r], p));
+        before(n, &all);
+        if (all <= room) {
+          piece = p;
+          break;
+        }
+      }
+    }
+    mine = 0;
+    for (int r = row0; r < row1; ++r) mine = capped_add(mine, s->tiles[r] * pieces_of(s->blocks[r], piece));
+    sum = before(mine, &units);
+    for (int r = row0; r < row1; ++r) {
+      s->first_unit[r] = sum;
+      sum = capped_add(sum, s->tiles[r] * pieces_of(s->blocks[r], piece));
+    }
+    if (t == 0) s->first_unit[a.n_rows] = units;
+    __syncthreads();
+    n_rows = a.n_rows;
+  }
+  int n_rows;
+  __device__ __forceinline__ Unit row_of(const Rows& rows, int x, bool is_tile) const {
+    Unit n;
+    n.row = __builtin_amdgcn_readfirstlane(seq_of(is_tile ? s->first_tile : s->first_unit, n_rows, x));
+    n.begin = rows.cu_tokens[n.row];
+    n.tokens = rows.cu_tokens[n.row + 1] - n.begin;
+    n.len = rows.seq_lens[n.row];
+    n.tiles = __builtin_amdgcn_readfirstlane(s->tiles[n.row]);
+    n.parts = pieces_of(__builtin_amdgcn_readfirstlane(s->blocks[n.row]), piece);
+    n.first = __builtin_amdgcn_readfirstlane(s->first_unit[n.row]);
+    n.part = 0;
+    n.tile = is_tile ? x - __builtin_amdgcn_readfirstlane(s->first_tile[n.row]) : 0;
+    return n;
+  }
+};
+
+template <typename Plan>
+__device__ __forceinline__ Unit unit_of(const Plan& plan, const Rows& rows, int u) {
+  Unit n = plan.row_of(rows, u, false);
+  const int local = u - n.first, tiles = max(n.tiles, 1);
   n.part = local / tiles;
-  n.tile = tiles - 1 - local % tiles;
+  n.tile = tiles - 1 - (local - n.part * tiles);
   return n;
 }
 
@@ -743,96 +792,127 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& ro
   }
 }
 
-template <int kFmt, bool kLse>
+template <int kFmt, bool kLse, typename Plan>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_prefill_kernel(PrefillArgs a,
                                                                                                          int room,
                                                                                                          RBS_ROWS_ARGS) {
   const Rows rows{page_table, seq_lens, cu_tokens};
-  __shared__ __align__(1024) unsigned char tiles[4 * kBlockBytes];
-  __shared__ int sums[4 * kWaves], bad[kKeys];
+  __shared__ __align__(1024) unsigned char tiles[4 * kBlockBytes + 128];
+  __shared__ int bad[kKeys];
   const Tiles t{tiles, tiles + 2 * kBlockBytes, bad};
-  static_assert(sizeof(int) * (3 * kMaxRows + 1) <= sizeof(tiles), "the plan lies where the tiles will be");
-  int* first = reinterpret_cast<int*>(tiles);
-  const Plan plan{first, first + kMaxRows + 1, first + 2 * kMaxRows + 1, sums};
-  const int piece = plan_units(a, rows, room, plan);
-  const int units = __builtin_amdgcn_readfirstlane(first[a.n_rows]);
-  const int bunch = bunch_of(units, a.n_kv_heads);
+  static_assert(sizeof(RowsPlan::Shared) <= sizeof(tiles), "the plan lies where the tiles will be");
+  Plan plan;
+  plan.make(a, rows, room, tiles);
   int g, i;
-  slot_of(blockIdx.x, a.n_kv_heads, bunch, &g, &i);
-  if (i >= units) return;
-  const Unit n = unit_of(a, rows, first, piece, i);
-  __syncthreads();  // every wave has read the offsets
-  attend_unit<kFmt, kLse>(a, rows, n, piece, g, t, n.parts > 1 ? a.workspace + (size_t)(g * units + i) * kPartFloats : nullptr);
+  slot_of(blockIdx.x, a.n_kv_heads, bunch_of(plan.units, a.n_kv_heads), &g, &i);
+  if (i >= plan.units) return;
+  const Unit n = unit_of(plan, rows, i);
+  if (std::is_same<Plan, RowsPlan>::value) __syncthreads();  // every wave has read the plan
+  attend_unit<kFmt, kLse>(a, rows, n, plan.piece, g, t,
+                          n.parts > 1 ? a.workspace + (size_t)(g * plan.units + i) * kPartFloats : nullptr);
 }
 
-// Joins the pieces of the tiles: a wave to 32 queries and 32 of their elements.
-template <int kFmt>
+// Joins the pieces of a tile, in their order: a workgroup to 32 queries and 32 of their
+// elements, a wave to every fourth piece.  Bound by latency: the loads of kBatch pieces
+// of a wave are on their way together.
+template <int kFmt, typename Plan>
 __global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArgs a, int room, RBS_ROWS_ARGS) {
   const Rows rows{page_table, seq_lens, cu_tokens};
-  __shared__ int first[kMaxRows + 1], counts[2 * kMaxRows], sums[4 * kWaves];
-  const int piece = plan_units(a, rows, room, Plan{first, counts, counts + kMaxRows, sums});
-  if (piece == INT_MAX) return;
-  const int units = __builtin_amdgcn_readfirstlane(first[a.n_rows]);
+  __shared__ union {
+    RowsPlan::Shared plan;
+    struct {
+      float m[kWaves][32], l[kWaves][32], l_exact[kWaves][32];
+      float4 o[kWaves][4][64];
+    } part;
+  } lds;
+  Plan plan;
+  plan.make(a, rows, room, &lds.plan);
+  if (plan.piece == INT_MAX) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5, l32 = lane & 31;
-  const int group = a.n_q_heads / a.n_kv_heads;
-  // Workgroup (unit of all KV heads, 32 elements); only the first piece's of a tile stays.
-  for (int b = blockIdx.x; b < units * a.n_kv_heads; b += gridDim.x) {
-    const int g = b / units, i = b - g * units;
-    const Unit n = unit_of(a, rows, first, piece, i);
-    if (n.part != 0 || n.parts == 1) continue;
-    const int tiles = (int)(((int64_t)n.tokens * group + kQueries - 1) / kQueries);
-    const int64_t queries = (int64_t)n.tokens * group, x = (int64_t)n.tile * kQueries + 32 * wave + l32;
-    if (x - l32 >= queries) continue;
-    const int dt = blockIdx.y;
-    const float* slots = a.workspace + (size_t)b * kPartFloats;
-    const size_t step = (size_t)tiles * kPartFloats;
-    const int at = kQueries * kHeadDim + 32 * wave + l32;
-    float m = -INFINITY;
-    for (int p = 0; p < n.parts; ++p) m = fmaxf(m, slots[p * step + at]);
-    const float ref = m == -INFINITY ? 0.f : m;
-    float l = 0.f, l_exact = 0.f;
-    f32x16 o{};
-    constexpr int kBatch = 4;
-    for (int p0 = 0; p0 < n.parts; p0 += kBatch) {
-      float pm[kBatch], pl[kBatch];
-      float4 w[kBatch][4];
+  const int group = a.n_q_heads / a.n_kv_heads, tile = blockIdx.x / a.n_kv_heads, g = blockIdx.x % a.n_kv_heads;
+  const int dt = blockIdx.y & 3, q0 = 32 * (blockIdx.y >> 2);
+  if (tile >= plan.tiles) return;
+  const Unit n = plan.row_of(rows, tile, true);
+  const int64_t queries = (int64_t)n.tokens * group, x0 = (int64_t)n.tile * kQueries + q0;
+  if (n.parts == 1 || x0 >= queries) return;
+  __syncthreads();  // every wave has read the plan
+  const float* slots = a.workspace + (size_t)(g * plan.units + n.first + n.tiles - 1 - n.tile) * kPartFloats;
+  const size_t step = (size_t)n.tiles * kPartFloats;
+  const int at = kQueries * kHeadDim + q0 + l32;
+  float m = -INFINITY, l = 0.f, l_exact = 0.f;
+  float4 o[4] = {};
+  constexpr int kBatch = 4;
+  for (int p0 = wave; p0 < n.parts; p0 += kWaves * kBatch) {
+    float pm[kBatch], pl[kBatch], pe[kBatch];
+    float4 w[kBatch][4];
 #pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        const float* slot = slots + min(p0 + k, n.parts - 1) * step;
-        pm[k] = slot[at];
-        pl[k] = slot[at + kQueries];
+    for (int k = 0; k < kBatch; ++k) {
+      const float* slot = slots + min(p0 + kWaves * k, n.parts - 1) * step;
+      pm[k] = slot[at];
+      pl[k] = slot[at + kQueries];
+      pe[k] = a.lse != nullptr ? slot[at + 2 * kQueries] : 0.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          w[k][e] = *reinterpret_cast<const float4*>(slot + wave * 32 * kHeadDim + 4 * (64 * (4 * dt + e) + lane));
-      }
+      for (int e = 0; e < 4; ++e)
+        w[k][e] = *reinterpret_cast<const float4*>(slot + q0 * kHeadDim + 4 * (64 * (4 * dt + e) + lane));
+    }
+    float top = m;
 #pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        // (A piece without keys of the query's, or behind the tile's last block, which wrote no values.)
-        if (p0 + k >= n.parts || pl[k] == 0.f) continue;
-        const float f = fast_exp2(pm[k] - ref);
-        l += pl[k] * f;
-        if (a.lse != nullptr) l_exact += slots[(p0 + k) * step + at + 2 * kQueries] * f;
+    for (int k = 0; k < kBatch; ++k) top = fmaxf(top, pm[k]);
+    const float ref = top == -INFINITY ? 0.f : top, keep = fast_exp2(m - ref);
+    m = top;
+    l *= keep;
+    l_exact *= keep;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          o[4 * e] += w[k][e].x * f;
-          o[4 * e + 1] += w[k][e].y * f;
-          o[4 * e + 2] += w[k][e].z * f;
-          o[4 * e + 3] += w[k][e].w * f;
-        }
+    for (int e = 0; e < 4; ++e) {
+      o[e].x *= keep; o[e].y *= keep; o[e].z *= keep; o[e].w *= keep;
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      // (A piece without keys of the query's, or behind the tile's last block, which wrote no values.)
+      if (p0 + kWaves * k >= n.parts || pl[k] == 0.f) continue;
+      const float f = fast_exp2(pm[k] - ref);
+      l += pl[k] * f;
+      l_exact += pe[k] * f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        o[e].x += w[k][e].x * f; o[e].y += w[k][e].y * f; o[e].z += w[k][e].z * f; o[e].w += w[k][e].w * f;
       }
     }
-    if (x >= queries) continue;
-    const int tok_i = (int)(x / group), head = g * group + (int)(x - (int64_t)tok_i * group), tok = n.begin + tok_i;
-    const float inv = l > 0.f ? head_factor<kFmt>(a, a.n_kv_heads + g) / l : l == 0.f ? 0.f : __builtin_nanf("");
-    uint16_t* row = a.O + head * a.q_head + tok * a.q_tok + 32 * dt + 4 * half;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      *reinterpret_cast<uint2*>(row + 8 * e) = make_uint2(two_bf16(o[4 * e] * inv, o[4 * e + 1] * inv),
-                                                          two_bf16(o[4 * e + 2] * inv, o[4 * e + 3] * inv));
-    if (a.lse != nullptr && half == 0 && dt == 0)
-      a.lse[(int64_t)head * a.n_tokens + tok] = l_exact == 0.f ? -INFINITY : (m + log2f(l_exact)) / kLog2e;
   }
+  if (half == 0) {
+    lds.part.m[wave][l32] = m;
+    lds.part.l[wave][l32] = l;
+    lds.part.l_exact[wave][l32] = l_exact;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) lds.part.o[wave][e][lane] = o[e];
+  __syncthreads();
+  // Each wave joins a quarter of the elements.
+  float top = lds.part.m[0][l32];
+#pragma unroll
+  for (int v = 1; v < kWaves; ++v) top = fmaxf(top, lds.part.m[v][l32]);
+  const float ref = top == -INFINITY ? 0.f : top;
+  l = l_exact = 0.f;
+  float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int v = 0; v < kWaves; ++v) {
+    const float pl = lds.part.l[v][l32];
+    if (pl == 0.f) continue;
+    const float f = fast_exp2(lds.part.m[v][l32] - ref);
+    l += pl * f;
+    l_exact += lds.part.l_exact[v][l32] * f;
+    const float4 w = lds.part.o[v][wave][lane];
+    r.x += w.x * f; r.y += w.y * f; r.z += w.z * f; r.w += w.w * f;
+  }
+  const int64_t x = x0 + l32;
+  if (x >= queries) return;
+  const int i = (int)(x / group), head = g * group + (int)(x - (int64_t)i * group), tok = n.begin + i;
+  const float inv = l > 0.f ? head_factor<kFmt>(a, a.n_kv_heads + g) / l : l == 0.f ? 0.f : __builtin_nanf("");
+  *reinterpret_cast<uint2*>(a.O + head * a.q_head + tok * a.q_tok + 32 * dt + 8 * wave + 4 * half) =
+      make_uint2(two_bf16(r.x * inv, r.y * inv), two_bf16(r.z * inv, r.w * inv));
+  if (a.lse != nullptr && half == 0 && dt == 0 && wave == 0)
+    a.lse[(int64_t)head * a.n_tokens + tok] = l_exact == 0.f ? -INFINITY : (top + log2f(l_exact)) / kLog2e;
 }
 
 template <int kFmt>
@@ -846,11 +926,14 @@ hipError_t launch(const PrefillArgs& a, hipStream_t s) {
   const int room = split ? kUnits / 2 / a.n_kv_heads : 0;
   // (Bunches round up a head's units, and the XCDs' shares of them.)
   const int grid = (int)((split ? kUnits : units) + 64 + 8 * a.n_kv_heads);
-  const auto kernel = a.lse != nullptr ? paged_prefill_kernel<kFmt, true> : paged_prefill_kernel<kFmt, false>;
+  const bool few = a.n_rows <= 64;
+  const auto kernel = few ? (a.lse != nullptr ? paged_prefill_kernel<kFmt, true, WavePlan> : paged_prefill_kernel<kFmt, false, WavePlan>)
+                          : (a.lse != nullptr ? paged_prefill_kernel<kFmt, true, RowsPlan> : paged_prefill_kernel<kFmt, false, RowsPlan>);
   hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), 0, s, a, room, a.page_table, a.seq_lens, a.cu_tokens);
-  if (split)
-    hipLaunchKernelGGL(paged_prefill_join_kernel<kFmt>, dim3(kUnits / 2, 4), dim3(kThreads), 0, s, a, room, a.page_table,
-                       a.seq_lens, a.cu_tokens);
+  if (split) {
+    const auto join = few ? paged_prefill_join_kernel<kFmt, WavePlan> : paged_prefill_join_kernel<kFmt, RowsPlan>;
+    hipLaunchKernelGGL(join, dim3((int)units, 16), dim3(kThreads), 0, s, a, room, a.page_table, a.seq_lens, a.cu_tokens);
+  }
   return hipGetLastError();
 }
 
