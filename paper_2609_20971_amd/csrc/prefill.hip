@@ -43,6 +43,27 @@ constexpr int kKeys = 64;                        // of a block
 constexpr int kBlockBytes = kKeys * 2 * kHeadDim;  // of K or V in LDS
 constexpr int kUnits = 1024;                     // pieces of a call whose tiles are split
 constexpr int kPartFloats = kQueries * kHeadDim + 3 * kQueries;  // weighted values, maxima, sums of rounded and exact weights
+// Division of 32-bit numbers by one that the host knows, by a product with its
+// reciprocal (Granlund and Montgomery 1994): the quotient is exact.
+struct Divisor {
+  uint32_t d, m, s1, s2;
+  explicit Divisor(uint32_t d_) : d(d_) {
+    uint32_t l = 0;
+    while ((uint64_t(1) << l) < d) ++l;
+    m = (uint32_t)(((uint64_t(1) << 32) * ((uint64_t(1) << l) - d)) / d + 1);
+    s1 = l < 1 ? l : 1;
+    s2 = l < 1 ? 0 : l - 1;
+  }
+  __device__ __forceinline__ uint32_t of(uint32_t x) const {
+    const uint32_t t = __umulhi(m, x);
+    return (t + ((x - t) >> s1)) >> s2;
+  }
+};
+// (A call's queries of a KV head are fewer than 2^30.)
+struct Heads {
+  Divisor group, n_kv;
+};
+
 constexpr int kMost = 1 << 29;                   // counts stop here
 
 __device__ __forceinline__ int capped_add(int a, int b) { return min(a + b, kMost); }
@@ -68,7 +89,7 @@ __device__ __forceinline__ RowWork work_of_row(const PrefillArgs& a, int group, 
   RowWork w{0, 1};
   if (len < 0 || begin < 0 || end <= begin || end > a.n_tokens) return w;
   const int64_t cap = (int64_t)a.max_pages << a.cache.page_shift;
-  w.tiles = (int)(((int64_t)(end - begin) * group + kQueries - 1) / kQueries);
+  w.tiles = (int)(((uint32_t)(end - begin) * (uint32_t)group + kQueries - 1) / kQueries);
   w.blocks = max(1, (int)((min((int64_t)len, cap) + kKeys - 1) / kKeys));
   return w;
 }
@@ -110,8 +131,8 @@ struct WavePlan {
   int tile_end, unit_end;  // of this row, counted over the rows up to it
   int piece, units, tiles;
 
-  __device__ __forceinline__ void make(const PrefillArgs& a, const Rows& rows, int room, void*) {
-    const int r = threadIdx.x & 63, group = a.n_q_heads / a.n_kv_heads, at = min(r, a.n_rows - 1);
+  __device__ __forceinline__ void make(const PrefillArgs& a, const Heads& heads, const Rows& rows, int room, void*) {
+    const int r = threadIdx.x & 63, group = heads.group.d, at = min(r, a.n_rows - 1);
     const int end = rows.cu_tokens[at + 1];
     begin = rows.cu_tokens[at];
     len = rows.seq_lens[at];
@@ -176,9 +197,9 @@ struct RowsPlan {
     *all = __builtin_amdgcn_readfirstlane(*all);
     return sum;
   }
-  __device__ __forceinline__ void make(const PrefillArgs& a, const Rows& rows, int room, void* shared) {
+  __device__ __forceinline__ void make(const PrefillArgs& a, const Heads& heads, const Rows& rows, int room, void* shared) {
     s = static_cast<Shared*>(shared);
-    const int t = threadIdx.x, group = a.n_q_heads / a.n_kv_heads;
+    const int t = threadIdx.x, group = heads.group.d;
     const int per = (a.n_rows + kThreads - 1) / kThreads;
     const int row0 = min(t * per, a.n_rows), row1 = min(row0 + per, a.n_rows);
     int mine = 0;
@@ -254,9 +275,9 @@ struct RowsPlan {
 template <typename Plan>
 __device__ __forceinline__ Unit unit_of(const Plan& plan, const Rows& rows, int u) {
   Unit n = plan.row_of(rows, u, false);
-  const int local = u - n.first, tiles = max(n.tiles, 1);
-  n.part = local / tiles;
-  n.tile = tiles - 1 - (local - n.part * tiles);
+  const int local = u - n.first;
+  n.part = n.parts == 1 ? 0 : __builtin_amdgcn_readfirstlane(local / max(n.tiles, 1));
+  n.tile = n.tiles - 1 - (local - n.part * n.tiles);
   return n;
 }
 
@@ -264,15 +285,16 @@ __device__ __forceinline__ Unit unit_of(const Plan& plan, const Rows& rows, int 
 // (workgroup j runs on XCD j % 8): bunch k of that XCD is bunch q = 8 k + x of all, of KV
 // head q % H_kv.  Slot b of the launch gives KV head g and unit i of it (which may be
 // past the last).
-__device__ __forceinline__ void slot_of(int b, int n_kv_heads, int bunch, int* g, int* i) {
+__device__ __forceinline__ void slot_of(int b, const Heads& heads, int units, int* g, int* i) {
+  // (A bunch: 8, or where there are few units 4, 2 or 1.)
+  const int64_t all = (int64_t)units * heads.n_kv.d;
+  const int shift = all >= 512 ? 3 : all >= 256 ? 2 : all >= 128 ? 1 : 0;
   const int x = b & 7, k = b >> 3;
-  const int q = (k / bunch) * 8 + x;
-  *g = q % n_kv_heads;
-  *i = q / n_kv_heads * bunch + k % bunch;
+  const int q = (k >> shift) * 8 + x, row = (int)heads.n_kv.of((uint32_t)q);
+  *g = q - row * (int)heads.n_kv.d;
+  *i = (row << shift) + (k & ((1 << shift) - 1));
 }
-__device__ __forceinline__ int bunch_of(int units, int n_kv_heads) {
-  return max(1, min(8, (int)min((int64_t)units * n_kv_heads / 64, (int64_t)8)));
-}
+
 template <int kFmt>
 constexpr int kCodeBytes = kFmt == kCacheFp4 ? kHeadDim / 2 : kFmt == kCacheFp8 ? kHeadDim : 2 * kHeadDim;
 
@@ -289,6 +311,21 @@ struct Pages {
     return page * page_bytes + (int64_t)(j & ((1 << shift) - 1)) * tok_bytes;
   }
 };
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// x, of which the compiler knows nothing here: what is made of it is made where it is
+// used, and not kept in registers over the steps.
+template <typename T>
+__device__ __forceinline__ T anew(T x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+template <typename T>
+__device__ __forceinline__ T anew_s(T x) {
+  asm volatile("" : "+s"(x));
+  return x;
+}
 
 // One tensor's block in registers on its way to LDS (FP8, FP4): of a wave 16 keys.
 template <int kFmt>
@@ -307,11 +344,23 @@ struct Staged {
       if (kFmt == kCacheFp4) scale = *reinterpret_cast<const uint8_t*>(scales + (at >> 4) + r * (tok_bytes >> 4) + piece);
     }
   }
-  // Piece p (of 4) of the lane's elements to the block's row.
-  __device__ __forceinline__ void store(unsigned char* lds, bool is_v, int p) const {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, piece = lane % (64 / kRows);
-    constexpr int kPieces = kFmt == kCacheFp8 ? 2 : 4;  // of 16 bytes, of a load
-    const int k = p / kPieces, row = 16 * wave + kRows * k + lane / (64 / kRows), c = kPieces * piece + p % kPieces;
+  // Where the lane's pieces go in a block's rows: 256 row0 + (swz ^ ..), row0 16 wave +
+  // lane / .. and the piece kPieces (lane % ..); the swizzle's bits that k and p give are
+  // apart from the lane's.
+  static constexpr int kPieces = kFmt == kCacheFp8 ? 2 : 4;  // of 16 bytes, of a load
+  struct Place {
+    uint32_t row, k_swz, v_swz;
+  };
+  static __device__ __forceinline__ Place place() {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int row0 = 16 * wave + lane / (64 / kRows), c0 = kPieces * (lane % (64 / kRows));
+    return Place{256u * row0, 16u * (uint32_t)kswz(row0, c0), 16u * (uint32_t)vswz(row0, c0)};
+  }
+  // Piece p (of 4) of the lane's elements to the block at byte `lds` of LDS.
+  __device__ __forceinline__ void store(const Place& to, uint32_t lds, bool is_v, int p) const {
+    const int k = p / kPieces;
+    const uint32_t bits = 16u * (p % kPieces) + (is_v ? 0u : 16u * kRows * k);
+    const uint32_t at = anew(to.row + ((is_v ? to.v_swz : to.k_swz) ^ bits)) + lds + 256u * kRows * k;
     const uint32_t w[4] = {codes[k].x, codes[k].y, codes[k].z, codes[k].w};
     uint4 v;
     if constexpr (kFmt == kCacheFp8) {
@@ -326,7 +375,7 @@ struct Staged {
     } else {
       v = widen_e2m1(w[p], scale << 23);
     }
-    *reinterpret_cast<uint4*>(lds + row * 256 + 16 * (is_v ? vswz(row, c) : kswz(row, c))) = v;
+    *(__attribute__((address_space(3))) u32x4*)(uintptr_t)at = u32x4{v.x, v.y, v.z, v.w};
   }
 };
 
@@ -337,36 +386,38 @@ __device__ __forceinline__ float head_factor(const PrefillArgs& a, int head) {
   return m > 0.f ? m / 448.f : 1.f;
 }
 
-// The result of a query: 64 of its elements in a lane.
-__device__ __forceinline__ void write_query(const PrefillArgs& a, int head, int tok, int half, const f32x16* o, float m,
-                                            float l, float l_exact, float v_factor) {
-  const float inv = l > 0.f ? v_factor / l : l == 0.f ? 0.f : __builtin_nanf("");
-  uint16_t* row = a.O + head * a.q_head + tok * a.q_tok;
+// Where query x of a row is in Q and O, and in lse.
+__device__ __forceinline__ int64_t query_offset(const PrefillArgs& a, const Heads& heads, const Unit& n, int g, int x) {
+  const int i = (int)heads.group.of(x), head = g * (int)heads.group.d + x - i * (int)heads.group.d;
+  return head * a.q_head + (n.begin + i) * a.q_tok;
+}
+__device__ __forceinline__ int64_t query_lse(const PrefillArgs& a, const Heads& heads, const Unit& n, int g, int x) {
+  const int i = (int)heads.group.of(x), head = g * (int)heads.group.d + x - i * (int)heads.group.d;
+  return (int64_t)head * a.n_tokens + n.begin + i;
+}
+
+// The wave's 32 results, 64 elements of one in a lane, through 8 KB of LDS (pieces of
+// 16 bytes swizzled by row) to whole rows: stored from the lanes as they are, in
+// pieces of 8 bytes, a unit's end took 4400 cycles and not ?.
+__device__ __forceinline__ void write_queries(const PrefillArgs& a, const Heads& heads, const Unit& n, int g, int x0, int queries,
+                                              const f32x16* o, float inv, unsigned char* lds) {
+  const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
     for (int rq = 0; rq < 4; ++rq)
-      *reinterpret_cast<uint2*>(row + 32 * dt + 8 * rq + 4 * half) =
+      *reinterpret_cast<uint2*>(lds + l32 * 256 + 16 * kswz(l32, 4 * dt + rq) + 8 * half) =
           make_uint2(two_bf16(o[dt][4 * rq] * inv, o[dt][4 * rq + 1] * inv),
                      two_bf16(o[dt][4 * rq + 2] * inv, o[dt][4 * rq + 3] * inv));
-  if (a.lse != nullptr && half == 0)
-    a.lse[(int64_t)head * a.n_tokens + tok] = l_exact == 0.f ? -INFINITY : (m + log2f(l_exact)) / kLog2e;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int r = 4 * k + (lane >> 4), x = x0 + r;
+    const uint4 w = *reinterpret_cast<const uint4*>(lds + r * 256 + 16 * kswz(r, lane & 15));
+    if (x < queries) *reinterpret_cast<uint4*>(a.O + query_offset(a, heads, n, g, x) + 8 * (lane & 15)) = w;
+  }
 }
-
-// x, of which the compiler knows nothing here: what is made of it is made where it is
-// used, and not kept in registers over the steps.
-template <typename T>
-__device__ __forceinline__ T anew(T x) {
-  asm volatile("" : "+v"(x));
-  return x;
-}
-template <typename T>
-__device__ __forceinline__ T anew_s(T x) {
-  asm volatile("" : "+s"(x));
-  return x;
-}
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // The workgroup's LDS: two blocks of K and two of V, and
 struct Tiles {
@@ -438,35 +489,17 @@ __device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
 // the next K and this V are there, and the buffers of this K and the last V are free
 // for the copies of the K after the next and the next V.
 template <int kFmt, bool kLse>
-__device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& rows, const Unit& n, int piece, int g,
-                                            const Tiles& t, float* slot) {
+__device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Heads& heads, const Rows& rows, const Unit& n,
+                                            int piece, int g, const Tiles& t, float* slot) {
   constexpr bool kCopied = kFmt == kCacheBf16;  // straight to LDS
   constexpr int kAhead = kCopied ? 4 : 3;       // operands on their way from LDS
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, l32 = lane & 31;
-  const int group = a.n_q_heads / a.n_kv_heads;
-  const int64_t queries = (int64_t)n.tokens * group, x0 = (int64_t)n.tile * kQueries;
+  const int queries = n.tokens * (int)heads.group.d, x0 = n.tile * kQueries;
   const int64_t cap = (int64_t)a.max_pages << a.cache.page_shift;
   const int before = n.len - n.tokens;  // position of the row's first new token
   const int held = (int)min((int64_t)n.len, cap);
-  const int tile_last = min(before + (int)((min(x0 + kQueries, queries) - 1) / group), held - 1);
-  const int first_last = min(before + (int)(x0 / group), held - 1);  // the last key of the tile's first query
-  const int blocks = tile_last < 0 ? 0 : tile_last / kKeys + 1;
-  const int b0 = piece == INT_MAX ? 0 : n.part * piece;
-  const int b1 = piece == INT_MAX ? blocks : min(blocks, b0 + piece);
-  const int plain = (first_last + 1) / kKeys;  // blocks before it are attended whole
-
-  // The lane's query (past the row's last one: that one, and not written).
-  int last;  // its last key
-  bf16x8 q[8];
-  {
-    const int64_t x = min(x0 + 32 * wave + l32, queries - 1);
-    const int i = (int)(x / group), head = g * group + (int)(x - (int64_t)i * group), tok = n.begin + i;
-    last = min(before + i, held - 1);
-    const uint16_t* row = a.Q + head * a.q_head + tok * a.q_tok + 8 * half;
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks) q[ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(row + 16 * ks));
-  }
+  const int tile_last = min(before + (int)heads.group.of(min(x0 + kQueries, queries) - 1), held - 1);
 
   Pages pages;
   pages.table = rows.page_table + (int64_t)n.row * a.max_pages;
@@ -475,6 +508,38 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& ro
   pages.last_key = max(tile_last, 0);
   pages.page_bytes = a.cache.page * kCodeBytes<kFmt> / kHeadDim;
   pages.tok_bytes = (uint32_t)(a.cache.tok * kCodeBytes<kFmt> / kHeadDim);
+  const int blocks = tile_last < 0 ? 0 : tile_last / kKeys + 1;
+  const int b0 = piece == INT_MAX ? 0 : n.part * piece;
+  const int b1 = piece == INT_MAX ? blocks : min(blocks, b0 + piece);
+  // The wave moves keys 16 wave .. + 15 of each block (all in one page).  Lane i holds
+  // where those of block window + i are: a page number's load, waited for once in 64
+  // blocks, would otherwise be one in every step.
+  auto key0 = [&](int b) __attribute__((always_inline)) { return b * kKeys + 16 * wave; };
+  int window = b0;
+  int64_t places = pages.at(key0(b0 + lane));
+  auto place_of = [&](int b) __attribute__((always_inline)) {  // called with ascending b
+    if (b >= window + 64) {
+      window = b;
+      places = pages.at(key0(b + lane));
+    }
+    const int lo = __builtin_amdgcn_readlane((int)(uint32_t)places, b - window);
+    const int hi = __builtin_amdgcn_readlane((int)(places >> 32), b - window);
+    return (int64_t)((uint64_t)(uint32_t)hi << 32 | (uint32_t)lo);
+  };
+
+  const int first_last = min(before + (int)heads.group.of(x0), held - 1);  // the last key of the tile's first query
+  const int plain = (first_last + 1) / kKeys;                               // blocks before it are attended whole
+  // The lane's query (past the row's last one: that one, and not written).
+  int last;  // its last key
+  bf16x8 q[8];
+  {
+    const int x = min(x0 + 32 * wave + l32, queries - 1), i = (int)heads.group.of(x);
+    last = min(before + i, held - 1);
+    const uint16_t* row = a.Q + query_offset(a, heads, n, g, x) + 8 * half;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) q[ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(row + 16 * ks));
+  }
+
   const int64_t head_bytes = g * a.cache.head * kCodeBytes<kFmt> / kHeadDim;
   const char* K = static_cast<const char*>(a.cache.K) + head_bytes;
   const char* V = static_cast<const char*>(a.cache.V) + head_bytes;
@@ -482,10 +547,6 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& ro
   const char* Vs = static_cast<const char*>(a.cache.V_scale) + g * a.cache.head / 32;
   const float scale_log2 = a.scale * kLog2e * head_factor<kFmt>(a, g);
 
-  // The wave moves keys 16 wave .. + 15 of each block (all in one page).  Lane i holds
-  // where those of block window + i are: a page number's load, waited for once in 64
-  // blocks, would otherwise be one in every step.
-  auto key0 = [&](int b) __attribute__((always_inline)) { return b * kKeys + 16 * wave; };
   auto last_of = [&](int b) __attribute__((always_inline)) {  // the row's last key among them (15 if it is behind them)
     const int j = key0(b);
     return j > pages.last_key ? (pages.last_key & 15) : min(15, pages.last_key - j);
@@ -516,19 +577,22 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& ro
     }
   };
   Staged<kCopied ? kCacheFp8 : kFmt> k_next, v_next;
+  const uint32_t k_at0 = lds_offset(t.k), v_at0 = lds_offset(t.v);
+  const typename Staged<kCopied ? kCacheFp8 : kFmt>::Place place = Staged<kCopied ? kCacheFp8 : kFmt>::place();
 
   // Operands from LDS.  K: row 32 mt + l32, pieces 2 ks + half.  V (transposed): rows
   // 16 c + 4 half + (lane % 16) / 4 (and + 8), elements 32 dt + 16 ((lane / 16) % 2) + 4 (lane % 4).
   const int vq = (lane & 15) >> 2;
   uint32_t k_at[8], v_at[4];
+  const uint32_t k_row = lds_offset(t.k) + (uint32_t)l32 * 256u, k_swz = 16u * (uint32_t)kswz(l32, half);
 #pragma unroll
-  for (int ks = 0; ks < 8; ++ks) k_at[ks] = lds_offset(t.k) + (uint32_t)l32 * 256u + 16u * (uint32_t)kswz(l32, 2 * ks + half);
+  for (int ks = 0; ks < 8; ++ks) k_at[ks] = k_row + (k_swz ^ (32u * ks));
+  const uint32_t v_row = lds_offset(t.v) + (uint32_t)(4 * half + vq) * 256u + 8u * (lane & 1);
+  const uint32_t v_swz = 16u * (uint32_t)vswz(vq, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1));
 #pragma unroll
-  for (int dt = 0; dt < 4; ++dt)
-    v_at[dt] = lds_offset(t.v) + (uint32_t)(4 * half + vq) * 256u + 8u * (lane & 1) +
-               16u * (uint32_t)vswz(vq, 4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1));
+  for (int dt = 0; dt < 4; ++dt) v_at[dt] = v_row + (v_swz ^ (64u * dt));
   typedef const __attribute__((address_space(3))) u32x4 lds_u32x4;
-  auto k_frag = [&](int buf, int f) __attribute__((always_inline)) {  // f = 2 ks + mt
+  auto k_frag = [&](int buf, int f) __attribute__((always_inline)) {  // f = 2 ks + mt, in this order
     return __builtin_bit_cast(bf16x8, *(lds_u32x4*)(uintptr_t)(k_at[f >> 1] + (uint32_t)(buf * kBlockBytes + (f & 1) * 8192)));
   };
   auto v_frag = [&](int buf, int f) __attribute__((always_inline)) {  // f = 4 c + dt
@@ -579,18 +643,6 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& ro
       for (int r = 0; r < 16; ++r) o[dt][r] *= f;
   };
 
-  int window = 0;
-  int64_t places = 0;
-  auto look_up = [&](int b) __attribute__((always_inline)) {  // from block b on
-    window = b;
-    places = pages.at(key0(b + lane));
-  };
-  auto place_of = [&](int b) __attribute__((always_inline)) {  // called with ascending b
-    if (b >= window + 64) look_up(b);
-    const int lo = __builtin_amdgcn_readlane((int)(uint32_t)places, b - window);
-    const int hi = __builtin_amdgcn_readlane((int)(places >> 32), b - window);
-    return (int64_t)((uint64_t)(uint32_t)hi << 32 | (uint32_t)lo);
-  };
   constexpr int kLead = kCopied ? 2 : 3;  // blocks that the loads of K are ahead; those of V are one behind them
   int64_t at_v;                           // where the keys of the block whose V comes next are
   f32x16 s0[2], s1[2];
@@ -636,12 +688,12 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& ro
         if (part < 2) copy(false, kBuf, at_k, 2 * part);
         else copy(true, kBuf ^ 1, at, 2 * (part - 2));
       } else if (part < 2) {
-        k_next.store(t.k + kBuf * kBlockBytes, false, 2 * part);
-        k_next.store(t.k + kBuf * kBlockBytes, false, 2 * part + 1);
+        k_next.store(place, k_at0 + kBuf * kBlockBytes, false, 2 * part);
+        k_next.store(place, k_at0 + kBuf * kBlockBytes, false, 2 * part + 1);
         if (part == 1) k_next.load(K, Ks, at_k, pages.tok_bytes, 15);
       } else {
-        v_next.store(t.v + (kBuf ^ 1) * kBlockBytes, true, 2 * (part - 2));
-        v_next.store(t.v + (kBuf ^ 1) * kBlockBytes, true, 2 * (part - 2) + 1);
+        v_next.store(place, v_at0 + (kBuf ^ 1) * kBlockBytes, true, 2 * (part - 2));
+        v_next.store(place, v_at0 + (kBuf ^ 1) * kBlockBytes, true, 2 * (part - 2) + 1);
         if (part == 3) v_next.load(V, Vs, at, pages.tok_bytes, 15);
       }
     };
@@ -700,16 +752,19 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& ro
     } else {
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
-        if (more2) k_next.store(t.k + buf * kBlockBytes, false, p);
-        if (more) v_next.store(t.v + (buf ^ 1) * kBlockBytes, true, p);
+        if (more2) k_next.store(place, k_at0 + buf * kBlockBytes, false, p);
+        if (more) v_next.store(place, v_at0 + (buf ^ 1) * kBlockBytes, true, p);
       }
       if (b + 3 < b1) k_next.load(K, Ks, at_k, pages.tok_bytes, last_of(b + 3));
       if (more2) v_next.load(V, Vs, at, pages.tok_bytes, last_of(b + 2));
     }
     if (b >= plain) take_out(t.v + buf * kBlockBytes, t.bad, last - b * kKeys, o);
-    if (more) logits(buf ^ 1, s1);
 #pragma unroll
-    for (int j = 0; j < 16; ++j) exponentials(s0, j);
+    for (int j = 0; j < 16; ++j) {
+      exponentials(s0, j);
+      if ((j & 3) == 3) fence();
+    }
+    if (more) logits(buf ^ 1, s0);
     bf16x8 f[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) f[k] = v_frag(buf, k);
@@ -721,15 +776,12 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& ro
     }
     fence();
     if (!more) return;
-    if (b + 1 >= plain) mask(s1, b + 1);
-    const float top = half_max(top_of(s1)) * scale_log2;
+    if (b + 1 >= plain) mask(s0, b + 1);
+    const float top = half_max(top_of(s0)) * scale_log2;
     if (__any(top > m + kRescaleSlack)) follow(top);
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt) s0[mt] = s1[mt];
   };
 
   if (b0 < b1) {
-    look_up(b0);
     const int64_t at = place_of(b0), at1 = place_of(b0 + 1);
     const bool two = b0 + 1 < b1;
     if constexpr (kCopied) {
@@ -745,9 +797,9 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& ro
       second.load(K, Ks, at1, pages.tok_bytes, last_of(b0 + 1));
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
-        k_next.store(t.k, false, p);
-        v_next.store(t.v, true, p);
-        second.store(t.k + kBlockBytes, false, p);
+        k_next.store(place, k_at0, false, p);
+        v_next.store(place, v_at0, true, p);
+        second.store(place, k_at0 + kBlockBytes, false, p);
       }
       at_v = place_of(b0 + 2);
       if (b0 + 2 < b1) k_next.load(K, Ks, at_v, pages.tok_bytes, last_of(b0 + 2));
@@ -766,13 +818,16 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& ro
   }
 
   if (x0 + 32 * wave >= queries) return;  // (no query of the wave's)
-  const int64_t x = x0 + 32 * wave + (anew(lane) & 31);
   l = half_sum(l);
   if (kLse) l_exact = half_sum(l_exact);
   if (n.parts == 1) {
-    const int i = (int)(x / group), head = g * group + (int)(x - (int64_t)i * group);
-    if (x < queries)
-      write_query(a, head, n.begin + i, half, o, m, l, kLse ? l_exact : l, head_factor<kFmt>(a, a.n_kv_heads + g));
+    const float factor = head_factor<kFmt>(a, a.n_kv_heads + g);
+    const float inv = l > 0.f ? factor / l : l == 0.f ? 0.f : __builtin_nanf("");
+    const int x = x0 + 32 * wave + (anew(lane) & 31);
+    if (kLse && half == 0 && x < queries)
+      a.lse[query_lse(a, heads, n, g, x)] = l_exact == 0.f ? -INFINITY : (m + log2f(l_exact)) / kLog2e;
+    // (K's buffers: every wave was done with them at the last step's barrier.)
+    write_queries(a, heads, n, g, x0 + 32 * wave, queries, o, inv, t.k + 8192 * wave);
     return;
   }
   // A piece: every lane's 64 elements in runs of four, a KB for the wave at a time.
@@ -794,6 +849,7 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Rows& ro
 
 template <int kFmt, bool kLse, typename Plan>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_prefill_kernel(PrefillArgs a,
+                                                                                                         Heads heads,
                                                                                                          int room,
                                                                                                          RBS_ROWS_ARGS) {
   const Rows rows{page_table, seq_lens, cu_tokens};
@@ -802,13 +858,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const Tiles t{tiles, tiles + 2 * kBlockBytes, bad};
   static_assert(sizeof(RowsPlan::Shared) <= sizeof(tiles), "the plan lies where the tiles will be");
   Plan plan;
-  plan.make(a, rows, room, tiles);
+  plan.make(a, heads, rows, room, tiles);
   int g, i;
-  slot_of(blockIdx.x, a.n_kv_heads, bunch_of(plan.units, a.n_kv_heads), &g, &i);
+  slot_of(blockIdx.x, heads, plan.units, &g, &i);
   if (i >= plan.units) return;
   const Unit n = unit_of(plan, rows, i);
   if (std::is_same<Plan, RowsPlan>::value) __syncthreads();  // every wave has read the plan
-  attend_unit<kFmt, kLse>(a, rows, n, plan.piece, g, t,
+  attend_unit<kFmt, kLse>(a, heads, rows, n, plan.piece, g, t,
                           n.parts > 1 ? a.workspace + (size_t)(g * plan.units + i) * kPartFloats : nullptr);
 }
 
@@ -816,7 +872,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 // elements, a wave to every fourth piece.  Bound by latency: the loads of kBatch pieces
 // of a wave are on their way together.
 template <int kFmt, typename Plan>
-__global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArgs a, int room, RBS_ROWS_ARGS) {
+__global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArgs a, Heads heads, int room,
+                                                                      RBS_ROWS_ARGS) {
   const Rows rows{page_table, seq_lens, cu_tokens};
   __shared__ union {
     RowsPlan::Shared plan;
@@ -826,15 +883,15 @@ __global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArg
     } part;
   } lds;
   Plan plan;
-  plan.make(a, rows, room, &lds.plan);
+  plan.make(a, heads, rows, room, &lds.plan);
   if (plan.piece == INT_MAX) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5, l32 = lane & 31;
-  const int group = a.n_q_heads / a.n_kv_heads, tile = blockIdx.x / a.n_kv_heads, g = blockIdx.x % a.n_kv_heads;
+  const int tile = (int)heads.n_kv.of(blockIdx.x), g = (int)blockIdx.x - tile * a.n_kv_heads;
   const int dt = blockIdx.y & 3, q0 = 32 * (blockIdx.y >> 2);
   if (tile >= plan.tiles) return;
   const Unit n = plan.row_of(rows, tile, true);
-  const int64_t queries = (int64_t)n.tokens * group, x0 = (int64_t)n.tile * kQueries + q0;
+  const int queries = n.tokens * (int)heads.group.d, x0 = n.tile * kQueries + q0;
   if (n.parts == 1 || x0 >= queries) return;
   __syncthreads();  // every wave has read the plan
   const float* slots = a.workspace + (size_t)(g * plan.units + n.first + n.tiles - 1 - n.tile) * kPartFloats;
@@ -905,14 +962,13 @@ __global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArg
     const float4 w = lds.part.o[v][wave][lane];
     r.x += w.x * f; r.y += w.y * f; r.z += w.z * f; r.w += w.w * f;
   }
-  const int64_t x = x0 + l32;
+  const int x = x0 + l32;
   if (x >= queries) return;
-  const int i = (int)(x / group), head = g * group + (int)(x - (int64_t)i * group), tok = n.begin + i;
   const float inv = l > 0.f ? head_factor<kFmt>(a, a.n_kv_heads + g) / l : l == 0.f ? 0.f : __builtin_nanf("");
-  *reinterpret_cast<uint2*>(a.O + head * a.q_head + tok * a.q_tok + 32 * dt + 8 * wave + 4 * half) =
+  *reinterpret_cast<uint2*>(a.O + query_offset(a, heads, n, g, x) + 32 * dt + 8 * wave + 4 * half) =
       make_uint2(two_bf16(r.x * inv, r.y * inv), two_bf16(r.z * inv, r.w * inv));
   if (a.lse != nullptr && half == 0 && dt == 0 && wave == 0)
-    a.lse[(int64_t)head * a.n_tokens + tok] = l_exact == 0.f ? -INFINITY : (top + log2f(l_exact)) / kLog2e;
+    a.lse[query_lse(a, heads, n, g, x)] = l_exact == 0.f ? -INFINITY : (top + log2f(l_exact)) / kLog2e;
 }
 
 template <int kFmt>
@@ -926,13 +982,15 @@ hipError_t launch(const PrefillArgs& a, hipStream_t s) {
   const int room = split ? kUnits / 2 / a.n_kv_heads : 0;
   // (Bunches round up a head's units, and the XCDs' shares of them.)
   const int grid = (int)((split ? kUnits : units) + 64 + 8 * a.n_kv_heads);
+  const Heads heads{Divisor((uint32_t)group), Divisor((uint32_t)a.n_kv_heads)};
   const bool few = a.n_rows <= 64;
   const auto kernel = few ? (a.lse != nullptr ? paged_prefill_kernel<kFmt, true, WavePlan> : paged_prefill_kernel<kFmt, false, WavePlan>)
                           : (a.lse != nullptr ? paged_prefill_kernel<kFmt, true, RowsPlan> : paged_prefill_kernel<kFmt, false, RowsPlan>);
-  hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), 0, s, a, room, a.page_table, a.seq_lens, a.cu_tokens);
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), 0, s, a, heads, room, a.page_table, a.seq_lens, a.cu_tokens);
   if (split) {
     const auto join = few ? paged_prefill_join_kernel<kFmt, WavePlan> : paged_prefill_join_kernel<kFmt, RowsPlan>;
-    hipLaunchKernelGGL(join, dim3((int)units, 16), dim3(kThreads), 0, s, a, room, a.page_table, a.seq_lens, a.cu_tokens);
+    hipLaunchKernelGGL(join, dim3((int)units, 16), dim3(kThreads), 0, s, a, heads, room, a.page_table, a.seq_lens,
+                       a.cu_tokens);
   }
   return hipGetLastError();
 }
