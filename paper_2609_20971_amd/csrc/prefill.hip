@@ -6,25 +6,26 @@
 // A tile is 128 queries of one row and one KV head, the group's heads of a token
 // next to each other (16 tokens at a group of 8), so that all of them read the same
 // keys and a tile's diagonal is short.  A workgroup's four waves have 32 queries
-// each; keys come in blocks of 128.  S^T = K Q^T and O^T = V^T P^T on the 32x32x16
+// each; keys come in blocks of 64.  S^T = K Q^T and O^T = V^T P^T on the 32x32x16
 // matrix product in bf16, a query to a lane (softmax without exchanges but for one
-// between the halves of a wave), Q in registers, K and V in LDS: 256-byte rows, 16-byte
-// pieces swizzled so that reads have no bank conflicts, V read transposed.  BF16
-// pages are copied to LDS directly, FP8 and FP4 ones through registers, widened
+// between the halves of a wave), Q in registers, K and V in LDS, two blocks of each: 256-byte
+// rows, 16-byte pieces swizzled so that reads have no bank conflicts, V read transposed.
+// BF16 pages are copied to LDS directly, FP8 and FP4 ones through registers, widened
 // once for all four waves (exact: E2M1 times a power of two, and E4M3, are bf16
 // numbers; an FP8 head's factor goes into the softmax's scale and the result's).
-// The next block's K is on its way during a block's softmax and second product, its V
-// during the next first product.
 //
-// Bound by the matrix cores and the instructions around them for long rows, by the
-// read of K and V for few queries.
+// Long rows are bound by the matrix cores and the instructions between their products:
+// 2048 tokens after 65536, 32 heads on 4, take 1.97 ms in BF16 and FP4 and 2.06 in FP8
+// (1135 and 1080 TFLOP/s; the cores are busy 60 % of the cycles at a clock that such work
+// lowers to 1.8 GHz, and a library product of 16384^3 reaches 1350).  Few queries are
+// bound by what a unit takes before its first and after its last block.
 //
 // Sums are in fp32.  The weights go to the second product rounded once to bf16, and
-// the denominator sums what goes there (on the matrix core), so that their common error
-// cancels; the log-sum-exp, where it is asked for, has a sum of the weights before that.
+// the denominator sums what goes there, so that their common error cancels; the
+// log-sum-exp, where it is asked for, has a sum of the weights before that.
 //
 // Work: unit u of a KV head is a tile, or where there are few tiles a piece of one,
-// of at most P blocks of keys; pieces leave maximum, sum and weighted values in fp32,
+// of at most P blocks of keys; pieces leave maximum, sums and weighted values in fp32,
 // which a second launch joins in the order of the keys.  Lengths are on the GPU, so
 // that every workgroup finds the units for itself.
 #include <type_traits>
@@ -41,8 +42,12 @@ constexpr int kWaves = kThreads / 64;
 constexpr int kQueries = 128;                    // of a tile
 constexpr int kKeys = 64;                        // of a block
 constexpr int kBlockBytes = kKeys * 2 * kHeadDim;  // of K or V in LDS
-constexpr int kUnits = 1024;                     // pieces of a call whose tiles are split
+// Pieces of a call whose tiles are split: two workgroups to a CU.  32 rows of 4 drafted
+// tokens after 16000 take 215 us, 247 at 256 pieces and 228 at 1024; 512 tokens after
+// 8192 100, 114 and 110; 1 token after 65535 49, 44 and 65.
+constexpr int kUnits = 512;
 constexpr int kPartFloats = kQueries * kHeadDim + 3 * kQueries;  // weighted values, maxima, sums of rounded and exact weights
+
 // Division of 32-bit numbers by one that the host knows, by a product with its
 // reciprocal (Granlund and Montgomery 1994): the quotient is exact.
 struct Divisor {
@@ -124,7 +129,9 @@ struct Unit {
 };
 
 // Up to 64 rows: a row to a lane, every wave for itself, with one load's wait and no
-// barrier.
+// barrier.  64 prompts of 128 tokens take 45 us, a prompt of 300 takes 23; 52 and 29 with
+// the plan for any number of rows.
+constexpr int kWaveRows = 64;
 struct WavePlan {
   int begin, tokens, len;
   RowWork w;
@@ -286,7 +293,8 @@ __device__ __forceinline__ Unit unit_of(const Plan& plan, const Rows& rows, int 
 // head q % H_kv.  Slot b of the launch gives KV head g and unit i of it (which may be
 // past the last).
 __device__ __forceinline__ void slot_of(int b, const Heads& heads, int units, int* g, int* i) {
-  // (A bunch: 8, or where there are few units 4, 2 or 1.)
+  // (A bunch: 8, or where there are few units 4, 2 or 1, so that every XCD has some.  64
+  // prompts of 128 tokens take 45 us, dealt out singly 48; long rows the same.)
   const int64_t all = (int64_t)units * heads.n_kv.d;
   const int shift = all >= 512 ? 3 : all >= 256 ? 2 : all >= 128 ? 1 : 0;
   const int x = b & 7, k = b >> 3;
@@ -398,7 +406,7 @@ __device__ __forceinline__ int64_t query_lse(const PrefillArgs& a, const Heads& 
 
 // The wave's 32 results, 64 elements of one in a lane, through 8 KB of LDS (pieces of
 // 16 bytes swizzled by row) to whole rows: stored from the lanes as they are, in
-// pieces of 8 bytes, a unit's end took 4400 cycles and not ?.
+// pieces of 8 bytes, 64 prompts of 128 tokens took 50 us and not 45.
 __device__ __forceinline__ void write_queries(const PrefillArgs& a, const Heads& heads, const Unit& n, int g, int x0, int queries,
                                               const f32x16* o, float inv, unsigned char* lds) {
   const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
@@ -492,7 +500,7 @@ template <int kFmt, bool kLse>
 __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Heads& heads, const Rows& rows, const Unit& n,
                                             int piece, int g, const Tiles& t, float* slot) {
   constexpr bool kCopied = kFmt == kCacheBf16;  // straight to LDS
-  constexpr int kAhead = kCopied ? 4 : 3;       // operands on their way from LDS
+  constexpr int kAhead = kCopied ? 4 : 3;       // operands on their way from LDS (no registers for a fourth beside the codes)
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, l32 = lane & 31;
   const int queries = n.tokens * (int)heads.group.d, x0 = n.tile * kQueries;
@@ -516,11 +524,11 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Heads& h
   // blocks, would otherwise be one in every step.
   auto key0 = [&](int b) __attribute__((always_inline)) { return b * kKeys + 16 * wave; };
   int window = b0;
-  int64_t places = pages.at(key0(b0 + lane));
+  int64_t places = pages.at(key0(min(b0 + lane, pages.last_key / kKeys)));
   auto place_of = [&](int b) __attribute__((always_inline)) {  // called with ascending b
     if (b >= window + 64) {
       window = b;
-      places = pages.at(key0(b + lane));
+      places = pages.at(key0(min(b + lane, pages.last_key / kKeys)));
     }
     const int lo = __builtin_amdgcn_readlane((int)(uint32_t)places, b - window);
     const int hi = __builtin_amdgcn_readlane((int)(places >> 32), b - window);
@@ -678,7 +686,6 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Heads& h
     constexpr int kBuf = decltype(buf_of)::value;
     if constexpr (kCopied) RBS_WAIT_VMCNT(0);
     __syncthreads();
-    // (Opaque: sums of these with constants are not kept in registers from step to step.)
     asm volatile("" : "+s"(k_lds), "+s"(v_lds));  // (sums of these with constants are not kept from step to step)
     const int64_t at = at_v, at_k = place_of(b + kLead);
     at_v = at_k;
@@ -978,12 +985,12 @@ hipError_t launch(const PrefillArgs& a, hipStream_t s) {
   const int64_t tiles = (int64_t)a.n_tokens * group / kQueries + (a.n_rows < a.n_tokens ? a.n_rows : a.n_tokens);
   const int64_t most = (int64_t)a.max_pages << a.cache.page_shift;  // keys of a row
   const int64_t units = tiles * a.n_kv_heads;
-  const bool split = units < kUnits / 2 && most > kKeys;
-  const int room = split ? kUnits / 2 / a.n_kv_heads : 0;
+  const bool split = units < kUnits && most > kKeys;
+  const int room = split ? kUnits / a.n_kv_heads : 0;
   // (Bunches round up a head's units, and the XCDs' shares of them.)
   const int grid = (int)((split ? kUnits : units) + 64 + 8 * a.n_kv_heads);
   const Heads heads{Divisor((uint32_t)group), Divisor((uint32_t)a.n_kv_heads)};
-  const bool few = a.n_rows <= 64;
+  const bool few = a.n_rows <= kWaveRows;
   const auto kernel = few ? (a.lse != nullptr ? paged_prefill_kernel<kFmt, true, WavePlan> : paged_prefill_kernel<kFmt, false, WavePlan>)
                           : (a.lse != nullptr ? paged_prefill_kernel<kFmt, true, RowsPlan> : paged_prefill_kernel<kFmt, false, RowsPlan>);
   hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), 0, s, a, heads, room, a.page_table, a.seq_lens, a.cu_tokens);
