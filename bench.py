@@ -82,7 +82,11 @@ def parse():
                    help="instead of the benchmark line: a prompt of the workload's length from a projection's output "
                         "(pages, norm and rotation, sparse prefill), then decode steps of this many requests with "
                         "that much in their paged cache")
-    p.add_argument("--serve-fp8", action="store_true", help="the serving mode's cache in FP8 (E4M3)")
+    fewer = p.add_mutually_exclusive_group()
+    fewer.add_argument("--serve-fp8", action="store_true", help="the serving mode's cache in FP8 (E4M3)")
+    fewer.add_argument("--serve-fp4", action="store_true", help="the serving mode's cache in 4 bits (E2M1, a scale for 32)")
+    p.add_argument("--serve-append", type=int, default=0,
+                   help="the serving mode: so many tokens of every request behind its prompt, in one call")
     p.add_argument("--layer-sweep", type=int, default=0,
                    help="instead of the benchmark line: this many layers of the 128K layer schedule "
                         "(per-layer key noise and needle counts), per-layer density and times, sparse vs "
@@ -953,7 +957,8 @@ def fp8_bench(args):
 def serve_bench(args):
     """One layer of a serving stack: a prompt's QKV projection output (random
     values) gets its pages, is normed, rotated and cached, and goes through the
-    sparse prefill; then decode steps of args.serve requests, each with a cached
+    sparse prefill; where asked for, more tokens of every request attend over the
+    pages; then decode steps of args.serve requests, each with a cached
     prompt of that length, replayed as one graph a step.  One JSON line."""
     import numpy as np
     import torch
@@ -971,10 +976,11 @@ def serve_bench(args):
         qkv = torch.randn(tokens, hq + 2 * hkv, d, generator=gen, device=dev, dtype=torch.bfloat16).transpose(0, 1)
         return qkv[:hq], qkv[hq:hq + hkv], qkv[hq + hkv:]
 
-    per_row = -(-(n + steps + 2) // page)
+    more = max(0, args.serve_append)
+    per_row = -(-(n + 4 * more + steps + 2) // page)
     pages = rbs.Pages.allocate(rows, per_row, rows * per_row, page, dev)
     amax = torch.full((2 * hkv,), 6.0, device=dev) if args.serve_fp8 else None
-    cache = rbs.PagedCache.allocate(rows * per_row, page, hkv, amax=amax, device=dev)
+    cache = rbs.PagedCache.allocate(rows * per_row, page, hkv, amax=amax, device=dev, fp4=args.serve_fp4)
     ones = torch.ones(d, dtype=torch.bfloat16, device=dev)
     inv_freq, factor = rbs.rope_frequencies(device=dev)
     rope = rbs.Rope(inv_freq, ones, ones, factor=factor)
@@ -1000,6 +1006,32 @@ def serve_bench(args):
 
     times = [one_prompt(row, *project(n)) for row in range(rows)]
     pages_ms, rope_ms, prefill_ms = (float(np.median(x)) for x in zip(*(times[1:] or times)))
+
+    def append(Q, K, V):
+        counts = torch.full((rows,), more, dtype=torch.int32, device=dev)
+        marks = _events(torch, 3)
+        step = rbs.rbs_pages_extend(pages, counts, rows * more)
+        sh = rbs.make_shape(rows * more, hq, hkv, w.block_size)
+        marks[0].record()
+        q, _ = rbs.rbs_qk_norm_rope(sh, rope, Q, K, step.positions, V=V, cache=cache, slots=step.slots, keep_k=False)
+        marks[1].record()
+        rbs.rbs_paged_prefill(sh, q, cache, pages.page_table, step.seq_lens, step.cu_tokens)
+        marks[2].record()
+        torch.cuda.synchronize()
+        if int(step.status.item()) != 0:
+            raise RuntimeError(f"rbs_pages_extend: status {int(step.status.item())}")
+        return [a.elapsed_time(b) for a, b in zip(marks, marks[1:])]
+
+    appended = {}
+    if more > 0:
+        times = [append(*project(rows * more)) for _ in range(4)]
+        rope_more, attend_more = (float(np.median(x)) for x in zip(*times[1:]))
+        # Two products; a token's keys (of the median of the last three calls) are those before it and its own.
+        flops = 4.0 * rows * hq * d * more * (n + 2 * more + (more + 1) / 2)
+        appended = {"append_tokens": more, "append_norm_rope_ms": round(rope_more, 4),
+                    "append_attention_ms": round(attend_more, 4), "append_tflops": round(flops / attend_more / 1e9, 1)}
+        _log(f"[serve] {more} tokens more of each row: norm and rotation {rope_more:.3f} ms, attention over the pages "
+             f"{attend_more:.3f} ms ({flops / attend_more / 1e9:.0f} TFLOP/s)")
 
     Q, K, V = project(rows)
     rows_shape = rbs.make_shape(rows, hq, hkv, w.block_size)
@@ -1027,16 +1059,17 @@ def serve_bench(args):
     if int(out.status.item()) != 0:
         raise RuntimeError(f"rbs_pages_extend: status {int(out.status.item())}")
     step_us = 1e3 * float(np.median([a.elapsed_time(b) for a, b in zip(marks, marks[1:])]))
-    read = rows * (n + steps // 2) * hkv * d * 2 * (1 if args.serve_fp8 else 2)
+    row_bytes = d // 2 + d // 32 if args.serve_fp4 else d if args.serve_fp8 else 2 * d
+    read = rows * (n + 4 * more + steps // 2) * hkv * 2 * row_bytes
     _log(f"[serve] prompt: pages {pages_ms:.3f} ms, norm and rotation {rope_ms:.3f} ms, prefill {prefill_ms:.3f} ms; "
          f"decode of {rows} rows {step_us:.1f} us ({read / step_us / 1e3:.0f} GB/s of keys and values)")
     print(json.dumps({
         "mode": "serve", "workload": w.name, "data": "synthetic", "rows": rows, "steps": steps,
-        "cache": "fp8 e4m3" if args.serve_fp8 else "bf16", "page_size": page,
+        "cache": "fp4 e2m1" if args.serve_fp4 else "fp8 e4m3" if args.serve_fp8 else "bf16", "page_size": page,
         "prompt_pages_ms": round(pages_ms, 4), "prompt_norm_rope_ms": round(rope_ms, 4),
         "prompt_prefill_ms": round(prefill_ms, 4), "decode_step_us": round(step_us, 2),
         "decode_kv_gbps": round(read / step_us / 1e3, 1),
-        "decode_tokens_per_s": round(rows / step_us * 1e6, 1),
+        "decode_tokens_per_s": round(rows / step_us * 1e6, 1), **appended,
     }), flush=True)
 
 

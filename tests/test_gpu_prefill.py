@@ -265,3 +265,21 @@ def test_pages_past_32_bits():
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
         del far, moved
         torch.cuda.empty_cache()
+
+
+def test_longest_row():
+    """A table of nearly 2^31 places, all of one page, and a length past it: every key 0 and every value 1, so that all
+    weights are 1 and the sums whole numbers (exact in a piece, of at most 2^22 + 64 keys, and off by a rounding each
+    where 512 pieces are joined)."""
+    page, columns = 256, 2 ** 23 - 1
+    cache = rbs.PagedCache.allocate(1, page, 1)
+    cache.K.zero_()
+    cache.V.fill_(1.0)
+    table = torch.zeros(1, columns, dtype=torch.int32, device="cuda")
+    Q = torch.randn(2, 8, D, generator=_gen(77)).to(torch.bfloat16).cuda().transpose(0, 1)
+    lse = torch.empty(8, 2, device="cuda")
+    O = rbs.rbs_paged_prefill(rbs.make_shape(2, 8, 1, 64), Q, cache, table, _ints([2 ** 31 - 1]), _ints([0, 2]), lse=lse)
+    assert bool((O == 1.0).all())
+    want = math.log(columns * page)
+    # The sum: 516 roundings; log2 and the change of base: 2 steps of the result's 31 each.
+    assert bool(((lse.cpu().double() - want).abs() <= 516 * R.U32 + 4 * want * R.U32).all())
