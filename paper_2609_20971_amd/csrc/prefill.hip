@@ -6,7 +6,8 @@
 // A tile is 128 queries of one row and one KV head, the group's heads of a token
 // next to each other (16 tokens at a group of 8), so that all of them read the same
 // keys and a tile's diagonal is short.  A workgroup's four waves have 32 queries
-// each; keys come in blocks of 64.  S^T = K Q^T and O^T = V^T P^T on the 32x32x16
+// each (of a row of at most 32 queries all of them, and every fourth block of keys each:
+// attend_few); keys come in blocks of 64.  S^T = K Q^T and O^T = V^T P^T on the 32x32x16
 // matrix product in bf16, a query to a lane (softmax without exchanges but for one
 // between the halves of a wave), Q in registers, K and V in LDS, two blocks of each: 256-byte
 // rows, 16-byte pieces swizzled so that reads have no bank conflicts, V read transposed.
@@ -41,6 +42,7 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kQueries = 128;                    // of a tile
 constexpr int kKeys = 64;                        // of a block
+constexpr int kFewQueries = 32;                  // a row's, up to which its keys are divided among the waves
 constexpr int kBlockBytes = kKeys * 2 * kHeadDim;  // of K or V in LDS
 // Pieces of a call whose tiles are split: two workgroups to a CU.  32 rows of 4 drafted
 // tokens after 16000 take 215 us, 247 at 256 pieces and 228 at 1024; 512 tokens after
@@ -352,16 +354,16 @@ struct Staged {
       if (kFmt == kCacheFp4) scale = *reinterpret_cast<const uint8_t*>(scales + (at >> 4) + r * (tok_bytes >> 4) + piece);
     }
   }
-  // Where the lane's pieces go in a block's rows: 256 row0 + (swz ^ ..), row0 16 wave +
-  // lane / .. and the piece kPieces (lane % ..); the swizzle's bits that k and p give are
+  // Where the lane's pieces go in a block's rows: 256 row0 + (swz ^ ..), row0 16 run +
+  // lane / .. (of the block's run of 16 keys) and the piece kPieces (lane % ..); the swizzle's bits that k and p give are
   // apart from the lane's.
   static constexpr int kPieces = kFmt == kCacheFp8 ? 2 : 4;  // of 16 bytes, of a load
   struct Place {
     uint32_t row, k_swz, v_swz;
   };
-  static __device__ __forceinline__ Place place() {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int row0 = 16 * wave + lane / (64 / kRows), c0 = kPieces * (lane % (64 / kRows));
+  static __device__ __forceinline__ Place place(int run) {
+    const int lane = threadIdx.x & 63;
+    const int row0 = 16 * run + lane / (64 / kRows), c0 = kPieces * (lane % (64 / kRows));
     return Place{256u * row0, 16u * (uint32_t)kswz(row0, c0), 16u * (uint32_t)vswz(row0, c0)};
   }
   // Piece p (of 4) of the lane's elements to the block at byte `lds` of LDS.
@@ -432,10 +434,33 @@ struct Tiles {
   unsigned char* k;
   unsigned char* v;
   int* bad;  // [kKeys]: the key's value is not finite
+  float (*sums)[kWaves][32];  // maximum, sum and exact sum of each wave's queries (attend_few)
 };
 
 __device__ __forceinline__ bool not_finite(uint32_t pair) {
   return (pair & 0x7f80u) == 0x7f80u || (pair & 0x7f800000u) == 0x7f800000u;
+}
+
+// A pair of values without those that are not finite.
+__device__ __forceinline__ uint32_t finite_only(uint32_t z) {
+  if ((z & 0x7f80u) == 0x7f80u) z &= 0xffff0000u;
+  if ((z & 0x7f800000u) == 0x7f800000u) z &= 0xffffu;
+  return z;
+}
+
+// The values of a key of the block at v that are not finite, added to the queries that attend it.
+__device__ __forceinline__ void add_not_finite(const unsigned char* v, int key, int limit, int half, f32x16* o) {
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int rq = 0; rq < 4; ++rq) {
+      const int d = 32 * dt + 8 * rq + 4 * half;
+      const uint2 w = *reinterpret_cast<const uint2*>(v + key * 256 + 16 * vswz(key, d >> 3) + 2 * (d & 7));
+      const float x[4] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (key <= limit && !(fabsf(x[e]) < INFINITY)) o[dt][4 * rq + e] += x[e];
+    }
 }
 
 // Masked blocks: a weight of 0 times a value that is not finite would be NaN, so
@@ -463,28 +488,37 @@ __device__ __forceinline__ void take_out(unsigned char* v, int* bad, int limit, 
 #pragma unroll 1
   for (int key = 0; key < kKeys; ++key) {
     if (__builtin_amdgcn_readfirstlane(bad[key]) == 0) continue;
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-      for (int rq = 0; rq < 4; ++rq) {
-        const int d = 32 * dt + 8 * rq + 4 * half;
-        const uint2 w = *reinterpret_cast<const uint2*>(v + key * 256 + 16 * vswz(key, d >> 3) + 2 * (d & 7));
-        const float x[4] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (key <= limit && !(fabsf(x[e]) < INFINITY)) o[dt][4 * rq + e] += x[e];
-      }
+    add_not_finite(v, key, limit, half, o);
   }
   __syncthreads();
 #pragma unroll 1
   for (int k = 0; k < 4 * kLoads; ++k) {
     uint32_t* at = reinterpret_cast<uint32_t*>(v) + tid + kThreads * k;
-    uint32_t z = *at;
-    if ((z & 0x7f80u) == 0x7f80u) z &= 0xffff0000u;
-    if ((z & 0x7f800000u) == 0x7f800000u) z &= 0xffffu;
-    *at = z;
+    *at = finite_only(*at);
   }
   __syncthreads();
+}
+
+// The same of a wave's own 32 keys.
+__device__ __forceinline__ void take_out_of_wave(unsigned char* v, int limit, f32x16* o) {
+  const int lane = anew((int)threadIdx.x & 63);
+  uint32_t bad = 0;  // a bit to a key
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const uint4 w = *reinterpret_cast<const uint4*>(v + 16 * (lane + 64 * k));
+    const uint64_t any = __ballot(not_finite(w.x) || not_finite(w.y) || not_finite(w.z) || not_finite(w.w));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bad |= (any >> (16 * e) & 0xffff) != 0 ? 1u << (4 * k + e) : 0u;
+  }
+  if (bad == 0) return;
+#pragma unroll 1
+  for (uint32_t rest = bad; rest != 0; rest &= rest - 1) add_not_finite(v, __builtin_ctz(rest), limit, lane >> 5, o);
+#pragma unroll 1
+  for (int k = 0; k < 32; ++k) {
+    uint32_t* at = reinterpret_cast<uint32_t*>(v) + lane + 64 * k;
+    *at = finite_only(*at);
+  }
+  asm volatile("" ::: "memory");
 }
 
 // The order of instructions is that of the source here.
@@ -586,7 +620,7 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Heads& h
   };
   Staged<kCopied ? kCacheFp8 : kFmt> k_next, v_next;
   const uint32_t k_at0 = lds_offset(t.k), v_at0 = lds_offset(t.v);
-  const typename Staged<kCopied ? kCacheFp8 : kFmt>::Place place = Staged<kCopied ? kCacheFp8 : kFmt>::place();
+  const typename Staged<kCopied ? kCacheFp8 : kFmt>::Place place = Staged<kCopied ? kCacheFp8 : kFmt>::place(wave);
 
   // Operands from LDS.  K: row 32 mt + l32, pieces 2 ks + half.  V (transposed): rows
   // 16 c + 4 half + (lane % 16) / 4 (and + 8), elements 32 dt + 16 ((lane / 16) % 2) + 4 (lane % 4).
@@ -854,6 +888,267 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Heads& h
   }
 }
 
+// A unit of a row of at most 32 queries: a wave has all of them and every fourth block of
+// 32 keys for itself, in its own quarter of LDS, so that no wave waits for another before
+// the end, where the waves' sums are joined.  K of the wave's next block (FP8, FP4: its
+// codes) is on its way during this one's exponentials and second product, V during the
+// next first product.  32 rows of 4 tokens after 16000, 32 heads on 4, take 204 us in
+// BF16, 114 in FP8 and 104 in FP4 (5.1, 4.6 and 2.7 TB/s; FP4 is bound by the instructions of the
+// widening and the softmax), and 218, 165 and 155 as tiles; rows of 33 to 64 queries, two
+// waves to a block, took 175 us in FP4 and as tiles 155.
+template <int kFmt, bool kLse>
+__device__ __forceinline__ void attend_few(const PrefillArgs& a, const Heads& heads, const Rows& rows, const Unit& n,
+                                           int piece, int g, const Tiles& t, float* slot) {
+  constexpr bool kCopied = kFmt == kCacheBf16;
+  constexpr int kOwn = 32;  // keys of a block
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int half = lane >> 5, l32 = lane & 31;
+  const int queries = n.tokens * (int)heads.group.d;
+  const int before = n.len - n.tokens;
+  const int held = (int)min((int64_t)n.len, (int64_t)a.max_pages << a.cache.page_shift);
+  const int tile_last = min(before + n.tokens - 1, held - 1);
+
+  Pages pages;
+  pages.table = rows.page_table + (int64_t)n.row * a.max_pages;
+  pages.n_pages = a.cache.n_pages;
+  pages.shift = a.cache.page_shift;
+  pages.last_key = max(tile_last, 0);
+  pages.page_bytes = a.cache.page * kCodeBytes<kFmt> / kHeadDim;
+  pages.tok_bytes = (uint32_t)(a.cache.tok * kCodeBytes<kFmt> / kHeadDim);
+  const int last_block = pages.last_key / kOwn, blocks = tile_last < 0 ? 0 : last_block + 1;
+  constexpr int kPer = kKeys / kOwn;
+  const int b0 = (piece == INT_MAX ? 0 : n.part * piece * kPer) + wave;
+  const int b1 = piece == INT_MAX ? blocks : min(blocks, (n.part + 1) * piece * kPer);
+  // Lane i holds where run i % 2 (of 16 keys) of the wave's block window + i / 2 is.
+  int window = b0;
+  auto look = [&](int b) __attribute__((always_inline)) {
+    return pages.at(min(b + kWaves * (lane >> 1), last_block) * kOwn + 16 * (lane & 1));
+  };
+  int64_t places = look(b0);
+  auto place_of = [&](int b, int run) __attribute__((always_inline)) {  // called with ascending b
+    if (b >= window + 32 * kWaves) {
+      window = b;
+      places = look(b);
+    }
+    const int i = 2 * ((b - window) / kWaves) + run;
+    const int lo = __builtin_amdgcn_readlane((int)(uint32_t)places, i);
+    const int hi = __builtin_amdgcn_readlane((int)(places >> 32), i);
+    return (int64_t)((uint64_t)(uint32_t)hi << 32 | (uint32_t)lo);
+  };
+  auto last_of = [&](int b, int run) __attribute__((always_inline)) {  // the row's last key among the run's (15 if it is behind them)
+    const int left = pages.last_key - b * kOwn - 16 * run;
+    return left < 0 ? pages.last_key & 15 : min(15, left);
+  };
+  const int first_last = min(before, held - 1);   // the last key of the row's first query
+  const int plain = (first_last + 1) / kOwn;      // blocks before it are attended whole
+  int last;
+  bf16x8 q[8];
+  {
+    const int x = min(l32, queries - 1), i = (int)heads.group.of(x);
+    last = min(before + i, held - 1);
+    const uint16_t* row = a.Q + query_offset(a, heads, n, g, x) + 8 * half;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) q[ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(row + 16 * ks));
+  }
+  const int64_t head_bytes = g * a.cache.head * kCodeBytes<kFmt> / kHeadDim;
+  const char* K = static_cast<const char*>(a.cache.K) + head_bytes;
+  const char* V = static_cast<const char*>(a.cache.V) + head_bytes;
+  const char* Ks = static_cast<const char*>(a.cache.K_scale) + g * a.cache.head / 32;
+  const char* Vs = static_cast<const char*>(a.cache.V_scale) + g * a.cache.head / 32;
+  const float scale_log2 = a.scale * kLog2e * head_factor<kFmt>(a, g);
+
+  // The wave's LDS: K, then V.
+  unsigned char* own = t.k + wave * 2 * kOwn * 256;
+  const uint32_t k_lds = __builtin_amdgcn_readfirstlane(lds_offset(own)), v_lds = k_lds + kOwn * 256;
+  auto copy = [&](bool is_v, int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int run = 0; run < 2; ++run) {
+      const char* from = (is_v ? V : K) + place_of(b, run);
+      const int top = last_of(b, run);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int r = 4 * c + (lane >> 4), piece_at = is_v ? vswz(r, lane & 15) : kswz(r, lane & 15);
+        lds_dma16(from, (uint32_t)min(r, top) * pages.tok_bytes + 16u * (uint32_t)piece_at,
+                  (is_v ? v_lds : k_lds) + 4096u * run + 1024u * c);
+      }
+    }
+  };
+  typedef Staged<kCopied ? kCacheFp8 : kFmt> Codes;
+  Codes k_next[2], v_next[2];
+  const typename Codes::Place place = Codes::place(0);
+  auto load = [&](Codes* to, bool is_v, int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int run = 0; run < 2; ++run)
+      to[run].load(is_v ? V : K, is_v ? Vs : Ks, place_of(b, run), pages.tok_bytes, last_of(b, run));
+  };
+  auto widen = [&](const Codes* from, bool is_v) __attribute__((always_inline)) {
+#pragma unroll
+    for (int run = 0; run < 2; ++run)
+#pragma unroll
+      for (int p = 0; p < 4; ++p) from[run].store(place, (is_v ? v_lds : k_lds) + 4096u * run, is_v, p);
+  };
+
+  const int vq = (lane & 15) >> 2;
+  const uint32_t k_row = k_lds + (uint32_t)l32 * 256u, k_swz = 16u * (uint32_t)kswz(l32, half);
+  const uint32_t v_row = v_lds + (uint32_t)(4 * half + vq) * 256u + 8u * (lane & 1);
+  const uint32_t v_swz = 16u * (uint32_t)vswz(vq, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1));
+  typedef const __attribute__((address_space(3))) u32x4 lds_u32x4;
+
+  float l = 0.f, l_exact = 0.f, m = -INFINITY, shift = 0.f;
+  f32x16 o[4];
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt) o[dt] = f32x16{};
+
+  if (b0 < b1) {
+    if constexpr (kCopied) {
+      copy(false, b0);
+      copy(true, b0);
+    } else {
+      load(k_next, false, b0);
+      load(v_next, true, b0);
+    }
+  }
+#pragma unroll 1
+  for (int b = b0; b < b1; b += kWaves) {
+    const int next = b + kWaves;
+    const bool more = next < b1;
+    if constexpr (kCopied) RBS_WAIT_VMCNT(8);  // (the eight copies of V may be on their way)
+    else widen(k_next, false);
+    f32x16 s{};
+    const uint32_t k_swz_ = anew(k_swz);
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks)
+      s = mfma_bf16(__builtin_bit_cast(bf16x8, *(lds_u32x4*)(uintptr_t)(k_row + (k_swz_ ^ (32u * ks)))), q[ks], s);
+    if (more) {
+      if constexpr (kCopied) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K has been read
+        copy(false, next);
+      } else {
+        load(k_next, false, next);
+      }
+    }
+    fence();
+    if (b >= plain) {
+      const int lim = last - b * kOwn - 4 * half;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = (8 * (r >> 2) + (r & 3)) > lim ? -INFINITY : s[r];
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[r]);
+    top = half_max(top) * scale_log2;
+    if (__any(top > m + kRescaleSlack)) {
+      const float m_new = top > m + kRescaleSlack ? top : m;
+      const float f = m_new == m ? 1.f : fast_exp2(m - m_new);
+      m = m_new;
+      shift = m == -INFINITY ? 0.f : m;
+      l *= f;
+      l_exact *= f;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[dt][r] *= f;
+    }
+    uint32_t pw[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float e0 = fast_exp2(fmaf(s[2 * j], scale_log2, -shift)), e1 = fast_exp2(fmaf(s[2 * j + 1], scale_log2, -shift));
+      if (kLse) l_exact += e0 + e1;
+      pw[j] = two_bf16(e0, e1);
+      const uint32_t ones = 0x3f803f80u;
+      l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw[j]), __builtin_bit_cast(bf16x2, ones), l, false);
+    }
+    if constexpr (kCopied) {
+      if (more) RBS_WAIT_VMCNT(8);  // (the next K's copies)
+      else RBS_WAIT_VMCNT(0);
+    } else {
+      widen(v_next, true);
+    }
+    asm volatile("" ::: "memory");
+    if (b >= plain) take_out_of_wave(own + kOwn * 256, last - b * kOwn, o);
+    const uint32_t v_swz_ = anew(v_swz);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      fence();
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) {
+        const uint32_t at = v_row + (v_swz_ ^ (64u * dt)) + 4096u * c;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)at);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(at + 8 * 256));
+        bf16x8 v;
+        __builtin_memcpy(&v, &lo, 8);
+        __builtin_memcpy(reinterpret_cast<unsigned char*>(&v) + 8, &hi, 8);
+        o[dt] = mfma_bf16(v, __builtin_bit_cast(bf16x8, make_uint4(pw[4 * c], pw[4 * c + 1], pw[4 * c + 2], pw[4 * c + 3])), o[dt]);
+      }
+    }
+    fence();
+    if (more) {
+      if constexpr (kCopied) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // V has been read
+        copy(true, next);
+      } else {
+        load(v_next, true, next);
+      }
+    }
+  }
+
+  // The waves' sums, joined: each takes a quarter of the elements from all of them.
+  l = half_sum(l);
+  if (kLse) l_exact = half_sum(l_exact);
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int k = 0; k < 16; ++k)
+    *reinterpret_cast<float4*>(own + 16 * (64 * k + lane)) = make_float4(o[k >> 2][4 * (k & 3)], o[k >> 2][4 * (k & 3) + 1],
+                                                                         o[k >> 2][4 * (k & 3) + 2], o[k >> 2][4 * (k & 3) + 3]);
+  if (half == 0) {
+    t.sums[0][wave][l32] = m;
+    t.sums[1][wave][l32] = l;
+    if (kLse) t.sums[2][wave][l32] = l_exact;
+  }
+  __syncthreads();
+  float top = t.sums[0][0][l32];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) top = fmaxf(top, t.sums[0][w][l32]);
+  const float ref = top == -INFINITY ? 0.f : top;
+  float f[kWaves];
+  l = l_exact = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const float wl = t.sums[1][w][l32];
+    f[w] = wl == 0.f ? 0.f : fast_exp2(t.sums[0][w][l32] - ref);
+    l += wl * f[w];
+    if (kLse && f[w] != 0.f) l_exact += t.sums[2][w][l32] * f[w];
+  }
+  const bool whole = n.parts == 1, mine = l32 < queries;
+  const float factor = head_factor<kFmt>(a, a.n_kv_heads + g);
+  const float inv = l > 0.f ? factor / l : l == 0.f ? 0.f : __builtin_nanf("");
+  if (half == 0 && wave == 0) {
+    if (!whole) {
+      float* sums = slot + kQueries * kHeadDim + l32;
+      sums[0] = top;
+      sums[kQueries] = l;
+      if (kLse) sums[2 * kQueries] = l_exact;
+    } else if (kLse && mine) {
+      a.lse[query_lse(a, heads, n, g, l32)] = l_exact == 0.f ? -INFINITY : (top + log2f(l_exact)) / kLog2e;
+    }
+  }
+  uint16_t* out = a.O + query_offset(a, heads, n, g, min(l32, queries - 1)) + 4 * half;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int k = 4 * wave + e;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (f[w] == 0.f) continue;
+      const float4 p = *reinterpret_cast<const float4*>(t.k + w * 2 * kOwn * 256 + 16 * (64 * k + lane));
+      v.x += p.x * f[w]; v.y += p.y * f[w]; v.z += p.z * f[w]; v.w += p.w * f[w];
+    }
+    if (!whole) *reinterpret_cast<float4*>(slot + 4 * (64 * k + lane)) = v;
+    else if (mine) *reinterpret_cast<uint2*>(out + 8 * k) = make_uint2(two_bf16(v.x * inv, v.y * inv), two_bf16(v.z * inv, v.w * inv));
+  }
+}
+
 template <int kFmt, bool kLse, typename Plan>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_prefill_kernel(PrefillArgs a,
                                                                                                          Heads heads,
@@ -862,7 +1157,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const Rows rows{page_table, seq_lens, cu_tokens};
   __shared__ __align__(1024) unsigned char tiles[4 * kBlockBytes + 128];
   __shared__ int bad[kKeys];
-  const Tiles t{tiles, tiles + 2 * kBlockBytes, bad};
+  __shared__ float sums[3][kWaves][32];
+  const Tiles t{tiles, tiles + 2 * kBlockBytes, bad, sums};
   static_assert(sizeof(RowsPlan::Shared) <= sizeof(tiles), "the plan lies where the tiles will be");
   Plan plan;
   plan.make(a, heads, rows, room, tiles);
@@ -871,8 +1167,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   if (i >= plan.units) return;
   const Unit n = unit_of(plan, rows, i);
   if (std::is_same<Plan, RowsPlan>::value) __syncthreads();  // every wave has read the plan
-  attend_unit<kFmt, kLse>(a, heads, rows, n, plan.piece, g, t,
-                          n.parts > 1 ? a.workspace + (size_t)(g * plan.units + i) * kPartFloats : nullptr);
+  float* slot = n.parts > 1 ? a.workspace + (size_t)(g * plan.units + i) * kPartFloats : nullptr;
+  if (n.tokens * (int)heads.group.d <= kFewQueries) attend_few<kFmt, kLse>(a, heads, rows, n, plan.piece, g, t, slot);
+  else attend_unit<kFmt, kLse>(a, heads, rows, n, plan.piece, g, t, slot);
 }
 
 // Joins the pieces of a tile, in their order: a workgroup to 32 queries and 32 of their

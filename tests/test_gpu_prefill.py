@@ -125,6 +125,12 @@ ROWS = [
     ([(0, 2600)], 32, 4, 128, "fp4", "heads", "tokens", 0, 0.0),                                                # whole tiles
     ([(0, 2600)], 32, 4, 16, "fp8", "heads", "tokens", 0, 0.0),
     ([(0, 2600), (31, 2)], 32, 4, 16, "bf16", "heads", "tokens", 0, 0.0),
+    # At most 32 queries to a row, whole rows to a unit (the longest past 4096 keys).
+    ([(9000, 3), (31, 1), (32, 1), (28, 4), (0, 32), (5, 27)] + [(20, 2)] * 66, 8, 8, 16, "bf16", "heads", "tokens", 0, 0.0),
+    ([(9000, 3), (31, 1), (32, 1), (28, 4), (0, 32), (5, 27)] + [(20, 2)] * 66, 8, 8, 32, "fp8", "heads", "heads", 3, 0.0),
+    ([(9000, 3), (31, 1), (32, 1), (28, 4), (0, 32), (5, 27)] + [(20, 2)] * 66, 8, 8, 16, "fp4", "tokens", "qkv", 0, 0.0),
+    ([(2500, 32), (2500, 33), (95, 32), (96, 1)], 4, 4, 16, "fp4", "heads", "tokens", 0, 0.0),
+    ([(2500, 4), (2500, 5), (90, 2)], 28, 4, 16, "bf16", "heads", "tokens", 0, 0.0),
 ]
 
 
@@ -134,7 +140,7 @@ def test_prefill(k):
     _say(f"[prefill] {len(rows)} rows, heads {hq}/{hkv}, page {page}, {fmt}")
     c = _case(rows, hq, hkv, page, fmt, layout, 300 + k, spare)
     O, lse = _run(c, scale, q_layout)
-    some = None if len(rows) < 40 else set(range(0, len(rows), 17))
+    some = None if len(rows) < 40 else set(range(6)) | set(range(0, len(rows), 17))
     _say(f"[prefill] {_check(c, O, lse, scale if scale > 0 else 1 / math.sqrt(D), some):.3f} of the tolerance")
     O2, _ = _run(c, scale, q_layout, lse=False)
     assert torch.equal(O, O2), "the same call again"
@@ -181,6 +187,18 @@ def test_infinite_values_are_attended():
     assert bool(O[:, :35].isfinite().all())
     assert bool((O[:, 35:48, 9] == math.inf).all()) and bool(O[:, 48:, 9].isnan().all())
     O[:, :, 9] = 0
+    assert bool(O.isfinite().all())
+
+
+def test_infinite_values_of_few_queries():
+    """The same where the waves divide the keys: 4 heads of 8 tokens; position 35 is attended by the last three."""
+    c = _case([(30, 8)], 4, 1, 16, "bf16", "heads", 49)
+    c["cache"].V[int(c["table"][0, 2]), 0, 3, 9] = math.inf    # position 35
+    c["cache"].V[int(c["table"][0, 0]), 0, 7, 70] = -math.inf  # position 7: attended by all
+    O, lse = _run(c)
+    assert bool(O[:, :5, 9].isfinite().all()) and bool((O[:, 5:, 9] == math.inf).all())
+    assert bool((O[:, :, 70] == -math.inf).all()) and bool(lse.isfinite().all())
+    O[:, :, 9] = O[:, :, 70] = 0
     assert bool(O.isfinite().all())
 
 
