@@ -44,10 +44,13 @@ constexpr int kQueries = 128;                    // of a tile
 constexpr int kKeys = 64;                        // of a block
 constexpr int kFewQueries = 32;                  // a row's, up to which its keys are divided among the waves
 constexpr int kBlockBytes = kKeys * 2 * kHeadDim;  // of K or V in LDS
-// Pieces of a call whose tiles are split: two workgroups to a CU.  32 rows of 4 drafted
-// tokens after 16000 take 215 us, 247 at 256 pieces and 228 at 1024; 512 tokens after
-// 8192 100, 114 and 110; 1 token after 65535 49, 44 and 65.
+// Pieces of a call whose tiles are split: two workgroups to a CU.  512 tokens after 8192
+// take 90 us, 100 at 256 pieces and at 1024; 32 rows of 4 drafted tokens after 16000 in
+// FP4 99, 140 and 108; 1 token after 65535 37, 34 and 48.
 constexpr int kUnits = 512;
+// Blocks of a piece, at least.  4 tokens after 16384 in FP4 take 19.6 us, 22.7 with pieces of 2;
+// 128 after 1024 19.5 and 21.0, 1 after 3000 14.5 and 13.9.
+constexpr int kLeast = 4;
 constexpr int kPartFloats = kQueries * kHeadDim + 3 * kQueries;  // weighted values, maxima, sums of rounded and exact weights
 
 // Division of 32-bit numbers by one that the host knows, by a product with its
@@ -118,9 +121,18 @@ struct Tries {
 };
 __device__ __forceinline__ Tries tries_of(int tiles, float blocks, int room) {
   Tries t;
-  t.least = __builtin_amdgcn_readfirstlane(max((int)fminf(blocks * 0.999f / room, (float)kMost), 1));
-  t.enough = __builtin_amdgcn_readfirstlane((int)fminf(blocks * 1.001f / (room - tiles), (float)kMost) + 1);
+  t.least = __builtin_amdgcn_readfirstlane(max((int)fminf(blocks * 0.999f / room, (float)kMost), kLeast));
+  t.enough = max(__builtin_amdgcn_readfirstlane((int)fminf(blocks * 1.001f / (room - tiles), (float)kMost) + 1), kLeast);
   return t;
+}
+
+// Whether pieces are worth their join: what the longest row's tiles save by them against
+// the join, in the time of a block by itself (1.24 us; beside another workgroup's 2).  A join
+// is a launch and the parts' way through memory.  Whole and in pieces: 1024 tokens 29 and
+// 41 us, 1024 after 2048 70 and 74, 1024 after 8192 191 and 170, 64 after 2048 44 and 20.
+__device__ __forceinline__ bool worth(float longest, int piece, int64_t units) {
+  const float u = (float)units, beside = fminf(fmaxf(u * (2.f / kUnits) - 1.f, 0.f), 1.f);
+  return __builtin_amdgcn_readfirstlane(longest - (float)piece * (1.f + 0.63f * beside) > 3.f + u * (1.f / 55.f)) != 0;
 }
 
 // A tile, or a piece of one.
@@ -131,10 +143,11 @@ struct Unit {
 };
 
 // Up to 64 rows: a row to a lane, every wave for itself, with one load's wait and no
-// barrier.  64 prompts of 128 tokens take 45 us, a prompt of 300 takes 23; 52 and 29 with
+// barrier.  64 prompts of 128 tokens take 44 us, a prompt of 300 takes 17; 51 and 27 with
 // the plan for any number of rows.
 constexpr int kWaveRows = 64;
 struct WavePlan {
+  struct Shared {};
   int begin, tokens, len;
   RowWork w;
   int tile_end, unit_end;  // of this row, counted over the rows up to it
@@ -152,8 +165,11 @@ struct WavePlan {
     tiles = __builtin_amdgcn_readlane(tile_end, 63);
     piece = INT_MAX;
     if (tiles > 0 && tiles < room) {
-      float blocks = (float)w.tiles * w.blocks;
-      for (int m = 1; m < 64; m *= 2) blocks += wave_xor_f(blocks, m);
+      float blocks = (float)w.tiles * w.blocks, longest = w.tiles > 0 ? (float)w.blocks : 0.f;
+      for (int m = 1; m < 64; m *= 2) {
+        blocks += wave_xor_f(blocks, m);
+        longest = fmaxf(longest, wave_xor_f(longest, m));
+      }
       const Tries t = tries_of(tiles, blocks, room);
       piece = t.enough;
       for (int p0 = t.least; piece == t.enough && p0 < t.enough && p0 < t.least + 8; p0 += 4)
@@ -162,6 +178,8 @@ struct WavePlan {
           const int n = wave_scan(w.tiles * pieces_of(w.blocks, p0 + k), capped_add);
           if (__builtin_amdgcn_readlane(n, 63) <= room) piece = p0 + k;
         }
+      const int n = __builtin_amdgcn_readlane(wave_scan(w.tiles * pieces_of(w.blocks, piece), capped_add), 63);
+      if (!worth(longest, piece, (int64_t)n * heads.n_kv.d)) piece = INT_MAX;
     }
     unit_end = wave_scan(w.tiles * pieces_of(w.blocks, piece), capped_add);
     units = __builtin_amdgcn_readlane(unit_end, 63);
@@ -212,7 +230,7 @@ struct RowsPlan {
     const int per = (a.n_rows + kThreads - 1) / kThreads;
     const int row0 = min(t * per, a.n_rows), row1 = min(row0 + per, a.n_rows);
     int mine = 0;
-    float blocks = 0.f;
+    float blocks = 0.f, longest = 0.f;
     bool descends = false;
     for (int r = row0; r < row1; ++r) {
       const int begin = rows.cu_tokens[r], end = rows.cu_tokens[r + 1];
@@ -222,6 +240,7 @@ struct RowsPlan {
       s->blocks[r] = w.blocks;
       mine = capped_add(mine, w.tiles);
       blocks += (float)w.tiles * w.blocks;
+      if (w.tiles > 0) longest = fmaxf(longest, (float)w.blocks);
     }
     if (__syncthreads_or(descends)) {
       for (int r = row0; r < row1; ++r) s->tiles[r] = 0;
@@ -235,13 +254,22 @@ struct RowsPlan {
     if (t == 0) s->first_tile[a.n_rows] = tiles;
     piece = INT_MAX;
     if (tiles > 0 && tiles < room) {
-      for (int m = 1; m < 64; m *= 2) blocks += wave_xor_f(blocks, m);
+      for (int m = 1; m < 64; m *= 2) {
+        blocks += wave_xor_f(blocks, m);
+        longest = fmaxf(longest, wave_xor_f(longest, m));
+      }
       __syncthreads();
-      if ((t & 63) == 0) s->sums[t >> 6] = __float_as_int(blocks);
+      if ((t & 63) == 0) {
+        s->sums[t >> 6] = __float_as_int(blocks);
+        s->sums[kWaves + (t >> 6)] = __float_as_int(longest);
+      }
       __syncthreads();
       blocks = 0.f;
 #pragma unroll
-      for (int v = 0; v < kWaves; ++v) blocks += __int_as_float(s->sums[v]);
+      for (int v = 0; v < kWaves; ++v) {
+        blocks += __int_as_float(s->sums[v]);
+        longest = fmaxf(longest, __int_as_float(s->sums[kWaves + v]));
+      }
       const Tries tr = tries_of(tiles, blocks, room);
       piece = tr.enough;
       for (int p = tr.least; p < tr.enough && p < tr.least + 8; ++p) {
@@ -253,6 +281,10 @@ struct RowsPlan {
           break;
         }
       }
+      int n = 0, all;
+      for (int r = row0; r < row1; ++r) n = capped_add(n, s->tiles[r] * pieces_of(s->blocks[r], piece));
+      before(n, &all);
+      if (!worth(longest, piece, (int64_t)all * heads.n_kv.d)) piece = INT_MAX;
     }
     mine = 0;
     for (int r = row0; r < row1; ++r) mine = capped_add(mine, s->tiles[r] * pieces_of(s->blocks[r], piece));
@@ -280,6 +312,11 @@ struct RowsPlan {
     return n;
   }
 };
+
+// Behind the parts: the blocks of a piece, for the join.
+__device__ __forceinline__ int* piece_of_call(const PrefillArgs& a) {
+  return reinterpret_cast<int*>(a.workspace + (size_t)kUnits * kPartFloats);
+}
 
 template <typename Plan>
 __device__ __forceinline__ Unit unit_of(const Plan& plan, const Rows& rows, int u) {
@@ -892,9 +929,9 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Heads& h
 // 32 keys for itself, in its own quarter of LDS, so that no wave waits for another before
 // the end, where the waves' sums are joined.  K of the wave's next block (FP8, FP4: its
 // codes) is on its way during this one's exponentials and second product, V during the
-// next first product.  32 rows of 4 tokens after 16000, 32 heads on 4, take 204 us in
-// BF16, 114 in FP8 and 104 in FP4 (5.1, 4.6 and 2.7 TB/s; FP4 is bound by the instructions of the
-// widening and the softmax), and 218, 165 and 155 as tiles; rows of 33 to 64 queries, two
+// next first product.  32 rows of 4 tokens after 16000, 32 heads on 4, take 198 us in
+// BF16, 110 in FP8 and 100 in FP4 (5.3, 4.8 and 2.8 TB/s; FP4 is bound by the instructions of the
+// widening and the softmax), and 218, 165 and 155 as tiles (with a costlier join); rows of 33 to 64 queries, two
 // waves to a block, took 175 us in FP4 and as tiles 155.
 template <int kFmt, bool kLse>
 __device__ __forceinline__ void attend_few(const PrefillArgs& a, const Heads& heads, const Rows& rows, const Unit& n,
@@ -1162,6 +1199,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   static_assert(sizeof(RowsPlan::Shared) <= sizeof(tiles), "the plan lies where the tiles will be");
   Plan plan;
   plan.make(a, heads, rows, room, tiles);
+  if (room > 0 && blockIdx.x == 0 && threadIdx.x == 0) *piece_of_call(a) = plan.piece;
   int g, i;
   slot_of(blockIdx.x, heads, plan.units, &g, &i);
   if (i >= plan.units) return;
@@ -1172,32 +1210,25 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   else attend_unit<kFmt, kLse>(a, heads, rows, n, plan.piece, g, t, slot);
 }
 
-// Joins the pieces of a tile, in their order: a workgroup to 32 queries and 32 of their
-// elements, a wave to every fourth piece.  Bound by latency: the loads of kBatch pieces
-// of a wave are on their way together.
-template <int kFmt, typename Plan>
-__global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArgs a, Heads heads, int room,
-                                                                      RBS_ROWS_ARGS) {
-  const Rows rows{page_table, seq_lens, cu_tokens};
-  __shared__ union {
-    RowsPlan::Shared plan;
-    struct {
-      float m[kWaves][32], l[kWaves][32], l_exact[kWaves][32];
-      float4 o[kWaves][4][64];
-    } part;
-  } lds;
-  Plan plan;
-  plan.make(a, heads, rows, room, &lds.plan);
-  if (plan.piece == INT_MAX) return;
+// Joins the pieces of a tile, in their order: an item is 32 queries and 32 of their
+// elements, a wave takes every fourth piece.  Bound by latency: the loads of kBatch pieces
+// of a wave are on their way together.  At most kJoiners workgroups, which make the plan
+// once for all their items, and not at all where the tiles are whole: with a workgroup to
+// an item, 256 tokens of 4 rows after 1024 each took 63 us and not 34.
+template <typename Plan>
+constexpr int kJoiners = std::is_same<Plan, WavePlan>::value ? 1024 : 256;  // (as many as fit at once)
+template <int kFmt, typename Plan, typename Part>
+__device__ __forceinline__ void join_item(const PrefillArgs& a, const Heads& heads, const Rows& rows, const Plan& plan,
+                                          int item, Part& part) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5, l32 = lane & 31;
-  const int tile = (int)heads.n_kv.of(blockIdx.x), g = (int)blockIdx.x - tile * a.n_kv_heads;
-  const int dt = blockIdx.y & 3, q0 = 32 * (blockIdx.y >> 2);
-  if (tile >= plan.tiles) return;
+  const int all = plan.tiles * a.n_kv_heads, y = __builtin_amdgcn_readfirstlane(item / all), x = item - y * all;
+  const int tile = (int)heads.n_kv.of((uint32_t)x), g = x - tile * a.n_kv_heads;
+  const int dt = y & 3, q0 = 32 * (y >> 2);
   const Unit n = plan.row_of(rows, tile, true);
   const int queries = n.tokens * (int)heads.group.d, x0 = n.tile * kQueries + q0;
   if (n.parts == 1 || x0 >= queries) return;
-  __syncthreads();  // every wave has read the plan
+  __syncthreads();  // (the last item has been read)
   const float* slots = a.workspace + (size_t)(g * plan.units + n.first + n.tiles - 1 - n.tile) * kPartFloats;
   const size_t step = (size_t)n.tiles * kPartFloats;
   const int at = kQueries * kHeadDim + q0 + l32;
@@ -1242,37 +1273,53 @@ __global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArg
     }
   }
   if (half == 0) {
-    lds.part.m[wave][l32] = m;
-    lds.part.l[wave][l32] = l;
-    lds.part.l_exact[wave][l32] = l_exact;
+    part.m[wave][l32] = m;
+    part.l[wave][l32] = l;
+    part.l_exact[wave][l32] = l_exact;
   }
 #pragma unroll
-  for (int e = 0; e < 4; ++e) lds.part.o[wave][e][lane] = o[e];
+  for (int e = 0; e < 4; ++e) part.o[wave][e][lane] = o[e];
   __syncthreads();
   // Each wave joins a quarter of the elements.
-  float top = lds.part.m[0][l32];
+  float top = part.m[0][l32];
 #pragma unroll
-  for (int v = 1; v < kWaves; ++v) top = fmaxf(top, lds.part.m[v][l32]);
+  for (int v = 1; v < kWaves; ++v) top = fmaxf(top, part.m[v][l32]);
   const float ref = top == -INFINITY ? 0.f : top;
   l = l_exact = 0.f;
   float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
   for (int v = 0; v < kWaves; ++v) {
-    const float pl = lds.part.l[v][l32];
+    const float pl = part.l[v][l32];
     if (pl == 0.f) continue;
-    const float f = fast_exp2(lds.part.m[v][l32] - ref);
+    const float f = fast_exp2(part.m[v][l32] - ref);
     l += pl * f;
-    l_exact += lds.part.l_exact[v][l32] * f;
-    const float4 w = lds.part.o[v][wave][lane];
+    l_exact += part.l_exact[v][l32] * f;
+    const float4 w = part.o[v][wave][lane];
     r.x += w.x * f; r.y += w.y * f; r.z += w.z * f; r.w += w.w * f;
   }
-  const int x = x0 + l32;
-  if (x >= queries) return;
+  const int mine = x0 + l32;
+  if (mine >= queries) return;
   const float inv = l > 0.f ? head_factor<kFmt>(a, a.n_kv_heads + g) / l : l == 0.f ? 0.f : __builtin_nanf("");
-  *reinterpret_cast<uint2*>(a.O + query_offset(a, heads, n, g, x) + 32 * dt + 8 * wave + 4 * half) =
+  *reinterpret_cast<uint2*>(a.O + query_offset(a, heads, n, g, mine) + 32 * dt + 8 * wave + 4 * half) =
       make_uint2(two_bf16(r.x * inv, r.y * inv), two_bf16(r.z * inv, r.w * inv));
   if (a.lse != nullptr && half == 0 && dt == 0 && wave == 0)
-    a.lse[query_lse(a, heads, n, g, x)] = l_exact == 0.f ? -INFINITY : (top + log2f(l_exact)) / kLog2e;
+    a.lse[query_lse(a, heads, n, g, mine)] = l_exact == 0.f ? -INFINITY : (top + log2f(l_exact)) / kLog2e;
+}
+
+template <int kFmt, typename Plan>
+__global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArgs a, Heads heads, int room,
+                                                                      RBS_ROWS_ARGS) {
+  const Rows rows{page_table, seq_lens, cu_tokens};
+  __shared__ typename Plan::Shared plan_lds;
+  __shared__ struct {
+    float m[kWaves][32], l[kWaves][32], l_exact[kWaves][32];
+    float4 o[kWaves][4][64];
+  } part;
+  if (*piece_of_call(a) == INT_MAX) return;
+  Plan plan;
+  plan.make(a, heads, rows, room, &plan_lds);
+  const int items = 16 * plan.tiles * a.n_kv_heads;
+  for (int item = blockIdx.x; item < items; item += gridDim.x) join_item<kFmt>(a, heads, rows, plan, item, part);
 }
 
 template <int kFmt>
@@ -1280,9 +1327,9 @@ hipError_t launch(const PrefillArgs& a, hipStream_t s) {
   const int group = a.n_q_heads / a.n_kv_heads;
   // At most so many tiles of a KV head.
   const int64_t tiles = (int64_t)a.n_tokens * group / kQueries + (a.n_rows < a.n_tokens ? a.n_rows : a.n_tokens);
-  const int64_t most = (int64_t)a.max_pages << a.cache.page_shift;  // keys of a row
+  const int64_t keys = (int64_t)a.max_pages << a.cache.page_shift;  // of a row, at most
   const int64_t units = tiles * a.n_kv_heads;
-  const bool split = units < kUnits && most > kKeys;
+  const bool split = units < kUnits && keys > kLeast * kKeys;
   const int room = split ? kUnits / a.n_kv_heads : 0;
   // (Bunches round up a head's units, and the XCDs' shares of them.)
   const int grid = (int)((split ? kUnits : units) + 64 + 8 * a.n_kv_heads);
@@ -1293,7 +1340,8 @@ hipError_t launch(const PrefillArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), 0, s, a, heads, room, a.page_table, a.seq_lens, a.cu_tokens);
   if (split) {
     const auto join = few ? paged_prefill_join_kernel<kFmt, WavePlan> : paged_prefill_join_kernel<kFmt, RowsPlan>;
-    hipLaunchKernelGGL(join, dim3((int)units, 16), dim3(kThreads), 0, s, a, heads, room, a.page_table, a.seq_lens,
+    const int items = 16 * (int)units, most = few ? kJoiners<WavePlan> : kJoiners<RowsPlan>;
+    hipLaunchKernelGGL(join, dim3(items < most ? items : most), dim3(kThreads), 0, s, a, heads, room, a.page_table, a.seq_lens,
                        a.cu_tokens);
   }
   return hipGetLastError();
@@ -1301,7 +1349,7 @@ hipError_t launch(const PrefillArgs& a, hipStream_t s) {
 
 }  // namespace
 
-size_t prefill_workspace_bytes() { return sizeof(float) * kUnits * kPartFloats; }
+size_t prefill_workspace_bytes() { return sizeof(float) * (kUnits * kPartFloats + 4); }
 
 hipError_t launch_paged_prefill(const PrefillArgs& a, hipStream_t s) {
   switch (a.cache.format) {
