@@ -620,6 +620,7 @@ size_t rbs_prefill_workspace_bytes(void);
  * unused (a negative length) or have no new token are skipped, and O and lse of tokens
  * that are no row's are left as they were.  A row whose offsets fall outside 0 ..
  * n_tokens is one without tokens; where offsets descend anywhere, no row has any.
+ * O and Q do not overlap (RBS_ERR_ARG where they are the same).
  * page_table int32 [n_rows][max_pages], seq_lens int32 [n_rows], trusted like
  * rbs_paged_decode's.  Results do not depend on timing; those of a row may differ in their
  * last bits with the rows beside it, whose lengths decide how a row is divided.

@@ -1008,6 +1008,7 @@ int rbs_paged_prefill(const rbs_shape* shape, const rbs_cache* cache, const void
   if (!aligned16(Q) || !aligned16(cu_tokens) || !aligned16(page_table) || !aligned16(seq_lens) || !aligned16(O) ||
       !aligned16(lse) || !aligned16(workspace))
     return RBS_ERR_ALIGN;
+  if (O == Q) return RBS_ERR_ARG;  // (a tile's pieces read its queries at different times)
   a.Q = static_cast<const uint16_t*>(Q);
   a.n_tokens = shape->n_tokens;
   a.n_rows = n_rows;

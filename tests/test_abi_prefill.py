@@ -45,6 +45,10 @@ def test_arguments():
     assert rbs.rbs_prefill_workspace_bytes() % 16 == 0
 
 
+def test_the_result_is_not_the_queries():
+    assert _prefill(Q=FAKE, O=FAKE) == ARG
+
+
 @pytest.mark.parametrize("over,code", [
     (dict(head_dim=64), UNSUPPORTED), (dict(n_tokens=0), SHAPE), (dict(n_tokens=(1 << 24) + 1), SHAPE),
     (dict(n_q_heads=3), SHAPE), (dict(n_q_heads=514), SHAPE), (dict(n_kv_heads=4), SHAPE), (dict(q_stride_tok=64), SHAPE),
