@@ -235,7 +235,7 @@ struct Tile {
 template <>
 struct Tile<kCacheFp4> {
   static constexpr int kSteps = kTile<kCacheFp4> / 16;
-  uint4 k[kSteps];         // key 4 (m % 4) + m / 4, elements 32 c ..: a matrix operand's row and block as they are
+  uint4 k[kSteps];         // key 4 (m % 4) + m / 4, elements 32 c ..
   int k_scale[kSteps];     // of these 32 elements
   uint32_t v[kSteps][4];   // key 4 x + c, elements 8 m ..
   int v_scale[kSteps];     // of key 4 (m % 4) + c, elements 32 (m / 4) ..: what the four lanes of a quad need, one each
@@ -337,77 +337,10 @@ struct Stream {
   }
 };
 
-// A wave's 16 queries as the right operand of K's products: q, and for FP4 keys
-// what multiplies its two halves.
-template <int kFmt>
-struct Queries {
-  uint4 q[4];
-};
-
-// FP4 keys go to the matrix core as they are, codes and scales, which takes queries
-// in 8 bits: two E4M3 numbers each (the value and 16 times what its rounding left),
-// over a power of two for the whole row.  A bf16 has 8 significant bits and each of
-// the two takes 4 of them, so that nothing is lost but below 2^-22 of the row's
-// largest magnitude (where E4M3 is subnormal: half a step, 2^-10, over 16, of
-// the 2^8 that the largest reaches).
-template <>
-struct Queries<kCacheFp4> {
-  i32x8 hi, lo;
-  int hi_scale, lo_scale;
-};
-
-// From the lane's elements 16 c .. + 15 (q[0], q[1]) and 64 + 16 c .. + 15 (q[2], q[3])
-// of its column, in the order in which the 8-bit operand holds them.
-__device__ __forceinline__ Queries<kCacheFp4> split_queries(const uint4* q) {
-  Queries<kCacheFp4> out;
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const uint32_t w = word_of(q[i >> 2], i & 3);
-    top = max(top, max(w & 0x7fffu, (w >> 16) & 0x7fffu));
-  }
-  top = __float_as_uint(over_rows(__uint_as_float(top), [](float a, float b) {
-    return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));
-  }));
-  const uint32_t e = min(max(top >> 7, 12u), 254u);  // biased exponent of the largest magnitude
-  const float f = __uint_as_float((261u - e) << 23);  // takes it to 2^7 .. 2^8
-  const bool bad = (top >> 7) == 255u;                // NaN or an infinity: every logit NaN
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    float y[4];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const uint32_t w = word_of(q[i >> 1], 2 * (i & 1) + k);
-      y[2 * k] = bf16_lo(w) * f;
-      y[2 * k + 1] = bf16_hi(w) * f;
-    }
-    int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-    hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], hi, true);
-    y[0] -= __builtin_amdgcn_cvt_f32_fp8(hi, 0);
-    y[1] -= __builtin_amdgcn_cvt_f32_fp8(hi, 1);
-    y[2] -= __builtin_amdgcn_cvt_f32_fp8(hi, 2);
-    y[3] -= __builtin_amdgcn_cvt_f32_fp8(hi, 3);
-    int lo = __builtin_amdgcn_cvt_pk_fp8_f32(16.f * y[0], 16.f * y[1], 0, false);
-    lo = __builtin_amdgcn_cvt_pk_fp8_f32(16.f * y[2], 16.f * y[3], lo, true);
-    out.hi[i] = bad ? 0x7f7f7f7f : hi;
-    out.lo[i] = bad ? 0 : lo;
-  }
-  out.hi_scale = (int)e - 7;
-  out.lo_scale = (int)e - 11;
-  return out;
-}
-
-// 16 keys of 128 elements times 16 queries, all of it in one product: K in E2M1 with
-// a scale for each 32 elements.
-__device__ __forceinline__ f32x4 mfma_fp4(const uint4& k, int k_scale, const i32x8& q, int q_scale, const f32x4& c) {
-  const i32x8 a = {(int)k.x, (int)k.y, (int)k.z, (int)k.w, 0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q, c, 4, 0, 0, k_scale, 0, q_scale);  // E2M1 by E4M3
-}
-
 // One tile from key j on added to a wave's state; `next` gives the offsets of the
 // tile to ask for (more: whether there is one).
 template <int kFmt>
-__device__ __forceinline__ void attend_tile(const Stream<kFmt>& st, Tile<kFmt>& tile, const Queries<kFmt>& queries,
+__device__ __forceinline__ void attend_tile(const Stream<kFmt>& st, Tile<kFmt>& tile, const uint4* q,
                                             float scale_log2, int j, int len, bool more, const int64_t* next,
                                             State& s) {
   constexpr int kSteps = Tile<kFmt>::kSteps;
@@ -417,11 +350,15 @@ __device__ __forceinline__ void attend_tile(const Stream<kFmt>& st, Tile<kFmt>& 
 #pragma unroll
   for (int h = 0; h < kSteps; ++h) {
     if constexpr (is_fp4<kFmt>) {
+      // Widened (exact).  The scaled product takes the codes as they are, with queries in two
+      // 8-bit parts, but loses what lies 2^-14 under the largest of a few neighbouring
+      // products (rows of 1 to 225 keys: lse off by 1e-6 of itself, 4e-8 here) and is no
+      // faster: one row of 131071 keys 26.3 us, 25.1 here; 32 of 9000 to 16384 the same.
       sc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
-      sc[h] = mfma_fp4(tile.k[h], tile.k_scale[h], queries.lo, queries.lo_scale, sc[h]);
-      sc[h] = mfma_fp4(tile.k[h], tile.k_scale[h], queries.hi, queries.hi_scale, sc[h]);
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        sc[h] = mfma16(widen_e2m1(word_of(tile.k[h], x), (uint32_t)tile.k_scale[h] << 23), q[x], sc[h]);
     } else if constexpr (is_fp8<kFmt>) {
-      const uint4* q = queries.q;
       // Rows 2 n and 2 n + 1 of the operand are the two halves of key n: the halves of
       // q with it in turn, of which every other row counts.
 #pragma unroll
@@ -438,7 +375,7 @@ __device__ __forceinline__ void attend_tile(const Stream<kFmt>& st, Tile<kFmt>& 
     } else {
       sc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int x = 0; x < 4; ++x) sc[h] = mfma16(tile.k[h][x], queries.q[x], sc[h]);
+      for (int x = 0; x < 4; ++x) sc[h] = mfma16(tile.k[h][x], q[x], sc[h]);
     }
   }
   if (more) st.load_k(tile, next);
@@ -678,20 +615,13 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       // Elements that the K operand's lane holds.
-      const int d = kFmt != kCacheBf16 ? 64 * (x >> 1) + 16 * c + 8 * (x & 1) : 32 * x + 8 * c;
+      const int d = is_fp4<kFmt> ? 32 * c + 8 * x : is_fp8<kFmt> ? 64 * (x >> 1) + 16 * c + 8 * (x & 1) : 32 * x + 8 * c;
       q[x] = make_uint4(0u, 0u, 0u, 0u);
       if (col < cols) q[x] = *reinterpret_cast<const uint4*>(a.Q + (head0 + col) * a.q_head + tok * a.q_tok + d);
     }
     // Waited for here: in the loop the wait for the first Q would be one for the
     // values on their way as well, at every tile.
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-    Queries<kFmt> queries;
-    if constexpr (is_fp4<kFmt>) {
-      queries = split_queries(q);
-    } else {
-#pragma unroll
-      for (int x = 0; x < 4; ++x) queries.q[x] = q[x];
-    }
     State s;
     s.m = -INFINITY;
     s.l = 0.f;
@@ -703,7 +633,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
       if (next.tile >= next.end) seek(r + 1);
       int64_t base[kSteps] = {};
       if (next.row >= 0) offsets(base);
-      attend_tile<kFmt>(st, tile, queries, scale_log2, j, len, next.row >= 0, base, s);
+      attend_tile<kFmt>(st, tile, q, scale_log2, j, len, next.row >= 0, base, s);
     }
     s.l = over_rows(s.l, [](float a, float b) { return a + b; });
 

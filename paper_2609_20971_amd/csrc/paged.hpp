@@ -132,7 +132,6 @@ __device__ __forceinline__ int wave_scan(int x, Op op) {
   return op(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));  // row_bcast 31
 }
 
-typedef int i32x8 __attribute__((ext_vector_type(8)));  // 32 bytes: an 8-bit matrix operand
 typedef __bf16 bf16x2 __attribute__((__vector_size__(2 * sizeof(__bf16))));
 
 // The scale byte of 32 elements whose largest magnitude has these 15 bits of bf16:

@@ -98,7 +98,7 @@ def cache_of(K, V, live, fmt, layout="heads", amax=None, bad="nan"):
 
 # ------------------------------------------------------------------ attention
 
-def attend(q, k, v, scale, last, fmt="bf16", one_part=False):
+def attend(q, k, v, scale, last, one_part=False):
     """Queries q fp64 [H_q][a][d] over keys 0 .. last[i] of k, v fp64 [H][n][d] (last < 0: none):
     O, lse and the tolerances of both.  one_part: weights held in bf16, their sum of the same."""
     hq, a = q.shape[:2]
@@ -119,10 +119,6 @@ def attend(q, k, v, scale, last, fmt="bf16", one_part=False):
     # absolute products, and as much of itself.
     size = torch.where(seen, torch.matmul(q.abs(), k.abs().transpose(1, 2)) * abs(scale), 0.0).amax(-1)
     ds = size * 134 * R.U32
-    if fmt == "fp4":
-        # Queries as two 8-bit numbers: off by 2^-22 of their row's largest magnitude.
-        sums = torch.where(seen, (k.abs().sum(-1) * abs(scale))[:, None, :], 0.0).amax(-1)
-        ds = ds + sums * q.abs().amax(-1) * 2.0 ** -22
     logits = torch.where(seen, s.abs(), 0.0).amax(-1)
     # The exponential (argument in units of log2: a step of it, then 2 steps).
     e = ds + logits * 2 * R.U32 + 4 * R.U32

@@ -111,7 +111,7 @@ def _check(server, k):
         assert bool(((lse[:, at] - l).abs() <= l_tol).all()), f"step {k}, row {row}"
         t = cu[row + 1] - 1
         last_ones.append(t)
-        o, l, o_tol, l_tol = C.attend(q[:, t:t + 1], keys, values, SCALE, torch.tensor([n - 1]), fmt)
+        o, l, o_tol, l_tol = C.attend(q[:, t:t + 1], keys, values, SCALE, torch.tensor([n - 1]))
         assert bool(((O1[:, t:t + 1] - o).abs() <= o_tol).all()) and bool(((lse1[:, t:t + 1] - l).abs() <= l_tol).all())
         for got, held in zip(read, (keys, values)):
             held = held[:, n - a:]

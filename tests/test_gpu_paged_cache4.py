@@ -313,7 +313,7 @@ def _check(c, O, lse, scale):
             assert bool(O[:, row].isnan().all()), f"unused row {row} was written"
             continue
         k, v = (R.gather(x, c["table"][row], n, c["page"]) for x in (K, V))
-        o, l, o_tol, l_tol = C.attend(c["q"][row].double()[:, None], k, v, scale, torch.tensor([n - 1]), c["fmt"])
+        o, l, o_tol, l_tol = C.attend(c["q"][row].double()[:, None], k, v, scale, torch.tensor([n - 1]))
         err = (O[:, row].cpu().double() - o[:, 0]).abs()
         assert bool((err <= o_tol[:, 0]).all()), f"row {row} of length {n}: {(err / o_tol[:, 0]).max():.3f} of the tolerance"
         if n > 0:
@@ -378,6 +378,28 @@ def test_decode_query_magnitudes():
     keep = torch.ones(8, 6, dtype=torch.bool)
     keep[3, 4] = keep[6, 5] = False
     assert torch.equal(O[keep.cuda()], clean[keep.cuda()])
+
+
+@pytest.mark.parametrize("other", [1, 3, 20, 40, 127])
+def test_decode_small_products_beside_large_ones(other):
+    """One key: a product of 16 and one of 2^-n, of elements next to each other and apart."""
+    n = 20
+    cache = rbs.PagedCache.allocate(n, 16, 1, fp4=True)
+    for t in (cache.K, cache.V):
+        t.zero_()
+    for t in (cache.K_scale, cache.V_scale):
+        t.fill_(127)
+    q, k = torch.zeros(n, D), torch.zeros(n, D)
+    q[:, 0], q[:, other] = 4.0, 2.0 ** -torch.arange(n)
+    k[:, 0], k[:, other] = 4.0, 1.0
+    codes, scales = C.e2m1_encode(k.to(torch.bfloat16))
+    cache.K[:, 0, 0], cache.K_scale[:, 0, 0] = codes.cuda(), scales.cuda()
+    lse = torch.empty(1, n, device="cuda")
+    rbs.rbs_paged_decode(rbs.make_shape(n, 1, 1, 64), q.to(torch.bfloat16).cuda()[None], cache,
+                         torch.arange(n, dtype=torch.int32, device="cuda")[:, None].contiguous(), _ints([1] * n), 1.0, lse=lse)
+    want = (q * k).double().sum(-1)
+    # The sum, two factors (log2 e and ln 2, each rounded too) and the result: 6 steps.
+    assert bool(((lse[0].cpu().double() - want).abs() <= 6 * R.U32 * want).all())
 
 
 def test_decode_nan_in_attended_places():
