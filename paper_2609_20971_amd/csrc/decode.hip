@@ -5,7 +5,7 @@
 // where the card has 300).  So everything is arranged for loads in flight:
 //
 // - K and V go from memory to registers as matrix operands, with no LDS and no
-//   barrier in the loop; a wave streams 32 keys at a time (64 in FP8) and asks for
+//   barrier in the loop; a wave streams 32 keys at a time (64 in FP8, FP4) and asks for
 //   the next ones, of the next row too, as soon as an operand has been used.
 // - S^T = K Q^T and O^T = V^T P^T in 16x16x32 products with the (up to 16) query
 //   heads of a KV head as columns.  Lane l holds column l % 16 of S and four keys
