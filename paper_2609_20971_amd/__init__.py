@@ -12,10 +12,12 @@
 
 and around a paged key-value cache (the tokens that follow a prompt):
 
-    pages = Pages.allocate(n_rows, max_pages, n_pages, page_size); cache = PagedCache.allocate(n_pages, page_size, H_kv)
+    pages = Pages.allocate(n_rows, max_pages, n_pages, page_size); cache = PagedCache.allocate(n_pages, page_size, H_kv)  # fp4=True: 4 bits
     step = rbs_pages_extend(pages, new_tokens, max_tokens)             # pages, positions, slots of new tokens
     Q, K = rbs_qk_norm_rope(shape, rope, Q, K, step.positions, V=V, cache=cache, slots=step.slots)
     O = rbs_paged_decode(shape, Q, cache, pages.page_table, step.seq_lens, cu_tokens=step.cu_tokens)
+    O = rbs_paged_prefill(shape, Q, cache, pages.page_table, step.seq_lens, step.cu_tokens)  # all new tokens of each row
+    rbs_cache_write(shape, K, V, cache, slots); K, V = rbs_cache_read(shape, cache, page_table, cu_tokens)  # plain rows
     rbs_pages_release(pages, released)                                 # finished rows
 """
 

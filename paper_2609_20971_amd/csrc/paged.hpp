@@ -1,5 +1,6 @@
-// The calls over a paged key-value cache (paged.hip, decode.hip): what api.hip
-// hands them, arguments validated, and what the two share on the device.
+// The calls over a paged key-value cache (paged.hip, cache.hip, decode.hip,
+// prefill.hip): what api.hip hands them, arguments validated, and what they share on
+// the device.
 #pragma once
 
 #include "rbs_device.hpp"
