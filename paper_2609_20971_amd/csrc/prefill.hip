@@ -1151,11 +1151,10 @@ __device__ __forceinline__ void attend_few(const PrefillArgs& a, const Heads& he
   float f[kWaves];
   l = l_exact = 0.f;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const float wl = t.sums[1][w][l32];
-    f[w] = wl == 0.f ? 0.f : fast_exp2(t.sums[0][w][l32] - ref);
-    l += wl * f[w];
-    if (kLse && f[w] != 0.f) l_exact += t.sums[2][w][l32] * f[w];
+  for (int w = 0; w < kWaves; ++w) {  // (a wave without keys: a factor of 0, sums of 0; a NaN stays one under any factor)
+    f[w] = fast_exp2(t.sums[0][w][l32] - ref);
+    l += t.sums[1][w][l32] * f[w];
+    if (kLse) l_exact += t.sums[2][w][l32] * f[w];
   }
   const bool whole = n.parts == 1, mine = l32 < queries;
   const float factor = head_factor<kFmt>(a, a.n_kv_heads + g);
@@ -1177,7 +1176,6 @@ __device__ __forceinline__ void attend_few(const PrefillArgs& a, const Heads& he
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      if (f[w] == 0.f) continue;
       const float4 p = *reinterpret_cast<const float4*>(t.k + w * 2 * kOwn * 256 + 16 * (64 * k + lane));
       v.x += p.x * f[w]; v.y += p.y * f[w]; v.z += p.z * f[w]; v.w += p.w * f[w];
     }
@@ -1229,18 +1227,23 @@ __device__ __forceinline__ void join_item(const PrefillArgs& a, const Heads& hea
   const int queries = n.tokens * (int)heads.group.d, x0 = n.tile * kQueries + q0;
   if (n.parts == 1 || x0 >= queries) return;
   __syncthreads();  // (the last item has been read)
+  // The pieces behind the tile's last block wrote no values.
+  const int64_t cap = (int64_t)a.max_pages << a.cache.page_shift;
+  const int last_query = min((n.tile + 1) * kQueries, queries) - 1;
+  const int tile_last = min(n.len - n.tokens + (int)heads.group.of(last_query), (int)min((int64_t)n.len, cap) - 1);
+  const int parts = tile_last < 0 ? 0 : min(n.parts, pieces_of(tile_last / kKeys + 1, plan.piece));
   const float* slots = a.workspace + (size_t)(g * plan.units + n.first + n.tiles - 1 - n.tile) * kPartFloats;
   const size_t step = (size_t)n.tiles * kPartFloats;
   const int at = kQueries * kHeadDim + q0 + l32;
   float m = -INFINITY, l = 0.f, l_exact = 0.f;
   float4 o[4] = {};
   constexpr int kBatch = 4;
-  for (int p0 = wave; p0 < n.parts; p0 += kWaves * kBatch) {
+  for (int p0 = wave; p0 < parts; p0 += kWaves * kBatch) {
     float pm[kBatch], pl[kBatch], pe[kBatch];
     float4 w[kBatch][4];
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
-      const float* slot = slots + min(p0 + kWaves * k, n.parts - 1) * step;
+      const float* slot = slots + min(p0 + kWaves * k, parts - 1) * step;
       pm[k] = slot[at];
       pl[k] = slot[at + kQueries];
       pe[k] = a.lse != nullptr ? slot[at + 2 * kQueries] : 0.f;
@@ -1261,8 +1264,7 @@ __device__ __forceinline__ void join_item(const PrefillArgs& a, const Heads& hea
     }
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
-      // (A piece without keys of the query's, or behind the tile's last block, which wrote no values.)
-      if (p0 + kWaves * k >= n.parts || pl[k] == 0.f) continue;
+      if (p0 + kWaves * k >= parts) continue;
       const float f = fast_exp2(pm[k] - ref);
       l += pl[k] * f;
       l_exact += pe[k] * f;
@@ -1289,10 +1291,8 @@ __device__ __forceinline__ void join_item(const PrefillArgs& a, const Heads& hea
   float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
   for (int v = 0; v < kWaves; ++v) {
-    const float pl = part.l[v][l32];
-    if (pl == 0.f) continue;
     const float f = fast_exp2(part.m[v][l32] - ref);
-    l += pl * f;
+    l += part.l[v][l32] * f;
     l_exact += part.l_exact[v][l32] * f;
     const float4 w = part.o[v][wave][lane];
     r.x += w.x * f; r.y += w.y * f; r.z += w.z * f; r.w += w.w * f;
