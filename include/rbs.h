@@ -611,7 +611,8 @@ size_t rbs_prefill_workspace_bytes(void);
  *   O = sum_j softmax_j(q . k_j * scale) v_j over j = 0 .. seq_lens[s] - a + i
  * with fp32 sums, the weights rounded once to bf16 (and summed as such), rounded
  * to bf16.  What later tokens hold, infinities and NaN too, does not reach a token's
- * result; an infinity in a value that is attended may give NaN.
+ * result; an infinity in a value that is attended may give NaN.  A NaN in the query, in an attended
+ * key or value reaches it, and logits of -inf alone give O = NaN, lse = -inf.
  * shape: n_tokens tokens of Q and O, those behind the last one of a padded batch
  * included (up to RBS_MAX_NEW_TOKENS), H_q (up to 512; n_tokens H_q up to 2^30) and
  * H_kv heads, strides of Q and O (any block_size; kv strides are not used).  softmax_scale

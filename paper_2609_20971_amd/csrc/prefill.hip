@@ -433,6 +433,12 @@ __device__ __forceinline__ float head_factor(const PrefillArgs& a, int head) {
   return m > 0.f ? m / 448.f : 1.f;
 }
 
+// What a query's weighted values are multiplied by, of their sum l, with keys up to its last one (negative: none, and
+// its result is 0).  Keys of no weight at all, from logits of -inf, give NaN.
+__device__ __forceinline__ float result_factor(float factor, float l, int last) {
+  return l > 0.f ? factor / l : last < 0 ? 0.f : __builtin_nanf("");
+}
+
 // Where query x of a row is in Q and O, and in lse.
 __device__ __forceinline__ int64_t query_offset(const PrefillArgs& a, const Heads& heads, const Unit& n, int g, int x) {
   const int i = (int)heads.group.of(x), head = g * (int)heads.group.d + x - i * (int)heads.group.d;
@@ -900,7 +906,7 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Heads& h
   if (kLse) l_exact = half_sum(l_exact);
   if (n.parts == 1) {
     const float factor = head_factor<kFmt>(a, a.n_kv_heads + g);
-    const float inv = l > 0.f ? factor / l : l == 0.f ? 0.f : __builtin_nanf("");
+    const float inv = result_factor(factor, l, last);
     const int x = x0 + 32 * wave + (anew(lane) & 31);
     if (kLse && half == 0 && x < queries)
       a.lse[query_lse(a, heads, n, g, x)] = l_exact == 0.f ? -INFINITY : (m + log2f(l_exact)) / kLog2e;
@@ -1158,7 +1164,7 @@ __device__ __forceinline__ void attend_few(const PrefillArgs& a, const Heads& he
   }
   const bool whole = n.parts == 1, mine = l32 < queries;
   const float factor = head_factor<kFmt>(a, a.n_kv_heads + g);
-  const float inv = l > 0.f ? factor / l : l == 0.f ? 0.f : __builtin_nanf("");
+  const float inv = result_factor(factor, l, last);
   if (half == 0 && wave == 0) {
     if (!whole) {
       float* sums = slot + kQueries * kHeadDim + l32;
@@ -1230,7 +1236,8 @@ __device__ __forceinline__ void join_item(const PrefillArgs& a, const Heads& hea
   // The pieces behind the tile's last block wrote no values.
   const int64_t cap = (int64_t)a.max_pages << a.cache.page_shift;
   const int last_query = min((n.tile + 1) * kQueries, queries) - 1;
-  const int tile_last = min(n.len - n.tokens + (int)heads.group.of(last_query), (int)min((int64_t)n.len, cap) - 1);
+  const int before = n.len - n.tokens, held = (int)min((int64_t)n.len, cap);
+  const int tile_last = min(before + (int)heads.group.of(last_query), held - 1);
   const int parts = tile_last < 0 ? 0 : min(n.parts, pieces_of(tile_last / kKeys + 1, plan.piece));
   const float* slots = a.workspace + (size_t)(g * plan.units + n.first + n.tiles - 1 - n.tile) * kPartFloats;
   const size_t step = (size_t)n.tiles * kPartFloats;
@@ -1299,7 +1306,8 @@ __device__ __forceinline__ void join_item(const PrefillArgs& a, const Heads& hea
   }
   const int mine = x0 + l32;
   if (mine >= queries) return;
-  const float inv = l > 0.f ? head_factor<kFmt>(a, a.n_kv_heads + g) / l : l == 0.f ? 0.f : __builtin_nanf("");
+  const int last = min(before + (int)heads.group.of(mine), held - 1);
+  const float inv = result_factor(head_factor<kFmt>(a, a.n_kv_heads + g), l, last);
   *reinterpret_cast<uint2*>(a.O + query_offset(a, heads, n, g, mine) + 32 * dt + 8 * wave + 4 * half) =
       make_uint2(two_bf16(r.x * inv, r.y * inv), two_bf16(r.z * inv, r.w * inv));
   if (a.lse != nullptr && half == 0 && dt == 0 && wave == 0)

@@ -103,3 +103,22 @@ def test_a_value_that_is_nan_of_a_small_weight(kind, fmt, low):
     assert bool((O[:, :new] == 2.0).all())
     # The sum of 32 ones is exact; the logit and the change of base are a few steps of 515.
     assert bool(((lse[:, :new].cpu().double() - (512 + math.log(32))).abs() <= 515 * 8 * 2.0 ** -24).all())
+
+
+@pytest.mark.parametrize("kind", range(4))
+def test_logits_of_minus_infinity_alone(kind):
+    """All keys of a token weigh nothing: the formula has 0 / 0, and zeros are for tokens without keys."""
+    rows, hq, hkv = KINDS[kind]
+    _say(f"[-inf] {rows}")
+    c = _case(rows, hq, hkv, 16, "bf16", "heads", 60 + kind)
+    clean, clean_lse = _run(c)
+    before, new = rows[0]
+    c["q"][:new] = 1.0
+    _set(c, "K", torch.arange(before + new), 1, -math.inf)
+    O, lse = _run(c)
+    assert bool(O[4:, :new].isnan().all()) and bool((lse[4:, :new] == -math.inf).all())
+    assert torch.equal(O[:, new:], clean[:, new:]) and torch.equal(lse[:, new:], clean_lse[:, new:])
+    c["lens"] = [new - 1, rows[1][1]]  # the first token is before the row's first key
+    O, lse = _run(c)
+    assert bool((O[:, 0] == 0).all()) and bool((lse[:, 0] == -math.inf).all())
+    assert bool(O[4:, 1:new].isnan().all())
