@@ -110,7 +110,9 @@ __device__ __forceinline__ RowWork work_of_row(const PrefillArgs& a, int group, 
 //
 // The pieces: at most so many blocks to a unit that there are at most `room` units, the
 // smallest such number, tried from below four at a time (a count over the rows for
-// each); where there are as many tiles as that, whole tiles.
+// each); where there are as many tiles as that, whole tiles.  It is found by the first
+// launch (known: 0) and left for the join, which derives the rest from it in whole numbers: the
+// rule's floats, compiled a second time, could round another way.
 __device__ __forceinline__ int pieces_of(int blocks, int piece) {
   return piece == INT_MAX ? 1 : (blocks + piece - 1) / piece;
 }
@@ -153,7 +155,7 @@ struct WavePlan {
   int tile_end, unit_end;  // of this row, counted over the rows up to it
   int piece, units, tiles;
 
-  __device__ __forceinline__ void make(const PrefillArgs& a, const Heads& heads, const Rows& rows, int room, void*) {
+  __device__ __forceinline__ void make(const PrefillArgs& a, const Heads& heads, const Rows& rows, int room, int known, void*) {
     const int r = threadIdx.x & 63, group = heads.group.d, at = min(r, a.n_rows - 1);
     const int end = rows.cu_tokens[at + 1];
     begin = rows.cu_tokens[at];
@@ -163,8 +165,8 @@ struct WavePlan {
     tokens = end - begin;
     tile_end = wave_scan(w.tiles, capped_add);
     tiles = __builtin_amdgcn_readlane(tile_end, 63);
-    piece = INT_MAX;
-    if (tiles > 0 && tiles < room) {
+    piece = known == 0 ? INT_MAX : known;
+    if (known == 0 && tiles > 0 && tiles < room) {
       float blocks = (float)w.tiles * w.blocks, longest = w.tiles > 0 ? (float)w.blocks : 0.f;
       for (int m = 1; m < 64; m *= 2) {
         blocks += wave_xor_f(blocks, m);
@@ -224,7 +226,8 @@ struct RowsPlan {
     *all = __builtin_amdgcn_readfirstlane(*all);
     return sum;
   }
-  __device__ __forceinline__ void make(const PrefillArgs& a, const Heads& heads, const Rows& rows, int room, void* shared) {
+  __device__ __forceinline__ void make(const PrefillArgs& a, const Heads& heads, const Rows& rows, int room, int known,
+                                       void* shared) {
     s = static_cast<Shared*>(shared);
     const int t = threadIdx.x, group = heads.group.d;
     const int per = (a.n_rows + kThreads - 1) / kThreads;
@@ -252,8 +255,8 @@ struct RowsPlan {
       sum = capped_add(sum, s->tiles[r]);
     }
     if (t == 0) s->first_tile[a.n_rows] = tiles;
-    piece = INT_MAX;
-    if (tiles > 0 && tiles < room) {
+    piece = known == 0 ? INT_MAX : known;
+    if (known == 0 && tiles > 0 && tiles < room) {
       for (int m = 1; m < 64; m *= 2) {
         blocks += wave_xor_f(blocks, m);
         longest = fmaxf(longest, wave_xor_f(longest, m));
@@ -1202,7 +1205,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const Tiles t{tiles, tiles + 2 * kBlockBytes, bad, sums};
   static_assert(sizeof(RowsPlan::Shared) <= sizeof(tiles), "the plan lies where the tiles will be");
   Plan plan;
-  plan.make(a, heads, rows, room, tiles);
+  plan.make(a, heads, rows, room, 0, tiles);
   if (room > 0 && blockIdx.x == 0 && threadIdx.x == 0) *piece_of_call(a) = plan.piece;
   int g, i;
   slot_of(blockIdx.x, heads, plan.units, &g, &i);
@@ -1315,17 +1318,17 @@ __device__ __forceinline__ void join_item(const PrefillArgs& a, const Heads& hea
 }
 
 template <int kFmt, typename Plan>
-__global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArgs a, Heads heads, int room,
-                                                                      RBS_ROWS_ARGS) {
+__global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(PrefillArgs a, Heads heads, RBS_ROWS_ARGS) {
   const Rows rows{page_table, seq_lens, cu_tokens};
   __shared__ typename Plan::Shared plan_lds;
   __shared__ struct {
     float m[kWaves][32], l[kWaves][32], l_exact[kWaves][32];
     float4 o[kWaves][4][64];
   } part;
-  if (*piece_of_call(a) == INT_MAX) return;
+  const int piece = __builtin_amdgcn_readfirstlane(*piece_of_call(a));
+  if (piece == INT_MAX) return;
   Plan plan;
-  plan.make(a, heads, rows, room, &plan_lds);
+  plan.make(a, heads, rows, 0, piece, &plan_lds);
   const int items = 16 * plan.tiles * a.n_kv_heads;
   for (int item = blockIdx.x; item < items; item += gridDim.x) join_item<kFmt>(a, heads, rows, plan, item, part);
 }
@@ -1349,7 +1352,7 @@ hipError_t launch(const PrefillArgs& a, hipStream_t s) {
   if (split) {
     const auto join = few ? paged_prefill_join_kernel<kFmt, WavePlan> : paged_prefill_join_kernel<kFmt, RowsPlan>;
     const int items = 16 * (int)units, most = few ? kJoiners<WavePlan> : kJoiners<RowsPlan>;
-    hipLaunchKernelGGL(join, dim3(items < most ? items : most), dim3(kThreads), 0, s, a, heads, room, a.page_table, a.seq_lens,
+    hipLaunchKernelGGL(join, dim3(items < most ? items : most), dim3(kThreads), 0, s, a, heads, a.page_table, a.seq_lens,
                        a.cu_tokens);
   }
   return hipGetLastError();
