@@ -609,8 +609,40 @@ size_t rbs_prefill_workspace_bytes(void);
  * cu_tokens[s + 1] - 1 of Q (a of them; int32 [n_rows + 1], ascending), which are the
  * last ones of its first seq_lens[s] cached tokens.  For query head h of token i of the row
  *   O = sum_j softmax_j(q . k_j * scale) v_j over j = 0 .. seq_lens[s] - a + i
- * with fp32 sums, the weights rounded once to bf16 (and summed as such), rounded
- * to bf16.  What later tokens hold, infinities and NaN too, does not reach a token's
+ * with fp32 sums, rounded to bf16.  The weights are rounded once to bf16 and summed as
+ * such; for a row of at most 32 queries of a KV head (its new tokens times H_q / H_kv:
+ * a few drafted tokens) they have two bf16 parts, off by 2^-16, as those of
+ * rbs_paged_decode have.
+ * What later tokens hold, infinities and NaN too, does not reach a token's result; an
+ * infinity in a value that is attended may give NaN.  A NaN in the query, in an attended
+ * key or value reaches it, and logits of -inf alone give O = NaN, lse = -inf.
+ * shape: n_tokens tokens of Q and O, those behind the last one of a padded batch
+ * included (up to RBS_MAX_NEW_TOKENS); lse: NULL or [H_q][n_tokens]; page_table
+ * [n_rows][max_pages], seq_lens [n_rows], n_rows up to RBS_MAX_ROWS.
+ * The query of row s is its last new token's, cu_tokens[s + 1] - 1, which attends
+ * over the row's first seq_lens[s] tokens; O and lse go to the same token.  Rows
+ * without a new token are skipped, and O and lse of tokens that are no row's last
+ * are left as they were.  A row whose offsets fall outside 0 .. n_tokens is one
+ * without a token.
+ */
+int rbs_paged_decode_packed(const rbs_shape* shape, const rbs_cache* cache, const void* Q, const int32_t* cu_tokens,
+                            int32_t n_rows, const int32_t* page_table, int32_t max_pages, const int32_t* seq_lens,
+                            float softmax_scale, void* O, float* lse, void* workspace, void* stream);
+
+/* Workspace of rbs_paged_prefill, 16-byte aligned; shared as the decode calls'. */
+size_t rbs_prefill_workspace_bytes(void);
+
+/*
+ * Attention of all new tokens of a batch over the rows' cached tokens (their own keys
+ * and values among them): whole prompts, parts of a prompt after what is cached
+ * already, drafted tokens to be checked, single tokens, in any mixture.  Tokens are
+ * packed as rbs_pages_extend packs them: row s has tokens cu_tokens[s] ..
+ * cu_tokens[s + 1] - 1 of Q (a of them; int32 [n_rows + 1], ascending), which are the
+ * last ones of its first seq_lens[s] cached tokens.  For query head h of token i of the row
+ *   O = sum_j softmax_j(q . k_j * scale) v_j over j = 0 .. seq_lens[s] - a + i
+ * with fp32 sums, rounded to bf16.  The weights are rounded once to bf16 and summed as
+ * such; for a row of at most 32 queries of a KV head (its new tokens times H_q / H_kv: a few
+ * drafted tokens) they have two bf16 parts, off by 2^-16, as those of rbs_paged_decode have.  What later tokens hold, infinities and NaN too, does not reach a token's
  * result; an infinity in a value that is attended may give NaN.  A NaN in the query, in an attended
  * key or value reaches it, and logits of -inf alone give O = NaN, lse = -inf.
  * shape: n_tokens tokens of Q and O, those behind the last one of a padded batch

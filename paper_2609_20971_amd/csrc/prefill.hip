@@ -21,9 +21,13 @@
 // lowers to 1.8 GHz, and a library product of 16384^3 reaches 1350).  Few queries are
 // bound by what a unit takes before its first and after its last block.
 //
-// Sums are in fp32.  The weights go to the second product rounded once to bf16, and
+// Sums are in fp32.  A tile's weights go to the second product rounded once to bf16, and
 // the denominator sums what goes there, so that their common error cancels; the
-// log-sum-exp, where it is asked for, has a sum of the weights before that.
+// log-sum-exp, where it is asked for, has a sum of the weights before that.  (A second
+// part would be half as much again of the products that bound it; the result is off from 64 bits by
+// 0.00193 of itself in the root mean square, its own rounding by 0.00167.)  Rows of at most 32
+// queries have the weights in two parts, as the decode calls do, so that a token that is
+// checked and one that is decoded differ by the rounding of the result.
 //
 // Work: unit u of a KV head is a tile, or where there are few tiles a piece of one,
 // of at most P blocks of keys; pieces leave maximum, sums and weighted values in fp32,
@@ -480,7 +484,7 @@ struct Tiles {
   unsigned char* k;
   unsigned char* v;
   int* bad;  // [kKeys]: the key's value is not finite
-  float (*sums)[kWaves][32];  // maximum, sum and exact sum of each wave's queries (attend_few)
+  float (*sums)[kWaves][32];  // maximum and sum of each wave's queries (attend_few)
 };
 
 __device__ __forceinline__ bool not_finite(uint32_t pair) {
@@ -938,10 +942,10 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Heads& h
 // 32 keys for itself, in its own quarter of LDS, so that no wave waits for another before
 // the end, where the waves' sums are joined.  K of the wave's next block (FP8, FP4: its
 // codes) is on its way during this one's exponentials and second product, V during the
-// next first product.  32 rows of 4 tokens after 16000, 32 heads on 4, take 198 us in
-// BF16, 110 in FP8 and 100 in FP4 (5.3, 4.8 and 2.8 TB/s; FP4 is bound by the instructions of the
-// widening and the softmax), and 218, 165 and 155 as tiles (with a costlier join); rows of 33 to 64 queries, two
-// waves to a block, took 175 us in FP4 and as tiles 155.
+// next first product.  32 rows of 4 tokens after 16000, 32 heads on 4, take 207 us in
+// BF16, 129 in FP8 and 113 in FP4 on the GPU (5.1, 4.1 and 2.5 TB/s; FP4 is bound by the instructions of the
+// widening and the softmax), with the weights in one part 207, 122 and 103; 218, 165 and 155 as tiles (with
+// a costlier join); rows of 33 to 64 queries, two waves to a block, took 175 us in FP4 and as tiles 155.
 template <int kFmt, bool kLse>
 __device__ __forceinline__ void attend_few(const PrefillArgs& a, const Heads& heads, const Rows& rows, const Unit& n,
                                            int piece, int g, const Tiles& t, float* slot) {
@@ -1040,7 +1044,7 @@ __device__ __forceinline__ void attend_few(const PrefillArgs& a, const Heads& he
   const uint32_t v_swz = 16u * (uint32_t)vswz(vq, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1));
   typedef const __attribute__((address_space(3))) u32x4 lds_u32x4;
 
-  float l = 0.f, l_exact = 0.f, m = -INFINITY, shift = 0.f;
+  float l = 0.f, m = -INFINITY, shift = 0.f;
   f32x16 o[4];
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt) o[dt] = f32x16{};
@@ -1090,20 +1094,22 @@ __device__ __forceinline__ void attend_few(const PrefillArgs& a, const Heads& he
       m = m_new;
       shift = m == -INFINITY ? 0.f : m;
       l *= f;
-      l_exact *= f;
 #pragma unroll
       for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] *= f;
     }
-    uint32_t pw[8];
+    // Two bf16 parts: the weight cut off, and the rest, off by 2^-16 of the weight together.  The
+    // rest is taken of the weight and 2^-22 of it: as positive as the weight is, so that
+    // an infinite value stays one (with 0, or a rest below 0, it would be NaN).
+    uint32_t pw[8], rest[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float e0 = fast_exp2(fmaf(s[2 * j], scale_log2, -shift)), e1 = fast_exp2(fmaf(s[2 * j + 1], scale_log2, -shift));
-      if (kLse) l_exact += e0 + e1;
-      pw[j] = two_bf16(e0, e1);
-      const uint32_t ones = 0x3f803f80u;
-      l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw[j]), __builtin_bit_cast(bf16x2, ones), l, false);
+      l += e0 + e1;
+      pw[j] = __builtin_amdgcn_perm(__float_as_uint(e1), __float_as_uint(e0), 0x07060302u);
+      constexpr float kAbove = 1.f + 1.f / (1 << 22);
+      rest[j] = two_bf16(fmaf(e0, kAbove, -bf16_lo(pw[j])), fmaf(e1, kAbove, -bf16_hi(pw[j])));
     }
     if constexpr (kCopied) {
       if (more) RBS_WAIT_VMCNT(8);  // (the next K's copies)
@@ -1126,6 +1132,7 @@ __device__ __forceinline__ void attend_few(const PrefillArgs& a, const Heads& he
         __builtin_memcpy(&v, &lo, 8);
         __builtin_memcpy(reinterpret_cast<unsigned char*>(&v) + 8, &hi, 8);
         o[dt] = mfma_bf16(v, __builtin_bit_cast(bf16x8, make_uint4(pw[4 * c], pw[4 * c + 1], pw[4 * c + 2], pw[4 * c + 3])), o[dt]);
+        o[dt] = mfma_bf16(v, __builtin_bit_cast(bf16x8, make_uint4(rest[4 * c], rest[4 * c + 1], rest[4 * c + 2], rest[4 * c + 3])), o[dt]);
       }
     }
     fence();
@@ -1141,7 +1148,6 @@ __device__ __forceinline__ void attend_few(const PrefillArgs& a, const Heads& he
 
   // The waves' sums, joined: each takes a quarter of the elements from all of them.
   l = half_sum(l);
-  if (kLse) l_exact = half_sum(l_exact);
   asm volatile("" ::: "memory");
 #pragma unroll
   for (int k = 0; k < 16; ++k)
@@ -1150,7 +1156,6 @@ __device__ __forceinline__ void attend_few(const PrefillArgs& a, const Heads& he
   if (half == 0) {
     t.sums[0][wave][l32] = m;
     t.sums[1][wave][l32] = l;
-    if (kLse) t.sums[2][wave][l32] = l_exact;
   }
   __syncthreads();
   float top = t.sums[0][0][l32];
@@ -1158,12 +1163,11 @@ __device__ __forceinline__ void attend_few(const PrefillArgs& a, const Heads& he
   for (int w = 1; w < kWaves; ++w) top = fmaxf(top, t.sums[0][w][l32]);
   const float ref = top == -INFINITY ? 0.f : top;
   float f[kWaves];
-  l = l_exact = 0.f;
+  l = 0.f;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {  // (a wave without keys: a factor of 0, sums of 0; a NaN stays one under any factor)
     f[w] = fast_exp2(t.sums[0][w][l32] - ref);
     l += t.sums[1][w][l32] * f[w];
-    if (kLse) l_exact += t.sums[2][w][l32] * f[w];
   }
   const bool whole = n.parts == 1, mine = l32 < queries;
   const float factor = head_factor<kFmt>(a, a.n_kv_heads + g);
@@ -1173,9 +1177,9 @@ __device__ __forceinline__ void attend_few(const PrefillArgs& a, const Heads& he
       float* sums = slot + kQueries * kHeadDim + l32;
       sums[0] = top;
       sums[kQueries] = l;
-      if (kLse) sums[2 * kQueries] = l_exact;
+      if (kLse) sums[2 * kQueries] = l;
     } else if (kLse && mine) {
-      a.lse[query_lse(a, heads, n, g, l32)] = l_exact == 0.f ? -INFINITY : (top + log2f(l_exact)) / kLog2e;
+      a.lse[query_lse(a, heads, n, g, l32)] = l == 0.f ? -INFINITY : (top + log2f(l)) / kLog2e;
     }
   }
   uint16_t* out = a.O + query_offset(a, heads, n, g, min(l32, queries - 1)) + 4 * half;
@@ -1201,7 +1205,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const Rows rows{page_table, seq_lens, cu_tokens};
   __shared__ __align__(1024) unsigned char tiles[4 * kBlockBytes + 128];
   __shared__ int bad[kKeys];
-  __shared__ float sums[3][kWaves][32];
+  __shared__ float sums[2][kWaves][32];
   const Tiles t{tiles, tiles + 2 * kBlockBytes, bad, sums};
   static_assert(sizeof(RowsPlan::Shared) <= sizeof(tiles), "the plan lies where the tiles will be");
   Plan plan;
