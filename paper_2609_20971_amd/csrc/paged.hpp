@@ -12,14 +12,14 @@ constexpr int kCacheBf16 = 0, kCacheFp8 = 1, kCacheFp4 = 4;  // RBS_CACHE_*
 
 // K and V of a paged cache: element (page, head, place, j) at page * page + ...
 struct CacheView {
-  int format;
   void* K;
   void* V;
   const float* amax;  // FP8 only
-  void* K_scale;      // FP4 only: that of element x (a multiple of 32) at byte x / 32
-  void* V_scale;
   int64_t page, head, tok;
   int n_pages, page_shift;
+  int format;
+  void* K_scale;      // FP4 only: that of element x (a multiple of 32) at byte x / 32
+  void* V_scale;
 };
 
 struct PagesArgs {

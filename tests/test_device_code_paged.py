@@ -1,4 +1,4 @@
-"""Properties of the paged prefill's gfx950 code, read from its disassembly (CPU only)."""
+"""Properties of the paged calls' gfx950 code, read from its disassembly (CPU only)."""
 
 from __future__ import annotations
 
@@ -18,3 +18,15 @@ def test_the_join_has_no_rule_of_its_own(listing):  # noqa: F811
                 found[join] += 1
                 assert bool(marks) != join, (name, marks[:3])
     assert found[True] >= 6 and found[False] >= 12
+
+
+def test_rotation_into_other_formats_has_no_code_of_fp4(listing):  # noqa: F811
+    """The packing of 4 bits takes registers that cost bf16 and FP8 callers waves: it is compiled apart."""
+    apart = {True: 0, False: 0}
+    for lines in listing:
+        for name, code in _functions(lines):
+            if "qk_norm_rope_kernel" in name:
+                packs = any("_fp4_" in x.split()[0] for _, x in code)
+                assert not (packs and any("_fp8_" in x.split()[0] for _, x in code)), name
+                apart[packs] += 1
+    assert apart[True] == apart[False] == 6
