@@ -549,6 +549,7 @@ int rbs_cache_write(const rbs_shape* shape, const rbs_shape* v_shape, const void
  * values come exactly, FP8 ones rounded once.  Tokens that are no row's, and
  * positions outside the row's page table, are left as they were.  page_table int32
  * [n_rows][max_pages], trusted like rbs_paged_decode's; lengths are not looked at.
+ * K and V do not overlap (RBS_ERR_ARG where they are the same).
  */
 int rbs_cache_read(const rbs_shape* shape, const rbs_cache* cache, const int32_t* cu_tokens, const int32_t* starts,
                    int32_t n_rows, const int32_t* page_table, int32_t max_pages, void* K, void* V, void* stream);

@@ -912,6 +912,7 @@ int rbs_cache_read(const rbs_shape* shape, const rbs_cache* cache, const int32_t
   if (cu_tokens == nullptr || page_table == nullptr || K == nullptr || V == nullptr) return RBS_ERR_NULL;
   if (!aligned16(cu_tokens) || !aligned16(starts) || !aligned16(page_table) || !aligned16(K) || !aligned16(V))
     return RBS_ERR_ALIGN;
+  if (K == V) return RBS_ERR_ARG;  // (keys and values would be written over each other)
   a.K = static_cast<uint16_t*>(K);
   a.V = static_cast<uint16_t*>(V);
   a.v_head = a.k_head;
