@@ -416,7 +416,8 @@ enum { RBS_CACHE_BF16 = 0, RBS_CACHE_FP8 = 1, RBS_CACHE_FP4 = 4 };
  *                   2^(b - 127), 255 for 32 NaN.  Written from bf16: the least power
  *                   of two (from 2^-126) that takes the 32's largest magnitude under
  *                   7, and the nearest code (ties to even); a NaN or an infinity
- *                   makes its 32 elements NaN.  68 bytes a row of 128.
+ *                   makes its 32 elements NaN.  (From 7/4 2^127 on the nearest code may
+ *                   stand for 2^128, an infinity.)  68 bytes a row of 128.
  */
 typedef struct {
   int32_t n_pages;     /* n_pages * page_size < 2^31 */
@@ -546,7 +547,8 @@ int rbs_cache_write(const rbs_shape* shape, const rbs_shape* v_shape, const void
  * s's at position starts[s] + t - cu_tokens[s] (int32 [n_rows], any alignment to
  * pages; NULL: from 0).  K, V (head, token, dimension) with the strides kv_* of
  * shape, whose n_tokens (up to RBS_MAX_NEW_TOKENS) tokens they hold.  BF16 and FP4
- * values come exactly, FP8 ones rounded once.  Tokens that are no row's, and
+ * values come exactly (2^128 and above as infinity); an FP8 value is its code times
+ * amax / 448, both rounded to fp32, then to bf16: off by at most 2^-8 + 2^-23 of itself.  Tokens that are no row's, and
  * positions outside the row's page table, are left as they were.  page_table int32
  * [n_rows][max_pages], trusted like rbs_paged_decode's; lengths are not looked at.
  * K and V do not overlap (RBS_ERR_ARG where they are the same).
