@@ -20,16 +20,17 @@ constexpr int kThreads = 256;
 constexpr int kTokens = 64;            // of a workgroup
 constexpr int kSteps = kTokens / 16;   // loads in flight: four rows of each of the four waves
 // Workgroups that a call of few tokens is spread over, by heads.  131072 FP4 tokens of 4
-// heads are written in 65 us at 2048, 68 at 4096 and 78 at 16384 (a wave's next head is
+// heads are written in 68 us at 2048, 70.5 at 4096 and 78 at 16384 (a wave's next head is
 // the next line of the same page); 32 rows of 100 to 9000 tokens, 8 heads, are read in
-// 84, 80 and 77 us.
+// 78, 73 and 75 us (call after call, three sets of rows in turn).
 constexpr int kWriteSpread = 2048, kReadSpread = 4096;
 
 // A call that moves this many bytes or more loads past the caches, which its loads would
 // only empty, and stores through them.  After a copy of 1 GB the same rows are read in
 // 70 us for FP4, 68 for FP8 and 103 for BF16; in 83, 90 and 115 with stores past the
 // caches too, in 88, 101 and 142 with the stores alone.  131072 tokens of 4 heads are
-// written in 71 us (FP4) and 88 (BF16), in 72 and 109 with stores past the caches too.
+// written in 71 us (FP4), 75 (FP8) and 88 (BF16): 4.8, 5.4 and 6.1 TB/s; FP4 and BF16 in 72 and 109
+// with stores past the caches too.
 constexpr int64_t kCachedBytes = int64_t(64) << 20;
 
 template <int kFmt>

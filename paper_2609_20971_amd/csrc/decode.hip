@@ -353,7 +353,7 @@ __device__ __forceinline__ void attend_tile(const Stream<kFmt>& st, Tile<kFmt>& 
       // Widened (exact).  The scaled product takes the codes as they are, with queries in two
       // 8-bit parts, but loses what lies 2^-14 under the largest of a few neighbouring
       // products (rows of 1 to 225 keys: lse off by 1e-6 of itself, 4e-8 here).  In time:
-      // 8 rows of 139000 keys 138 us, 150 here; 32 of 9000 to 16384 87.4 both; one of 131071
+      // 8 rows of 139000 keys 138 us, 130 to 150 here; 32 of 9000 to 16384 87.4 both; one of 131071
       // 26.3, 25.1 here.
       sc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll

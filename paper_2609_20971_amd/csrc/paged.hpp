@@ -139,7 +139,8 @@ typedef __bf16 bf16x2 __attribute__((__vector_size__(2 * sizeof(__bf16))));
 // 2^(byte - 127) is the least power of two (from 2^-126) that takes it under 7, so
 // that it rounds to 6 or less and no element is off by more than half a step of the
 // codes' largest binade (7 / 4 of a power of two is where the 32 carries into the
-// exponent).  255: a NaN or an infinity among them.
+// exponent).  255: a NaN or an infinity among them.  (From 7 / 4 2^127 on the nearest code
+// stands for 2^128, which bf16 and fp32 have as infinity.)
 __device__ __forceinline__ uint32_t fp4_scale(uint32_t top) {
   return (top >> 7) == 255u ? 255u : (uint32_t)max((int)((top + 32u) >> 7) - 2, 1);
 }

@@ -16,9 +16,10 @@
 // numbers; an FP8 head's factor goes into the softmax's scale and the result's).
 //
 // Long rows are bound by the matrix cores and the instructions between their products:
-// 2048 tokens after 65536, 32 heads on 4, take 1.97 ms in BF16 and FP4 and 2.06 in FP8
-// (1135 and 1080 TFLOP/s; the cores are busy 60 % of the cycles at a clock that such work
-// lowers to 1.8 GHz, and a library product of 16384^3 reaches 1350).  Few queries are
+// 2048 tokens after 65536, 32 heads on 4, take 1.95 to 2.03 ms in every format (1145 to 1100
+// TFLOP/s; a library product of 16384^3 reaches 1350).  BF16: the cores are busy 58 % of the
+// cycles at a clock that such work lowers to 1.7 to 1.8 GHz (16384 tokens).  FP4: 50 % at
+// 1.9, with bank conflicts of the widened V's way into LDS in a quarter of the cycles.  Few queries are
 // bound by what a unit takes before its first and after its last block.
 //
 // Sums are in fp32.  A tile's weights go to the second product rounded once to bf16, and
@@ -49,11 +50,11 @@ constexpr int kKeys = 64;                        // of a block
 constexpr int kFewQueries = 32;                  // a row's, up to which its keys are divided among the waves
 constexpr int kBlockBytes = kKeys * 2 * kHeadDim;  // of K or V in LDS
 // Pieces of a call whose tiles are split: two workgroups to a CU.  512 tokens after 8192
-// take 90 us, 100 at 256 pieces and at 1024; 32 rows of 4 drafted tokens after 16000 in
-// FP4 99, 140 and 108; 1 token after 65535 37, 34 and 48.
+// take 94 us, 102 at 256 pieces and 106 at 1024; 32 rows of 4 drafted tokens after 16000 in
+// FP4 114, 155 and 122; 1 token after 65535 44, 41 and 55.
 constexpr int kUnits = 512;
-// Blocks of a piece, at least.  4 tokens after 16384 in FP4 take 19.6 us, 22.7 with pieces of 2;
-// 128 after 1024 19.5 and 21.0, 1 after 3000 14.5 and 13.9.
+// Blocks of a piece, at least.  4 tokens after 16384 in FP4 take 20.4 us, 22.8 with pieces of 2;
+// 128 after 1024 20.6 and 21.7, 1 after 3000 14.6 and 14.0.
 constexpr int kLeast = 4;
 constexpr int kPartFloats = kQueries * kHeadDim + 3 * kQueries;  // weighted values, maxima, sums of rounded and exact weights
 
@@ -134,8 +135,8 @@ __device__ __forceinline__ Tries tries_of(int tiles, float blocks, int room) {
 
 // Whether pieces are worth their join: what the longest row's tiles save by them against
 // the join, in the time of a block by itself (1.24 us; beside another workgroup's 2).  A join
-// is a launch and the parts' way through memory.  Whole and in pieces: 1024 tokens 29 and
-// 41 us, 1024 after 2048 70 and 74, 1024 after 8192 191 and 170, 64 after 2048 44 and 20.
+// is a launch and the parts' way through memory.  Whole and in pieces: 1024 tokens 30 and
+// 41 us, 1024 after 2048 67 and 72, 1024 after 8192 177 and 164, 64 after 2048 45 and 20.
 __device__ __forceinline__ bool worth(float longest, int piece, int64_t units) {
   const float u = (float)units, beside = fminf(fmaxf(u * (2.f / kUnits) - 1.f, 0.f), 1.f);
   return __builtin_amdgcn_readfirstlane(longest - (float)piece * (1.f + 0.63f * beside) > 3.f + u * (1.f / 55.f)) != 0;
@@ -943,7 +944,7 @@ __device__ __forceinline__ void attend_unit(const PrefillArgs& a, const Heads& h
 // the end, where the waves' sums are joined.  K of the wave's next block (FP8, FP4: its
 // codes) is on its way during this one's exponentials and second product, V during the
 // next first product.  32 rows of 4 tokens after 16000, 32 heads on 4, take 207 us in
-// BF16, 129 in FP8 and 113 in FP4 on the GPU (5.1, 4.1 and 2.5 TB/s; FP4 is bound by the instructions of the
+// BF16, 129 in FP8 and 114 in FP4 on the GPU (5.1, 4.1 and 2.4 TB/s; FP4 is bound by the instructions of the
 // widening and the softmax), with the weights in one part 207, 122 and 103; 218, 165 and 155 as tiles (with
 // a costlier join); rows of 33 to 64 queries, two waves to a block, took 175 us in FP4 and as tiles 155.
 template <int kFmt, bool kLse>
